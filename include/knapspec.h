@@ -418,6 +418,108 @@ typedef struct {
 ks_status ks_generate_speculative(ks_model* m, const ks_spec_params* params, int32_t n_tokens,
                                   int32_t* out, ks_spec_stats* stats, int32_t* accepted_per_step);
 
+/* ------------------------------------------- 8-bit paged key/value cache */
+
+/* Keys and values of many sequences in one pool of pages, 8 bits a value, for
+ * callers that serve several sequences or long contexts (an addition of this
+ * library; the paper's models keep a bf16 cache).  The cache of one layer is
+ *   data[n_pages][n_kv_heads][page_tokens / 16] records,
+ * a record holding 16 consecutive tokens of one head:
+ *   key codes    [2][head_dim / 16][8 tokens][16 dims]
+ *   value codes  [head_dim][16 tokens], token t at byte
+ *                4 ((t % 8) / 2) + 2 (t / 8) + t % 2
+ *   float key_scale, value_scale, and 24 unused bytes.
+ * A value is code * scale; codes are e4m3 (OCP FP8), scales powers of two, one
+ * for the 16 tokens' keys and one for their values: the smallest 2^e, e >= -126,
+ * with every finite |x| <= 448 * 2^e.  Infinities and NaN are stored as NaN.
+ * head_dim 64 or 128; page_tokens a multiple of 16. */
+typedef struct {
+    void* data;              /* dev, 16-byte aligned, ks_kv8_bytes() bytes; needs no initial value */
+    int32_t n_pages, page_tokens, n_kv_heads, head_dim;
+} ks_kv8_cache;
+
+/* The sequences of a call.  Sequence s has its tokens on the pages
+ * page_table[s][0 ..] in order, lengths[s] of them, and the batch's rows
+ * row_offsets[s] .. row_offsets[s + 1] - 1 are its last tokens: row i of r is
+ * token lengths[s] - r + i.  Rows from row_offsets[n_seqs] on (padding up to
+ * n_rows) belong to no sequence: nothing is read or written for them.  All
+ * arrays are device memory and read by the kernels, so a captured call follows
+ * their contents; n_seqs, table_ld and n_rows are fixed by the call.
+ * What the host cannot check is checked on the device and ORed into *status
+ * (never cleared by a call), bit 0: a page outside the pool (its tokens are not
+ * written, read as zeros, and unseen by the attention); bit 1: offsets that
+ * decrease or pass n_rows, or a length below 0 or above the pages (taken as the
+ * nearest possible value); bit 2: a token before position 0 or past the RoPE
+ * table (not appended, or stored as zeros); bit 3: a bounded wait gave up.
+ * No two sequences of a call may append to the same block. */
+#define KS_KV8_BAD_PAGE 1
+#define KS_KV8_BAD_BATCH 2
+#define KS_KV8_BAD_POSITION 4
+#define KS_KV8_TIMEOUT 8
+typedef struct {
+    const int32_t* page_table;   /* dev [n_seqs][table_ld]                      */
+    const int32_t* row_offsets;  /* dev [n_seqs + 1], row_offsets[0] usually 0  */
+    const int32_t* lengths;      /* dev [n_seqs], at most table_ld page_tokens  */
+    int32_t n_seqs, table_ld, n_rows;
+    int32_t* status;             /* dev, or NULL                                */
+} ks_kv8_batch;
+
+/* New rows.  Head h of row r starts at k + r k_row + h k_head (elements); the
+ * head's values are contiguous.  rope: [rope_rows][head_dim / 2][2] (cos, sin)
+ * fp32 as rotate-half RoPE takes them, row = the token's position; NULL: keys
+ * and queries are stored as given.  q (or NULL): queries of the same rows,
+ * rotated into q_out (bf16). */
+typedef struct {
+    const void *k, *v, *q;
+    int32_t dtype;               /* of k, v, q: KS_DTYPE_F32 or KS_DTYPE_BF16 */
+    int32_t n_q_heads;
+    int64_t k_row, k_head, v_row, v_head, q_row, q_head;
+    const float* rope;
+    int32_t rope_rows;
+    void* q_out;
+    int64_t q_out_row, q_out_head;
+} ks_kv8_rows;
+
+/* Bytes of a cache; 0 for sizes that are not supported. */
+size_t ks_kv8_bytes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, int32_t head_dim);
+
+/* Rotate the batch's rows, quantise and write them to their pages.  A block
+ * whose first tokens are already in the cache goes on: its scale never falls,
+ * and if a new token raises it, the stored codes are multiplied by the power
+ * of two between (exact but where a code becomes subnormal).  A row at a
+ * block's start begins it anew.  Tokens of the last block behind the row are
+ * zeroed.  Rows may overwrite tokens of an earlier call (a rejected draft). */
+ks_status ks_kv8_append(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_rows* rows, void* stream);
+
+/* The values of the batch's rows: k_out, v_out (dev, dtype) at
+ * row * row_stride + head * head_stride elements. */
+ks_status ks_kv8_read(const ks_kv8_cache* cache, const ks_kv8_batch* batch, void* k_out, void* v_out, int32_t dtype,
+                      int64_t row_stride, int64_t head_stride, void* stream);
+
+/* Causal attention of the batch's rows, whose keys and values are in the
+ * cache: out = softmax(scale q K^T) V over the tokens up to the row's own;
+ * query head h reads KV head h / (n_q_heads / n_kv_heads), at most 64 query
+ * heads a KV head.  q, out: bf16, strides in elements.  lse (dev float
+ * [n_rows][n_q_heads], or NULL): the logarithm of the sum of exponentials.  A
+ * row that sees no token gives zeros and lse -inf.  A NaN key makes the rows
+ * that see it NaN, a NaN value that dim of them; unseen ones do nothing.
+ * workspace: dev, 256-byte aligned, ks_kv8_attention_workspace() bytes for
+ * the call's n_seqs and n_rows or more, zeroed once before its first use and
+ * left so by every call; calls that run at the same time need one each. */
+typedef struct {
+    const void* q;
+    int64_t q_row, q_head;
+    void* out;
+    int64_t out_row, out_head;
+    float* lse;
+    int32_t n_q_heads;
+    float scale;
+    void* workspace;
+    size_t workspace_bytes;
+} ks_kv8_attn;
+size_t ks_kv8_attention_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_rows);
+ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_attn* attn, void* stream);
+
 /* ------------------------------------------------------------ diagnostics */
 
 /* Copy a window of device state to the caller (for tests):

@@ -1,0 +1,118 @@
+// The 8-bit paged key/value cache: record layout, code conversions and the
+// batch's sequences, shared by the kernels that write and read it.
+//
+// A record holds one block of kKv8Block tokens of one KV head: e4m3 key codes
+// as [2][HD / 16][8 tokens][16 dims] and value codes as [HD dims][16 tokens]
+// (token t at byte v_byte(t)), so that every 8 x 16-byte matrix that the
+// attention feeds to the tensor cores is 128 contiguous bytes and no
+// transposition or swizzle is left to do, then the two scales (fp32 powers of
+// two) and 24 unused bytes.  Keys, values and scales of a block are one
+// contiguous piece: one asynchronous copy brings them.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace ks {
+
+constexpr int kKv8Block = 16;
+__host__ __device__ constexpr int kv8_record(int hd) { return 2 * kKv8Block * hd + 32; }
+constexpr int kKv8BadPage = 1, kKv8BadBatch = 2, kKv8BadPosition = 4, kKv8Timeout = 8;
+
+// Byte of token t in a row of value codes: lane t of a quad of the score
+// product holds tokens 2t, 2t + 1, 8 + 2t, 9 + 2t, and the value product takes
+// four neighbouring bytes of a lane.
+KS_DEV int v_byte(int t) { return 4 * ((t & 7) >> 1) + 2 * (t >> 3) + (t & 1); }
+// Byte of (token, dim) among a record's key codes.
+template <int HD>
+KS_DEV int k_byte(int t, int d) {
+    return ((t >> 3) * (HD / 16) + (d >> 4)) * 128 + (t & 7) * 16 + (d & 15);
+}
+
+// Two floats as e4m3 codes, nearest even (lo in the low byte).
+KS_DEV uint16_t to_e4m3x2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+KS_DEV float2 from_e4m3x2(uint16_t v) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(v));
+    return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+KS_DEV void kv8_flag(const Kv8Args& a, int code) {
+    if (a.status) atomicOr(a.status, code);
+}
+
+// Sequence s of the batch: its rows [row0, row0 + rows) and its length, the
+// rows among it.  Row i is token len - rows + i.  Values outside the batch's
+// own sizes are brought inside (and flagged): nothing is addressed by them
+// that does not exist.
+struct Kv8Seq {
+    int row0, rows, len;
+};
+KS_DEV int kv8_row0(const Kv8Args& a, int s) { return min(max(__ldg(a.offsets + s), 0), a.n_rows); }
+KS_DEV Kv8Seq kv8_seq(const Kv8Args& a, int s) {
+    const int o0 = __ldg(a.offsets + s), o1 = __ldg(a.offsets + s + 1), n = __ldg(a.lengths + s);
+    Kv8Seq q;
+    q.row0 = min(max(o0, 0), a.n_rows);
+    q.rows = min(max(o1, q.row0), a.n_rows) - q.row0;
+    q.len = min(max(n, 0), a.capacity);
+    return q;
+}
+KS_DEV bool kv8_seq_bad(const Kv8Args& a, int s) {
+    const int o0 = __ldg(a.offsets + s), o1 = __ldg(a.offsets + s + 1), n = __ldg(a.lengths + s);
+    return o0 < 0 || o1 < o0 || o1 > a.n_rows || n < 0 || n > a.capacity;
+}
+
+// The last sequence s with first(s) <= x (0 if there is none), first not
+// decreasing, found by one warp with 32 probes a round.
+template <class F>
+KS_DEV int kv8_find(int n_seqs, int x, F&& first) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n_seqs;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, i = lo + step * lane;
+        const unsigned yes = __ballot_sync(0xffffffffu, i < hi && (lane == 0 || first(i) <= x));
+        lo += step * (__popc(yes) - 1);
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+// The record of block b of sequence s and head h, or null for a page that the
+// pool does not have.
+KS_DEV unsigned char* kv8_record_at(const Kv8Args& a, int s, int b, int h, int rec) {
+    const int page = __ldg(a.table + (size_t)s * a.table_ld + b / a.bpp);
+    if (page < 0 || page >= a.n_pages) return nullptr;
+    return a.data + (((size_t)page * a.hk + h) * a.bpp + b % a.bpp) * rec;
+}
+
+// The touched blocks of a batch: block slots of sequence s begin at
+// row0 / 16 + 2 s, which leaves room for every block that its rows can touch
+// (r rows touch at most (r + 30) / 16 of them) without a sum over the
+// sequences.
+struct Kv8Slot {
+    int s, blk, first, last;   // sequence, block; tokens [first, last) of the block are the batch's rows
+    int row;                   // batch row of the block's token 0 (it may be before the sequence's rows)
+};
+KS_DEV bool kv8_slot(const Kv8Args& a, int slot, Kv8Slot& w) {
+    w.s = kv8_find(a.n_seqs, slot, [&](int s) { return kv8_row0(a, s) / kKv8Block + 2 * s; });
+    const Kv8Seq q = kv8_seq(a, w.s);   // of the first sequence for slots before its own
+    const int start = max(q.len - q.rows, 0), b = slot - (q.row0 / kKv8Block + 2 * w.s);
+    w.blk = start / kKv8Block + b;
+    if (b == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        if (kv8_seq_bad(a, w.s)) kv8_flag(a, kKv8BadBatch);
+        if (q.len < q.rows) kv8_flag(a, kKv8BadPosition);
+    }
+    if (b < 0 || q.rows == 0 || w.blk * kKv8Block >= q.len) return false;
+    w.first = max(start - w.blk * kKv8Block, 0);
+    w.last = min(q.len - w.blk * kKv8Block, kKv8Block);
+    w.row = q.row0 + w.blk * kKv8Block - (q.len - q.rows);
+    return true;
+}
+
+}  // namespace ks

@@ -62,6 +62,29 @@ class KsSpecStats(C.Structure):
                 ("resolves", C.c_int64), ("attn_skipped", C.c_int64), ("mlp_skipped", C.c_int64)]
 
 
+class KsKv8Cache(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32)]
+
+
+class KsKv8Batch(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("row_offsets", C.c_void_p), ("lengths", C.c_void_p),
+                ("n_seqs", C.c_int32), ("table_ld", C.c_int32), ("n_rows", C.c_int32), ("status", C.c_void_p)]
+
+
+class KsKv8Rows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("dtype", C.c_int32),
+                ("n_q_heads", C.c_int32), ("k_row", C.c_int64), ("k_head", C.c_int64), ("v_row", C.c_int64),
+                ("v_head", C.c_int64), ("q_row", C.c_int64), ("q_head", C.c_int64), ("rope", C.c_void_p),
+                ("rope_rows", C.c_int32), ("q_out", C.c_void_p), ("q_out_row", C.c_int64), ("q_out_head", C.c_int64)]
+
+
+class KsKv8Attn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64), ("out", C.c_void_p),
+                ("out_row", C.c_int64), ("out_head", C.c_int64), ("lse", C.c_void_p), ("n_q_heads", C.c_int32),
+                ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 class KsError(RuntimeError):
     def __init__(self, status: int, where: str, msg: str):
         super().__init__(f"{where}: {_status_name(status)}: {msg}")
@@ -113,6 +136,12 @@ _SIGS = {
     "ks_kernel_bytes": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_double)]),
     "ks_launch_count": (C.c_int64, [C.c_void_p]),
     "ks_transfer_bytes": (C.c_int, [C.c_void_p, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]),
+    "ks_kv8_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "ks_kv8_append": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Rows), C.c_void_p]),
+    "ks_kv8_read": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.c_void_p, C.c_void_p, C.c_int32,
+                              C.c_int64, C.c_int64, C.c_void_p]),
+    "ks_kv8_attention_workspace": (C.c_size_t, [C.POINTER(KsKv8Cache), C.c_int32, C.c_int32, C.c_int32]),
+    "ks_kv8_attention": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Attn), C.c_void_p]),
     "ks_status_str": (C.c_char_p, [C.c_int]),
     "ks_last_error": (C.c_char_p, []),
 }
@@ -416,6 +445,33 @@ def ks_select_tpt(h: int, lat: "KsLatency", n_sublayers: int, n_candidates: int,
     check(load().ks_select_tpt(h, C.byref(lat), n_candidates, max_gamma, mask.ctypes.data, C.byref(g),
                                C.byref(t), alphas.ctypes.data, cand.ctypes.data), "ks_select_tpt")
     return mask, g.value, t.value, alphas, cand
+
+
+# ------------------------------------------------- 8-bit paged cache
+KV8_BAD_PAGE, KV8_BAD_BATCH, KV8_BAD_POSITION, KV8_TIMEOUT = 1, 2, 4, 8
+
+
+def ks_kv8_bytes(n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(load().ks_kv8_bytes(n_pages, page_tokens, n_kv_heads, head_dim))
+
+
+def ks_kv8_append(cache: KsKv8Cache, batch: KsKv8Batch, rows: KsKv8Rows, stream=None):
+    check(load().ks_kv8_append(C.byref(cache), C.byref(batch), C.byref(rows), _stream_ptr(stream)), "ks_kv8_append")
+
+
+def ks_kv8_read(cache: KsKv8Cache, batch: KsKv8Batch, k_out, v_out, dtype: int, row_stride: int, head_stride: int,
+                stream=None):
+    check(load().ks_kv8_read(C.byref(cache), C.byref(batch), _ptr(k_out), _ptr(v_out), dtype, row_stride, head_stride,
+                             _stream_ptr(stream)), "ks_kv8_read")
+
+
+def ks_kv8_attention_workspace(cache: KsKv8Cache, n_q_heads: int, n_seqs: int, n_rows: int) -> int:
+    return int(load().ks_kv8_attention_workspace(C.byref(cache), n_q_heads, n_seqs, n_rows))
+
+
+def ks_kv8_attention(cache: KsKv8Cache, batch: KsKv8Batch, attn: KsKv8Attn, stream=None):
+    check(load().ks_kv8_attention(C.byref(cache), C.byref(batch), C.byref(attn), _stream_ptr(stream)),
+          "ks_kv8_attention")
 
 
 def ks_launch_count(h: int) -> int:
