@@ -504,8 +504,8 @@ ks_status ks_kv8_read(const ks_kv8_cache* cache, const ks_kv8_batch* batch, void
  * row that sees no token gives zeros and lse -inf.  A NaN key makes the rows
  * that see it NaN, a NaN value that dim of them; unseen ones do nothing.
  * workspace: dev, 256-byte aligned, ks_kv8_attention_workspace() bytes for
- * the call's n_seqs and n_rows or more, zeroed once before its first use and
- * left so by every call; calls that run at the same time need one each. */
+ * the call's n_seqs and n_rows or more; its contents matter to no later call,
+ * and calls that run at the same time need one each. */
 typedef struct {
     const void* q;
     int64_t q_row, q_head;

@@ -296,7 +296,7 @@ struct Kv8AttnArgs {
 };
 constexpr int kKv8MaxGroup = 64;    // query heads a KV head
 cudaError_t launch_kv8_append(int dtype, const Kv8Args& a, const Kv8RowArgs& r, cudaStream_t s);
-size_t kv8_attention_workspace(int hd, int hk, int hq, int n_seqs, int n_rows);
+size_t kv8_attention_workspace(int hd, int group, int n_rows);
 cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s);
 
 }  // namespace ks

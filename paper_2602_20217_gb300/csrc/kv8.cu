@@ -20,16 +20,6 @@ namespace {
 constexpr int kAppendThreads = 128;
 constexpr int kAppendQHeads = 4;     // query heads of a CTA that rotates queries
 
-KS_DEV bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-// 2^e of the block: see the head of this file.  448 = 1.75 * 2^8.
-KS_DEV float scale_for(float amax) {
-    const unsigned b = __float_as_uint(amax);
-    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);
-    return __uint_as_float((unsigned)(max(e, -126) + 127) << 23);
-}
-// 1 / s for a power of two from 2^-126 to 2^127
-KS_DEV float inverse_pow2(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
-
 // Four codes times a power of two at most 1.
 KS_DEV uint32_t rescale4(uint32_t v, float f) {
     const float2 a = from_e4m3x2((uint16_t)v), b = from_e4m3x2((uint16_t)(v >> 16));
@@ -434,7 +424,7 @@ extern "C" size_t ks_kv8_attention_workspace(const ks_kv8_cache* cache, int32_t 
         n_q_heads < 1 || n_q_heads > kMaxHeads || n_q_heads % cache->n_kv_heads ||
         n_q_heads / cache->n_kv_heads > kKv8MaxGroup || n_seqs < 0 || n_seqs > kMaxSeqs || n_rows < 0 || n_rows > kMaxRows)
         return 0;
-    return kv8_attention_workspace(cache->head_dim, cache->n_kv_heads, n_q_heads, n_seqs, n_rows);
+    return kv8_attention_workspace(cache->head_dim, n_q_heads / cache->n_kv_heads, n_rows);
 }
 
 extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_attn* attn,
@@ -465,7 +455,7 @@ extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_ba
         set_error("ks_kv8_attention: null or misaligned queries or output, or bad strides");
         return KS_ERR_INVALID_ARG;
     }
-    const size_t need = kv8_attention_workspace(a.hd, a.hk, attn->n_q_heads, a.n_seqs, a.n_rows);
+    const size_t need = kv8_attention_workspace(a.hd, attn->n_q_heads / a.hk, a.n_rows);
     if (!attn->workspace || !aligned(attn->workspace, 256)) {
         set_error("ks_kv8_attention: null or misaligned workspace");
         return KS_ERR_INVALID_ARG;

@@ -43,6 +43,16 @@ KS_DEV float2 from_e4m3x2(uint16_t v) {
     return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+KS_DEV bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+// Smallest 2^e, e >= -126, with amax <= 448 * 2^e (448 = 1.75 * 2^8).
+KS_DEV float scale_for(float amax) {
+    const unsigned b = __float_as_uint(amax);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);
+    return __uint_as_float((unsigned)(max(e, -126) + 127) << 23);
+}
+// 1 / s for a power of two from 2^-126 to 2^127
+KS_DEV float inverse_pow2(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
+
 KS_DEV void kv8_flag(const Kv8Args& a, int code) {
     if (a.status) atomicOr(a.status, code);
 }

@@ -131,13 +131,13 @@ class Cache8:
         return k_out, v_out
 
     def attention_workspace(self, n_q_heads: int, n_seqs: int, n_rows: int):
-        """Zeroed workspace of attention() for these sizes or smaller ones; calls that run at once need one each."""
+        """A workspace of attention() for these sizes or smaller ones; calls that run at once need one each."""
         import torch
         n = ks.ks_kv8_attention_workspace(self.c, n_q_heads, n_seqs, n_rows)
         if n == 0:
             raise ks.KsError(ks.KS_ERR_INVALID_ARG, "attention_workspace", f"{n_q_heads} query heads over "
                              f"{self.n_kv_heads}, {n_seqs} sequences, {n_rows} rows")
-        return torch.zeros(n, dtype=torch.uint8, device=self.device)
+        return torch.empty(n, dtype=torch.uint8, device=self.device)
 
     def attention(self, batch: Batch8, q, scale=None, out=None, lse=None, workspace=None, stream=None):
         """Causal attention of the batch's rows: q, out [n_rows, n_q_heads, head_dim] bf16, lse [n_rows, n_q_heads]

@@ -111,7 +111,7 @@ def attend(pool, rows, hq, seed=1, pad=0, lengths=None, q=None, scale=None, want
     out = torch.full((n, hq, hd), 7.0, dtype=torch.bfloat16, device="cuda")
     lse = torch.full((n, hq), 7.0, device="cuda")
     work = d["cache"].attention_workspace(hq, len(pool.lens), n)
-    work.fill_(0)
+    work.fill_(0xff)
     scale = hd ** -0.5 if scale is None else scale
     d["cache"].attention(d["batch"], qt, scale=scale, out=out, lse=lse, workspace=work)
     torch.cuda.synchronize()
