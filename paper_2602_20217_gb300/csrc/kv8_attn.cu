@@ -33,6 +33,7 @@
 // The record's layout makes every operand a run of ldmatrix rows without bank
 // conflicts and P's accumulator layout the next product's operand.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv8.cuh"
 #include "tma.cuh"
@@ -43,132 +44,143 @@ namespace {
 
 constexpr int kConsumers = 4;
 constexpr int kThreads = 32 * (kConsumers + 1);
-constexpr int kTileBlocks = 8;
-constexpr int kTile = kTileBlocks * kKv8Block;
-constexpr int kStages = 2;
+constexpr int kSteps = 4;           // steps of a tile
 constexpr int kMaxCtas = 480;       // the workspace has room for this many
 constexpr int kMaxRowsOfUnit = 64;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kWeightUp = 16384.f;
+// A unit's fixed cost (queries, joining its warps, output) in the time of 128
+// keys, for the cut into runs.
+constexpr int kUnitCost = 2;
 
 struct Plan {
+    int tile;           // keys of a tile
+    int cost;           // a unit's fixed cost in tiles
     int wr;             // warps of different rows
     int tq;             // tokens of a group
     int rg;             // rows of a group, at least tq query groups
     int ctas;
     bool q_wide;        // queries can be read 8 bytes at a time
     float* part;        // [2 ctas][rg][HD + 4]: m, l, -, -, o
-    int4* desc;         // [ctas]: the unit that begins in this CTA's run and ends in a later one's: s (-1: none), h, g, last CTA
+    int4* desc;         // [ctas]: the unit that begins in this CTA's run and ends in a later one's: first batch row,
+                        // query rows (0: no such unit), KV head, last CTA
 };
 
 // Tiles of group g; a group whose rows see nothing has one as well (its rows get zeros).
-KS_DEV int group_tiles(const Kv8Seq& q, int tq, int g) {
-    const int last = q.len - q.rows + min(q.rows, (g + 1) * tq) - 1;
-    return last < 0 ? 1 : last / kTile + 1;
+KS_DEV int group_tiles(const Kv8Seq& q, const Plan& p, int g) {
+    const int last = q.len - q.rows + min(q.rows, (g + 1) * p.tq) - 1;
+    return last < 0 ? 1 : (unsigned)last / (unsigned)p.tile + 1;
 }
 KS_DEV int groups_of(const Kv8Seq& q, int tq) { return (q.rows + tq - 1) / tq; }
-KS_DEV long long head_tiles(const Kv8Seq& q, int tq) {
-    long long n = 0;
-    for (int g = 0; g < groups_of(q, tq); ++g) n += group_tiles(q, tq, g);
+// What the units of one head of a sequence take on the line of all units.
+KS_DEV int head_length(const Kv8Seq& q, const Plan& p) {
+    int n = 0;
+    for (int g = 0; g < groups_of(q, p.tq); ++g) n += group_tiles(q, p, g) + p.cost;
     return n;
 }
 
-// A place in the sequence of all tiles: the unit and its next tile.
-struct Cursor {
-    int s, h, g, tile, tiles;
+// The line of all units, each its fixed cost and its tiles long, cut into equal runs
+// [x0, x1): a CTA works on the tiles in its run.
+struct Run {
+    int ctas, each, more;       // runs of each + 1 (the first `more`), then of each
+    int x0, x1;
+    KS_DEV void cut(int total, int most, int cta) {
+        ctas = min(most, total);
+        each = ctas ? total / ctas : 0;
+        more = total - each * ctas;
+        x0 = cta * each + min(cta, more);
+        x1 = x0 + each + (cta < more);
+    }
+    KS_DEV int cta_of(int x) const {
+        const int b = more * (each + 1);
+        return x < b ? x / (each + 1) : more + (x - b) / each;
+    }
+};
+
+// A segment: tiles [tile, end) of a unit, whose first tile is at `first` on the line.
+struct Segment {
+    int s, h, g, tile, end, tiles, first;
     Kv8Seq q;
-    KS_DEV void unit(const Kv8Args& a, int tq) { tiles = group_tiles(q, tq, g); }
-    KS_DEV void next(const Kv8Args& a, int tq) {
-        tile = 0;
-        if (++g >= groups_of(q, tq)) {
+    KS_DEV void at(const Run& r, const Plan& p, int start) {
+        tiles = group_tiles(q, p, g);
+        first = start + p.cost;
+        tile = max(0, r.x0 - first);
+        end = min(tiles, r.x1 - first);
+    }
+    // the next unit, if a tile of it is in the run
+    KS_DEV bool next(const Kv8Args& a, const Run& r, const Plan& p) {
+        const int start = first + tiles;
+        if (start + p.cost >= r.x1) return false;
+        if (++g >= groups_of(q, p.tq)) {
             g = 0;
             if (++h >= a.hk) {
                 h = 0;
                 do {
-                    if (++s >= a.n_seqs) return;
+                    if (++s >= a.n_seqs) return false;
                     q = kv8_seq(a, s);
                 } while (q.rows == 0);
             }
         }
-        unit(a, tq);
+        at(r, p, start);
+        return true;
     }
 };
 
-struct Run {
-    long long total, x0, x1;    // all tiles, this CTA's
-    int ctas;                   // with tiles
-    Cursor at;
-};
-
-// This CTA's run: the total over the sequences, then the sequence of the first
-// tile.  Every thread of the CTA takes part.
-KS_DEV bool find_run(const Kv8Args& a, const Plan& p, Run& r, long long* scratch) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
-    auto tiles_of = [&](int s) -> long long {
-        if (s >= a.n_seqs) return 0;
-        if (cta == 0 && kv8_seq_bad(a, s)) kv8_flag(a, kKv8BadBatch);
-        return a.hk * head_tiles(kv8_seq(a, s), p.tq);
+// This CTA's run and its first segment; false if it has none.  Every warp finds
+// it by itself, 32 sequences at a time.
+KS_DEV bool find_run(const Kv8Args& a, const Plan& p, Run& r, Segment& k) {
+    const int lane = threadIdx.x & 31, cta = blockIdx.x;
+    Kv8Seq mine{};
+    auto load = [&](int c) {
+        const int s = c + lane;
+        if (s >= a.n_seqs) {
+            mine = Kv8Seq{};
+            return 0;
+        }
+        mine = kv8_seq(a, s);
+        return a.hk * head_length(mine, p);
     };
-    // inclusive sums over the CTA's threads; the last is the chunk's total
-    auto scan = [&](long long v) {
+    int total = 0, v = 0;
+    for (int c = 0; c < a.n_seqs; c += 32) {
+        v = load(c);
+        if (cta == 0 && c + lane < a.n_seqs && kv8_seq_bad(a, c + lane)) kv8_flag(a, kKv8BadBatch);
+        total += __reduce_add_sync(0xffffffffu, v);
+    }
+    r.cut(total, p.ctas, cta);
+    if (cta >= r.ctas) return false;
+    int start = 0;                               // of the sequence's units on the line
+    for (int c = 0;; c += 32) {
+        if (a.n_seqs > 32) v = load(c);
+        int u = v;                               // inclusive sums
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long u = __shfl_up_sync(0xffffffffu, v, o);
-            if (lane >= o) v += u;
+            const int w = __shfl_up_sync(0xffffffffu, u, o);
+            if (lane >= o) u += w;
         }
-        __syncthreads();
-        if (lane == 31) scratch[warp] = v;
-        __syncthreads();
-        for (int i = 0; i < warp; ++i) v += scratch[i];
-        return v;
-    };
-    auto all = [&]() {
-        long long t = 0;
-        for (int i = 0; i < kThreads / 32; ++i) t += scratch[i];
-        return t;
-    };
-    r.total = 0;
-    long long first = 0, sum = 0;
-    for (int c = 0; c < a.n_seqs; c += kThreads) {
-        const long long v = tiles_of(c + tid);
-        const long long u = scan(v);
-        if (c == 0) first = v, sum = u;
-        r.total += all();
-    }
-    r.ctas = (int)min((long long)p.ctas, r.total);
-    if (cta >= r.ctas) return false;
-    r.x0 = r.total * cta / r.ctas;
-    r.x1 = r.total * (cta + 1) / r.ctas;
-    int* place = reinterpret_cast<int*>(scratch + 8);
-    long long* before = scratch + 9;
-    long long base = 0;
-    for (int c = 0;; c += kThreads) {
-        const long long v = c == 0 ? first : tiles_of(c + tid), u = c == 0 ? sum : scan(v);
-        if (r.x0 >= base + u - v && r.x0 < base + u) {
-            *place = c + tid;
-            *before = base + u - v;
+        const unsigned past = __ballot_sync(0xffffffffu, start + u > r.x0);
+        if (past) {
+            const int i = __ffs(past) - 1;
+            k.s = c + i;
+            k.q.row0 = __shfl_sync(0xffffffffu, mine.row0, i);
+            k.q.rows = __shfl_sync(0xffffffffu, mine.rows, i);
+            k.q.len = __shfl_sync(0xffffffffu, mine.len, i);
+            start += __shfl_sync(0xffffffffu, u - v, i);
+            break;
         }
-        if (c + kThreads >= a.n_seqs) break;
-        if (c == 0) scan(v);       // scratch holds the last chunk's totals
-        base += all();
+        start += __shfl_sync(0xffffffffu, u, 31);
     }
-    __syncthreads();
-    Cursor& k = r.at;
-    k.s = *place;
-    k.q = kv8_seq(a, k.s);
-    long long rem = r.x0 - *before;
-    const long long w = head_tiles(k.q, p.tq);
-    k.h = (int)(rem / w);
-    rem %= w;
+    const int len = head_length(k.q, p);
+    k.h = (r.x0 - start) / len;
+    start += k.h * len;
     k.g = 0;
-    k.unit(a, p.tq);
-    while (rem >= k.tiles) {
-        rem -= k.tiles;
+    for (;;) {
+        k.at(r, p, start);
+        if (r.x0 < k.first + k.tiles) break;
+        start = k.first + k.tiles;
         ++k.g;
-        k.unit(a, p.tq);
     }
-    k.tile = (int)rem;
-    return true;
+    // a run that ends before the unit's first tile has nothing to do
+    return k.end > k.tile;
 }
 
 KS_DEV void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -225,81 +237,153 @@ struct Rows {
     }
 };
 
-template <int HD>
+// A CTA's shared memory.  SB: records of a step.
+template <int HD, int NQ, int SB>
 struct Smem {
     static constexpr int REC = kv8_record(HD);
-    static constexpr int TILE = kTileBlocks * REC;
-    static constexpr int comb(int nq) { return 8 * nq * HD * 4; }           // a warp's o
-    static constexpr int bytes(int nq) {
-        return kStages * TILE + 2 * comb(nq) + 2 * 8 * nq * 8 + HD * 4 + 2 * kStages * 8 + 16 * 8 + kStages * 8;
-    }
+    static constexpr int BLOCKS = kSteps * SB;                   // records of a tile
+    static constexpr int TILE = BLOCKS * REC;
+    static constexpr int STAGES = NQ == 1 ? 4 : 2;
+    static constexpr int HALF = NQ * (HD / 32) * 4 * 32;         // floats: half of a warp's o
+    unsigned char ring[STAGES][TILE];
+    float comb[kConsumers][HALF];
+    float2 ml[kConsumers][8 * NQ];
+    int nan_from[3][HD];                                         // first key whose value is NaN, a segment each
+    int any_nan[3];
+    int present[STAGES];                                         // records that were copied
+    uint64_t full[STAGES], empty[STAGES];
 };
 
-template <int HD, int NQ>
+// o[i][c] = NaN for i and c that are not known when compiling (rare)
+template <int DT>
+KS_DEV void set_nan(float (&o)[DT][4], int i, int c) {
+#pragma unroll
+    for (int j = 0; j < DT; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i == j && c == k) o[j][k] = __uint_as_float(0x7fc00000u);
+}
+
+// Warps wk and wk ^ bit have the same rows: each gives half of its CUR tiles of
+// dims (all in o[.][0 .. CUR)) to the other and keeps the sum of the other half
+// in o[.][0 .. CUR / 2).  Returns the first kept tile of the CUR.
+template <int NQ, int DT, int CUR>
+KS_DEV int join(float (&o)[NQ][DT][4], float (&m)[NQ], float (&l)[NQ], float* comb, float2* ml, int warp, int other,
+                bool upper) {
+    constexpr int H = CUR / 2, SLOT = NQ * (DT / 2) * 4 * 32;
+    const int lane = threadIdx.x & 31, g = lane >> 2, q4 = lane & 3;
+    float* mine = comb + warp * SLOT + lane;
+    const float* theirs = comb + other * SLOT + lane;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                mine[((n * H + i) * 4 + c) * 32] = upper ? o[n][i][c] : o[n][H + i][c];
+                if (upper) o[n][i][c] = o[n][H + i][c];
+            }
+        if (q4 == 0) ml[warp * 8 * NQ + 8 * n + g] = make_float2(m[n], l[n]);
+    }
+    consumers_sync();
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const float2 u = ml[other * 8 * NQ + 8 * n + g];
+        const float top = fmaxf(m[n], u.x), ref = top == -INFINITY ? 0.f : top;
+        const float fa = exp2_approx(m[n] - ref), fb = exp2_approx(u.x - ref);
+        m[n] = top;
+        l[n] = __fadd_rn(__fmul_rn(l[n], fa), __fmul_rn(u.y, fb));      // the same bits in both warps
+        const float a0 = __shfl_sync(0xffffffffu, fa, 8 * q4), a1 = __shfl_sync(0xffffffffu, fa, 8 * q4 + 4);
+        const float b0 = __shfl_sync(0xffffffffu, fb, 8 * q4), b1 = __shfl_sync(0xffffffffu, fb, 8 * q4 + 4);
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                o[n][i][c] = o[n][i][c] * (c & 1 ? a1 : a0) + theirs[((n * H + i) * 4 + c) * 32] * (c & 1 ? b1 : b0);
+    }
+    consumers_sync();
+    return upper ? H : 0;
+}
+
+template <int HD, int NQ, int SB>
 __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     kv8_attention_kernel(const Kv8Args a, const Kv8AttnArgs t, const Plan p) {
-    constexpr int REC = kv8_record(HD), TILE = Smem<HD>::TILE, DT = HD / 16, KJ = HD / 32;
-    extern __shared__ __align__(128) unsigned char smem[];
-    unsigned char* ring = smem;
-    float* comb = reinterpret_cast<float*>(ring + kStages * TILE);          // [2][NQ DT 4][32]
-    float2* ml = reinterpret_cast<float2*>(comb + 2 * NQ * DT * 4 * 32);    // [2][8 NQ]
-    int* nan_from = reinterpret_cast<int*>(ml + 2 * 8 * NQ);                // [HD]: first key whose value is NaN
-    uint64_t* full = reinterpret_cast<uint64_t*>(nan_from + HD);
-    uint64_t* empty = full + kStages;
-    long long* scratch = reinterpret_cast<long long*>(empty + kStages);     // [16]
-    volatile int* present = reinterpret_cast<volatile int*>(scratch + 16);  // [kStages] records that were copied
+    using S = Smem<HD, NQ, SB>;
+    constexpr int REC = S::REC, BLOCKS = S::BLOCKS, STAGES = S::STAGES, DT = HD / 16, KJ = HD / 32;
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    S& sm = *reinterpret_cast<S*>(smem_raw);
+    volatile int* present = sm.present;
 
-    if (a.stop && *a.stop) return;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    grid_launch_dependents();
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(&full[i], 1);
-            mbar_init(&empty[i], kConsumers);
+        for (int i = 0; i < STAGES; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], kConsumers);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    for (int i = tid; i < HD; i += kThreads) nan_from[i] = INT32_MAX;
+    for (int i = tid; i < 3 * HD; i += kThreads) sm.nan_from[0][i] = INT32_MAX;
+    if (tid < 3) sm.any_nan[tid] = 0;
+    __syncthreads();
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (a.stop && *a.stop) return;
     Run run;
-    if (!find_run(a, p, run, scratch)) {
-        if (tid == 0) p.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    Segment at;
+    if (!find_run(a, p, run, at)) {
+        if (tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
-    __syncthreads();
-    Cursor at = run.at;
-    long long left = run.x1 - run.x0;
     const int G = t.hq / a.hk;
 
     if (warp == kConsumers) {
         // ------------------------------------------------------- producer
-        int it = 0;
-        bool alive = true;
-        while (left > 0 && alive) {
-            const Rows rows(at.q, p.tq, at.g, G);
-            const int last = rows.pos0 + rows.n / G - 1;         // of the group's keys
-            const int end = at.tile + (int)min((long long)(at.tiles - at.tile), left);
-            for (int tile = at.tile; tile < end; ++tile, ++it) {
-                const int st = it % kStages, b = tile * kTileBlocks + lane;
-                // the page's number is on its way while the stage is still read
-                const bool wanted = lane < kTileBlocks && b * kKv8Block <= last;
-                const unsigned char* rec = wanted ? kv8_record_at(a, at.s, b, at.h, REC) : nullptr;
-                if (wanted && !rec) kv8_flag(a, kKv8BadPage);
-                const unsigned have = __ballot_sync(0xffffffffu, rec != nullptr);
-                alive = mbar_wait(&empty[st], ((it / kStages) & 1) ^ 1, kWaitLimitNs);
+        // Page numbers are read a group of tiles ahead, across segments: under
+        // load such a read takes microseconds.
+        constexpr int TILES = 32 / BLOCKS;                       // tiles of a group, a block per lane
+        auto pages = [&](const Segment& k, int tile) {
+            const int b = tile * BLOCKS + lane;
+            const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
+            if (b * kKv8Block > last || tile + lane / BLOCKS >= k.end) return -1;
+            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + b / a.bpp);
+            return page >= 0 && page < a.n_pages ? page : -2;
+        };
+        int it = 0, tile = at.tile, page = pages(at, tile);
+        bool alive = true, more = true;
+        while (more && alive) {
+            // the group after this one
+            Segment next = at;
+            int next_tile = tile + TILES;
+            if (next_tile >= at.end) {
+                more = next.next(a, run, p);
+                next_tile = next.tile;
+            }
+            const int next_page = more ? pages(next, next_tile) : -1;
+            if (page == -2) kv8_flag(a, kKv8BadPage);
+            const int b = tile * BLOCKS + lane;
+            const unsigned char* rec =
+                page >= 0 ? a.data + (((size_t)page * a.hk + at.h) * a.bpp + b % a.bpp) * REC : nullptr;
+            const unsigned have = __ballot_sync(0xffffffffu, rec != nullptr);
+            for (int i = 0; i < TILES && tile + i < at.end; ++i, ++it) {
+                const int st = it % STAGES;
+                const unsigned mask = have >> (i * BLOCKS) & ((1u << BLOCKS) - 1);
+                alive = mbar_wait(&sm.empty[st], ((it / STAGES) & 1) ^ 1, kWaitLimitNs);
                 if (!alive) break;
                 if (lane == 0) {
-                    present[st] = (int)have;
-                    mbar_expect_tx(&full[st], __popc(have) * REC);
+                    present[st] = (int)mask;
+                    mbar_expect_tx(&sm.full[st], __popc(mask) * REC);
                 }
                 __syncwarp();
-                if (rec) bulk_load(ring + st * TILE + lane * REC, rec, REC, &full[st]);
+                if (rec && lane / BLOCKS == i) bulk_load(sm.ring[st] + lane % BLOCKS * REC, rec, REC, &sm.full[st]);
             }
-            left -= end - at.tile;
-            if (left > 0) at.next(a, p.tq);
+            at = next;
+            tile = next_tile;
+            page = next_page;
         }
         if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
         // no copy may be in flight when the CTA ends
-        for (int i = max(0, it - kStages); i < it; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, kWaitLimitNs);
+        for (int i = max(0, it - STAGES); i < it; ++i)
+            mbar_wait(&sm.full[i % STAGES], (i / STAGES) & 1, kWaitLimitNs);
         return;
     }
 
@@ -309,9 +393,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     const int m0 = wri * 8 * NQ;
     int it = 0;
     bool alive = true, began = false;
-    while (left > 0) {
+    for (int buf = 0;; buf = buf == 2 ? 0 : buf + 1) {
         const Rows rows(at.q, p.tq, at.g, G);
-        const int t0 = at.tile, t1 = at.tile + (int)min((long long)(at.tiles - at.tile), left);
         // this warp's queries, in two codes
         uint32_t qa[NQ][KJ][4];
         float qf[NQ];
@@ -326,19 +409,22 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
             const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head;
             lim[n] = valid ? rows.pos0 + tok : INT32_MAX;
             float x[KJ * 2][4], top = 0.f;
+            // all loads first, without a branch between them
+            uint2 raw[KJ * 2];
+            if (p.q_wide) {
+#pragma unroll
+                for (int j = 0; j < 2 * KJ; ++j) raw[j] = *reinterpret_cast<const uint2*>(src + 16 * j + 4 * q4);
+            } else {
+                const unsigned short* e = reinterpret_cast<const unsigned short*>(src) + 4 * q4;
+#pragma unroll
+                for (int j = 0; j < 2 * KJ; ++j)
+                    raw[j] = make_uint2(e[16 * j] | (uint32_t)e[16 * j + 1] << 16, e[16 * j + 2] | (uint32_t)e[16 * j + 3] << 16);
+            }
 #pragma unroll
             for (int j = 0; j < 2 * KJ; ++j) {
-                const __nv_bfloat16* e = src + 16 * j + 4 * q4;
-                if (!valid) {
-                    x[j][0] = x[j][1] = x[j][2] = x[j][3] = 0.f;
-                } else if (p.q_wide) {
-                    const uint2 v = *reinterpret_cast<const uint2*>(e);
-                    x[j][0] = bf16_lo(v.x); x[j][1] = bf16_hi(v.x);
-                    x[j][2] = bf16_lo(v.y); x[j][3] = bf16_hi(v.y);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[j][i] = __bfloat162float(e[i]);
-                }
+                if (!valid) raw[j] = make_uint2(0, 0);
+                x[j][0] = bf16_lo(raw[j].x); x[j][1] = bf16_hi(raw[j].x);
+                x[j][2] = bf16_lo(raw[j].y); x[j][3] = bf16_hi(raw[j].y);
             }
 #pragma unroll
             for (int j = 0; j < 2 * KJ; ++j)
@@ -370,22 +456,22 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
             for (int i = 0; i < DT; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
         }
 
-        for (int tile = t0; tile < t1; ++tile, ++it) {
-            const int st = it % kStages;
-            if (alive) alive = mbar_wait(&full[st], (it / kStages) & 1, kWaitLimitNs);
+        for (int tile = at.tile; tile < at.end; ++tile, ++it) {
+            const int st = it % STAGES;
+            if (alive) alive = mbar_wait(&sm.full[st], (it / STAGES) & 1, kWaitLimitNs);
             const int have = alive && wn > 0 ? present[st] : 0;
-            for (int step = wk; step < 4; step += WK) {
-                const int got = have >> (2 * step) & 3, key0 = tile * kTile + 32 * step;
+            for (int step = wk; step < kSteps; step += WK) {
+                const int got = have >> (SB * step) & ((1 << SB) - 1), key0 = (tile * kSteps + step) * SB * kKv8Block;
                 if (got == 0 || key0 > lim_last) continue;
-                const unsigned char* rec = ring + st * TILE + 2 * step * REC;
+                const unsigned char* rec = sm.ring[st] + SB * step * REC;
                 const uint32_t base = smem_u32(rec);
-                const bool edge = got != 3 || key0 + 31 > lim_first;
-                float2 sc[2];                                    // key and value scales
-                sc[0] = *reinterpret_cast<const float2*>(rec + 32 * HD);
-                sc[1] = *reinterpret_cast<const float2*>(rec + REC + 32 * HD);
-                float s[NQ][4][4];
+                const bool edge = got != (1 << SB) - 1 || key0 + SB * kKv8Block - 1 > lim_first;
+                float2 sc[SB];                                   // key and value scales
 #pragma unroll
-                for (int nb = 0; nb < 4; ++nb) {
+                for (int i = 0; i < SB; ++i) sc[i] = *reinterpret_cast<const float2*>(rec + i * REC + 32 * HD);
+                float s[NQ][2 * SB][4];
+#pragma unroll
+                for (int nb = 0; nb < 2 * SB; ++nb) {
                     const uint32_t kb = base + (nb >> 1) * REC + (nb & 1) * 8 * HD + lane * 16;
 #pragma unroll
                     for (int n = 0; n < NQ; ++n) s[n][nb][0] = s[n][nb][1] = s[n][nb][2] = s[n][nb][3] = 0.f;
@@ -401,22 +487,27 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     }
                 }
                 // values of a record that is not there count for nothing
-                const float v0 = got & 1 ? sc[0].y : 0.f, v1 = got & 2 ? sc[1].y : 0.f;
-                const float vnew = fmaxf(vref, fmaxf(v0, v1)), vinv = inverse_pow2(vnew), vfac = vref * vinv;
-                const float w0 = v0 * vinv * kWeightUp, w1 = v1 * vinv * kWeightUp;
+                float vnew = vref, w[SB];
+#pragma unroll
+                for (int i = 0; i < SB; ++i) {
+                    w[i] = got >> i & 1 ? sc[i].y : 0.f;
+                    vnew = fmaxf(vnew, w[i]);
+                }
+                const float vinv = inverse_pow2(vnew), vfac = vref * vinv;
+#pragma unroll
+                for (int i = 0; i < SB; ++i) w[i] = w[i] * vinv * kWeightUp;    // in this order: vinv may be 2^126
                 vref = vnew;
-                uint32_t pb[NQ][4];
+                uint32_t pb[NQ][2 * SB];
                 float fac[NQ];
                 bool same = true;
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) {
-                    const float f0 = qf[n] * sc[0].x, f1 = qf[n] * sc[1].x;
-                    float x[4][2], top = m[n];
+                    float x[2 * SB][2], top = m[n];
 #pragma unroll
-                    for (int nb = 0; nb < 4; ++nb)
+                    for (int nb = 0; nb < 2 * SB; ++nb)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            x[nb][e] = (s[n][nb][e] + s[n][nb][2 + e]) * (nb < 2 ? f0 : f1);
+                            x[nb][e] = (s[n][nb][e] + s[n][nb][2 + e]) * (qf[n] * sc[nb >> 1].x);
                             if (edge && (key0 + 8 * nb + 2 * q4 + e > lim[n] || !(got >> (nb >> 1) & 1)))
                                 x[nb][e] = -INFINITY;
                             top = fmaxf(top, x[nb][e]);
@@ -427,11 +518,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     m[n] = top;
                     float sum = 0.f;
 #pragma unroll
-                    for (int nb = 0; nb < 4; ++nb) {
+                    for (int nb = 0; nb < 2 * SB; ++nb) {
                         const float p0 = exp2_approx(x[nb][0] - ref), p1 = exp2_approx(x[nb][1] - ref);
                         sum += p0 + p1;
-                        const float w = nb < 2 ? w0 : w1;
-                        pb[n][nb] = f16_pack(p0 * w, p1 * w);
+                        pb[n][nb] = f16_pack(p0 * w[nb >> 1], p1 * w[nb >> 1]);
                     }
                     l[n] = l[n] * al + sum;
                     fac[n] = al * vfac;
@@ -449,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     }
                 }
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
+                for (int kb = 0; kb < SB; ++kb) {
                     if (!(got >> kb & 1)) continue;
 #pragma unroll
                     for (int dd = 0; dd < DT / 2; ++dd) {
@@ -462,9 +552,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                             for (int i = 0; i < 4; ++i) {
                                 uint32_t nan = ((vf[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
                                 if (nan) {
+                                    sm.any_nan[buf] = 1;
                                     for (int c = 0; c < 4; ++c)
                                         if (nan >> (8 * c + 7) & 1)
-                                            atomicMin(&nan_from[32 * dd + 8 * i + g],
+                                            atomicMin(&sm.nan_from[buf][32 * dd + 8 * i + g],
                                                       key0 + 16 * kb + 2 * q4 + (c & 1) + 8 * (c >> 1));
                                     vf[i] &= ~((nan >> 7) * 0xffu);
                                 }
@@ -482,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&empty[st]);
+            if (lane == 0) mbar_arrive(&sm.empty[st]);
         }
 
         // ------------------------------------------------- segment's end
@@ -495,48 +586,58 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[n][i][c] *= up;
         }
-        // join the warps with the same rows, halving their number each time
-        consumers_sync();
-        for (int d = WK / 2; d > 0; d >>= 1) {
-            const int buf = (wk & (d - 1)) * p.wr + wri;         // of the pair
-            float* mine = comb + buf * NQ * DT * 4 * 32 + lane;
-            if (wk >= d && wk < 2 * d) {
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-                    for (int i = 0; i < DT; ++i)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) mine[((n * DT + i) * 4 + c) * 32] = o[n][i][c];
-                    if (q4 == 0) ml[buf * 8 * NQ + 8 * n + g] = make_float2(m[n], l[n]);
-                }
-            }
-            consumers_sync();
-            if (wk < d) {
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-                    const float2 u = ml[buf * 8 * NQ + 8 * n + g];
-                    const float top = fmaxf(m[n], u.x), ref = top == -INFINITY ? 0.f : top;
-                    const float fa = exp2_approx(m[n] - ref), fb = exp2_approx(u.x - ref);
-                    m[n] = top;
-                    l[n] = l[n] * fa + u.y * fb;
-                    const float a0 = __shfl_sync(0xffffffffu, fa, 8 * q4), a1 = __shfl_sync(0xffffffffu, fa, 8 * q4 + 4);
-                    const float b0 = __shfl_sync(0xffffffffu, fb, 8 * q4), b1 = __shfl_sync(0xffffffffu, fb, 8 * q4 + 4);
-#pragma unroll
-                    for (int i = 0; i < DT; ++i)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            o[n][i][c] = o[n][i][c] * (c & 1 ? a1 : a0) + mine[((n * DT + i) * 4 + c) * 32] * (c & 1 ? b1 : b0);
-                }
-            }
-            consumers_sync();
-        }
-        const bool whole = t0 == 0 && t1 == at.tiles;
-        if (wk == 0 && wn > 0) {
-            float* slot = p.part + (size_t)(2 * blockIdx.x + (t0 == 0)) * p.rg * (HD + 4);
+        // the next segment's NaN marks: who read this buffer two segments ago has passed a barrier since
+        const int clear = buf == 2 ? 0 : buf + 1;
+        for (int i = tid; i < HD; i += 32 * kConsumers) sm.nan_from[clear][i] = INT32_MAX;
+        if (tid == 0) sm.any_nan[clear] = 0;
+        consumers_sync();                                        // and this segment's are complete
+        // join the warps with the same rows; each ends with DT / WK tiles of dims
+        int dt0 = 0;
+        float* comb = sm.comb[0];
+        float2* ml = sm.ml[0];
+        if (WK >= 2) dt0 = join<NQ, DT, DT>(o, m, l, comb, ml, warp, warp ^ 2, warp & 2);
+        if (WK == 4) dt0 += join<NQ, DT, DT / 2>(o, m, l, comb, ml, warp, warp ^ 1, warp & 1);
+        const bool whole = at.tile == 0 && at.end == at.tiles;
+        const bool any_nan = sm.any_nan[buf];
+        if (wn > 0) {
+            float* slot = p.part + (size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg * (HD + 4);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
+                const float inv = whole ? (l[n] == 0.f ? 0.f : 1.f / l[n]) : 1.f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float f = __shfl_sync(0xffffffffu, inv, 8 * q4 + 4 * e);
+                    const int r = m0 + 8 * n + 2 * q4 + e;
+                    if (any_nan) {
+                        const int seen = rows.pos0 + r / G;
+                        for (int i = 0; i < DT; ++i)
+                            for (int c = 0; c < 2; ++c)
+                                if (i < DT / WK && sm.nan_from[buf][16 * (dt0 + i) + 8 * c + g] <= seen)
+                                    set_nan<DT>(o[n], i, 2 * c + e);
+                    }
+                    if (r >= rows.n) continue;
+                    if (whole) {
+                        const int tok = r / G;
+                        __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row +
+                                             (int64_t)(at.h * G + r - tok * G) * t.out_head + 16 * dt0 + g;
+#pragma unroll
+                        for (int i = 0; i < DT; ++i)
+                            if (i < DT / WK) {
+                                out[16 * i] = __float2bfloat16_rn(o[n][i][e] * f);
+                                out[16 * i + 8] = __float2bfloat16_rn(o[n][i][2 + e] * f);
+                            }
+                    } else {
+                        float* out = slot + (size_t)r * (HD + 4) + 4 + 16 * dt0 + g;
+#pragma unroll
+                        for (int i = 0; i < DT; ++i)
+                            if (i < DT / WK) {
+                                out[16 * i] = o[n][i][e];
+                                out[16 * i + 8] = o[n][i][2 + e];
+                            }
+                    }
+                }
                 const int m_row = m0 + 8 * n + g;
-                if (q4 == 0 && m_row < rows.n) {
+                if (wk == 0 && q4 == 0 && m_row < rows.n) {
                     if (!whole) {
                         *reinterpret_cast<float2*>(slot + (size_t)m_row * (HD + 4)) = make_float2(m[n], l[n]);
                     } else if (t.lse) {
@@ -545,109 +646,111 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                             l[n] == 0.f ? -INFINITY : (m[n] + log2f(l[n])) * kLn2;
                     }
                 }
-                const float inv = whole ? (l[n] == 0.f ? 0.f : 1.f / l[n]) : 1.f;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float f = __shfl_sync(0xffffffffu, inv, 8 * q4 + 4 * e);
-                    const int r = m0 + 8 * n + 2 * q4 + e;
-                    if (r >= rows.n) continue;
-                    const int tok = r / G, seen = rows.pos0 + tok;
-                    __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row + (int64_t)(at.h * G + r - tok * G) * t.out_head;
-#pragma unroll
-                    for (int i = 0; i < DT; ++i)
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const int d = 16 * i + 8 * c + g;
-                            float v = o[n][i][2 * c + e] * f;
-                            if (nan_from[d] <= seen) v = __uint_as_float(0x7fc00000u);
-                            if (whole) out[d] = __float2bfloat16_rn(v);
-                            else slot[(size_t)r * (HD + 4) + 4 + d] = v;
-                        }
-                }
             }
         }
-        if (!whole && t0 == 0) {
+        if (!whole && at.tile == 0) {
             began = true;
-            if (tid == 0) {
-                const long long end = run.x1 - left + at.tiles;        // first tile after the unit
-                p.desc[blockIdx.x] = make_int4(at.s, at.h, at.g, (int)((end * run.ctas - 1) / run.total));
-            }
+            if (tid == 0)
+                p.desc[blockIdx.x] = make_int4(rows.row0, rows.n, at.h, run.cta_of(at.first + at.tiles - 1));
         }
-        left -= t1 - t0;
-        if (left > 0) {
-            consumers_sync();                                    // nan_from is read
-            for (int i = tid; i < HD; i += 32 * kConsumers) nan_from[i] = INT32_MAX;
-            consumers_sync();
-            at.next(a, p.tq);
-        }
+        if (!at.next(a, run, p)) break;
     }
     if (tid == 0) {
-        if (!began) p.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        if (!began) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         if (!alive) kv8_flag(a, kKv8Timeout);
     }
 }
 
-// Merge of the units that lie in several runs: CTA (x, y) takes kMergeRows rows
-// of the unit that begins in run x; the two warps of a row take every other
-// segment and meet in shared memory.
-constexpr int kMergeRows = 4, kMergeThreads = 64 * kMergeRows;
-template <int HD>
+// Merge of the units that lie in several runs: CTA (x, y) takes the x-th such
+// unit and 16 / MW of its rows.  The MW warps of a row take every so many of its
+// segments, each with its own maximum, and meet in shared memory: 8 where there
+// are fewer units than segments of one, else 2.
+constexpr int kMergeThreads = 512;
+template <int HD, int MW>
 __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args a, const Kv8AttnArgs t, const Plan p) {
-    constexpr int V = HD / 32;
+    constexpr int V = HD / 32, BATCH = 8, RW = kMergeThreads / 32 / MW;
+    using Vec = typename std::conditional<V == 4, float4, float2>::type;
+    static_assert(kMaxCtas <= kMergeThreads, "a thread per run");
+    __shared__ float acc_s[RW][MW][HD];
+    __shared__ float2 ml_s[RW][MW];
+    __shared__ int counts[kMergeThreads / 32];
+    __shared__ int4 unit;
+    __shared__ int run_x;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp % MW, G = t.hq / a.hk;
+    if (tid == 0) unit = make_int4(0, 0, 0, 0);
     grid_dependency_wait();
     if (a.stop && *a.stop) return;
-    const int4 u = p.desc[blockIdx.x];
-    if (u.x < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp & 1, G = t.hq / a.hk;
-    const Rows rows(kv8_seq(a, u.x), p.tq, u.z, G);
-    const int r = blockIdx.y * kMergeRows + (warp >> 1), parts = u.w - (int)blockIdx.x + 1;
-    __shared__ float other[kMergeRows][HD];
-    // segment i: run x + i; the first one is its run's second slot, a later one its first
+    // the x-th run in which such a unit begins
+    const int4 mine = tid < p.ctas ? p.desc[tid] : make_int4(0, 0, 0, 0);
+    const unsigned begins = __ballot_sync(0xffffffffu, mine.y > 0);
+    if (lane == 0) counts[warp] = __popc(begins);
+    __syncthreads();
+    int rank = __popc(begins & ((1u << lane) - 1));
+    for (int i = 0; i < warp; ++i) rank += counts[i];
+    if (mine.y > 0 && rank == (int)blockIdx.x) {
+        unit = mine;
+        run_x = tid;
+    }
+    __syncthreads();
+    const int4 u = unit;
+    const int rr = warp / MW, r = blockIdx.y * RW + rr;
+    if ((int)blockIdx.y * RW >= u.y) return;
+    const int first = run_x;
+    // segment i: run first + i; the first one is its run's second slot, a later one its first
     auto part = [&](int i) {
-        return p.part + ((size_t)(2 * (blockIdx.x + i) + (i == 0)) * p.rg + r) * (HD + 4);
+        return p.part + ((size_t)(2 * (first + i) + (i == 0)) * p.rg + r) * (HD + 4);
     };
+    const int parts = u.w - first + 1, n = r < u.y && parts > wm ? (parts - wm - 1) / MW + 1 : 0;
     float acc[V], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
-    if (r < rows.n) {
-        for (int i = lane; i < parts; i += 32) m = fmaxf(m, part(i)[0]);
-        m = warp_max(m);
-        const float ref = m == -INFINITY ? 0.f : m;
-        for (int c = 0; c < parts; c += 32) {
-            float w = 0.f;
-            if (c + lane < parts) {
-                const float2 x = *reinterpret_cast<const float2*>(part(c + lane));
-                w = exp2_approx(x.x - ref);
-                l += x.y * w;
-            }
-            const int n = min(32, parts - c);
-#pragma unroll 8
-            for (int i = half; i < n; i += 2) {
-                const float f = __shfl_sync(0xffffffffu, w, i);
-                const float* o = part(c + i) + 4 + V * lane;
-                if constexpr (V == 4) {
-                    const float4 x = *reinterpret_cast<const float4*>(o);
-                    acc[0] = fmaf(f, x.x, acc[0]); acc[1] = fmaf(f, x.y, acc[1]);
-                    acc[2] = fmaf(f, x.z, acc[2]); acc[3] = fmaf(f, x.w, acc[3]);
-                } else {
-                    const float2 x = *reinterpret_cast<const float2*>(o);
-                    acc[0] = fmaf(f, x.x, acc[0]); acc[1] = fmaf(f, x.y, acc[1]);
-                }
-            }
+    for (int c = 0; c < n; c += BATCH) {
+        float2 x = make_float2(-INFINITY, 0.f);
+        float o[BATCH][V];
+        if (lane < BATCH && c + lane < n) x = *reinterpret_cast<const float2*>(part(wm + (c + lane) * MW));
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+            if (c + i < n)
+                *reinterpret_cast<Vec*>(o[i]) =
+                    *reinterpret_cast<const Vec*>(part(wm + (c + i) * MW) + 4 + V * lane);
+        const float top = fmaxf(m, warp_max(x.x)), ref = top == -INFINITY ? 0.f : top;
+        const float old = exp2_approx(m - ref), w = exp2_approx(x.x - ref);
+        m = top;
+        l = l * old + warp_sum(x.y * w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] *= old;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const float f = __shfl_sync(0xffffffffu, w, i);
+            if (c + i < n)
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] = fmaf(f, o[i][j], acc[j]);
         }
-        l = warp_sum(l);
     }
-    if (half == 1)
 #pragma unroll
-        for (int i = 0; i < V; ++i) other[warp >> 1][V * lane + i] = acc[i];
+    for (int i = 0; i < V; ++i) acc_s[rr][wm][V * lane + i] = acc[i];
+    if (lane == 0) ml_s[rr][wm] = make_float2(m, l);
     __syncthreads();
-    if (half == 1 || r >= rows.n) return;
-    const int tok = r / G, head = u.y * G + r - tok * G;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row + (int64_t)head * t.out_head + V * lane;
+    if (wm != 0 || r >= u.y) return;
+    float top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) out[i] = __float2bfloat16_rn((acc[i] + other[warp >> 1][V * lane + i]) * inv);
-    if (t.lse && lane == 0) t.lse[(size_t)(rows.row0 + tok) * t.hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    for (int i = 0; i < MW; ++i) top = fmaxf(top, ml_s[rr][i].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < MW; ++i) {
+        const float f = exp2_approx(ml_s[rr][i].x - ref);
+        sum = fmaf(ml_s[rr][i].y, f, sum);
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = fmaf(acc_s[rr][i][V * lane + j], f, acc[j]);
+    }
+    const int tok = r / G, head = u.z * G + r - tok * G;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    __nv_bfloat16* out = t.out + (int64_t)(u.x + tok) * t.out_row + (int64_t)head * t.out_head + V * lane;
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = __float2bfloat16_rn(acc[i] * inv);
+    if (t.lse && lane == 0) t.lse[(size_t)(u.x + tok) * t.hq + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 // Rows of a group: the next of 8, 16, 32, 64 at or above the batch's average of
@@ -659,25 +762,40 @@ int rows_of_unit(int G, int64_t n_rows, int64_t n_seqs) {
     return rg;
 }
 
-template <int HD, int NQ>
-cudaError_t launch_hd(const Kv8Args& a, const Kv8AttnArgs& t, Plan p, bool split, cudaStream_t s) {
-    const int bytes = Smem<HD>::bytes(NQ);
-    static const cudaError_t set = cudaFuncSetAttribute(kv8_attention_kernel<HD, NQ>,
-                                                        cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (set != cudaSuccess) return set;
-    kv8_attention_kernel<HD, NQ><<<p.ctas, kThreads, bytes, s>>>(a, t, p);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || !split) return e;
+template <int HD, int NQ, int SB>
+cudaError_t launch_hd(const Kv8Args& a, const Kv8AttnArgs& t, Plan p, cudaStream_t s) {
+    const int G = t.hq / a.hk, bytes = sizeof(Smem<HD, NQ, SB>);
+    p.tile = kSteps * SB * kKv8Block;
+    p.cost = 128 * kUnitCost / p.tile;
+    const int64_t tiles = (a.capacity + p.tile - 1) / p.tile;
+    const int64_t units = (int64_t)a.hk * (a.n_rows / p.tq + a.n_seqs), most = units * (tiles + p.cost);
+    if (most > INT32_MAX) return cudaErrorInvalidValue;
+    p.ctas = (int)std::min<int64_t>(std::min(kMaxCtas, sm_count() * (NQ == 1 ? 3 : 2)), most);
+    auto kern = kv8_attention_kernel<HD, NQ, SB>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(p.ctas, (p.rg + kMergeRows - 1) / kMergeRows);
-    cfg.blockDim = dim3(kMergeThreads);
+    cfg.gridDim = dim3(p.ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv8_merge_kernel<HD>, a, t, p);
+    e = cudaLaunchKernelEx(&cfg, kern, a, t, p);
+    if (e != cudaSuccess || tiles <= 1) return e;      // no unit has a tile to cut off
+    const int used = std::min(p.rg, p.tq * G);
+    cfg.blockDim = dim3(kMergeThreads);
+    cfg.dynamicSmemBytes = 0;
+    const int x = (int)std::min<int64_t>(p.ctas, units);
+    if (units * units < p.ctas) {
+        cfg.gridDim = dim3(x, (used + 1) / 2);
+        return cudaLaunchKernelEx(&cfg, kv8_merge_kernel<HD, 8>, a, t, p);
+    }
+    cfg.gridDim = dim3(x, (used + 7) / 8);
+    return cudaLaunchKernelEx(&cfg, kv8_merge_kernel<HD, 2>, a, t, p);
 }
 
 }  // namespace
@@ -694,16 +812,11 @@ cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStr
     p.rg = rows_of_unit(G, a.n_rows, a.n_seqs);
     p.tq = p.rg / G;
     p.wr = p.rg <= 16 ? 1 : p.rg / 16;
-    const int64_t tiles = (a.capacity + kTile - 1) / kTile;
-    const int64_t most = (int64_t)a.hk * (a.n_rows / p.tq + a.n_seqs) * std::max<int64_t>(tiles, 1);
-    p.ctas = (int)std::min<int64_t>(std::min(kMaxCtas, sm_count() * (p.rg == 8 ? 3 : 2)), most);
     p.q_wide = reinterpret_cast<uintptr_t>(t.q) % 8 == 0 && t.q_row % 4 == 0 && t.q_head % 4 == 0;
     p.desc = static_cast<int4*>(t.workspace);
     p.part = reinterpret_cast<float*>(p.desc + kMaxCtas);
-    const bool split = tiles > 1;
-    if (a.hd == 128)
-        return p.rg == 8 ? launch_hd<128, 1>(a, t, p, split, s) : launch_hd<128, 2>(a, t, p, split, s);
-    return p.rg == 8 ? launch_hd<64, 1>(a, t, p, split, s) : launch_hd<64, 2>(a, t, p, split, s);
+    if (a.hd == 128) return p.rg == 8 ? launch_hd<128, 1, 1>(a, t, p, s) : launch_hd<128, 2, 2>(a, t, p, s);
+    return p.rg == 8 ? launch_hd<64, 1, 1>(a, t, p, s) : launch_hd<64, 2, 2>(a, t, p, s);
 }
 
 }  // namespace ks

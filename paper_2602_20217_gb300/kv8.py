@@ -14,9 +14,13 @@ place.  Calls go to torch's current stream unless one is given.
 """
 from __future__ import annotations
 
-import ctypes as C
+import torch
+from torch import cuda as _cuda
 
 from . import knapspec as ks
+
+_BF16 = (torch.bfloat16,)
+_KINDS = {torch.bfloat16: (ks.KS_DTYPE_BF16, _BF16), torch.float32: (ks.KS_DTYPE_F32, (torch.float32,))}
 
 
 def _check(t, name: str, dtypes, ndim: int, device):
@@ -33,7 +37,6 @@ class Batch8:
     lengths int32 [n_seqs] on the device; status: int32 [1] for what only the device can see."""
 
     def __init__(self, page_table, row_offsets, lengths, n_rows: int, status=None):
-        import torch
         dev = page_table.device
         _check(page_table, "page_table", (torch.int32,), 2, dev)
         _check(row_offsets, "row_offsets", (torch.int32,), 1, dev)
@@ -61,7 +64,6 @@ class Cache8:
     """One layer's cache.  data: uint8, at least nbytes of it (allocated here if not given)."""
 
     def __init__(self, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, data=None, device="cuda"):
-        import torch
         self.nbytes = ks.ks_kv8_bytes(n_pages, page_tokens, n_kv_heads, head_dim)
         if self.nbytes == 0:
             raise ks.KsError(ks.KS_ERR_INVALID_ARG, "Cache8", f"sizes not supported: {n_pages} pages of {page_tokens} "
@@ -75,64 +77,62 @@ class Cache8:
         self.c = ks.KsKv8Cache(data.data_ptr(), n_pages, page_tokens, n_kv_heads, head_dim)
 
     def _stream(self, stream):
-        import torch
-        if self.device.index != torch.cuda.current_device():
+        if self.device.index != _cuda.current_device():
             raise ValueError(f"the cache is on {self.device}, not on the current device")
-        return torch.cuda.current_stream() if stream is None else stream
+        return _cuda.current_stream().cuda_stream if stream is None else ks._stream_ptr(stream)
 
-    def _rows(self, t, name, dtypes, batch, heads):
-        _check(t, name, dtypes, 3, self.device)
-        if t.shape[0] < batch.n_rows or (heads is not None and t.shape[1] != heads) or t.shape[2] != self.head_dim:
-            raise ValueError(f"{name}: shape {tuple(t.shape)} for {batch.n_rows} rows, head_dim {self.head_dim}")
-        if t.stride(2) != 1:
-            raise ValueError(f"{name}: a head's values are not contiguous")
+    def _rows(self, t, name, kinds, batch, heads=None):
+        """Row and head stride of a [rows, heads, head_dim] tensor, after its checks."""
+        shape, stride = t.shape, t.stride()
+        if (len(shape) != 3 or shape[2] != self.head_dim or shape[0] < batch.n_rows or t.dtype not in kinds or
+                t.device != self.device or stride[2] != 1 or (heads is not None and shape[1] != heads)):
+            _check(t, name, kinds, 3, self.device)
+            raise ValueError(f"{name}: shape {tuple(shape)}, strides {stride} for {batch.n_rows} rows, "
+                             f"{'any' if heads is None else heads} heads of {self.head_dim} contiguous values")
+        return stride[0], stride[1]
 
     def append(self, batch: Batch8, k, v, rope=None, q=None, q_out=None, stream=None):
         """Append k, v [n_rows, n_kv_heads, head_dim] (fp32 or bf16); rope [positions, head_dim / 2, 2] fp32 rotates
         the keys, and the queries q [n_rows, n_q_heads, head_dim] into q_out (bf16)."""
-        import torch
         s = self._stream(stream)
-        kinds = (k.dtype,) if k.dtype in (torch.float32, torch.bfloat16) else (torch.float32, torch.bfloat16)
-        self._rows(k, "k", kinds, batch, self.n_kv_heads)
-        self._rows(v, "v", kinds, batch, self.n_kv_heads)
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
-        r = ks.KsKv8Rows(k.data_ptr(), v.data_ptr(), None,
-                         ks.KS_DTYPE_BF16 if k.dtype == torch.bfloat16 else ks.KS_DTYPE_F32, 0,
-                         k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+        code, kinds = _KINDS.get(k.dtype, (0, tuple(_KINDS)))
+        k_row, k_head = self._rows(k, "k", kinds, batch, self.n_kv_heads)
+        v_row, v_head = self._rows(v, "v", kinds, batch, self.n_kv_heads)
+        angles, positions = None, 0
         if rope is not None:
-            _check(rope, "rope", (torch.float32,), 3, self.device)
-            if tuple(rope.shape[1:]) != (self.head_dim // 2, 2) or not rope.is_contiguous():
-                raise ValueError(f"rope: shape {tuple(rope.shape)}")
-            r.rope, r.rope_rows = rope.data_ptr(), rope.shape[0]
-        if (q is None) != (q_out is None):
+            shape = rope.shape
+            if rope.dtype != torch.float32 or rope.device != self.device or len(shape) != 3 or \
+                    shape[1] != self.head_dim // 2 or shape[2] != 2 or not rope.is_contiguous():
+                raise ValueError(f"rope: {rope.dtype} of shape {tuple(shape)} on {rope.device}")
+            angles, positions = rope.data_ptr(), shape[0]
+        if q is None and q_out is None:
+            r = ks.KsKv8Rows(k.data_ptr(), v.data_ptr(), None, code, 0, k_row, k_head, v_row, v_head, 0, 0, angles,
+                             positions)
+        elif q is None or q_out is None:
             raise ValueError("q and q_out go together")
-        if q is not None:
-            self._rows(q, "q", kinds, batch, None)
-            self._rows(q_out, "q_out", (torch.bfloat16,), batch, q.shape[1])
-            r.q, r.n_q_heads, r.q_row, r.q_head = q.data_ptr(), q.shape[1], q.stride(0), q.stride(1)
-            r.q_out, r.q_out_row, r.q_out_head = q_out.data_ptr(), q_out.stride(0), q_out.stride(1)
+        else:
+            q_row, q_head = self._rows(q, "q", kinds, batch)
+            o_row, o_head = self._rows(q_out, "q_out", _BF16, batch, q.shape[1])
+            r = ks.KsKv8Rows(k.data_ptr(), v.data_ptr(), q.data_ptr(), code, q.shape[1], k_row, k_head, v_row, v_head,
+                             q_row, q_head, angles, positions, q_out.data_ptr(), o_row, o_head)
         ks.ks_kv8_append(self.c, batch.c, r, s)
 
     def read(self, batch: Batch8, k_out, v_out, stream=None):
         """The values of the batch's rows into k_out, v_out [n_rows, n_kv_heads, head_dim] (fp32 or bf16)."""
-        import torch
         s = self._stream(stream)
-        kinds = (k_out.dtype,) if k_out.dtype in (torch.float32, torch.bfloat16) else (torch.float32, torch.bfloat16)
-        self._rows(k_out, "k_out", kinds, batch, self.n_kv_heads)
-        self._rows(v_out, "v_out", kinds, batch, self.n_kv_heads)
-        if k_out.stride() != v_out.stride():
-            raise ValueError("k_out and v_out differ in their strides")
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
-        ks.ks_kv8_read(self.c, batch.c, k_out, v_out,
-                       ks.KS_DTYPE_BF16 if k_out.dtype == torch.bfloat16 else ks.KS_DTYPE_F32,
-                       k_out.stride(0), k_out.stride(1), s)
+        code, kinds = _KINDS.get(k_out.dtype, (0, tuple(_KINDS)))
+        strides = self._rows(k_out, "k_out", kinds, batch, self.n_kv_heads)
+        if self._rows(v_out, "v_out", kinds, batch, self.n_kv_heads) != strides:
+            raise ValueError("k_out and v_out differ in their strides")
+        ks.ks_kv8_read(self.c, batch.c, k_out.data_ptr(), v_out.data_ptr(), code, *strides, s)
         return k_out, v_out
 
     def attention_workspace(self, n_q_heads: int, n_seqs: int, n_rows: int):
         """A workspace of attention() for these sizes or smaller ones; calls that run at once need one each."""
-        import torch
         n = ks.ks_kv8_attention_workspace(self.c, n_q_heads, n_seqs, n_rows)
         if n == 0:
             raise ks.KsError(ks.KS_ERR_INVALID_ARG, "attention_workspace", f"{n_q_heads} query heads over "
@@ -142,26 +142,25 @@ class Cache8:
     def attention(self, batch: Batch8, q, scale=None, out=None, lse=None, workspace=None, stream=None):
         """Causal attention of the batch's rows: q, out [n_rows, n_q_heads, head_dim] bf16, lse [n_rows, n_q_heads]
         fp32.  scale: head_dim ** -0.5 if not given.  Returns out."""
-        import torch
         s = self._stream(stream)
-        self._rows(q, "q", (torch.bfloat16,), batch, None)
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
+        q_row, q_head = self._rows(q, "q", _BF16, batch)
         hq = q.shape[1]
         if out is None:
             out = torch.zeros(q.shape, dtype=torch.bfloat16, device=self.device)
-        self._rows(out, "out", (torch.bfloat16,), batch, hq)
+        o_row, o_head = self._rows(out, "out", _BF16, batch, hq)
+        sums = None
         if lse is not None:
             _check(lse, "lse", (torch.float32,), 2, self.device)
             if lse.shape[0] < batch.n_rows or lse.shape[1] != hq or not lse.is_contiguous():
                 raise ValueError(f"lse: shape {tuple(lse.shape)}")
+            sums = lse.data_ptr()
         if workspace is None:
             workspace = self.attention_workspace(hq, batch.n_seqs, batch.n_rows)
         elif workspace.device != self.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
             raise ValueError("workspace: contiguous bytes on the cache's device expected")
-        a = ks.KsKv8Attn(q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
-                         None if lse is None else lse.data_ptr(), hq,
-                         float(self.head_dim ** -0.5 if scale is None else scale), workspace.data_ptr(),
-                         workspace.numel())
+        a = ks.KsKv8Attn(q.data_ptr(), q_row, q_head, out.data_ptr(), o_row, o_head, sums, hq,
+                         self.head_dim ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel())
         ks.ks_kv8_attention(self.c, batch.c, a, s)
         return out
