@@ -297,6 +297,7 @@ struct Kv8AttnArgs {
 constexpr int kKv8MaxGroup = 64;    // query heads a KV head
 cudaError_t launch_kv8_append(int dtype, const Kv8Args& a, const Kv8RowArgs& r, cudaStream_t s);
 size_t kv8_attention_workspace(int hd, int group, int n_rows);
+bool kv8_attention_fits(const Kv8Args& a, int hq);     // false: too many units and tiles for one call
 cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s);
 
 }  // namespace ks

@@ -455,6 +455,10 @@ extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_ba
         set_error("ks_kv8_attention: null or misaligned queries or output, or bad strides");
         return KS_ERR_INVALID_ARG;
     }
+    if (!kv8_attention_fits(a, attn->n_q_heads)) {
+        set_error("ks_kv8_attention: %d rows over up to %d tokens are too much for one call", a.n_rows, a.capacity);
+        return KS_ERR_UNSUPPORTED;
+    }
     const size_t need = kv8_attention_workspace(a.hd, attn->n_q_heads / a.hk, a.n_rows);
     if (!attn->workspace || !aligned(attn->workspace, 256)) {
         set_error("ks_kv8_attention: null or misaligned workspace");

@@ -1,27 +1,20 @@
-// Causal attention over the 8-bit paged cache, any number of rows a sequence.
+// Causal attention over the 8-bit paged cache: units of at most 16 query rows
+// (decoding), the merge of split units for every size, and the choice between
+// this kernel and the tcgen05 one (kv8_tc.cu).  kv8_plan.cuh cuts the work.
 //
-// Work.  A unit is (sequence, KV head, group of rows): a group is as many whole
-// tokens as give at most RG query rows (token x query head of the KV head), and
-// its keys come in tiles of 128.  The units' tiles, one after the other, are cut
-// into equal runs, one per resident CTA, so a long sequence among short ones or
-// few heads at a long context keep every SM busy; the lengths are read on the
-// device.  A run's part of a unit is a segment.  Units that lie in several runs
-// leave (m, l, o) per segment, merged in run order by a second launch; the
-// result depends on the batch, never on timing.
-//
-// A CTA is a producer warp and four consumer warps around a ring of two tiles.
-// A tile is 8 records of the cache, one contiguous copy each, wherever their
-// pages are.  RG = 8 NQ WR rows: WR warps take 8 NQ rows each, and the 4 / WR
-// warps with the same rows take every so many of a tile's four 32-key steps,
-// with softmax statistics of their own, joined at the segment's end.
+// A CTA is a producer warp and four consumer warps around a ring of tiles of
+// 64 NQ keys.  A tile is 4 NQ records of the cache, one contiguous copy each,
+// wherever their pages are.  All four warps have the unit's 8 NQ rows, each
+// takes one 16 NQ-key step of every tile, with softmax statistics of its own,
+// and they are joined at the segment's end.
 //
 // A step, per 8 rows:
-//   S (8 rows x 32 keys) = Q K^T by m16n8k32 e4m3: the cached codes go to the
-//     tensor cores as they are (they run at four times the f16 rate of the same
-//     instruction: 4000 against 1024 multiply-adds per SM and clock), and the
-//     16 rows of the A operand are the queries' 8 rows in two codes each, hi =
-//     e4m3(q 2^-e), lo = e4m3(q 2^-e - hi), which holds every bf16 query down
-//     to 2^-10 of its row's largest element exactly;
+//   S (8 rows x 16 keys) = Q K^T by m16n8k32 e4m3: the cached codes go to the
+//     tensor cores as they are (4000 multiply-adds per SM and clock in this
+//     instruction, 1024 in its f16 form), and the 16 rows of the A operand are
+//     the queries' 8 rows in two codes each, hi = e4m3(q 2^-e), lo = e4m3(q
+//     2^-e - hi), which hold every bf16 query down to 2^-10 of its row's
+//     largest element exactly;
 //   online softmax in fp32, base 2, the keys' block scale folded into the
 //     scores;
 //   O^T (dims x 8 rows) += V^T P^T by m16n8k16 f16: P in 11 bits, times the
@@ -35,8 +28,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "kv8.cuh"
-#include "tma.cuh"
+#include "kv8_plan.cuh"
 
 namespace ks {
 
@@ -44,151 +36,8 @@ namespace {
 
 constexpr int kConsumers = 4;
 constexpr int kThreads = 32 * (kConsumers + 1);
-constexpr int kSteps = 4;           // steps of a tile
-constexpr int kMaxCtas = 480;       // the workspace has room for this many
-constexpr int kMaxRowsOfUnit = 64;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kWeightUp = 16384.f;
-// A unit's fixed cost (queries, joining its warps, output) in the time of 128
-// keys, for the cut into runs.
-constexpr int kUnitCost = 2;
 
-struct Plan {
-    int tile;           // keys of a tile
-    int cost;           // a unit's fixed cost in tiles
-    int wr;             // warps of different rows
-    int tq;             // tokens of a group
-    int rg;             // rows of a group, at least tq query groups
-    int ctas;
-    bool q_wide;        // queries can be read 8 bytes at a time
-    float* part;        // [2 ctas][rg][HD + 4]: m, l, -, -, o
-    int4* desc;         // [ctas]: the unit that begins in this CTA's run and ends in a later one's: first batch row,
-                        // query rows (0: no such unit), KV head, last CTA
-};
-
-// Tiles of group g; a group whose rows see nothing has one as well (its rows get zeros).
-KS_DEV int group_tiles(const Kv8Seq& q, const Plan& p, int g) {
-    const int last = q.len - q.rows + min(q.rows, (g + 1) * p.tq) - 1;
-    return last < 0 ? 1 : (unsigned)last / (unsigned)p.tile + 1;
-}
-KS_DEV int groups_of(const Kv8Seq& q, int tq) { return (q.rows + tq - 1) / tq; }
-// What the units of one head of a sequence take on the line of all units.
-KS_DEV int head_length(const Kv8Seq& q, const Plan& p) {
-    int n = 0;
-    for (int g = 0; g < groups_of(q, p.tq); ++g) n += group_tiles(q, p, g) + p.cost;
-    return n;
-}
-
-// The line of all units, each its fixed cost and its tiles long, cut into equal runs
-// [x0, x1): a CTA works on the tiles in its run.
-struct Run {
-    int ctas, each, more;       // runs of each + 1 (the first `more`), then of each
-    int x0, x1;
-    KS_DEV void cut(int total, int most, int cta) {
-        ctas = min(most, total);
-        each = ctas ? total / ctas : 0;
-        more = total - each * ctas;
-        x0 = cta * each + min(cta, more);
-        x1 = x0 + each + (cta < more);
-    }
-    KS_DEV int cta_of(int x) const {
-        const int b = more * (each + 1);
-        return x < b ? x / (each + 1) : more + (x - b) / each;
-    }
-};
-
-// A segment: tiles [tile, end) of a unit, whose first tile is at `first` on the line.
-struct Segment {
-    int s, h, g, tile, end, tiles, first;
-    Kv8Seq q;
-    KS_DEV void at(const Run& r, const Plan& p, int start) {
-        tiles = group_tiles(q, p, g);
-        first = start + p.cost;
-        tile = max(0, r.x0 - first);
-        end = min(tiles, r.x1 - first);
-    }
-    // the next unit, if a tile of it is in the run
-    KS_DEV bool next(const Kv8Args& a, const Run& r, const Plan& p) {
-        const int start = first + tiles;
-        if (start + p.cost >= r.x1) return false;
-        if (++g >= groups_of(q, p.tq)) {
-            g = 0;
-            if (++h >= a.hk) {
-                h = 0;
-                do {
-                    if (++s >= a.n_seqs) return false;
-                    q = kv8_seq(a, s);
-                } while (q.rows == 0);
-            }
-        }
-        at(r, p, start);
-        return true;
-    }
-};
-
-// This CTA's run and its first segment; false if it has none.  Every warp finds
-// it by itself, 32 sequences at a time.
-KS_DEV bool find_run(const Kv8Args& a, const Plan& p, Run& r, Segment& k) {
-    const int lane = threadIdx.x & 31, cta = blockIdx.x;
-    Kv8Seq mine{};
-    auto load = [&](int c) {
-        const int s = c + lane;
-        if (s >= a.n_seqs) {
-            mine = Kv8Seq{};
-            return 0;
-        }
-        mine = kv8_seq(a, s);
-        return a.hk * head_length(mine, p);
-    };
-    int total = 0, v = 0;
-    for (int c = 0; c < a.n_seqs; c += 32) {
-        v = load(c);
-        if (cta == 0 && c + lane < a.n_seqs && kv8_seq_bad(a, c + lane)) kv8_flag(a, kKv8BadBatch);
-        total += __reduce_add_sync(0xffffffffu, v);
-    }
-    r.cut(total, p.ctas, cta);
-    if (cta >= r.ctas) return false;
-    int start = 0;                               // of the sequence's units on the line
-    for (int c = 0;; c += 32) {
-        if (a.n_seqs > 32) v = load(c);
-        int u = v;                               // inclusive sums
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int w = __shfl_up_sync(0xffffffffu, u, o);
-            if (lane >= o) u += w;
-        }
-        const unsigned past = __ballot_sync(0xffffffffu, start + u > r.x0);
-        if (past) {
-            const int i = __ffs(past) - 1;
-            k.s = c + i;
-            k.q.row0 = __shfl_sync(0xffffffffu, mine.row0, i);
-            k.q.rows = __shfl_sync(0xffffffffu, mine.rows, i);
-            k.q.len = __shfl_sync(0xffffffffu, mine.len, i);
-            start += __shfl_sync(0xffffffffu, u - v, i);
-            break;
-        }
-        start += __shfl_sync(0xffffffffu, u, 31);
-    }
-    const int len = head_length(k.q, p);
-    k.h = (r.x0 - start) / len;
-    start += k.h * len;
-    k.g = 0;
-    for (;;) {
-        k.at(r, p, start);
-        if (r.x0 < k.first + k.tiles) break;
-        start = k.first + k.tiles;
-        ++k.g;
-    }
-    // a run that ends before the unit's first tile has nothing to do
-    return k.end > k.tile;
-}
-
-KS_DEV void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-        "l"(src), "r"(bytes), "r"(smem_u32(bar))
-        : "memory");
-}
 KS_DEV void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -198,21 +47,6 @@ KS_DEV void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-KS_DEV uint32_t f16_of(uint16_t codes) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(codes));
-    return h;
-}
-KS_DEV uint32_t f16_pack(float lo, float hi) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
-    return h;
-}
-KS_DEV float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 KS_DEV float quad_max(float v) {
     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
@@ -224,24 +58,12 @@ KS_DEV float quad_sum(float v) {
 }
 KS_DEV void consumers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-// A unit's rows, as its segments and the merge see them.
-struct Rows {
-    int n;              // query rows: tokens x G
-    int row0;           // batch row of the first token
-    int pos0;           // its position; negative positions see nothing
-    KS_DEV Rows(const Kv8Seq& q, int tq, int g, int G) {
-        const int t0 = g * tq, t = min(q.rows - t0, tq);
-        n = t * G;
-        row0 = q.row0 + t0;
-        pos0 = q.len - q.rows + t0;
-    }
-};
-
-// A CTA's shared memory.  SB: records of a step.
-template <int HD, int NQ, int SB>
+// A CTA's shared memory.
+template <int HD, int NQ>
 struct Smem {
     static constexpr int REC = kv8_record(HD);
-    static constexpr int BLOCKS = kSteps * SB;                   // records of a tile
+    static constexpr int SB = NQ;                                // records of a step
+    static constexpr int BLOCKS = kConsumers * SB;                   // records of a tile
     static constexpr int TILE = BLOCKS * REC;
     static constexpr int STAGES = NQ == 1 ? 4 : 2;
     static constexpr int HALF = NQ * (HD / 32) * 4 * 32;         // floats: half of a warp's o
@@ -305,11 +127,11 @@ KS_DEV int join(float (&o)[NQ][DT][4], float (&m)[NQ], float (&l)[NQ], float* co
     return upper ? H : 0;
 }
 
-template <int HD, int NQ, int SB>
+template <int HD, int NQ>
 __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
-    kv8_attention_kernel(const Kv8Args a, const Kv8AttnArgs t, const Plan p) {
-    using S = Smem<HD, NQ, SB>;
-    constexpr int REC = S::REC, BLOCKS = S::BLOCKS, STAGES = S::STAGES, DT = HD / 16, KJ = HD / 32;
+    kv8_attention_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
+    using S = Smem<HD, NQ>;
+    constexpr int REC = S::REC, SB = S::SB, BLOCKS = S::BLOCKS, STAGES = S::STAGES, DT = HD / 16, KJ = HD / 32;
     extern __shared__ __align__(128) unsigned char smem_raw[];
     S& sm = *reinterpret_cast<S*>(smem_raw);
     volatile int* present = sm.present;
@@ -389,8 +211,6 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 
     // ----------------------------------------------------------- consumers
     const int g = lane >> 2, q4 = lane & 3;
-    const int wri = warp % p.wr, wk = warp / p.wr, WK = kConsumers / p.wr;
-    const int m0 = wri * 8 * NQ;
     int it = 0;
     bool alive = true, began = false;
     for (int buf = 0;; buf = buf == 2 ? 0 : buf + 1) {
@@ -399,11 +219,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         uint32_t qa[NQ][KJ][4];
         float qf[NQ];
         int lim[NQ];                                             // last key that the row sees
-        const int wn = min(rows.n - m0, 8 * NQ);                 // rows of this warp
-        const int lim_first = rows.pos0 + m0 / G, lim_last = rows.pos0 + (m0 + wn - 1) / G;
+        const int lim_first = rows.pos0, lim_last = rows.pos0 + (rows.n - 1) / G;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            const int m = m0 + 8 * n + g;
+            const int m = 8 * n + g;
             const bool valid = m < rows.n;
             const int tok = valid ? m / G : 0, head = at.h * G + (valid ? m - tok * G : 0);
             const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head;
@@ -459,11 +278,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         for (int tile = at.tile; tile < at.end; ++tile, ++it) {
             const int st = it % STAGES;
             if (alive) alive = mbar_wait(&sm.full[st], (it / STAGES) & 1, kWaitLimitNs);
-            const int have = alive && wn > 0 ? present[st] : 0;
-            for (int step = wk; step < kSteps; step += WK) {
-                const int got = have >> (SB * step) & ((1 << SB) - 1), key0 = (tile * kSteps + step) * SB * kKv8Block;
-                if (got == 0 || key0 > lim_last) continue;
-                const unsigned char* rec = sm.ring[st] + SB * step * REC;
+            const int have = alive ? present[st] : 0;
+            const int got = have >> (SB * warp) & ((1 << SB) - 1), key0 = (tile * kConsumers + warp) * SB * kKv8Block;
+            if (got != 0 && key0 <= lim_last) {
+                const unsigned char* rec = sm.ring[st] + SB * warp * REC;
                 const uint32_t base = smem_u32(rec);
                 const bool edge = got != (1 << SB) - 1 || key0 + SB * kKv8Block - 1 > lim_first;
                 float2 sc[SB];                                   // key and value scales
@@ -591,15 +409,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         for (int i = tid; i < HD; i += 32 * kConsumers) sm.nan_from[clear][i] = INT32_MAX;
         if (tid == 0) sm.any_nan[clear] = 0;
         consumers_sync();                                        // and this segment's are complete
-        // join the warps with the same rows; each ends with DT / WK tiles of dims
-        int dt0 = 0;
-        float* comb = sm.comb[0];
-        float2* ml = sm.ml[0];
-        if (WK >= 2) dt0 = join<NQ, DT, DT>(o, m, l, comb, ml, warp, warp ^ 2, warp & 2);
-        if (WK == 4) dt0 += join<NQ, DT, DT / 2>(o, m, l, comb, ml, warp, warp ^ 1, warp & 1);
+        // join the warps; each ends with a quarter of the dims
+        int dt0 = join<NQ, DT, DT>(o, m, l, sm.comb[0], sm.ml[0], warp, warp ^ 2, warp & 2);
+        dt0 += join<NQ, DT, DT / 2>(o, m, l, sm.comb[0], sm.ml[0], warp, warp ^ 1, warp & 1);
         const bool whole = at.tile == 0 && at.end == at.tiles;
         const bool any_nan = sm.any_nan[buf];
-        if (wn > 0) {
+        {
             float* slot = p.part + (size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg * (HD + 4);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
@@ -607,12 +422,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float f = __shfl_sync(0xffffffffu, inv, 8 * q4 + 4 * e);
-                    const int r = m0 + 8 * n + 2 * q4 + e;
+                    const int r = 8 * n + 2 * q4 + e;
                     if (any_nan) {
                         const int seen = rows.pos0 + r / G;
-                        for (int i = 0; i < DT; ++i)
+                        for (int i = 0; i < DT / 4; ++i)
                             for (int c = 0; c < 2; ++c)
-                                if (i < DT / WK && sm.nan_from[buf][16 * (dt0 + i) + 8 * c + g] <= seen)
+                                if (sm.nan_from[buf][16 * (dt0 + i) + 8 * c + g] <= seen)
                                     set_nan<DT>(o[n], i, 2 * c + e);
                     }
                     if (r >= rows.n) continue;
@@ -621,23 +436,21 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                         __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row +
                                              (int64_t)(at.h * G + r - tok * G) * t.out_head + 16 * dt0 + g;
 #pragma unroll
-                        for (int i = 0; i < DT; ++i)
-                            if (i < DT / WK) {
-                                out[16 * i] = __float2bfloat16_rn(o[n][i][e] * f);
-                                out[16 * i + 8] = __float2bfloat16_rn(o[n][i][2 + e] * f);
-                            }
+                        for (int i = 0; i < DT / 4; ++i) {
+                            out[16 * i] = __float2bfloat16_rn(o[n][i][e] * f);
+                            out[16 * i + 8] = __float2bfloat16_rn(o[n][i][2 + e] * f);
+                        }
                     } else {
                         float* out = slot + (size_t)r * (HD + 4) + 4 + 16 * dt0 + g;
 #pragma unroll
-                        for (int i = 0; i < DT; ++i)
-                            if (i < DT / WK) {
-                                out[16 * i] = o[n][i][e];
-                                out[16 * i + 8] = o[n][i][2 + e];
-                            }
+                        for (int i = 0; i < DT / 4; ++i) {
+                            out[16 * i] = o[n][i][e];
+                            out[16 * i + 8] = o[n][i][2 + e];
+                        }
                     }
                 }
-                const int m_row = m0 + 8 * n + g;
-                if (wk == 0 && q4 == 0 && m_row < rows.n) {
+                const int m_row = 8 * n + g;
+                if (warp == 0 && q4 == 0 && m_row < rows.n) {
                     if (!whole) {
                         *reinterpret_cast<float2*>(slot + (size_t)m_row * (HD + 4)) = make_float2(m[n], l[n]);
                     } else if (t.lse) {
@@ -667,10 +480,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 // are fewer units than segments of one, else 2.
 constexpr int kMergeThreads = 512;
 template <int HD, int MW>
-__global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args a, const Kv8AttnArgs t, const Plan p) {
+__global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
     constexpr int V = HD / 32, BATCH = 8, RW = kMergeThreads / 32 / MW;
     using Vec = typename std::conditional<V == 4, float4, float2>::type;
-    static_assert(kMaxCtas <= kMergeThreads, "a thread per run");
+    static_assert(kKv8MaxCtas <= kMergeThreads, "a thread per run");
     __shared__ float acc_s[RW][MW][HD];
     __shared__ float2 ml_s[RW][MW];
     __shared__ int counts[kMergeThreads / 32];
@@ -753,70 +566,75 @@ __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args 
     if (t.lse && lane == 0) t.lse[(size_t)(u.x + tok) * t.hq + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-// Rows of a group: the next of 8, 16, 32, 64 at or above the batch's average of
-// query rows per sequence and KV head, and above G (whole tokens).
+// Query rows of a unit: 8 or 16 for this file's kernel, else the tcgen05
+// kernel's 128, by the batch's average per sequence and KV head, and at least G
+// (whole tokens).
 int rows_of_unit(int G, int64_t n_rows, int64_t n_seqs) {
     const int64_t avg = n_seqs > 0 ? (n_rows * G + n_seqs - 1) / n_seqs : 0;
-    int rg = 8;
-    while (rg < kMaxRowsOfUnit && (rg < avg || rg < G)) rg *= 2;
-    return rg;
+    const int64_t need = std::max<int64_t>(avg, G);
+    return need <= 8 ? 8 : need <= 16 ? 16 : kKv8TcRows;
 }
 
-template <int HD, int NQ, int SB>
-cudaError_t launch_hd(const Kv8Args& a, const Kv8AttnArgs& t, Plan p, cudaStream_t s) {
-    const int G = t.hq / a.hk, bytes = sizeof(Smem<HD, NQ, SB>);
-    p.tile = kSteps * SB * kKv8Block;
+template <int HD, int NQ>
+cudaError_t launch_few(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s) {
+    auto kern = kv8_attention_kernel<HD, NQ>;
+    constexpr int bytes = sizeof(Smem<HD, NQ>);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, a, t, p, s);
+}
+
+template <int HD>
+cudaError_t launch_merge(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, int64_t units, cudaStream_t s) {
+    const int x = (int)std::min<int64_t>(p.ctas, units), rows = p.tq * (t.hq / a.hk);
+    if (units * units < p.ctas)
+        return launch_kv8(kv8_merge_kernel<HD, 8>, dim3(x, (rows + 1) / 2), kMergeThreads, 0, a, t, p, s);
+    return launch_kv8(kv8_merge_kernel<HD, 2>, dim3(x, (rows + 7) / 8), kMergeThreads, 0, a, t, p, s);
+}
+
+// The plan of a call; false if its line of tiles is too long for 32 bits.
+bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& tiles) {
+    const int G = hq / a.hk;
+    p = Kv8Plan{};
+    p.rg = rows_of_unit(G, a.n_rows, a.n_seqs);
+    p.tq = p.rg / G;
+    p.tile = p.rg == 8 ? 64 : 128;
     p.cost = 128 * kUnitCost / p.tile;
-    const int64_t tiles = (a.capacity + p.tile - 1) / p.tile;
-    const int64_t units = (int64_t)a.hk * (a.n_rows / p.tq + a.n_seqs), most = units * (tiles + p.cost);
-    if (most > INT32_MAX) return cudaErrorInvalidValue;
-    p.ctas = (int)std::min<int64_t>(std::min(kMaxCtas, sm_count() * (NQ == 1 ? 3 : 2)), most);
-    auto kern = kv8_attention_kernel<HD, NQ, SB>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(p.ctas);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kern, a, t, p);
-    if (e != cudaSuccess || tiles <= 1) return e;      // no unit has a tile to cut off
-    const int used = std::min(p.rg, p.tq * G);
-    cfg.blockDim = dim3(kMergeThreads);
-    cfg.dynamicSmemBytes = 0;
-    const int x = (int)std::min<int64_t>(p.ctas, units);
-    if (units * units < p.ctas) {
-        cfg.gridDim = dim3(x, (used + 1) / 2);
-        return cudaLaunchKernelEx(&cfg, kv8_merge_kernel<HD, 8>, a, t, p);
-    }
-    cfg.gridDim = dim3(x, (used + 7) / 8);
-    return cudaLaunchKernelEx(&cfg, kv8_merge_kernel<HD, 2>, a, t, p);
+    tiles = (a.capacity + (int64_t)p.tile - 1) / p.tile;
+    units = (int64_t)a.hk * (a.n_rows / p.tq + a.n_seqs);
+    return units * (tiles + p.cost) <= INT32_MAX;
 }
 
 }  // namespace
 
-size_t kv8_attention_workspace(int hd, int G, int n_rows) {
-    const int64_t rows = (int64_t)n_rows * G;
-    const int rg = rows >= kMaxRowsOfUnit ? kMaxRowsOfUnit : rows_of_unit(G, n_rows, 1);
-    return sizeof(float) * 2 * kMaxCtas * (size_t)rg * (hd + 4) + sizeof(int4) * kMaxCtas;
+size_t kv8_attention_workspace(int hd, int group, int n_rows) {
+    // fewer sequences never need smaller units
+    const size_t rg = rows_of_unit(group, n_rows, 1);
+    return sizeof(float) * 2 * (rg == kKv8TcRows ? kKv8TcCtas : kKv8MaxCtas) * rg * (hd + 4) + sizeof(int4) * kKv8MaxCtas;
+}
+
+bool kv8_attention_fits(const Kv8Args& a, int hq) {
+    Kv8Plan p;
+    int64_t units, tiles;
+    return make_plan(a, hq, p, units, tiles);
 }
 
 cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s) {
-    const int G = t.hq / a.hk;
-    Plan p{};
-    p.rg = rows_of_unit(G, a.n_rows, a.n_seqs);
-    p.tq = p.rg / G;
-    p.wr = p.rg <= 16 ? 1 : p.rg / 16;
-    p.q_wide = reinterpret_cast<uintptr_t>(t.q) % 8 == 0 && t.q_row % 4 == 0 && t.q_head % 4 == 0;
+    Kv8Plan p;
+    int64_t units, tiles;
+    if (!make_plan(a, t.hq, p, units, tiles)) return cudaErrorInvalidValue;
+    const int resident = p.rg == kKv8TcRows ? std::min(sm_count(), kKv8TcCtas)
+                                            : std::min(sm_count() * (p.rg == 8 ? 3 : 2), kKv8MaxCtas);
+    p.ctas = (int)std::min<int64_t>(resident, units * (tiles + p.cost));
+    p.q_wide = reinterpret_cast<uintptr_t>(t.q) % 16 == 0 && t.q_row % 8 == 0 && t.q_head % 8 == 0;
+    p.out_wide = reinterpret_cast<uintptr_t>(t.out) % 16 == 0 && t.out_row % 8 == 0 && t.out_head % 8 == 0;
     p.desc = static_cast<int4*>(t.workspace);
-    p.part = reinterpret_cast<float*>(p.desc + kMaxCtas);
-    if (a.hd == 128) return p.rg == 8 ? launch_hd<128, 1, 1>(a, t, p, s) : launch_hd<128, 2, 2>(a, t, p, s);
-    return p.rg == 8 ? launch_hd<64, 1, 1>(a, t, p, s) : launch_hd<64, 2, 2>(a, t, p, s);
+    p.part = reinterpret_cast<float*>(p.desc + kKv8MaxCtas);
+    cudaError_t e;
+    if (p.rg == kKv8TcRows) e = launch_kv8_tc(a, t, p, s);
+    else if (a.hd == 128) e = p.rg == 8 ? launch_few<128, 1>(a, t, p, s) : launch_few<128, 2>(a, t, p, s);
+    else e = p.rg == 8 ? launch_few<64, 1>(a, t, p, s) : launch_few<64, 2>(a, t, p, s);
+    if (e != cudaSuccess || tiles <= 1) return e;       // no unit has a tile to cut off
+    return a.hd == 128 ? launch_merge<128>(a, t, p, units, s) : launch_merge<64>(a, t, p, units, s);
 }
 
 }  // namespace ks

@@ -1,0 +1,554 @@
+// Causal attention over the 8-bit paged cache with units of 128 query rows:
+// verify passes of many rows and prompts, on tcgen05.
+//
+// S (128 rows x 128 keys) = Q K^T by kind::f8f6f4, with the cached key codes as
+// they are and the queries in two e4m3 codes each, hi and lo (see
+// kv8_attn.cu), two products into one accumulator: as many tensor cycles as one
+// f16 product, without converting K.  O (rows x dims) += P V by kind::f16, P from
+// TMEM in 11 bits, V converted to f16 once per tile by two warps.
+// Shared memory carries per 128-key tile 64 KB of the first product's operands,
+// 32 KB of the second's and 48 KB of the conversion: 1150 clocks at 128 bytes,
+// against 1340 clocks in which 33 KB of the cache arrive at the HBM's rate, so
+// padding the rows up to 128 costs nothing that bytes do not; with all 128 rows
+// in use the tensor pipe has 1024 clocks of work and the softmax about as many.
+//
+// Warps 0..3 and 4..7 are two softmax streams, a thread per row each: even tiles
+// of a segment and odd ones, with a maximum, a sum and an accumulator each
+// (TMEM: S0 S1 O0 O1, P in the first half of its S), joined at the segment's
+// end, so that one stream's softmax runs under the other's products.  Warps 8
+// and 9 convert V, warp 10 issues the products, warp 11 the copies: a record's
+// keys, values and scales go to three places, keys and values of a tile
+// contiguous, which is the layout that the descriptors without a swizzle take.
+//
+// The running maximum is raised, and O rescaled, only when a tile exceeds it by
+// 2^8 (weights then reach 2^15, within f16, and count down to 2^-24: 2^-31 of
+// the row's maximum or less).  Values' scales are relative to vref, a power of
+// two at least the largest seen.
+#include "kv8_plan.cuh"
+#include "umma.cuh"
+
+namespace ks {
+
+namespace {
+
+constexpr int kSoftmaxWarps = 8, kConvertWarps = 2;
+constexpr int kThreads = 32 * (kSoftmaxWarps + kConvertWarps + 2);
+constexpr int kRows = kKv8TcRows, kTile = 128, kBlocks = kTile / kKv8Block;
+constexpr int kRing = 3;            // tiles of keys, and of values
+constexpr int kNear = 8;            // tiles whose scales are kept
+constexpr float kLazy = 8.f, kUp = 7.f;
+
+template <int HD>
+struct Smem {
+    static constexpr int TILE = kTile * HD;
+    unsigned char q[2][kRows * HD];             // hi, lo: [row / 8][HD / 16][8][16]
+    unsigned char k[kRing][TILE];               // [key / 8][HD / 16][8][16]
+    unsigned char v[kRing][TILE];               // [key / 16][HD][16]
+    unsigned char v16[2][2 * TILE];             // f16 [key / 8][HD][8]
+    float4 scale[kNear][kBlocks];               // key scale, value scale
+    float4 join[2][kRows];                      // m, l, vref of a stream
+    float qf[kRows];
+    int nan_from[4][HD];                        // first key whose value is NaN, a segment each
+    int any_nan[4];
+    int present[kNear];
+    uint64_t scales[kNear], k_full[kRing], k_free[kRing], v_full[kRing], v_free[kRing], v16_full[2], v16_free[2];
+    uint64_t q_full, s_full[2], p_full[2], o_full[2], o_free;
+    uint32_t tmem;
+};
+
+KS_DEV void umma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p; }" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// K-major operand without a swizzle: 8-row x 16-byte matrices of 128 contiguous
+// bytes, lbo apart along K and sbo apart along M or N.
+KS_DEV uint64_t desc_plain(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) | (1ull << 46);
+}
+// fp32 accumulators; e4m3 for kind::f8f6f4 and f16 for kind::f16 are both type 0
+__host__ __device__ constexpr uint32_t idesc_of(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24); }
+
+KS_DEV void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+KS_DEV void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
+    using S = Smem<HD>;
+    constexpr int REC = kv8_record(HD), PART = kKv8Block * HD;   // a record's keys (or values)
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    S& sm = *reinterpret_cast<S*>(smem_raw);
+    volatile int* present = sm.present;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (warp == 10) tmem_alloc<1>(&sm.tmem, 512);
+    if (tid == 0) {
+        for (int i = 0; i < kNear; ++i) mbar_init(&sm.scales[i], 1);
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&sm.k_full[i], 1);
+            mbar_init(&sm.k_free[i], 1);
+            mbar_init(&sm.v_full[i], 1);
+            mbar_init(&sm.v_free[i], kConvertWarps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sm.v16_full[i], kConvertWarps);
+            mbar_init(&sm.v16_free[i], 1);
+            mbar_init(&sm.s_full[i], 1);
+            mbar_init(&sm.p_full[i], 4);
+            mbar_init(&sm.o_full[i], 2);        // the products' commit, and an arrival that orders nan_from before it
+        }
+        mbar_init(&sm.q_full, kSoftmaxWarps);
+        mbar_init(&sm.o_free, kSoftmaxWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (int i = tid; i < 4 * HD; i += kThreads) sm.nan_from[0][i] = INT32_MAX;
+    if (tid < 4) sm.any_nan[tid] = 0;
+    umma_fence_before();
+    __syncthreads();
+    umma_fence_after();
+    const uint32_t tmem = sm.tmem;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    Run run;
+    Segment at;
+    const bool stopped = a.stop && *a.stop;
+    const bool work = !stopped && find_run(a, p, run, at);
+    if (!work && !stopped && tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    const int G = t.hq / a.hk;
+
+    if (!work) {
+        // nothing in this run
+    } else if (warp == 11) {
+        // ---------------------------------------------------------- copies
+        // Page numbers are read a group of tiles ahead, across segments.
+        constexpr int TILES = 32 / kBlocks;
+        auto pages = [&](const Segment& k, int tile) {
+            const int b = tile * kBlocks + lane;
+            const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
+            if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
+            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + b / a.bpp);
+            return page >= 0 && page < a.n_pages ? page : -2;
+        };
+        int it = 0, tile = at.tile, page = pages(at, tile);
+        bool alive = true, more = true;
+        while (more && alive) {
+            Segment next = at;
+            int next_tile = tile + TILES;
+            if (next_tile >= at.end) {
+                more = next.next(a, run, p);
+                next_tile = next.tile;
+            }
+            const int next_page = more ? pages(next, next_tile) : -1;
+            if (page == -2) kv8_flag(a, kKv8BadPage);
+            const int b = tile * kBlocks + lane;
+            const unsigned char* rec =
+                page >= 0 ? a.data + (((size_t)page * a.hk + at.h) * a.bpp + b % a.bpp) * REC : nullptr;
+            const unsigned have = __ballot_sync(0xffffffffu, rec != nullptr);
+            for (int i = 0; i < TILES && tile + i < at.end; ++i, ++it) {
+                const int st = it % kRing, near = it % kNear, odd = ((it / kRing) & 1) ^ 1;
+                const unsigned mask = have >> (i * kBlocks) & ((1u << kBlocks) - 1);
+                alive = mbar_wait(&sm.k_free[st], odd, kWaitLimitNs) && mbar_wait(&sm.v_free[st], odd, kWaitLimitNs);
+                if (!__all_sync(0xffffffffu, alive)) {
+                    alive = false;
+                    break;
+                }
+                if (lane == 0) {
+                    const int n = __popc(mask);
+                    present[near] = (int)mask;
+                    mbar_expect_tx(&sm.scales[near], n * 16);
+                    mbar_expect_tx(&sm.k_full[st], n * PART);
+                    mbar_expect_tx(&sm.v_full[st], n * PART);
+                }
+                __syncwarp();
+                if (rec && lane / kBlocks == i) {
+                    const int r = lane % kBlocks;
+                    bulk_load(sm.k[st] + r * PART, rec, PART, &sm.k_full[st]);
+                    bulk_load(&sm.scale[near][r], rec + 2 * PART, 16, &sm.scales[near]);
+                    bulk_load(sm.v[st] + r * PART, rec + PART, PART, &sm.v_full[st]);
+                }
+            }
+            at = next;
+            tile = next_tile;
+            page = next_page;
+        }
+        if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
+        // no copy may be in flight when the CTA ends
+        for (int i = max(0, it - kNear); i < it; ++i) {
+            mbar_wait(&sm.scales[i % kNear], (i / kNear) & 1, kWaitLimitNs);
+            if (i < it - kRing) continue;
+            mbar_wait(&sm.k_full[i % kRing], (i / kRing) & 1, kWaitLimitNs);
+            mbar_wait(&sm.v_full[i % kRing], (i / kRing) & 1, kWaitLimitNs);
+        }
+    } else if (warp == 10) {
+        // -------------------------------------------------------- products
+        if (lane == 0) {
+            constexpr uint32_t kIdS = idesc_of(kTile), kIdO = idesc_of(HD);
+            bool ok = true;
+            int it0 = 0, seg = 0, n[2] = {0, 0};     // tiles before the segment, segments, tiles of each stream
+            do {
+                const int cnt = at.end - at.tile;
+                ok = mbar_wait(&sm.q_full, seg & 1, kWaitLimitNs);
+                auto scores = [&](int j) {
+                    const int st = (it0 + j) % kRing;
+                    ok = ok && mbar_wait(&sm.k_full[st], ((it0 + j) / kRing) & 1, kWaitLimitNs);
+                    if (!ok) return;
+                    umma_fence_after();
+                    const uint32_t kb = smem_u32(sm.k[st]);
+#pragma unroll
+                    for (int part = 0; part < 2; ++part)
+#pragma unroll
+                        for (int c = 0; c < HD / 32; ++c)
+                            umma_e4m3(tmem + 128 * (j & 1), desc_plain(smem_u32(sm.q[part]) + 256 * c, 128, 8 * HD),
+                                      desc_plain(kb + 256 * c, 128, 8 * HD), kIdS, part > 0 || c > 0);
+                    umma_commit(&sm.k_free[st]);
+                    umma_commit(&sm.s_full[j & 1]);
+                };
+                scores(0);
+                if (cnt > 1) scores(1);
+                if (seg > 0) ok = ok && mbar_wait(&sm.o_free, (seg - 1) & 1, kWaitLimitNs);
+                for (int j = 0; j < cnt && ok; ++j) {
+                    const int i = j & 1, b = (it0 + j) & 1;
+                    ok = mbar_wait(&sm.p_full[i], n[i] & 1, kWaitLimitNs) &&
+                         mbar_wait(&sm.v16_full[b], ((it0 + j) >> 1) & 1, kWaitLimitNs);
+                    if (!ok) break;
+                    ++n[i];
+                    umma_fence_after();
+                    const uint32_t vb = smem_u32(sm.v16[b]);
+#pragma unroll
+                    for (int c = 0; c < kTile / 16; ++c)
+                        umma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 8 * c, desc_plain(vb + 32 * HD * c, 16 * HD, 128),
+                                kIdO, j > 1 || c > 0);
+                    umma_commit(&sm.v16_free[b]);
+                    umma_commit(&sm.o_full[i]);
+                    mbar_arrive(&sm.o_full[i]);
+                    if (j + 2 < cnt) scores(j + 2);
+                }
+                it0 += cnt;
+                ++seg;
+            } while (ok && at.next(a, run, p));
+            if (!ok) kv8_flag(a, kKv8Timeout);
+        }
+        __syncwarp();
+    } else if (warp >= kSoftmaxWarps) {
+        // ------------------------------------------------------ V to f16
+        const int ct = tid - 32 * kSoftmaxWarps;
+        bool alive = true;
+        int it = 0, seg = 0;
+        do {
+            const Rows rows(at.q, p.tq, at.g, G);
+            for (int tile = at.tile; tile < at.end; ++tile, ++it) {
+                const int st = it % kRing, b = it & 1, near = it % kNear;
+                alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs) &&
+                        mbar_wait(&sm.v_full[st], (it / kRing) & 1, kWaitLimitNs) &&
+                        mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
+                if (tile == at.tile) {
+                    // Clear the next segment's marks.  The products of the tile two before are done, so those of
+                    // the segment two back have begun and the readers of the one three back, who had this
+                    // buffer, have left; and neither warp marks the next segment before both have cleared.
+                    for (int i = ct; i < HD; i += 32 * kConvertWarps) sm.nan_from[(seg + 1) & 3][i] = INT32_MAX;
+                    if (ct == 0) sm.any_nan[(seg + 1) & 3] = 0;
+                    asm volatile("bar.sync 2, 64;" ::: "memory");
+                }
+                const int have = present[near];
+                const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
+                const unsigned char* src = sm.v[st];
+                unsigned char* dst = sm.v16[b];
+#pragma unroll 4
+                for (int i = ct; i < kBlocks * HD; i += 32 * kConvertWarps) {
+                    const int r = i / HD, d = i % HD;
+                    uint4 x = *reinterpret_cast<const uint4*>(src + i * 16);
+                    if (edge) {
+                        // a NaN that not every row sees would pass through a weight of zero: it is taken out, and
+                        // the rows that do see it get their NaN at the end
+                        uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+                        if (!(have >> r & 1)) x = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t nan = ((w[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                            if (nan) {
+                                sm.any_nan[seg & 3] = 1;
+                                for (int c = 0; c < 4; ++c)
+                                    if (nan >> (8 * c + 7) & 1)
+                                        atomicMin(&sm.nan_from[seg & 3][d],
+                                                  tile * kTile + 16 * r + 2 * j + (c & 1) + 8 * (c >> 1));
+                                w[j] &= ~((nan >> 7) * 0xffu);
+                            }
+                        }
+                    }
+                    *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) =
+                        make_uint4(f16_of((uint16_t)x.x), f16_of((uint16_t)x.y), f16_of((uint16_t)x.z), f16_of((uint16_t)x.w));
+                    *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) =
+                        make_uint4(f16_of((uint16_t)(x.x >> 16)), f16_of((uint16_t)(x.y >> 16)),
+                                   f16_of((uint16_t)(x.z >> 16)), f16_of((uint16_t)(x.w >> 16)));
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sm.v16_full[b]);
+                    mbar_arrive(&sm.v_free[st]);
+                }
+            }
+            ++seg;
+        } while (at.next(a, run, p));
+        if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
+    } else {
+        // --------------------------------------------------------- softmax
+        const int i = warp >> 2, quad = warp & 3, row = 32 * quad + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(32 * quad) << 16);
+        const uint32_t s_at = lanes + 128 * i, o_at = lanes + 256 + 128 * i;
+        bool alive = true, began = false;
+        int it0 = 0, seg = 0, n = 0;                 // tiles before the segment, segments, tiles of this stream
+        for (;;) {
+            const Rows rows(at.q, p.tq, at.g, G);
+            const int cnt = at.end - at.tile;
+            {
+                // the unit's queries in two codes: two threads a row
+                const int qr = tid >> 1, half = tid & 1;
+                const bool valid = qr < rows.n;
+                const int tok = valid ? qr / G : 0, head = at.h * G + (valid ? qr - tok * G : 0);
+                const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head + half * (HD / 2);
+                uint4 raw[HD / 16];
+                if (p.q_wide) {
+#pragma unroll
+                    for (int c = 0; c < HD / 16; ++c) raw[c] = *reinterpret_cast<const uint4*>(src + 8 * c);
+                } else {
+                    const unsigned short* e = reinterpret_cast<const unsigned short*>(src);
+#pragma unroll
+                    for (int c = 0; c < HD / 16; ++c)
+                        raw[c] = make_uint4(e[8 * c] | (uint32_t)e[8 * c + 1] << 16, e[8 * c + 2] | (uint32_t)e[8 * c + 3] << 16,
+                                            e[8 * c + 4] | (uint32_t)e[8 * c + 5] << 16, e[8 * c + 6] | (uint32_t)e[8 * c + 7] << 16);
+                }
+                float top = 0.f;
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(raw);
+#pragma unroll
+                for (int c = 0; c < HD / 4; ++c) {
+                    const float x0 = bf16_lo(w[c]), x1 = bf16_hi(w[c]);
+                    if (finite(x0)) top = fmaxf(top, fabsf(x0));
+                    if (finite(x1)) top = fmaxf(top, fabsf(x1));
+                }
+                if (!valid) top = 0.f;
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                // a scale below zero goes into the codes' sign, so that the factors of the scores are positive
+                const float sc = scale_for(top), inv = t.scale < 0.f ? -inverse_pow2(sc) : inverse_pow2(sc);
+                if (half == 0) sm.qf[qr] = sc * (fabsf(t.scale) * kLog2e);
+#pragma unroll
+                for (int c = 0; c < HD / 32; ++c) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x[4] = {bf16_lo(w[8 * c + 2 * j]), bf16_hi(w[8 * c + 2 * j]),
+                                      bf16_lo(w[8 * c + 2 * j + 1]), bf16_hi(w[8 * c + 2 * j + 1])};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (!finite(x[e])) x[e] = __uint_as_float(0x7fc00000u);   // the row becomes NaN
+                            x[e] = valid ? x[e] * inv : 0.f;
+                        }
+                        const uint16_t h0 = to_e4m3x2(x[0], x[1]), h1 = to_e4m3x2(x[2], x[3]);
+                        const float2 f0 = from_e4m3x2(h0), f1 = from_e4m3x2(h1);
+                        hi[j] = h0 | (uint32_t)h1 << 16;
+                        lo[j] = to_e4m3x2(x[0] - f0.x, x[1] - f0.y) | (uint32_t)to_e4m3x2(x[2] - f1.x, x[3] - f1.y) << 16;
+                    }
+                    const int to = (qr >> 3) * 8 * HD + (half * (HD / 32) + c) * 128 + (qr & 7) * 16;
+                    *reinterpret_cast<uint4*>(sm.q[0] + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4*>(sm.q[1] + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
+                fence_async_smem();
+                softmax_sync();                      // qf too
+                if (lane == 0) mbar_arrive(&sm.q_full);
+            }
+            const float qf = sm.qf[row];
+            const int lim = row < rows.n ? rows.pos0 + row / G : INT32_MAX;
+            float m = -INFINITY, l = 0.f, vref = 0.f;
+            bool first = true;
+            for (int j = i; j < cnt; j += 2, ++n) {
+                const int tile = at.tile + j, near = (it0 + j) % kNear;
+                alive = alive && mbar_wait(&sm.scales[near], ((it0 + j) / kNear) & 1, kWaitLimitNs) &&
+                        mbar_wait(&sm.s_full[i], n & 1, kWaitLimitNs);
+                __syncwarp();
+                umma_fence_after();
+                if (32 * quad >= rows.n) {           // no row: P stays what it is, in lanes that nobody reads
+                    if (lane == 0) mbar_arrive(&sm.p_full[i]);
+                    continue;
+                }
+                const int have = present[near];
+                const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
+                // half of the scores at a time, twice: all 128 would not fit the registers
+                uint32_t s[2][32];
+                auto load = [&](int h) {
+                    tmem_ld32(s[0], s_at + 64 * h);
+                    tmem_ld32(s[1], s_at + 64 * h + 32);
+                    tmem_wait_ld();
+                    tmem_pin(s[0]);
+                    tmem_pin(s[1]);
+                    if (!edge) return;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int q = 0; q < 32; ++q)
+                            if (tile * kTile + 64 * h + 32 * c + q > lim || !(have >> (4 * h + 2 * c + q / 16) & 1))
+                                s[c][q] = 0xff800000u;
+                };
+                auto factor = [&](int c) { return fmaxf(qf * sm.scale[near][c].x, 1e-36f); };   // above zero: -inf stays
+                float top = m, vtop = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    load(h);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float x = __uint_as_float(s[c / 2][16 * (c & 1)]);
+#pragma unroll
+                        for (int q = 1; q < 16; ++q) x = fmaxf(x, __uint_as_float(s[c / 2][16 * (c & 1) + q]));
+                        top = fmaxf(top, x * factor(4 * h + c));
+                        if (have >> (4 * h + c) & 1) vtop = fmaxf(vtop, sm.scale[near][4 * h + c].y);
+                    }
+                }
+                const bool grow = top > m + kLazy;   // only this row's own reference moves
+                const bool louder = vtop > vref;
+                if (__any_sync(0xffffffffu, grow) || louder) {
+                    const float mnew = grow ? top : m, vnew = louder ? 4.f * vtop : vref;
+                    const float down = m == -INFINITY ? 0.f : exp2_approx(m - mnew);
+                    l *= down;
+                    if (!first) {
+                        const float fac = down * (vref * inverse_pow2(vnew));
+                        alive = alive && mbar_wait(&sm.o_full[i], (n - 1) & 1, kWaitLimitNs);
+                        __syncwarp();
+                        umma_fence_after();
+#pragma unroll
+                        for (int c = 0; c < HD / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32(o, o_at + 32 * c);
+                            tmem_wait_ld();
+                            tmem_pin(o);
+#pragma unroll
+                            for (int q = 0; q < 32; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * fac);
+                            tmem_st32(o_at + 32 * c, o);
+                        }
+                        tmem_wait_st();
+                    }
+                    m = mnew;
+                    vref = vnew;
+                }
+                first = false;
+                const float ref = (m == -INFINITY ? 0.f : m) - kUp, vinv = inverse_pow2(vref);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    load(h);
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int b = 4 * h + c;
+                        const float f = factor(b), w = have >> b & 1 ? sm.scale[near][b].y * vinv : 0.f;
+                        float part = 0.f;
+#pragma unroll
+                        for (int q = 0; q < 16; q += 2) {
+                            const float p0 = exp2_approx(fmaf(__uint_as_float(s[c / 2][16 * (c & 1) + q]), f, -ref));
+                            const float p1 = exp2_approx(fmaf(__uint_as_float(s[c / 2][16 * (c & 1) + q + 1]), f, -ref));
+                            part += p0 + p1;
+                            pk[8 * c + q / 2] = f16_pack(p0 * w, p1 * w);
+                        }
+                        l += part;
+                    }
+                    tmem_st32(s_at + 32 * h, pk);    // over scores that are in registers or used
+                }
+                tmem_wait_st();
+                umma_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.p_full[i]);
+            }
+            // ---------------------------------------------- segment's end
+            const bool mine = cnt > i;               // this stream had a tile
+            if (mine) alive = alive && mbar_wait(&sm.o_full[i], (n - 1) & 1, kWaitLimitNs);
+            sm.join[i][row] = make_float4(m, l, vref, 0.f);
+            umma_fence_before();
+            softmax_sync();
+            umma_fence_after();
+            // both streams' O over half of the dims each
+            const float4 u0 = sm.join[0][row], u1 = sm.join[1][row];
+            const float top = fmaxf(u0.x, u1.x), ref = top == -INFINITY ? 0.f : top;
+            const float e0 = exp2_approx(u0.x - ref), e1 = exp2_approx(u1.x - ref), sum = u0.y * e0 + u1.y * e1;
+            const bool whole = at.tile == 0 && at.end == at.tiles;
+            const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+            const float c0 = e0 * u0.z * inv, c1 = e1 * u1.z * inv;
+            const bool valid = row < rows.n, any_nan = sm.any_nan[seg & 3];
+            const int tok = valid ? row / G : 0, head = at.h * G + (valid ? row - tok * G : 0);
+            float* slot = p.part + ((size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg + row) * (HD + 4);
+            __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row + (int64_t)head * t.out_head;
+#pragma unroll
+            for (int c = 0; c < HD / 64; ++c) {
+                const int d0 = i * (HD / 2) + 32 * c;
+                uint32_t x[32], y[32];
+                tmem_ld32(x, lanes + 256 + d0);
+                tmem_ld32(y, lanes + 384 + d0);
+                tmem_wait_ld();
+                tmem_pin(x);
+                tmem_pin(y);
+#pragma unroll
+                for (int q = 0; q < 32; ++q) {
+                    float v = __uint_as_float(x[q]) * c0;
+                    if (cnt > 1) v = fmaf(__uint_as_float(y[q]), c1, v);
+                    if (any_nan && sm.nan_from[seg & 3][d0 + q] <= lim) v = __uint_as_float(0x7fc00000u);
+                    x[q] = __float_as_uint(v);
+                }
+                if (!valid) continue;
+                if (!whole) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        *reinterpret_cast<uint4*>(slot + 4 + d0 + 4 * q) = make_uint4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                } else if (p.out_wide) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t b[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            b[k] = pack_bf16(__uint_as_float(x[8 * q + 2 * k]), __uint_as_float(x[8 * q + 2 * k + 1]));
+                        *reinterpret_cast<uint4*>(out + d0 + 8 * q) = make_uint4(b[0], b[1], b[2], b[3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) out[d0 + q] = __float2bfloat16_rn(__uint_as_float(x[q]));
+                }
+            }
+            if (valid && i == 0) {
+                // l and o carry the factor 2^kUp
+                if (!whole) *reinterpret_cast<float2*>(slot) = make_float2(top - kUp, sum);
+                else if (t.lse) t.lse[(size_t)(rows.row0 + tok) * t.hq + head] = sum == 0.f ? -INFINITY : (top - kUp + log2f(sum)) * kLn2;
+            }
+            if (!whole && at.tile == 0) {
+                began = true;
+                if (tid == 0) p.desc[blockIdx.x] = make_int4(rows.row0, rows.n, at.h, run.cta_of(at.first + at.tiles - 1));
+            }
+            umma_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.o_free);
+            it0 += cnt;
+            ++seg;
+            if (!at.next(a, run, p)) break;
+        }
+        if (tid == 0) {
+            if (!began) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+            if (!alive) kv8_flag(a, kKv8Timeout);
+        }
+    }
+    umma_fence_before();
+    __syncthreads();
+    if (warp == 10) {
+        umma_fence_after();
+        tmem_free<1>(tmem, 512);
+    }
+}
+
+template <int HD>
+cudaError_t launch_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s) {
+    auto kern = kv8_tc_kernel<HD>;
+    constexpr int bytes = sizeof(Smem<HD>);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, a, t, p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s) {
+    return a.hd == 128 ? launch_tc<128>(a, t, p, s) : launch_tc<64>(a, t, p, s);
+}
+
+}  // namespace ks
