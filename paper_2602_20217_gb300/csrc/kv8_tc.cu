@@ -37,6 +37,25 @@ constexpr int kRows = kKv8TcRows, kTile = 128, kBlocks = kTile / kKv8Block;
 constexpr int kRing = 3;            // tiles of keys, and of values
 constexpr int kNear = 8;            // tiles whose scales are kept
 constexpr float kLazy = 8.f, kUp = 7.f;
+constexpr float kQuiet = 1.f / 16384.f;
+
+// Values' scales are taken relative to vref, which follows the tiles of a
+// segment in order: four times the loudest block seen, raised when one passes
+// it.  Both the converting warps and the streams compute it.
+KS_DEV float next_vref(float vref, const float4* scale, int have) {
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c)
+        if (have >> c & 1) top = fmaxf(top, scale[c].y);
+    return top > vref ? 4.f * top : vref;
+}
+// The part of a block's relative scale that the f16 values carry: codes of 2^-9
+// and more stay exact down to 2^-14.  Quieter blocks have the rest in the weights.
+KS_DEV float value_factor(float scale, float vinv) { return fmaxf(scale * vinv, kQuiet); }
+KS_DEV uint32_t f16_times(uint32_t v, __half2 f) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&v), f);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
 
 template <int HD>
 struct Smem {
@@ -70,6 +89,20 @@ KS_DEV uint64_t desc_plain(uint32_t addr, uint32_t lbo, uint32_t sbo) {
 // fp32 accumulators; e4m3 for kind::f8f6f4 and f16 for kind::f16 are both type 0
 __host__ __device__ constexpr uint32_t idesc_of(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24); }
 
+KS_DEV float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("{ .reg .b64 x, y, z; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; mov.b64 z, {%5, %6}; fma.rn.f32x2 %0, x, y, z; }"
+        : "=l"(r)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
+}
+KS_DEV float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("{ .reg .b64 x, y; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; add.rn.f32x2 %0, x, y; }"
+        : "=l"(r)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
+}
 KS_DEV void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 KS_DEV void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
@@ -236,6 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
         int it = 0, seg = 0;
         do {
             const Rows rows(at.q, p.tq, at.g, G);
+            float vref = 0.f;
             for (int tile = at.tile; tile < at.end; ++tile, ++it) {
                 const int st = it % kRing, b = it & 1, near = it % kNear;
                 alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs) &&
@@ -251,19 +285,44 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 }
                 const int have = present[near];
                 const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
+                vref = next_vref(vref, sm.scale[near], have);
+                const float vinv = inverse_pow2(vref);
                 const unsigned char* src = sm.v[st];
                 unsigned char* dst = sm.v16[b];
-#pragma unroll 4
-                for (int i = ct; i < kBlocks * HD; i += 32 * kConvertWarps) {
-                    const int r = i / HD, d = i % HD;
-                    uint4 x = *reinterpret_cast<const uint4*>(src + i * 16);
-                    if (edge) {
+                auto convert = [&](int r, int d, uint4 x) {
+                    const __half2 f = __float2half2_rn(value_factor(sm.scale[near][r].y, vinv));
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    uint32_t lo[4], hi[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        lo[j] = f16_times(f16_of((uint16_t)w[j]), f);
+                        hi[j] = f16_times(f16_of((uint16_t)(w[j] >> 16)), f);
+                    }
+                    *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                };
+                constexpr int STEP = 32 * kConvertWarps, N = kBlocks * HD / STEP, BATCH = 8;
+                if (!edge) {
+#pragma unroll 1
+                    for (int c = 0; c < N; c += BATCH) {
+                        uint4 x[BATCH];
+#pragma unroll
+                        for (int i = 0; i < BATCH; ++i)
+                            x[i] = *reinterpret_cast<const uint4*>(src + ((c + i) * STEP + ct) * 16);
+#pragma unroll
+                        for (int i = 0; i < BATCH; ++i) convert(((c + i) * STEP + ct) / HD, ((c + i) * STEP + ct) % HD, x[i]);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = ct; i < kBlocks * HD; i += STEP) {
+                        const int r = i / HD, d = i % HD;
                         // a NaN that not every row sees would pass through a weight of zero: it is taken out, and
                         // the rows that do see it get their NaN at the end
-                        uint32_t* w = reinterpret_cast<uint32_t*>(&x);
-                        if (!(have >> r & 1)) x = make_uint4(0, 0, 0, 0);
+                        uint4 x = *reinterpret_cast<const uint4*>(src + i * 16);
+                        uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
+                            if (!(have >> r & 1)) w[j] = 0;
                             const uint32_t nan = ((w[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
                             if (nan) {
                                 sm.any_nan[seg & 3] = 1;
@@ -274,12 +333,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                                 w[j] &= ~((nan >> 7) * 0xffu);
                             }
                         }
+                        if (have >> r & 1) {
+                            convert(r, d, make_uint4(w[0], w[1], w[2], w[3]));
+                        } else {
+                            *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) = make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(0, 0, 0, 0);
+                        }
                     }
-                    *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) =
-                        make_uint4(f16_of((uint16_t)x.x), f16_of((uint16_t)x.y), f16_of((uint16_t)x.z), f16_of((uint16_t)x.w));
-                    *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) =
-                        make_uint4(f16_of((uint16_t)(x.x >> 16)), f16_of((uint16_t)(x.y >> 16)),
-                                   f16_of((uint16_t)(x.z >> 16)), f16_of((uint16_t)(x.w >> 16)));
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -389,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                                 s[c][q] = 0xff800000u;
                 };
                 auto factor = [&](int c) { return fmaxf(qf * sm.scale[near][c].x, 1e-36f); };   // above zero: -inf stays
-                float top = m, vtop = 0.f;
+                float top = m;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     load(h);
@@ -399,13 +459,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
 #pragma unroll
                         for (int q = 1; q < 16; ++q) x = fmaxf(x, __uint_as_float(s[c / 2][16 * (c & 1) + q]));
                         top = fmaxf(top, x * factor(4 * h + c));
-                        if (have >> (4 * h + c) & 1) vtop = fmaxf(vtop, sm.scale[near][4 * h + c].y);
                     }
                 }
                 const bool grow = top > m + kLazy;   // only this row's own reference moves
-                const bool louder = vtop > vref;
-                if (__any_sync(0xffffffffu, grow) || louder) {
-                    const float mnew = grow ? top : m, vnew = louder ? 4.f * vtop : vref;
+                // vref passes the other stream's tile before this one
+                float vnew = vref;
+                if (j > 0) {
+                    const int before = (it0 + j - 1) % kNear;
+                    alive = alive && mbar_wait(&sm.scales[before], ((it0 + j - 1) / kNear) & 1, kWaitLimitNs);
+                    vnew = next_vref(vnew, sm.scale[before], present[before]);
+                }
+                vnew = next_vref(vnew, sm.scale[near], have);
+                if (__any_sync(0xffffffffu, grow) || vnew != vref) {
+                    const float mnew = grow ? top : m;
                     const float down = m == -INFINITY ? 0.f : exp2_approx(m - mnew);
                     l *= down;
                     if (!first) {
@@ -430,23 +496,36 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 }
                 first = false;
                 const float ref = (m == -INFINITY ? 0.f : m) - kUp, vinv = inverse_pow2(vref);
+                bool quiet = false;
+#pragma unroll
+                for (int c = 0; c < kBlocks; ++c) quiet = quiet || ((have >> c & 1) && sm.scale[near][c].y * vinv < kQuiet);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     load(h);
                     uint32_t pk[32];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const int b = 4 * h + c;
-                        const float f = factor(b), w = have >> b & 1 ? sm.scale[near][b].y * vinv : 0.f;
-                        float part = 0.f;
+                        const float f = factor(4 * h + c);
+                        float2 part = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int q = 0; q < 16; q += 2) {
-                            const float p0 = exp2_approx(fmaf(__uint_as_float(s[c / 2][16 * (c & 1) + q]), f, -ref));
-                            const float p1 = exp2_approx(fmaf(__uint_as_float(s[c / 2][16 * (c & 1) + q + 1]), f, -ref));
-                            part += p0 + p1;
-                            pk[8 * c + q / 2] = f16_pack(p0 * w, p1 * w);
+                            const float2 x = fma2(make_float2(__uint_as_float(s[c / 2][16 * (c & 1) + q]),
+                                                              __uint_as_float(s[c / 2][16 * (c & 1) + q + 1])),
+                                                  make_float2(f, f), make_float2(-ref, -ref));
+                            const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                            part = add2(part, e);
+                            pk[8 * c + q / 2] = f16_pack(e.x, e.y);
                         }
-                        l += part;
+                        l += part.x + part.y;
+                    }
+                    if (quiet) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float y = have >> (4 * h + c) & 1 ? sm.scale[near][4 * h + c].y * vinv : 1.f;
+                            const __half2 w = __float2half2_rn(fminf(y * (1.f / kQuiet), 1.f));
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) pk[8 * c + q] = f16_times(pk[8 * c + q], w);
+                        }
                     }
                     tmem_st32(s_at + 32 * h, pk);    // over scores that are in registers or used
                 }
