@@ -5,7 +5,7 @@
 // they are and the queries in two e4m3 codes each, hi and lo (see
 // kv8_attn.cu), two products into one accumulator: as many tensor cycles as one
 // f16 product, without converting K.  O (rows x dims) += P V by kind::f16, P from
-// TMEM in 11 bits, V converted to f16 once per tile by two warps.
+// TMEM in 11 bits, V converted to f16 once per tile by four warps.
 // Shared memory carries per 128-key tile 64 KB of the first product's operands,
 // 32 KB of the second's and 48 KB of the conversion: 1150 clocks at 128 bytes,
 // against 1340 clocks in which 33 KB of the cache arrive at the HBM's rate, so
@@ -16,7 +16,7 @@
 // of a segment and odd ones, with a maximum, a sum and an accumulator each
 // (TMEM: S0 S1 O0 O1, P in the first half of its S), joined at the segment's
 // end, so that one stream's softmax runs under the other's products.  Warps 8
-// and 9 convert V, warp 10 issues the products, warp 11 the copies: a record's
+// to 11 convert V, warp 12 issues the products, warp 13 the copies: a record's
 // keys, values and scales go to three places, keys and values of a tile
 // contiguous, which is the layout that the descriptors without a swizzle take.
 //
@@ -31,7 +31,7 @@ namespace ks {
 
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kConvertWarps = 2;
+constexpr int kSoftmaxWarps = 8, kConvertWarps = 4, kProductWarp = 12, kCopyWarp = 13;
 constexpr int kThreads = 32 * (kSoftmaxWarps + kConvertWarps + 2);
 constexpr int kRows = kKv8TcRows, kTile = 128, kBlocks = kTile / kKv8Block;
 constexpr int kRing = 3;            // tiles of keys, and of values
@@ -103,8 +103,14 @@ KS_DEV float2 add2(float2 a, float2 b) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
 }
+KS_DEV float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 KS_DEV void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 KS_DEV void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+KS_DEV void convert_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
@@ -114,17 +120,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
     S& sm = *reinterpret_cast<S*>(smem_raw);
     volatile int* present = sm.present;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (warp == 10) tmem_alloc<1>(&sm.tmem, 512);
+    if (warp == kProductWarp) tmem_alloc<1>(&sm.tmem, 512);
     if (tid == 0) {
         for (int i = 0; i < kNear; ++i) mbar_init(&sm.scales[i], 1);
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&sm.k_full[i], 1);
             mbar_init(&sm.k_free[i], 1);
             mbar_init(&sm.v_full[i], 1);
-            mbar_init(&sm.v_free[i], kConvertWarps);
+            mbar_init(&sm.v_free[i], kConvertWarps / 2);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sm.v16_full[i], kConvertWarps);
+            mbar_init(&sm.v16_full[i], kConvertWarps / 2);
             mbar_init(&sm.v16_free[i], 1);
             mbar_init(&sm.s_full[i], 1);
             mbar_init(&sm.p_full[i], 4);
@@ -151,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
 
     if (!work) {
         // nothing in this run
-    } else if (warp == 11) {
+    } else if (warp == kCopyWarp) {
         // ---------------------------------------------------------- copies
         // Page numbers are read a group of tiles ahead, across segments.
         constexpr int TILES = 32 / kBlocks;
@@ -212,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
             mbar_wait(&sm.k_full[i % kRing], (i / kRing) & 1, kWaitLimitNs);
             mbar_wait(&sm.v_full[i % kRing], (i / kRing) & 1, kWaitLimitNs);
         }
-    } else if (warp == 10) {
+    } else if (warp == kProductWarp) {
         // -------------------------------------------------------- products
         if (lane == 0) {
             constexpr uint32_t kIdS = idesc_of(kTile), kIdO = idesc_of(HD);
@@ -264,7 +270,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
         __syncwarp();
     } else if (warp >= kSoftmaxWarps) {
         // ------------------------------------------------------ V to f16
-        const int ct = tid - 32 * kSoftmaxWarps;
+        // two warps a tile, even and odd ones: a tile's fixed latencies pass under the other's work
+        const int mine = (warp - kSoftmaxWarps) / (kConvertWarps / 2), ct = tid % (16 * kConvertWarps);
         bool alive = true;
         int it = 0, seg = 0;
         do {
@@ -272,25 +279,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
             float vref = 0.f;
             for (int tile = at.tile; tile < at.end; ++tile, ++it) {
                 const int st = it % kRing, b = it & 1, near = it % kNear;
-                alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs) &&
-                        mbar_wait(&sm.v_full[st], (it / kRing) & 1, kWaitLimitNs) &&
-                        mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
+                if (b == mine) alive = alive && mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
                 if (tile == at.tile) {
                     // Clear the next segment's marks.  The products of the tile two before are done, so those of
                     // the segment two back have begun and the readers of the one three back, who had this
-                    // buffer, have left; and neither warp marks the next segment before both have cleared.
-                    for (int i = ct; i < HD; i += 32 * kConvertWarps) sm.nan_from[(seg + 1) & 3][i] = INT32_MAX;
-                    if (ct == 0) sm.any_nan[(seg + 1) & 3] = 0;
-                    asm volatile("bar.sync 2, 64;" ::: "memory");
+                    // buffer, have left; and nobody marks the next segment before all have cleared.
+                    convert_sync();
+                    for (int i = tid - 32 * kSoftmaxWarps; i < HD; i += 32 * kConvertWarps)
+                        sm.nan_from[(seg + 1) & 3][i] = INT32_MAX;
+                    if (tid == 32 * kSoftmaxWarps) sm.any_nan[(seg + 1) & 3] = 0;
+                    convert_sync();
                 }
+                alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs);
                 const int have = present[near];
-                const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
                 vref = next_vref(vref, sm.scale[near], have);
+                if (b != mine) continue;
+                alive = alive && mbar_wait(&sm.v_full[st], (it / kRing) & 1, kWaitLimitNs);
+                const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
                 const float vinv = inverse_pow2(vref);
                 const unsigned char* src = sm.v[st];
                 unsigned char* dst = sm.v16[b];
-                auto convert = [&](int r, int d, uint4 x) {
-                    const __half2 f = __float2half2_rn(value_factor(sm.scale[near][r].y, vinv));
+                auto convert = [&](int r, int d, uint4 x, __half2 f) {
                     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
                     uint32_t lo[4], hi[4];
 #pragma unroll
@@ -301,7 +310,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                     *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 };
-                constexpr int STEP = 32 * kConvertWarps, N = kBlocks * HD / STEP, BATCH = 8;
+                auto factor = [&](int r) { return __float2half2_rn(value_factor(sm.scale[near][r].y, vinv)); };
+                constexpr int STEP = 16 * kConvertWarps, N = kBlocks * HD / STEP, BATCH = 8;
                 if (!edge) {
 #pragma unroll 1
                     for (int c = 0; c < N; c += BATCH) {
@@ -310,7 +320,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                         for (int i = 0; i < BATCH; ++i)
                             x[i] = *reinterpret_cast<const uint4*>(src + ((c + i) * STEP + ct) * 16);
 #pragma unroll
-                        for (int i = 0; i < BATCH; ++i) convert(((c + i) * STEP + ct) / HD, ((c + i) * STEP + ct) % HD, x[i]);
+                        for (int i = 0; i < BATCH; ++i) {
+                            const int v = (c + i) * STEP, r = v / HD;        // a pass is within a record
+                            convert(r, v % HD + ct, x[i], factor(r));
+                        }
                     }
                 } else {
 #pragma unroll 1
@@ -334,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                             }
                         }
                         if (have >> r & 1) {
-                            convert(r, d, make_uint4(w[0], w[1], w[2], w[3]));
+                            convert(r, d, make_uint4(w[0], w[1], w[2], w[3]), factor(r));
                         } else {
                             *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) = make_uint4(0, 0, 0, 0);
                             *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(0, 0, 0, 0);
@@ -432,7 +445,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 }
                 const int have = present[near];
                 const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
-                // half of the scores at a time, twice: all 128 would not fit the registers
+                if (edge) {
+                    // what a row does not see becomes -inf where it lies, so that the passes below need no mask
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[32];
+                        tmem_ld32(x, s_at + 32 * c);
+                        tmem_wait_ld();
+                        tmem_pin(x);
+#pragma unroll
+                        for (int q = 0; q < 32; ++q)
+                            if (tile * kTile + 32 * c + q > lim || !(have >> (2 * c + q / 16) & 1)) x[q] = 0xff800000u;
+                        tmem_st32(s_at + 32 * c, x);
+                    }
+                    tmem_wait_st();
+                }
+                // Two passes over 64 scores at a time: all 128 would not fit the registers.  The loops stay loops:
+                // unrolled, the roles' code together no longer fits the instruction cache (stalls for instructions
+                // were a quarter of all, and a tile of the softmax took 6700 clocks).
                 uint32_t s[2][32];
                 auto load = [&](int h) {
                     tmem_ld32(s[0], s_at + 64 * h);
@@ -440,25 +470,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     tmem_wait_ld();
                     tmem_pin(s[0]);
                     tmem_pin(s[1]);
-                    if (!edge) return;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int q = 0; q < 32; ++q)
-                            if (tile * kTile + 64 * h + 32 * c + q > lim || !(have >> (4 * h + 2 * c + q / 16) & 1))
-                                s[c][q] = 0xff800000u;
                 };
-                auto factor = [&](int c) { return fmaxf(qf * sm.scale[near][c].x, 1e-36f); };   // above zero: -inf stays
+                auto factor = [&](int b) { return fmaxf(qf * sm.scale[near][b].x, 1e-36f); };   // above zero: -inf stays
                 float top = m;
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     load(h);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        float x = __uint_as_float(s[c / 2][16 * (c & 1)]);
+                        const uint32_t* v = &s[c / 2][16 * (c & 1)];
+                        float x[4];                  // four chains
 #pragma unroll
-                        for (int q = 1; q < 16; ++q) x = fmaxf(x, __uint_as_float(s[c / 2][16 * (c & 1) + q]));
-                        top = fmaxf(top, x * factor(4 * h + c));
+                        for (int q = 0; q < 4; ++q)
+                            x[q] = fmaxf(max3(__uint_as_float(v[q]), __uint_as_float(v[4 + q]), __uint_as_float(v[8 + q])),
+                                         __uint_as_float(v[12 + q]));
+                        top = fmaxf(top, fmaxf(max3(x[0], x[1], x[2]), x[3]) * factor(4 * h + c));
                     }
                 }
                 const bool grow = top > m + kLazy;   // only this row's own reference moves
@@ -479,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                         alive = alive && mbar_wait(&sm.o_full[i], (n - 1) & 1, kWaitLimitNs);
                         __syncwarp();
                         umma_fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < HD / 32; ++c) {
                             uint32_t o[32];
                             tmem_ld32(o, o_at + 32 * c);
@@ -499,29 +525,31 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 bool quiet = false;
 #pragma unroll
                 for (int c = 0; c < kBlocks; ++c) quiet = quiet || ((have >> c & 1) && sm.scale[near][c].y * vinv < kQuiet);
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     load(h);
                     uint32_t pk[32];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
+                        const uint32_t* v = &s[c / 2][16 * (c & 1)];
                         const float f = factor(4 * h + c);
-                        float2 part = make_float2(0.f, 0.f);
+                        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                         for (int q = 0; q < 16; q += 2) {
-                            const float2 x = fma2(make_float2(__uint_as_float(s[c / 2][16 * (c & 1) + q]),
-                                                              __uint_as_float(s[c / 2][16 * (c & 1) + q + 1])),
+                            const float2 x = fma2(make_float2(__uint_as_float(v[q]), __uint_as_float(v[q + 1])),
                                                   make_float2(f, f), make_float2(-ref, -ref));
-                            const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-                            part = add2(part, e);
-                            pk[8 * c + q / 2] = f16_pack(e.x, e.y);
+                            const float2 y = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                            part[q / 2 & 1] = add2(part[q / 2 & 1], y);
+                            pk[8 * c + q / 2] = f16_pack(y.x, y.y);
                         }
-                        l += part.x + part.y;
+                        part[0] = add2(part[0], part[1]);
+                        l += part[0].x + part[0].y;
                     }
                     if (quiet) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const float y = have >> (4 * h + c) & 1 ? sm.scale[near][4 * h + c].y * vinv : 1.f;
+                            const int b = 4 * h + c;
+                            const float y = have >> b & 1 ? sm.scale[near][b].y * vinv : 1.f;
                             const __half2 w = __float2half2_rn(fminf(y * (1.f / kQuiet), 1.f));
 #pragma unroll
                             for (int q = 0; q < 8; ++q) pk[8 * c + q] = f16_times(pk[8 * c + q], w);
@@ -610,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
     }
     umma_fence_before();
     __syncthreads();
-    if (warp == 10) {
+    if (warp == kProductWarp) {
         umma_fence_after();
         tmem_free<1>(tmem, 512);
     }
