@@ -20,10 +20,13 @@
 // keys, values and scales go to three places, keys and values of a tile
 // contiguous, which is the layout that the descriptors without a swizzle take.
 //
-// The running maximum is raised, and O rescaled, only when a tile exceeds it by
-// 2^8 (weights then reach 2^15, within f16, and count down to 2^-24: 2^-31 of
-// the row's maximum or less).  Values' scales are relative to vref, a power of
-// two at least the largest seen.
+// The weights are 2^(x - m + 10) with a reference m that is the maximum seen when
+// it was set, rounded up to a whole number, not the running one: a row's m is
+// raised (and its l, O and the weights of the tile so far multiplied down by a
+// power of two, without rounding) only when its weights of 32 keys add up to
+// more than 2^15.5.  So most tiles need no maximum at all, no weight passes f16,
+// and weights count down to f16's 2^-24: 2^-34 of the largest, or 2^-39 where
+// the reference lags behind it.
 #include "kv8_plan.cuh"
 #include "umma.cuh"
 
@@ -36,7 +39,7 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + kConvertWarps + 2);
 constexpr int kRows = kKv8TcRows, kTile = 128, kBlocks = kTile / kKv8Block;
 constexpr int kRing = 3;            // tiles of keys, and of values
 constexpr int kNear = 8;            // tiles whose scales are kept
-constexpr float kLazy = 8.f, kUp = 7.f;
+constexpr float kUp = 10.f, kMost = 46340.f;
 constexpr float kQuiet = 1.f / 16384.f;
 
 // Values' scales are taken relative to vref, which follows the tiles of a
@@ -67,10 +70,11 @@ struct Smem {
     float4 scale[kNear][kBlocks];               // key scale, value scale
     float4 join[2][kRows];                      // m, l, vref of a stream
     float qf[kRows];
+    float vref[kNear];                          // of a tile; negative: one of its blocks is quiet
     int nan_from[4][HD];                        // first key whose value is NaN, a segment each
     int any_nan[4];
     int present[kNear];
-    uint64_t scales[kNear], k_full[kRing], k_free[kRing], v_full[kRing], v_free[kRing], v16_full[2], v16_free[2];
+    uint64_t scales[kNear], vref_set[kNear], k_full[kRing], k_free[kRing], v_full[kRing], v_free[kRing], v16_full[2], v16_free[2];
     uint64_t q_full, s_full[2], p_full[2], o_full[2], o_free;
     uint32_t tmem;
 };
@@ -103,12 +107,26 @@ KS_DEV float2 add2(float2 a, float2 b) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
 }
-KS_DEV float max3(float a, float b, float c) {
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
 KS_DEV void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// 2^d for a whole d <= 0 (-inf: 0)
+KS_DEV float pow2_below(float d) { return d < -126.f ? 0.f : __uint_as_float((uint32_t)(127 + (int)d) << 23); }
+// The first n x 32 weights of a row, in TMEM, times f <= 1, in two factors: below
+// 2^-24 f is no f16 number, but its products with weights up to 2^15.5 are.
+KS_DEV void scale_weights(uint32_t at, int n, float f) {
+    const float f1 = fmaxf(f, kQuiet);
+    const __half2 w1 = __float2half2_rn(f1), w2 = __float2half2_rn(f / f1);
+#pragma unroll 1
+    for (int c = 0; c < n; ++c) {
+        uint32_t x[16];
+        tmem_wait_st();
+        tmem_ld16(x, at + 16 * c);
+        tmem_wait_ld();
+        tmem_pin(x);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) x[q] = f16_times(f16_times(x[q], w1), w2);
+        tmem_st16(at + 16 * c, x);
+    }
+}
 KS_DEV void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 KS_DEV void convert_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 
@@ -122,7 +140,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (warp == kProductWarp) tmem_alloc<1>(&sm.tmem, 512);
     if (tid == 0) {
-        for (int i = 0; i < kNear; ++i) mbar_init(&sm.scales[i], 1);
+        for (int i = 0; i < kNear; ++i) {
+            mbar_init(&sm.scales[i], 1);
+            mbar_init(&sm.vref_set[i], 1);
+        }
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&sm.k_full[i], 1);
             mbar_init(&sm.k_free[i], 1);
@@ -279,7 +300,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
             float vref = 0.f;
             for (int tile = at.tile; tile < at.end; ++tile, ++it) {
                 const int st = it % kRing, b = it & 1, near = it % kNear;
-                if (b == mine) alive = alive && mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
+                alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs);
+                const int have = present[near];
+                vref = next_vref(vref, sm.scale[near], have);
+                const float vinv = inverse_pow2(vref);
+                if (b == mine) {
+                    if (ct == 0) {
+                        bool quiet = false;
+#pragma unroll
+                        for (int c = 0; c < kBlocks; ++c)
+                            quiet = quiet || ((have >> c & 1) && sm.scale[near][c].y * vinv < kQuiet);
+                        sm.vref[near] = quiet ? -vref : vref;
+                        mbar_arrive(&sm.vref_set[near]);
+                    }
+                    alive = alive && mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
+                }
                 if (tile == at.tile) {
                     // Clear the next segment's marks.  The products of the tile two before are done, so those of
                     // the segment two back have begun and the readers of the one three back, who had this
@@ -290,13 +325,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     if (tid == 32 * kSoftmaxWarps) sm.any_nan[(seg + 1) & 3] = 0;
                     convert_sync();
                 }
-                alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs);
-                const int have = present[near];
-                vref = next_vref(vref, sm.scale[near], have);
                 if (b != mine) continue;
                 alive = alive && mbar_wait(&sm.v_full[st], (it / kRing) & 1, kWaitLimitNs);
                 const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
-                const float vinv = inverse_pow2(vref);
                 const unsigned char* src = sm.v[st];
                 unsigned char* dst = sm.v16[b];
                 auto convert = [&](int r, int d, uint4 x, __half2 f) {
@@ -311,19 +342,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 };
                 auto factor = [&](int r) { return __float2half2_rn(value_factor(sm.scale[near][r].y, vinv)); };
-                constexpr int STEP = 16 * kConvertWarps, N = kBlocks * HD / STEP, BATCH = 8;
+                constexpr int STEP = 16 * kConvertWarps, N = kBlocks * HD / STEP, PER = HD / STEP;   // passes a record
                 if (!edge) {
+                    // all loads first: they wait behind the products' reads of shared memory
+                    uint4 x[N];
+                    __half2 f[kBlocks];
+#pragma unroll
+                    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const uint4*>(src + (i * STEP + ct) * 16);
+#pragma unroll
+                    for (int r = 0; r < kBlocks; ++r) f[r] = factor(r);
 #pragma unroll 1
-                    for (int c = 0; c < N; c += BATCH) {
-                        uint4 x[BATCH];
+                    for (int c = 0; c < N; c += 8) {
 #pragma unroll
-                        for (int i = 0; i < BATCH; ++i)
-                            x[i] = *reinterpret_cast<const uint4*>(src + ((c + i) * STEP + ct) * 16);
+                        for (int i = 0; i < 8; ++i)
+                            convert((c + i) / PER, (i % PER) * STEP + ct, x[i], f[i / PER]);
 #pragma unroll
-                        for (int i = 0; i < BATCH; ++i) {
-                            const int v = (c + i) * STEP, r = v / HD;        // a pass is within a record
-                            convert(r, v % HD + ct, x[i], factor(r));
-                        }
+                        for (int i = 0; i + 8 < N; ++i) x[i] = x[i + 8];
+#pragma unroll
+                        for (int r = 0; r + 8 / PER < kBlocks; ++r) f[r] = f[r + 8 / PER];
                     }
                 } else {
 #pragma unroll 1
@@ -433,20 +469,41 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
             const int lim = row < rows.n ? rows.pos0 + row / G : INT32_MAX;
             float m = -INFINITY, l = 0.f, vref = 0.f;
             bool first = true;
+            auto rescale = [&](float fac) {           // O, once the products before are in it
+                alive = alive && mbar_wait(&sm.o_full[i], (n - 1) & 1, kWaitLimitNs);
+                __syncwarp();
+                umma_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < HD / 16; ++c) {
+                    uint32_t o[16];
+                    tmem_ld16(o, o_at + 16 * c);
+                    tmem_wait_ld();
+                    tmem_pin(o);
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * fac);
+                    tmem_st16(o_at + 16 * c, o);
+                }
+                tmem_wait_st();
+            };
             for (int j = i; j < cnt; j += 2, ++n) {
                 const int tile = at.tile + j, near = (it0 + j) % kNear;
-                alive = alive && mbar_wait(&sm.scales[near], ((it0 + j) / kNear) & 1, kWaitLimitNs) &&
-                        mbar_wait(&sm.s_full[i], n & 1, kWaitLimitNs);
+                alive = alive && mbar_wait(&sm.vref_set[near], ((it0 + j) / kNear) & 1, kWaitLimitNs);
+                // read before the scores are there: shared memory is the products' while they run, and a load
+                // between them takes hundreds of clocks
+                float f[kBlocks];
+#pragma unroll
+                for (int c = 0; c < kBlocks; ++c) f[c] = fmaxf(qf * sm.scale[near][c].x, 1e-36f);   // above zero: -inf stays
+                const int have = present[near];
+                const float vnow = sm.vref[near], vnew = fabsf(vnow);
+                alive = alive && mbar_wait(&sm.s_full[i], n & 1, kWaitLimitNs);
                 __syncwarp();
                 umma_fence_after();
                 if (32 * quad >= rows.n) {           // no row: P stays what it is, in lanes that nobody reads
                     if (lane == 0) mbar_arrive(&sm.p_full[i]);
                     continue;
                 }
-                const int have = present[near];
-                const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
-                if (edge) {
-                    // what a row does not see becomes -inf where it lies, so that the passes below need no mask
+                if (have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0) {
+                    // what a row does not see becomes -inf where it lies, so that the pass below needs no mask
 #pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         uint32_t x[32];
@@ -460,103 +517,67 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     }
                     tmem_wait_st();
                 }
-                // Two passes over 64 scores at a time: all 128 would not fit the registers.  The loops stay loops:
-                // unrolled, the roles' code together no longer fits the instruction cache (stalls for instructions
-                // were a quarter of all, and a tile of the softmax took 6700 clocks).
-                uint32_t s[2][32];
-                auto load = [&](int h) {
-                    tmem_ld32(s[0], s_at + 64 * h);
-                    tmem_ld32(s[1], s_at + 64 * h + 32);
-                    tmem_wait_ld();
-                    tmem_pin(s[0]);
-                    tmem_pin(s[1]);
-                };
-                auto factor = [&](int b) { return fmaxf(qf * sm.scale[near][b].x, 1e-36f); };   // above zero: -inf stays
-                float top = m;
-#pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    load(h);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t* v = &s[c / 2][16 * (c & 1)];
-                        float x[4];                  // four chains
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            x[q] = fmaxf(max3(__uint_as_float(v[q]), __uint_as_float(v[4 + q]), __uint_as_float(v[8 + q])),
-                                         __uint_as_float(v[12 + q]));
-                        top = fmaxf(top, fmaxf(max3(x[0], x[1], x[2]), x[3]) * factor(4 * h + c));
-                    }
-                }
-                const bool grow = top > m + kLazy;   // only this row's own reference moves
-                // vref passes the other stream's tile before this one
-                float vnew = vref;
-                if (j > 0) {
-                    const int before = (it0 + j - 1) % kNear;
-                    alive = alive && mbar_wait(&sm.scales[before], ((it0 + j - 1) / kNear) & 1, kWaitLimitNs);
-                    vnew = next_vref(vnew, sm.scale[before], present[before]);
-                }
-                vnew = next_vref(vnew, sm.scale[near], have);
-                if (__any_sync(0xffffffffu, grow) || vnew != vref) {
-                    const float mnew = grow ? top : m;
-                    const float down = m == -INFINITY ? 0.f : exp2_approx(m - mnew);
-                    l *= down;
-                    if (!first) {
-                        const float fac = down * (vref * inverse_pow2(vnew));
-                        alive = alive && mbar_wait(&sm.o_full[i], (n - 1) & 1, kWaitLimitNs);
-                        __syncwarp();
-                        umma_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < HD / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32(o, o_at + 32 * c);
-                            tmem_wait_ld();
-                            tmem_pin(o);
-#pragma unroll
-                            for (int q = 0; q < 32; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * fac);
-                            tmem_st32(o_at + 32 * c, o);
-                        }
-                        tmem_wait_st();
-                    }
-                    m = mnew;
+                if (vnew != vref) {
+                    if (!first) rescale(vref * inverse_pow2(vnew));
                     vref = vnew;
                 }
-                first = false;
-                const float ref = (m == -INFINITY ? 0.f : m) - kUp, vinv = inverse_pow2(vref);
-                bool quiet = false;
-#pragma unroll
-                for (int c = 0; c < kBlocks; ++c) quiet = quiet || ((have >> c & 1) && sm.scale[near][c].y * vinv < kQuiet);
+                // 32 scores at a time, in a loop that stays one: unrolled, the roles' code together no longer fits
+                // the instruction cache, and a tile of the softmax takes up to 6700 clocks instead of 1500.
+                bool tried = false;
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    load(h);
-                    uint32_t pk[32];
+                for (int c = 0; c < 4;) {
+                    uint32_t s[32], pk[16];
+                    tmem_ld32(s, s_at + 32 * c);
+                    const float f0 = c < 2 ? (c == 0 ? f[0] : f[2]) : (c == 2 ? f[4] : f[6]);
+                    const float f1 = c < 2 ? (c == 0 ? f[1] : f[3]) : (c == 2 ? f[5] : f[7]);
+                    const float ref = (m == -INFINITY ? 0.f : m) - kUp;
+                    tmem_wait_ld();
+                    tmem_pin(s);
+                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t* v = &s[c / 2][16 * (c & 1)];
-                        const float f = factor(4 * h + c);
-                        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                        for (int q = 0; q < 16; q += 2) {
-                            const float2 x = fma2(make_float2(__uint_as_float(v[q]), __uint_as_float(v[q + 1])),
-                                                  make_float2(f, f), make_float2(-ref, -ref));
-                            const float2 y = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-                            part[q / 2 & 1] = add2(part[q / 2 & 1], y);
-                            pk[8 * c + q / 2] = f16_pack(y.x, y.y);
-                        }
-                        part[0] = add2(part[0], part[1]);
-                        l += part[0].x + part[0].y;
+                    for (int q = 0; q < 32; q += 2) {
+                        const float fq = q < 16 ? f0 : f1;
+                        const float2 x = fma2(make_float2(__uint_as_float(s[q]), __uint_as_float(s[q + 1])),
+                                              make_float2(fq, fq), make_float2(-ref, -ref));
+                        const float2 y = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                        part[q / 2 & 1] = add2(part[q / 2 & 1], y);
+                        pk[q / 2] = f16_pack(y.x, y.y);
                     }
-                    if (quiet) {
+                    part[0] = add2(part[0], part[1]);
+                    const float sum = part[0].x + part[0].y;
+                    // at most kMost: no weight passes f16; just raised, it is at most 2^15
+                    const bool raise = sum > kMost || (m == -INFINITY && !tried);
+                    if (__any_sync(0xffffffffu, raise)) {
+                        float top = m;
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int b = 4 * h + c;
+                        for (int q = 0; q < 32; ++q) top = fmaxf(top, __uint_as_float(s[q]) * (q < 16 ? f0 : f1));
+                        // only this row's own reference moves, to a whole number: the factor is exact
+                        const float mnew = raise ? fmaxf(m, ceilf(top)) : m;
+                        const float fac = m == mnew ? 1.f : pow2_below(m - mnew);
+                        l *= fac;
+                        m = mnew;
+                        if (!first) rescale(fac);
+                        scale_weights(s_at, c, fac);             // of this tile so far
+                        tried = true;
+                        continue;
+                    }
+                    tried = false;
+                    l += sum;
+                    if (vnow < 0.f) {                // a quiet block
+                        const float vinv = inverse_pow2(vref);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int b = 2 * c + e;
                             const float y = have >> b & 1 ? sm.scale[near][b].y * vinv : 1.f;
                             const __half2 w = __float2half2_rn(fminf(y * (1.f / kQuiet), 1.f));
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) pk[8 * c + q] = f16_times(pk[8 * c + q], w);
+                            for (int q = 0; q < 8; ++q) pk[8 * e + q] = f16_times(pk[8 * e + q], w);
                         }
                     }
-                    tmem_st32(s_at + 32 * h, pk);    // over scores that are in registers or used
+                    tmem_st16(s_at + 16 * c, pk);    // over scores that are used
+                    ++c;
                 }
+                first = false;
                 tmem_wait_st();
                 umma_fence_before();
                 __syncwarp();
