@@ -39,7 +39,7 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + kConvertWarps + 2);
 constexpr int kRows = kKv8TcRows, kTile = 128, kBlocks = kTile / kKv8Block;
 constexpr int kRing = 3;            // tiles of keys, and of values
 constexpr int kNear = 8;            // tiles whose scales are kept
-constexpr float kUp = 10.f, kMost = 46340.f;
+constexpr float kUp = 7.f, kMost = 46340.f;
 constexpr float kQuiet = 1.f / 16384.f;
 
 // Values' scales are taken relative to vref, which follows the tiles of a
@@ -108,6 +108,12 @@ KS_DEV float2 add2(float2 a, float2 b) {
     return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
 }
 KS_DEV void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// v[i] of a register array, for an i that is not known when compiling
+KS_DEV float pick(const float (&v)[kBlocks], int i) {
+    const float a = i & 1 ? v[1] : v[0], b = i & 1 ? v[3] : v[2], c = i & 1 ? v[5] : v[4], d = i & 1 ? v[7] : v[6];
+    const float e = i & 2 ? b : a, f = i & 2 ? d : c;
+    return i & 4 ? f : e;
+}
 // 2^d for a whole d <= 0 (-inf: 0)
 KS_DEV float pow2_below(float d) { return d < -126.f ? 0.f : __uint_as_float((uint32_t)(127 + (int)d) << 23); }
 // The first n x 32 weights of a row, in TMEM, times f <= 1, in two factors: below
@@ -402,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
         if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
     } else {
         // --------------------------------------------------------- softmax
-        const int i = warp >> 2, quad = warp & 3, row = 32 * quad + lane;
+        const int i = warp >> 2, quad = warp & 3, lane_row = 32 * quad + lane;
         const uint32_t lanes = tmem + ((uint32_t)(32 * quad) << 16);
         const uint32_t s_at = lanes + 128 * i, o_at = lanes + 256 + 128 * i;
         bool alive = true, began = false;
@@ -410,11 +416,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
         for (;;) {
             const Rows rows(at.q, p.tq, at.g, G);
             const int cnt = at.end - at.tile;
+            // Few rows: they stand in the 128 two or four times, and the warps of a copy take 64 or 32 of a tile's keys
+            // (TMEM lanes belong to warps: the other warps could not help with them).  Their weights of the other
+            // keys are zeros, and the copies' O are added at the end.
+            const int copies = rows.n <= 32 ? 4 : rows.n <= 64 ? 2 : 1, per = 4 / copies;
+            const int row = 32 * (quad % per) + lane, c0 = quad / per * per, c1 = c0 + per;     // own 32-key chunks
             {
                 // the unit's queries in two codes: two threads a row
-                const int qr = tid >> 1, half = tid & 1;
-                const bool valid = qr < rows.n;
-                const int tok = valid ? qr / G : 0, head = at.h * G + (valid ? qr - tok * G : 0);
+                const int qr = tid >> 1, half = tid & 1, ur = qr & (kRows / copies - 1);
+                const bool valid = ur < rows.n;
+                const int tok = valid ? ur / G : 0, head = at.h * G + (valid ? ur - tok * G : 0);
                 const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head + half * (HD / 2);
                 uint4 raw[HD / 16];
                 if (p.q_wide) {
@@ -439,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 // a scale below zero goes into the codes' sign, so that the factors of the scores are positive
                 const float sc = scale_for(top), inv = t.scale < 0.f ? -inverse_pow2(sc) : inverse_pow2(sc);
-                if (half == 0) sm.qf[qr] = sc * (fabsf(t.scale) * kLog2e);
+                if (half == 0 && qr < kRows / copies) sm.qf[qr] = sc * (fabsf(t.scale) * kLog2e);
 #pragma unroll
                 for (int c = 0; c < HD / 32; ++c) {
                     uint32_t hi[4], lo[4];
@@ -498,14 +509,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 alive = alive && mbar_wait(&sm.s_full[i], n & 1, kWaitLimitNs);
                 __syncwarp();
                 umma_fence_after();
-                if (32 * quad >= rows.n) {           // no row: P stays what it is, in lanes that nobody reads
+                if (32 * (quad % per) >= rows.n) {   // no row: P stays what it is, in lanes that nobody reads
                     if (lane == 0) mbar_arrive(&sm.p_full[i]);
                     continue;
                 }
                 if (have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0) {
                     // what a row does not see becomes -inf where it lies, so that the pass below needs no mask
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = c0; c < c1; ++c) {
                         uint32_t x[32];
                         tmem_ld32(x, s_at + 32 * c);
                         tmem_wait_ld();
@@ -521,15 +532,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     if (!first) rescale(vref * inverse_pow2(vnew));
                     vref = vnew;
                 }
-                // 32 scores at a time, in a loop that stays one: unrolled, the roles' code together no longer fits
-                // the instruction cache, and a tile of the softmax takes up to 6700 clocks instead of 1500.
-                bool tried = false;
+                if (__any_sync(0xffffffffu, m == -INFINITY)) {
+                    float top = m;
 #pragma unroll 1
-                for (int c = 0; c < 4;) {
+                    for (int c = c0; c < c1; ++c) {
+                        uint32_t x[32];
+                        tmem_ld32(x, s_at + 32 * c);
+                        const float f0 = pick(f, 2 * c), f1 = pick(f, 2 * c + 1);
+                        tmem_wait_ld();
+                        tmem_pin(x);
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) top = fmaxf(top, __uint_as_float(x[q]) * (q < 16 ? f0 : f1));
+                    }
+                    if (m == -INFINITY) m = ceilf(top);          // l and O are still zero
+                }
+                // 32 scores at a time, in a loop that stays one: unrolled, the roles' code together no longer fits
+                // the instruction cache, and a tile of the softmax takes up to 6700 clocks.
+#pragma unroll 1
+                for (int c = c0; c < c1;) {
                     uint32_t s[32], pk[16];
                     tmem_ld32(s, s_at + 32 * c);
-                    const float f0 = c < 2 ? (c == 0 ? f[0] : f[2]) : (c == 2 ? f[4] : f[6]);
-                    const float f1 = c < 2 ? (c == 0 ? f[1] : f[3]) : (c == 2 ? f[5] : f[7]);
+                    const float f0 = pick(f, 2 * c), f1 = pick(f, 2 * c + 1);
                     const float ref = (m == -INFINITY ? 0.f : m) - kUp;
                     tmem_wait_ld();
                     tmem_pin(s);
@@ -545,8 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     }
                     part[0] = add2(part[0], part[1]);
                     const float sum = part[0].x + part[0].y;
-                    // at most kMost: no weight passes f16; just raised, it is at most 2^15
-                    const bool raise = sum > kMost || (m == -INFINITY && !tried);
+                    const bool raise = sum > kMost;              // else no weight passes f16; just raised, it is at most 2^12
                     if (__any_sync(0xffffffffu, raise)) {
                         float top = m;
 #pragma unroll
@@ -557,11 +579,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                         l *= fac;
                         m = mnew;
                         if (!first) rescale(fac);
-                        scale_weights(s_at, c, fac);             // of this tile so far
-                        tried = true;
+                        scale_weights(s_at + 16 * c0, c - c0, fac);      // of this tile so far
                         continue;
                     }
-                    tried = false;
                     l += sum;
                     if (vnow < 0.f) {                // a quiet block
                         const float vinv = inverse_pow2(vref);
@@ -577,6 +597,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     tmem_st16(s_at + 16 * c, pk);    // over scores that are used
                     ++c;
                 }
+                if (copies > 1) {
+                    uint32_t zero[16];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) zero[q] = 0;
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c)
+                        if (c < c0 || c >= c1) tmem_st16(s_at + 16 * c, zero);
+                }
                 first = false;
                 tmem_wait_st();
                 umma_fence_before();
@@ -586,22 +614,30 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
             // ---------------------------------------------- segment's end
             const bool mine = cnt > i;               // this stream had a tile
             if (mine) alive = alive && mbar_wait(&sm.o_full[i], (n - 1) & 1, kWaitLimitNs);
-            sm.join[i][row] = make_float4(m, l, vref, 0.f);
+            sm.join[i][lane_row] = make_float4(m, l, vref, 0.f);
             umma_fence_before();
             softmax_sync();
             umma_fence_after();
-            // both streams' O over half of the dims each
-            const float4 u0 = sm.join[0][row], u1 = sm.join[1][row];
-            const float top = fmaxf(u0.x, u1.x), ref = top == -INFINITY ? 0.f : top;
-            const float e0 = exp2_approx(u0.x - ref), e1 = exp2_approx(u1.x - ref), sum = u0.y * e0 + u1.y * e1;
+            // both streams' O over half of the dims each, relative to the maximum over streams and copies
+            float top = -INFINITY, sum = 0.f;
+            for (int c = 0; c < copies; ++c)
+                top = fmaxf(top, fmaxf(sm.join[0][row + c * per * 32].x, sm.join[1][row + c * per * 32].x));
+            const float ref = top == -INFINITY ? 0.f : top;
+            for (int c = 0; c < copies; ++c)
+                for (int k = 0; k < 2; ++k) {
+                    const float4 u = sm.join[k][row + c * per * 32];
+                    sum = fmaf(u.y, exp2_approx(u.x - ref), sum);
+                }
+            const float4 u0 = sm.join[0][lane_row], u1 = sm.join[1][lane_row];
+            const float o0 = exp2_approx(u0.x - ref) * u0.z, o1 = exp2_approx(u1.x - ref) * u1.z;
             const bool whole = at.tile == 0 && at.end == at.tiles;
             const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
-            const float c0 = e0 * u0.z * inv, c1 = e1 * u1.z * inv;
             const bool valid = row < rows.n, any_nan = sm.any_nan[seg & 3];
             const int tok = valid ? row / G : 0, head = at.h * G + (valid ? row - tok * G : 0);
             float* slot = p.part + ((size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg + row) * (HD + 4);
             __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row + (int64_t)head * t.out_head;
-#pragma unroll
+            float* pile = reinterpret_cast<float*>(sm.q);        // free: every product with it is done
+#pragma unroll 1
             for (int c = 0; c < HD / 64; ++c) {
                 const int d0 = i * (HD / 2) + 32 * c;
                 uint32_t x[32], y[32];
@@ -612,12 +648,33 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 tmem_pin(y);
 #pragma unroll
                 for (int q = 0; q < 32; ++q) {
-                    float v = __uint_as_float(x[q]) * c0;
-                    if (cnt > 1) v = fmaf(__uint_as_float(y[q]), c1, v);
+                    float v = __uint_as_float(x[q]) * o0;
+                    if (cnt > 1) v = fmaf(__uint_as_float(y[q]), o1, v);
+                    x[q] = __float_as_uint(v);
+                }
+                // add the copies, half of them at a time: 32 x 32 values a warp
+                for (int n = copies / 2; n > 0; n /= 2) {
+                    const int copy = quad / per;
+                    softmax_sync();
+                    if (copy >= n && copy < 2 * n) {
+                        float* to = pile + (i * 2 + (quad - n * per)) * 1024 + lane;
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) to[32 * q] = __uint_as_float(x[q]);
+                    }
+                    softmax_sync();
+                    if (copy < n) {
+                        const float* from = pile + (i * 2 + quad) * 1024 + lane;
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) x[q] = __float_as_uint(__uint_as_float(x[q]) + from[32 * q]);
+                    }
+                }
+                if (quad >= per || !valid) continue;
+#pragma unroll
+                for (int q = 0; q < 32; ++q) {
+                    float v = __uint_as_float(x[q]) * inv;
                     if (any_nan && sm.nan_from[seg & 3][d0 + q] <= lim) v = __uint_as_float(0x7fc00000u);
                     x[q] = __float_as_uint(v);
                 }
-                if (!valid) continue;
                 if (!whole) {
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
@@ -636,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     for (int q = 0; q < 32; ++q) out[d0 + q] = __float2bfloat16_rn(__uint_as_float(x[q]));
                 }
             }
-            if (valid && i == 0) {
+            if (valid && i == 0 && quad < per) {
                 // l and o carry the factor 2^kUp
                 if (!whole) *reinterpret_cast<float2*>(slot) = make_float2(top - kUp, sum);
                 else if (t.lse) t.lse[(size_t)(rows.row0 + tok) * t.hq + head] = sum == 0.f ? -INFINITY : (top - kUp + log2f(sum)) * kLn2;
@@ -645,6 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                 began = true;
                 if (tid == 0) p.desc[blockIdx.x] = make_int4(rows.row0, rows.n, at.h, run.cta_of(at.first + at.tiles - 1));
             }
+            if (copies > 1) softmax_sync();          // the pile is read: the next queries may go there
             umma_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.o_free);
