@@ -262,6 +262,18 @@ bool make_wide_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t K
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_kv8_map(CUtensorMap* map, const void* base, uint64_t records, uint32_t hd, uint32_t box_records) {
+    auto encode = tensor_map_encoder();
+    if (!encode || records > INT32_MAX || (reinterpret_cast<uintptr_t>(base) & 15) != 0) return false;
+    const cuuint64_t dims[2] = {4 * (cuuint64_t)hd + 4, records};      // 8-byte elements of a record
+    const cuuint64_t strides[1] = {32 * (cuuint64_t)hd + 32};
+    const cuuint32_t box[2] = {2 * hd, box_records};
+    const cuuint32_t estr[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, 2, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_wide_kv_map(CUtensorMap* map, const void* base, uint64_t rows, uint32_t hd) {
     auto encode = tensor_map_encoder();
     if (!encode || hd % 64 != 0 || (reinterpret_cast<uintptr_t>(base) & 15) != 0) return false;

@@ -52,6 +52,8 @@ bool make_chunk_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t 
 // swizzle (an operand's stage), and 128 whole cache rows of hd elements.
 bool make_wide_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t K);
 bool make_wide_kv_map(CUtensorMap* map, const void* base, uint64_t rows, uint32_t hd);
+// Map of the 8-bit cache's records (kv8.cuh): boxes of box_records records' keys, or values.
+bool make_kv8_map(CUtensorMap* map, const void* base, uint64_t records, uint32_t hd, uint32_t box_records);
 
 // ----------------------------------------------------------------- chain
 // bf16 models: a run of consecutive projections (phases) in one persistent

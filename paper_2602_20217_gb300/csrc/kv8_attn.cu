@@ -580,15 +580,15 @@ cudaError_t launch_few(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p,
     auto kern = kv8_attention_kernel<HD, NQ>;
     constexpr int bytes = sizeof(Smem<HD, NQ>);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, a, t, p, s);
+    return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, s, a, t, p);
 }
 
 template <int HD>
 cudaError_t launch_merge(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, int64_t units, cudaStream_t s) {
     const int x = (int)std::min<int64_t>(p.ctas, units), rows = p.tq * (t.hq / a.hk);
     if (units * units < p.ctas)
-        return launch_kv8(kv8_merge_kernel<HD, 8>, dim3(x, (rows + 1) / 2), kMergeThreads, 0, a, t, p, s);
-    return launch_kv8(kv8_merge_kernel<HD, 2>, dim3(x, (rows + 7) / 8), kMergeThreads, 0, a, t, p, s);
+        return launch_kv8(kv8_merge_kernel<HD, 8>, dim3(x, (rows + 1) / 2), kMergeThreads, 0, s, a, t, p);
+    return launch_kv8(kv8_merge_kernel<HD, 2>, dim3(x, (rows + 7) / 8), kMergeThreads, 0, s, a, t, p);
 }
 
 // The plan of a call; false if its line of tiles is too long for 32 bits.

@@ -29,6 +29,7 @@ struct Kv8Plan {
     int tq;             // tokens of a group
     int rg;             // rows of a group, at least tq query groups
     int ctas;
+    int run;            // records of a copy (tcgen05 kernel)
     bool q_wide, out_wide;  // queries can be read, the output written 16 bytes at a time
     float* part;        // [2 ctas][rg][HD + 4]: m, l, -, -, o
     int4* desc;         // [ctas]: the unit that begins in this CTA's run and ends in a later one's: first batch row,
@@ -187,9 +188,8 @@ struct Rows {
 };
 
 // Programmatic launch: the kernel waits for what is before it by itself.
-template <class K>
-cudaError_t launch_kv8(K kern, dim3 grid, int threads, int smem, const Kv8Args& a, const Kv8AttnArgs& t,
-                       const Kv8Plan& p, cudaStream_t s) {
+template <class K, class... Args>
+cudaError_t launch_kv8(K kern, dim3 grid, int threads, int smem, cudaStream_t s, const Args&... args) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
@@ -200,7 +200,7 @@ cudaError_t launch_kv8(K kern, dim3 grid, int threads, int smem, const Kv8Args& 
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, a, t, p);
+    return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
 cudaError_t launch_kv8_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s);   // kv8_tc.cu

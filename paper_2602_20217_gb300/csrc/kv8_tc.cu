@@ -45,7 +45,7 @@ constexpr float kQuiet = 1.f / 16384.f;
 // Values' scales are taken relative to vref, which follows the tiles of a
 // segment in order: four times the loudest block seen, raised when one passes
 // it.  Both the converting warps and the streams compute it.
-KS_DEV float next_vref(float vref, const float4* scale, int have) {
+KS_DEV float next_vref(float vref, const float2* scale, int have) {
     float top = 0.f;
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c)
@@ -67,7 +67,7 @@ struct Smem {
     unsigned char k[kRing][TILE];               // [key / 8][HD / 16][8][16]
     unsigned char v[kRing][TILE];               // [key / 16][HD][16]
     unsigned char v16[2][2 * TILE];             // f16 [key / 8][HD][8]
-    float4 scale[kNear][kBlocks];               // key scale, value scale
+    float2 scale[kNear][kBlocks];               // key scale, value scale
     float4 join[2][kRows];                      // m, l, vref of a stream
     float qf[kRows];
     float vref[kNear];                          // of a tile; negative: one of its blocks is quiet
@@ -137,7 +137,8 @@ KS_DEV void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 KS_DEV void convert_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 
 template <int HD>
-__global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
+__global__ void __launch_bounds__(kThreads, 1)
+    kv8_tc_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p, const __grid_constant__ CUtensorMap map) {
     using S = Smem<HD>;
     constexpr int REC = kv8_record(HD), PART = kKv8Block * HD;   // a record's keys (or values)
     extern __shared__ __align__(128) unsigned char smem_raw[];
@@ -195,6 +196,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
             const int page = __ldg(a.table + (size_t)k.s * a.table_ld + b / a.bpp);
             return page >= 0 && page < a.n_pages ? page : -2;
         };
+        // a run of p.run records is one copy of keys and one of values
+        const int r = lane % kBlocks;
+        const unsigned heads = p.run == 8 ? 0x01u : p.run == 4 ? 0x11u : p.run == 2 ? 0x55u : 0xffu;
         int it = 0, tile = at.tile, page = pages(at, tile);
         bool alive = true, more = true;
         while (more && alive) {
@@ -206,10 +210,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
             }
             const int next_page = more ? pages(next, next_tile) : -1;
             if (page == -2) kv8_flag(a, kKv8BadPage);
-            const int b = tile * kBlocks + lane;
-            const unsigned char* rec =
-                page >= 0 ? a.data + (((size_t)page * a.hk + at.h) * a.bpp + b % a.bpp) * REC : nullptr;
-            const unsigned have = __ballot_sync(0xffffffffu, rec != nullptr);
+            const int record = page >= 0 ? (page * a.hk + at.h) * a.bpp + (tile * kBlocks + lane) % a.bpp : -1;
+            // the scales come by ordinary loads, behind the first copies
+            float2 scale = make_float2(0.f, 0.f);
+            if (record >= 0) scale = __ldg(reinterpret_cast<const float2*>(a.data + (size_t)record * REC + 2 * PART));
+            const unsigned have = __ballot_sync(0xffffffffu, record >= 0);
             for (int i = 0; i < TILES && tile + i < at.end; ++i, ++it) {
                 const int st = it % kRing, near = it % kNear, odd = ((it / kRing) & 1) ^ 1;
                 const unsigned mask = have >> (i * kBlocks) & ((1u << kBlocks) - 1);
@@ -219,19 +224,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
                     break;
                 }
                 if (lane == 0) {
-                    const int n = __popc(mask);
+                    const uint32_t bytes = __popc(mask & heads) * p.run * PART;
                     present[near] = (int)mask;
-                    mbar_expect_tx(&sm.scales[near], n * 16);
-                    mbar_expect_tx(&sm.k_full[st], n * PART);
-                    mbar_expect_tx(&sm.v_full[st], n * PART);
+                    mbar_expect_tx(&sm.k_full[st], bytes);
+                    mbar_expect_tx(&sm.v_full[st], bytes);
                 }
                 __syncwarp();
-                if (rec && lane / kBlocks == i) {
-                    const int r = lane % kBlocks;
-                    bulk_load(sm.k[st] + r * PART, rec, PART, &sm.k_full[st]);
-                    bulk_load(&sm.scale[near][r], rec + 2 * PART, 16, &sm.scales[near]);
-                    bulk_load(sm.v[st] + r * PART, rec + PART, PART, &sm.v_full[st]);
+                if (lane / kBlocks == i && record >= 0) {
+                    if (heads >> r & 1) {
+                        tma_2d(sm.k[st] + r * PART, &map, 0, record, &sm.k_full[st]);
+                        tma_2d(sm.v[st] + r * PART, &map, PART / 8, record, &sm.v_full[st]);
+                    }
+                    sm.scale[near][r] = scale;
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.scales[near]);
             }
             at = next;
             tile = next_tile;
@@ -239,9 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
         }
         if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
         // no copy may be in flight when the CTA ends
-        for (int i = max(0, it - kNear); i < it; ++i) {
-            mbar_wait(&sm.scales[i % kNear], (i / kNear) & 1, kWaitLimitNs);
-            if (i < it - kRing) continue;
+        for (int i = max(0, it - kRing); i < it; ++i) {
             mbar_wait(&sm.k_full[i % kRing], (i / kRing) & 1, kWaitLimitNs);
             mbar_wait(&sm.v_full[i % kRing], (i / kRing) & 1, kWaitLimitNs);
         }
@@ -724,11 +729,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_tc_kernel(const Kv8Args a, co
 }
 
 template <int HD>
-cudaError_t launch_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s) {
+cudaError_t launch_tc(const Kv8Args& a, const Kv8AttnArgs& t, Kv8Plan p, cudaStream_t s) {
     auto kern = kv8_tc_kernel<HD>;
     constexpr int bytes = sizeof(Smem<HD>);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, a, t, p, s);
+    if (e != cudaSuccess) return e;
+    // records of a page in one copy, as many as divide a page's and a tile's: a copy costs its unit about 78 clocks,
+    // and 24 small ones a tile (keys, values and scales of each record) took 1870, more than the tile's bytes
+    p.run = a.bpp % 8 == 0 ? 8 : a.bpp % 4 == 0 ? 4 : a.bpp % 2 == 0 ? 2 : 1;
+    CUtensorMap map;
+    if (!make_kv8_map(&map, a.data, (uint64_t)a.n_pages * a.hk * a.bpp, HD, p.run)) return cudaErrorInvalidValue;
+    return launch_kv8(kern, dim3(p.ctas), kThreads, bytes, s, a, t, p, map);
 }
 
 }  // namespace
