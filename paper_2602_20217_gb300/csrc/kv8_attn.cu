@@ -2,11 +2,11 @@
 // (decoding), the merge of split units for every size, and the choice between
 // this kernel and the tcgen05 one (kv8_tc.cu).  kv8_plan.cuh cuts the work.
 //
-// A CTA is a producer warp and four consumer warps around a ring of tiles of
-// 64 NQ keys.  A tile is 4 NQ records of the cache, one contiguous copy each,
-// wherever their pages are.  All four warps have the unit's 8 NQ rows, each
-// takes one 16 NQ-key step of every tile, with softmax statistics of its own,
-// and they are joined at the segment's end.
+// A CTA is a producer warp and four consumer warps around a ring of four tiles
+// of 64 keys.  A tile is four records of the cache, contiguous ones in one copy,
+// wherever their pages are.  The unit's 8 NQ rows are every warp's, each takes
+// one 16-key step of a tile, with softmax statistics of its own, and they are
+// joined at the segment's end.
 //
 // A step, per 8 rows:
 //   S (8 rows x 16 keys) = Q K^T by m16n8k32 e4m3: the cached codes go to the
@@ -36,6 +36,7 @@ namespace {
 
 constexpr int kConsumers = 4;
 constexpr int kThreads = 32 * (kConsumers + 1);
+constexpr int kBlocks = 4, kTile = kBlocks * kKv8Block, kStages = 4;
 constexpr float kWeightUp = 16384.f;
 
 KS_DEV void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -62,18 +63,17 @@ KS_DEV void consumers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 template <int HD, int NQ>
 struct Smem {
     static constexpr int REC = kv8_record(HD);
-    static constexpr int SB = NQ;                                // records of a step
-    static constexpr int BLOCKS = kConsumers * SB;                   // records of a tile
-    static constexpr int TILE = BLOCKS * REC;
-    static constexpr int STAGES = NQ == 1 ? 4 : 2;
+    static constexpr int TILE = kBlocks * REC;
     static constexpr int HALF = NQ * (HD / 32) * 4 * 32;         // floats: half of a warp's o
-    unsigned char ring[STAGES][TILE];
+    static constexpr bool Q = NQ > 1;                            // queries here instead of in registers
+    unsigned char ring[kStages][TILE];
     float comb[kConsumers][HALF];
+    uint32_t q[Q ? NQ * (HD / 32) * 4 * 32 : 4];                 // [NQ][HD / 32] A operands, 4 matrices each
     float2 ml[kConsumers][8 * NQ];
     int nan_from[3][HD];                                         // first key whose value is NaN, a segment each
     int any_nan[3];
-    int present[STAGES];                                         // records that were copied
-    uint64_t full[STAGES], empty[STAGES];
+    int present[kStages];                                        // records that were copied
+    uint64_t full[kStages], empty[kStages];
 };
 
 // o[i][c] = NaN for i and c that are not known when compiling (rare)
@@ -131,14 +131,14 @@ template <int HD, int NQ>
 __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     kv8_attention_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
     using S = Smem<HD, NQ>;
-    constexpr int REC = S::REC, SB = S::SB, BLOCKS = S::BLOCKS, STAGES = S::STAGES, DT = HD / 16, KJ = HD / 32;
+    constexpr int REC = S::REC, DT = HD / 16, KJ = HD / 32;
     extern __shared__ __align__(128) unsigned char smem_raw[];
     S& sm = *reinterpret_cast<S*>(smem_raw);
     volatile int* present = sm.present;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int i = 0; i < STAGES; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(&sm.full[i], 1);
             mbar_init(&sm.empty[i], kConsumers);
         }
@@ -162,11 +162,11 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         // ------------------------------------------------------- producer
         // Page numbers are read a group of tiles ahead, across segments: under
         // load such a read takes microseconds.
-        constexpr int TILES = 32 / BLOCKS;                       // tiles of a group, a block per lane
+        constexpr int TILES = 32 / kBlocks;                      // tiles of a group, a block per lane
         auto pages = [&](const Segment& k, int tile) {
-            const int b = tile * BLOCKS + lane;
+            const int b = tile * kBlocks + lane;
             const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
-            if (b * kKv8Block > last || tile + lane / BLOCKS >= k.end) return -1;
+            if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
             const int page = __ldg(a.table + (size_t)k.s * a.table_ld + b / a.bpp);
             return page >= 0 && page < a.n_pages ? page : -2;
         };
@@ -182,21 +182,28 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
             }
             const int next_page = more ? pages(next, next_tile) : -1;
             if (page == -2) kv8_flag(a, kKv8BadPage);
-            const int b = tile * BLOCKS + lane;
+            const int b = tile * kBlocks + lane;
             const unsigned char* rec =
                 page >= 0 ? a.data + (((size_t)page * a.hk + at.h) * a.bpp + b % a.bpp) * REC : nullptr;
             const unsigned have = __ballot_sync(0xffffffffu, rec != nullptr);
+            // one copy for records that follow each other: the lane of the first one makes it
+            const unsigned char* before = reinterpret_cast<const unsigned char*>(
+                __shfl_up_sync(0xffffffffu, reinterpret_cast<unsigned long long>(rec), 1));
+            const bool head = rec != nullptr && (lane % kBlocks == 0 || before == nullptr || rec != before + REC);
+            const unsigned ends = (__ballot_sync(0xffffffffu, head || rec == nullptr) | 0x11111111u) >> lane >> 1;
+            const int length = min(ends ? __ffs(ends) : 32, kBlocks - lane % kBlocks);
             for (int i = 0; i < TILES && tile + i < at.end; ++i, ++it) {
-                const int st = it % STAGES;
-                const unsigned mask = have >> (i * BLOCKS) & ((1u << BLOCKS) - 1);
-                alive = mbar_wait(&sm.empty[st], ((it / STAGES) & 1) ^ 1, kWaitLimitNs);
+                const int st = it % kStages;
+                const unsigned mask = have >> (i * kBlocks) & ((1u << kBlocks) - 1);
+                alive = mbar_wait(&sm.empty[st], ((it / kStages) & 1) ^ 1, kWaitLimitNs);
                 if (!alive) break;
                 if (lane == 0) {
                     present[st] = (int)mask;
                     mbar_expect_tx(&sm.full[st], __popc(mask) * REC);
                 }
                 __syncwarp();
-                if (rec && lane / BLOCKS == i) bulk_load(sm.ring[st] + lane % BLOCKS * REC, rec, REC, &sm.full[st]);
+                if (head && lane / kBlocks == i)
+                    bulk_load(sm.ring[st] + lane % kBlocks * REC, rec, length * REC, &sm.full[st]);
             }
             at = next;
             tile = next_tile;
@@ -204,8 +211,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         }
         if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
         // no copy may be in flight when the CTA ends
-        for (int i = max(0, it - STAGES); i < it; ++i)
-            mbar_wait(&sm.full[i % STAGES], (i / STAGES) & 1, kWaitLimitNs);
+        for (int i = max(0, it - kStages); i < it; ++i)
+            mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, kWaitLimitNs);
         return;
     }
 
@@ -216,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     for (int buf = 0;; buf = buf == 2 ? 0 : buf + 1) {
         const Rows rows(at.q, p.tq, at.g, G);
         // this warp's queries, in two codes
-        uint32_t qa[NQ][KJ][4];
+        uint32_t qa[S::Q ? 1 : NQ][S::Q ? 1 : KJ][4];
         float qf[NQ];
         int lim[NQ];                                             // last key that the row sees
         const int lim_first = rows.pos0, lim_last = rows.pos0 + (rows.n - 1) / G;
@@ -261,11 +268,21 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     const float* v = x[2 * j + half];
                     const uint16_t h0 = to_e4m3x2(v[0] * inv, v[1] * inv), h1 = to_e4m3x2(v[2] * inv, v[3] * inv);
                     const float2 f0 = from_e4m3x2(h0), f1 = from_e4m3x2(h1);
-                    qa[n][j][2 * half] = h0 | (uint32_t)h1 << 16;
-                    qa[n][j][2 * half + 1] = to_e4m3x2(v[0] * inv - f0.x, v[1] * inv - f0.y) |
-                                             (uint32_t)to_e4m3x2(v[2] * inv - f1.x, v[3] * inv - f1.y) << 16;
+                    const uint32_t hi = h0 | (uint32_t)h1 << 16;
+                    const uint32_t lo = to_e4m3x2(v[0] * inv - f0.x, v[1] * inv - f0.y) |
+                                        (uint32_t)to_e4m3x2(v[2] * inv - f1.x, v[3] * inv - f1.y) << 16;
+                    if constexpr (S::Q) {
+                        if (warp == 0) {             // matrix i of (n, j), row g, bytes 4 q4 ..
+                            sm.q[(n * KJ + j) * 128 + 64 * half + lane] = hi;
+                            sm.q[(n * KJ + j) * 128 + 64 * half + 32 + lane] = lo;
+                        }
+                    } else {
+                        qa[n][j][2 * half] = hi;
+                        qa[n][j][2 * half + 1] = lo;
+                    }
                 }
         }
+        if constexpr (S::Q) consumers_sync();
         float m[NQ], l[NQ], vref = 0.f, o[NQ][DT][4];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -276,58 +293,54 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         }
 
         for (int tile = at.tile; tile < at.end; ++tile, ++it) {
-            const int st = it % STAGES;
-            if (alive) alive = mbar_wait(&sm.full[st], (it / STAGES) & 1, kWaitLimitNs);
-            const int have = alive ? present[st] : 0;
-            const int got = have >> (SB * warp) & ((1 << SB) - 1), key0 = (tile * kConsumers + warp) * SB * kKv8Block;
-            if (got != 0 && key0 <= lim_last) {
-                const unsigned char* rec = sm.ring[st] + SB * warp * REC;
+            const int st = it % kStages;
+            if (alive) alive = mbar_wait(&sm.full[st], (it / kStages) & 1, kWaitLimitNs);
+            const int have = alive ? present[st] : 0, key0 = tile * kTile + warp * kKv8Block;
+            if ((have >> warp & 1) && key0 <= lim_last) {
+                const unsigned char* rec = sm.ring[st] + warp * REC;
                 const uint32_t base = smem_u32(rec);
-                const bool edge = got != (1 << SB) - 1 || key0 + SB * kKv8Block - 1 > lim_first;
-                float2 sc[SB];                                   // key and value scales
+                const bool edge = key0 + kKv8Block - 1 > lim_first;
+                const float2 sc = *reinterpret_cast<const float2*>(rec + 32 * HD);       // key and value scales
+                float s[NQ][2][4];
 #pragma unroll
-                for (int i = 0; i < SB; ++i) sc[i] = *reinterpret_cast<const float2*>(rec + i * REC + 32 * HD);
-                float s[NQ][2 * SB][4];
+                for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int nb = 0; nb < 2 * SB; ++nb) {
-                    const uint32_t kb = base + (nb >> 1) * REC + (nb & 1) * 8 * HD + lane * 16;
+                    for (int c = 0; c < 4; ++c) s[n][0][c] = s[n][1][c] = 0.f;
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) s[n][nb][0] = s[n][nb][1] = s[n][nb][2] = s[n][nb][3] = 0.f;
+                for (int j = 0; j < KJ / 2; ++j) {
+                    uint32_t k0[4], k1[4];
+                    ldsm_x4(k0, base + lane * 16 + j * 512);
+                    ldsm_x4(k1, base + 8 * HD + lane * 16 + j * 512);
 #pragma unroll
-                    for (int j = 0; j < KJ / 2; ++j) {
-                        uint32_t kf[4];
-                        ldsm_x4(kf, kb + j * 512);
+                    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                        for (int n = 0; n < NQ; ++n) {
-                            mma_e4m3(s[n][nb], qa[n][2 * j], kf[0], kf[1]);
-                            mma_e4m3(s[n][nb], qa[n][2 * j + 1], kf[2], kf[3]);
+                        for (int e = 0; e < 2; ++e) {
+                            if constexpr (S::Q) {
+                                uint32_t q[4];
+                                ldsm_x4(q, smem_u32(sm.q + (n * KJ + 2 * j + e) * 128) + lane * 16);
+                                mma_e4m3(s[n][0], q, k0[2 * e], k0[2 * e + 1]);
+                                mma_e4m3(s[n][1], q, k1[2 * e], k1[2 * e + 1]);
+                            } else {
+                                mma_e4m3(s[n][0], qa[n][2 * j + e], k0[2 * e], k0[2 * e + 1]);
+                                mma_e4m3(s[n][1], qa[n][2 * j + e], k1[2 * e], k1[2 * e + 1]);
+                            }
                         }
-                    }
                 }
-                // values of a record that is not there count for nothing
-                float vnew = vref, w[SB];
-#pragma unroll
-                for (int i = 0; i < SB; ++i) {
-                    w[i] = got >> i & 1 ? sc[i].y : 0.f;
-                    vnew = fmaxf(vnew, w[i]);
-                }
-                const float vinv = inverse_pow2(vnew), vfac = vref * vinv;
-#pragma unroll
-                for (int i = 0; i < SB; ++i) w[i] = w[i] * vinv * kWeightUp;    // in this order: vinv may be 2^126
+                const float vnew = fmaxf(vref, sc.y), vinv = inverse_pow2(vnew), vfac = vref * vinv;
+                const float w = sc.y * vinv * kWeightUp;         // in this order: vinv may be 2^126
                 vref = vnew;
-                uint32_t pb[NQ][2 * SB];
+                uint32_t pb[NQ][2];
                 float fac[NQ];
                 bool same = true;
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) {
-                    float x[2 * SB][2], top = m[n];
+                    float x[2][2], top = m[n];
 #pragma unroll
-                    for (int nb = 0; nb < 2 * SB; ++nb)
+                    for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            x[nb][e] = (s[n][nb][e] + s[n][nb][2 + e]) * (qf[n] * sc[nb >> 1].x);
-                            if (edge && (key0 + 8 * nb + 2 * q4 + e > lim[n] || !(got >> (nb >> 1) & 1)))
-                                x[nb][e] = -INFINITY;
+                            x[nb][e] = (s[n][nb][e] + s[n][nb][2 + e]) * (qf[n] * sc.x);
+                            if (edge && key0 + 8 * nb + 2 * q4 + e > lim[n]) x[nb][e] = -INFINITY;
                             top = fmaxf(top, x[nb][e]);
                         }
                     top = quad_max(top);
@@ -336,10 +349,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     m[n] = top;
                     float sum = 0.f;
 #pragma unroll
-                    for (int nb = 0; nb < 2 * SB; ++nb) {
+                    for (int nb = 0; nb < 2; ++nb) {
                         const float p0 = exp2_approx(x[nb][0] - ref), p1 = exp2_approx(x[nb][1] - ref);
                         sum += p0 + p1;
-                        pb[n][nb] = f16_pack(p0 * w[nb >> 1], p1 * w[nb >> 1]);
+                        pb[n][nb] = f16_pack(p0 * w, p1 * w);
                     }
                     l[n] = l[n] * al + sum;
                     fac[n] = al * vfac;
@@ -357,36 +370,32 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     }
                 }
 #pragma unroll
-                for (int kb = 0; kb < SB; ++kb) {
-                    if (!(got >> kb & 1)) continue;
+                for (int dd = 0; dd < DT / 2; ++dd) {
+                    uint32_t vf[4];
+                    ldsm_x4(vf, base + 16 * HD + dd * 512 + lane * 16);
+                    if (edge) {
+                        // tokens that not every row sees: a NaN would pass through a weight of zero.  It is taken
+                        // out, and the rows that do see it get their NaN at the end.
 #pragma unroll
-                    for (int dd = 0; dd < DT / 2; ++dd) {
-                        uint32_t vf[4];
-                        ldsm_x4(vf, base + kb * REC + 16 * HD + dd * 512 + lane * 16);
-                        if (edge) {
-                            // tokens that not every row sees: a NaN would pass through a weight of zero.  It is
-                            // taken out, and the rows that do see it get their NaN at the end.
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t nan = ((vf[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-                                if (nan) {
-                                    sm.any_nan[buf] = 1;
-                                    for (int c = 0; c < 4; ++c)
-                                        if (nan >> (8 * c + 7) & 1)
-                                            atomicMin(&sm.nan_from[buf][32 * dd + 8 * i + g],
-                                                      key0 + 16 * kb + 2 * q4 + (c & 1) + 8 * (c >> 1));
-                                    vf[i] &= ~((nan >> 7) * 0xffu);
-                                }
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t nan = ((vf[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                            if (nan) {
+                                sm.any_nan[buf] = 1;
+                                for (int c = 0; c < 4; ++c)
+                                    if (nan >> (8 * c + 7) & 1)
+                                        atomicMin(&sm.nan_from[buf][32 * dd + 8 * i + g],
+                                                  key0 + 2 * q4 + (c & 1) + 8 * (c >> 1));
+                                vf[i] &= ~((nan >> 7) * 0xffu);
                             }
                         }
+                    }
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const uint32_t r0 = vf[2 * half], r1 = vf[2 * half + 1];
-                            const uint32_t af[4] = {f16_of((uint16_t)r0), f16_of((uint16_t)r1), f16_of((uint16_t)(r0 >> 16)),
-                                                    f16_of((uint16_t)(r1 >> 16))};
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t r0 = vf[2 * half], r1 = vf[2 * half + 1];
+                        const uint32_t af[4] = {f16_of((uint16_t)r0), f16_of((uint16_t)r1), f16_of((uint16_t)(r0 >> 16)),
+                                                f16_of((uint16_t)(r1 >> 16))};
 #pragma unroll
-                            for (int n = 0; n < NQ; ++n) mma_f16(o[n][2 * dd + half], af, pb[n][2 * kb], pb[n][2 * kb + 1]);
-                        }
+                        for (int n = 0; n < NQ; ++n) mma_f16(o[n][2 * dd + half], af, pb[n][0], pb[n][1]);
                     }
                 }
             }
@@ -566,14 +575,18 @@ __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args 
     if (t.lse && lane == 0) t.lse[(size_t)(u.x + tok) * t.hq + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-// Query rows of a unit: 8 or 16 for this file's kernel, else the tcgen05
-// kernel's 128, by the batch's average per sequence and KV head, and at least G
-// (whole tokens).
+// Query rows of a unit by the batch's average per sequence and KV head, and at
+// least G (whole tokens): 8 or 16 for this file's kernel, else the tcgen05
+// kernel's 128.  On the Qwen3-32B shape at 64k, 16 rows take 41 us here and 49 us
+// there; 24 rows take 74 us here (three row tiles of registers spill), 32 in two
+// warps of 16 rows 65 us, and 56 us there.
 int rows_of_unit(int G, int64_t n_rows, int64_t n_seqs) {
     const int64_t avg = n_seqs > 0 ? (n_rows * G + n_seqs - 1) / n_seqs : 0;
     const int64_t need = std::max<int64_t>(avg, G);
     return need <= 8 ? 8 : need <= 16 ? 16 : kKv8TcRows;
 }
+// CTAs of an SM
+int resident(int rg) { return rg == kKv8TcRows ? 1 : rg == 8 ? 3 : 2; }
 
 template <int HD, int NQ>
 cudaError_t launch_few(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s) {
@@ -597,7 +610,7 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& ti
     p = Kv8Plan{};
     p.rg = rows_of_unit(G, a.n_rows, a.n_seqs);
     p.tq = p.rg / G;
-    p.tile = p.rg == 8 ? 64 : 128;
+    p.tile = p.rg == kKv8TcRows ? 128 : kTile;
     p.cost = 128 * kUnitCost / p.tile;
     tiles = (a.capacity + (int64_t)p.tile - 1) / p.tile;
     units = (int64_t)a.hk * (a.n_rows / p.tq + a.n_seqs);
@@ -607,9 +620,12 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& ti
 }  // namespace
 
 size_t kv8_attention_workspace(int hd, int group, int n_rows) {
-    // fewer sequences never need smaller units
-    const size_t rg = rows_of_unit(group, n_rows, 1);
-    return sizeof(float) * 2 * (rg == kKv8TcRows ? kKv8TcCtas : kKv8MaxCtas) * rg * (hd + 4) + sizeof(int4) * kKv8MaxCtas;
+    // A call with more sequences may have smaller units, whose CTAs are more: the largest of all up to this size.
+    const int most = rows_of_unit(group, n_rows, 1);
+    size_t rows = 0;
+    for (int rg : {8, 16, kKv8TcRows})
+        if (rg <= most) rows = std::max(rows, (size_t)2 * kKv8Sms * resident(rg) * rg);
+    return sizeof(float) * rows * (hd + 4) + sizeof(int4) * kKv8MaxCtas;
 }
 
 bool kv8_attention_fits(const Kv8Args& a, int hq) {
@@ -622,17 +638,18 @@ cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStr
     Kv8Plan p;
     int64_t units, tiles;
     if (!make_plan(a, t.hq, p, units, tiles)) return cudaErrorInvalidValue;
-    const int resident = p.rg == kKv8TcRows ? std::min(sm_count(), kKv8TcCtas)
-                                            : std::min(sm_count() * (p.rg == 8 ? 3 : 2), kKv8MaxCtas);
-    p.ctas = (int)std::min<int64_t>(resident, units * (tiles + p.cost));
+    p.ctas = (int)std::min<int64_t>(std::min(sm_count(), kKv8Sms) * resident(p.rg), units * (tiles + p.cost));
     p.q_wide = reinterpret_cast<uintptr_t>(t.q) % 16 == 0 && t.q_row % 8 == 0 && t.q_head % 8 == 0;
     p.out_wide = reinterpret_cast<uintptr_t>(t.out) % 16 == 0 && t.out_row % 8 == 0 && t.out_head % 8 == 0;
     p.desc = static_cast<int4*>(t.workspace);
     p.part = reinterpret_cast<float*>(p.desc + kKv8MaxCtas);
     cudaError_t e;
+    auto few = [&](auto hd) {
+        constexpr int HD = decltype(hd)::value;
+        return p.rg == 8 ? launch_few<HD, 1>(a, t, p, s) : launch_few<HD, 2>(a, t, p, s);
+    };
     if (p.rg == kKv8TcRows) e = launch_kv8_tc(a, t, p, s);
-    else if (a.hd == 128) e = p.rg == 8 ? launch_few<128, 1>(a, t, p, s) : launch_few<128, 2>(a, t, p, s);
-    else e = p.rg == 8 ? launch_few<64, 1>(a, t, p, s) : launch_few<64, 2>(a, t, p, s);
+    else e = a.hd == 128 ? few(std::integral_constant<int, 128>{}) : few(std::integral_constant<int, 64>{});
     if (e != cudaSuccess || tiles <= 1) return e;       // no unit has a tile to cut off
     return a.hd == 128 ? launch_merge<128>(a, t, p, units, s) : launch_merge<64>(a, t, p, units, s);
 }

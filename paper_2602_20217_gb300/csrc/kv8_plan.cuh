@@ -16,7 +16,7 @@
 
 namespace ks {
 
-constexpr int kKv8MaxCtas = 480, kKv8TcCtas = 160;  // the workspace has room for this many
+constexpr int kKv8Sms = 160, kKv8MaxCtas = 3 * kKv8Sms;    // the workspace has room for this many
 constexpr int kKv8TcRows = 128;     // query rows of a unit of the tcgen05 kernel
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A unit's fixed cost (queries, joining its warps, output) in the time of 128
