@@ -275,6 +275,7 @@ struct Kv8Args {            // cache and batch
     int n_seqs, table_ld, n_rows;
     int capacity;           // tokens that a sequence's pages can hold
     int* status;            // or null
+    bool by_seq;            // append, read: how the grid counts blocks (set by the launch)
     const int* stop;        // draft passes: the launch does nothing when *stop != 0 (null: always runs)
 };
 struct Kv8RowArgs {         // the rows to append; strides in elements

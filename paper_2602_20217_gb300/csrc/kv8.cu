@@ -10,6 +10,7 @@
 // power of two, which rounds only where a code becomes subnormal.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "kv8.cuh"
 
@@ -17,8 +18,8 @@ namespace ks {
 
 namespace {
 
-constexpr int kAppendThreads = 128;
-constexpr int kAppendQHeads = 4;     // query heads of a CTA that rotates queries
+constexpr int kThreads = 128;
+constexpr int kQHeads = 16;          // query heads of a CTA that rotates queries
 
 // Four codes times a power of two at most 1.
 KS_DEV uint32_t rescale4(uint32_t v, float f) {
@@ -26,111 +27,155 @@ KS_DEV uint32_t rescale4(uint32_t v, float f) {
     return (uint32_t)to_e4m3x2(a.x * f, a.y * f) | (uint32_t)to_e4m3x2(b.x * f, b.y * f) << 16;
 }
 
-// A lane's elements of a head vector: HD / 64 neighbours of the first half and
-// their partners of the second.
-template <int HD, typename T>
-KS_DEV void load_vector(const T* p, float (&x)[HD / 32]) {
-    const int lane = threadIdx.x & 31;
-    constexpr int V = HD / 64;
+// Eight neighbouring elements, as loaded (bf16 pairs, or floats).  WIDE: 16-byte aligned.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint32_t w[4];
+    KS_DEV void get(float (&x)[8]) const {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        x[e] = to_float(p[V * lane + e]);
-        x[V + e] = to_float(p[HD / 2 + V * lane + e]);
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = bf16_lo(w[i]);
+            x[2 * i + 1] = bf16_hi(w[i]);
+        }
+    }
+};
+template <>
+struct Raw8<float> {
+    float w[8];
+    KS_DEV void get(float (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = w[i];
+    }
+};
+template <bool WIDE>
+KS_DEV void load8(const __nv_bfloat16* p, Raw8<__nv_bfloat16>& x) {
+    if constexpr (WIDE) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        x.w[0] = v.x; x.w[1] = v.y; x.w[2] = v.z; x.w[3] = v.w;
+    } else {
+        const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.w[i] = e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
     }
 }
-template <int HD>
-KS_DEV void rotate(const float* rope, int pos, float (&x)[HD / 32]) {
-    const int lane = threadIdx.x & 31;
-    constexpr int V = HD / 64;
-    const float2* cs = reinterpret_cast<const float2*>(rope + (size_t)pos * HD) + V * lane;
+template <bool WIDE>
+KS_DEV void load8(const float* p, Raw8<float>& x) {
+    if constexpr (WIDE) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w;
+        x.w[4] = b.x; x.w[5] = b.y; x.w[6] = b.z; x.w[7] = b.w;
+    } else {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const float2 c = __ldg(cs + e);
-        const float u = x[e], w = x[V + e];
-        x[e] = u * c.x - w * c.y;
-        x[V + e] = w * c.x + u * c.y;
+        for (int i = 0; i < 8; ++i) x.w[i] = p[i];
+    }
+}
+template <bool WIDE>
+KS_DEV void store8(__nv_bfloat16* p, const float (&x)[8]) {
+    if constexpr (WIDE) {
+        *reinterpret_cast<uint4*>(p) =
+            make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
+    }
+}
+template <bool WIDE>
+KS_DEV void store8(float* p, const float (&x)[8]) {
+    if constexpr (WIDE) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = x[i];
+    }
+}
+// Eight (cos, sin) of a position from dim j on.
+template <bool WIDE>
+KS_DEV void load_angles(const float* row, int j, float2 (&cs)[8]) {
+    const float2* p = reinterpret_cast<const float2*>(row) + j;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 v = __ldg(reinterpret_cast<const float4*>(p) + i);
+            cs[2 * i] = make_float2(v.x, v.y);
+            cs[2 * i + 1] = make_float2(v.z, v.w);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) cs[i] = __ldg(p + i);
+    }
+}
+KS_DEV void rotate8(const float2 (&cs)[8], float (&a)[8], float (&b)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float u = a[i], w = b[i];
+        a[i] = u * cs[i].x - w * cs[i].y;
+        b[i] = w * cs[i].x + u * cs[i].y;
     }
 }
 
-// One CTA per (block slot, KV head): the block's new keys and values, from
-// registers, into a copy of its record in shared memory, from where whole
-// 16-byte pieces go out.  A block that goes on keeps its old tokens (their
-// record is read while the new rows are); the tokens behind the last one are
-// zeros.  Further CTAs of a slot rotate the queries of its tokens.
-template <int HD, typename T>
-__global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const Kv8Args a, const Kv8RowArgs r) {
-    constexpr int N = HD / 32, V = HD / 64, REC = kv8_record(HD), CODES = kKv8Block * HD;
-    constexpr int WARPS = kAppendThreads / 32, PER = kKv8Block / WARPS;
-    if (a.stop && *a.stop) return;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    Kv8Slot w;
-    if (!kv8_slot(a, blockIdx.x, w)) return;
-    const int pos0 = w.blk * kKv8Block;
-    if ((int)blockIdx.y >= a.hk) {
-        const int h0 = ((int)blockIdx.y - a.hk) * kAppendQHeads;
-        for (int i = warp; i < kKv8Block * kAppendQHeads; i += WARPS) {
-            const int t = i / kAppendQHeads, h = h0 + i % kAppendQHeads;
-            if (t < w.first || t >= w.last || h >= r.hq) continue;
-            float x[N];
-            load_vector<HD, T>(static_cast<const T*>(r.q) + (int64_t)(w.row + t) * r.q_row + (int64_t)h * r.q_head, x);
-            if (r.rope) {
-                if (pos0 + t < r.rope_rows) rotate<HD>(r.rope, pos0 + t, x);
-                else
-                    for (int e = 0; e < N; ++e) x[e] = 0.f;
-            }
-            __nv_bfloat16* o = r.q_out + (int64_t)(w.row + t) * r.q_out_row + (int64_t)h * r.q_out_head;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                o[V * lane + e] = __float2bfloat16_rn(x[e]);
-                o[HD / 2 + V * lane + e] = __float2bfloat16_rn(x[V + e]);
-            }
-        }
-        return;
-    }
-    const int h = blockIdx.y;
+// A record's value codes in shared memory, 16 bytes a dim and 16 unused bytes
+// after every 8 dims: threads 8 dims apart use different banks.
+KS_DEV int v_row(int d) { return d * 16 + (d >> 3) * 16; }
+
+// A block of KV head blockIdx.y.
+template <int HD, typename T, bool WIDE>
+KS_DEV void append_block(const Kv8Args& a, const Kv8RowArgs& r, const Kv8Slot& w, int group, int d0, int d1) {
+    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, WARPS = kThreads / 32, PIECES = 2 * HD / kThreads;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, h = blockIdx.y, pos0 = w.blk * kKv8Block;
     unsigned char* rec = kv8_record_at(a, w.s, w.blk, h, REC);
     if (!rec) {
         if (tid == 0) kv8_flag(a, kKv8BadPage);
         return;
     }
-    __shared__ __align__(16) unsigned char codes[2 * CODES];
+    __shared__ __align__(16) unsigned char kc[CODES], vc[CODES + HD * 2];
     __shared__ float top[2][WARPS];
     const bool goes_on = w.first > 0;
-    uint4 old[2 * CODES / 16 / kAppendThreads];
+    uint4 old[PIECES];
     float2 stored = make_float2(0.f, 0.f);
     if (goes_on) {
         stored = *reinterpret_cast<const float2*>(rec + 2 * CODES);
 #pragma unroll
-        for (int i = 0; i < 2 * CODES / 16 / kAppendThreads; ++i)
-            old[i] = reinterpret_cast<const uint4*>(rec)[tid + i * kAppendThreads];
+        for (int i = 0; i < PIECES; ++i) old[i] = reinterpret_cast<const uint4*>(rec)[tid + i * kThreads];
     }
-    float k[PER][N], v[PER][N], k_top = 0.f, v_top = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int t = warp * PER + i;
-        if (t < w.first || t >= w.last) continue;
-        load_vector<HD, T>(static_cast<const T*>(r.k) + (int64_t)(w.row + t) * r.k_row + (int64_t)h * r.k_head, k[i]);
-        load_vector<HD, T>(static_cast<const T*>(r.v) + (int64_t)(w.row + t) * r.v_row + (int64_t)h * r.v_head, v[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int t = warp * PER + i;
-        if (t < w.first || t >= w.last) continue;
+    // HD 64: the second half of the threads has no token
+    const int t = group;
+    const bool mine = t >= w.first && t < w.last;
+    float k[2][8], v[2][8], k_top = 0.f, v_top = 0.f;
+    if (mine) {
+        const T* ks = static_cast<const T*>(r.k) + (int64_t)(w.row + t) * r.k_row + (int64_t)h * r.k_head;
+        const T* vs = static_cast<const T*>(r.v) + (int64_t)(w.row + t) * r.v_row + (int64_t)h * r.v_head;
+        Raw8<T> raw[4];
+        load8<WIDE>(ks + d0, raw[0]);
+        load8<WIDE>(ks + d1, raw[1]);
+        load8<WIDE>(vs + d0, raw[2]);
+        load8<WIDE>(vs + d1, raw[3]);
+        raw[0].get(k[0]);
+        raw[1].get(k[1]);
+        raw[2].get(v[0]);
+        raw[3].get(v[1]);
         if (r.rope) {
             if (pos0 + t < r.rope_rows) {
-                rotate<HD>(r.rope, pos0 + t, k[i]);
+                float2 cs[8];
+                load_angles<WIDE>(r.rope + (size_t)(pos0 + t) * HD, d0, cs);
+                rotate8(cs, k[0], k[1]);
             } else {
-                if (lane == 0) kv8_flag(a, kKv8BadPosition);
-                for (int e = 0; e < N; ++e) k[i][e] = v[i][e] = 0.f;
+                if (d0 == 0) kv8_flag(a, kKv8BadPosition);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) k[0][e] = k[1][e] = v[0][e] = v[1][e] = 0.f;
             }
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if (finite(k[i][e])) k_top = fmaxf(k_top, fabsf(k[i][e]));
-            else k[i][e] = __uint_as_float(0x7fc00000u);    // infinities too: the type has none
-            if (finite(v[i][e])) v_top = fmaxf(v_top, fabsf(v[i][e]));
-            else v[i][e] = __uint_as_float(0x7fc00000u);
-        }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (finite(k[i][e])) k_top = fmaxf(k_top, fabsf(k[i][e]));
+                else k[i][e] = __uint_as_float(0x7fc00000u);    // infinities too: the type has none
+                if (finite(v[i][e])) v_top = fmaxf(v_top, fabsf(v[i][e]));
+                else v[i][e] = __uint_as_float(0x7fc00000u);
+            }
     }
     k_top = warp_max(k_top);
     v_top = warp_max(v_top);
@@ -150,110 +195,208 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const Kv8Arg
         vs = fmaxf(vs, stored.y);
     }
     const float kf = stored.x / ks, vf = stored.y / vs;
+    if (goes_on || w.last < kKv8Block) {             // tokens that no thread brings
 #pragma unroll
-    for (int i = 0; i < 2 * CODES / 16 / kAppendThreads; ++i) {
-        const int at = (tid + i * kAppendThreads) * 16;     // byte of this piece
-        uint4 c = make_uint4(0, 0, 0, 0);
-        if (goes_on) {
+        for (int i = 0; i < PIECES; ++i) {
+            const int at = (tid + i * kThreads) * 16;       // byte of this piece
+            uint4 c = make_uint4(0, 0, 0, 0);
             if (at < CODES) {                               // a token's 16 dims
-                const int t = (at >= CODES / 2 ? 8 : 0) + (at >> 4 & 7);
-                if (t < w.first) {
+                const int tok = (at >= CODES / 2 ? 8 : 0) + (at >> 4 & 7);
+                if (goes_on && tok < w.first) {
                     c = old[i];
                     if (kf != 1.f)
                         c = make_uint4(rescale4(c.x, kf), rescale4(c.y, kf), rescale4(c.z, kf), rescale4(c.w, kf));
                 }
+                *reinterpret_cast<uint4*>(kc + at) = c;
             } else {                                        // a dim's 16 tokens
-                c = old[i];
-                if (vf != 1.f)
-                    c = make_uint4(rescale4(c.x, vf), rescale4(c.y, vf), rescale4(c.z, vf), rescale4(c.w, vf));
-                uint32_t* q = reinterpret_cast<uint32_t*>(&c);
+                if (goes_on) {
+                    c = old[i];
+                    if (vf != 1.f)
+                        c = make_uint4(rescale4(c.x, vf), rescale4(c.y, vf), rescale4(c.z, vf), rescale4(c.w, vf));
+                    uint32_t* q = reinterpret_cast<uint32_t*>(&c);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {               // tokens 2j, 2j + 1, 8 + 2j, 9 + 2j
-                    uint32_t keep = 0;
-                    if (2 * j < w.first) keep |= 0xffu;
-                    if (2 * j + 1 < w.first) keep |= 0xff00u;
-                    if (8 + 2 * j < w.first) keep |= 0xff0000u;
-                    if (9 + 2 * j < w.first) keep |= 0xff000000u;
-                    q[j] &= keep;
+                    for (int j = 0; j < 4; ++j) {           // tokens 2j, 2j + 1, 8 + 2j, 9 + 2j
+                        uint32_t keep = 0;
+                        if (2 * j < w.first) keep |= 0xffu;
+                        if (2 * j + 1 < w.first) keep |= 0xff00u;
+                        if (8 + 2 * j < w.first) keep |= 0xff0000u;
+                        if (9 + 2 * j < w.first) keep |= 0xff000000u;
+                        q[j] &= keep;
+                    }
                 }
+                *reinterpret_cast<uint4*>(vc + v_row((at - CODES) / 16)) = c;
             }
         }
-        reinterpret_cast<uint4*>(codes)[tid + i * kAppendThreads] = c;
+        __syncthreads();
     }
-    __syncthreads();
-    const float ki = inverse_pow2(ks), vi = inverse_pow2(vs);
+    if (mine) {
+        const float ki = inverse_pow2(ks), vi = inverse_pow2(vs);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int t = warp * PER + i;
-        if (t < w.first || t >= w.last) continue;
+        for (int i = 0; i < 2; ++i) {
+            const int d = i ? d1 : d0;
+            uint32_t c[2];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int d = half * (HD / 2) + V * lane;
-            if constexpr (V == 2) {
-                const uint16_t kc = to_e4m3x2(k[i][2 * half] * ki, k[i][2 * half + 1] * ki);
-                const uint16_t vc = to_e4m3x2(v[i][2 * half] * vi, v[i][2 * half + 1] * vi);
-                *reinterpret_cast<uint16_t*>(codes + k_byte<HD>(t, d)) = kc;
-                codes[CODES + d * 16 + v_byte(t)] = (unsigned char)vc;
-                codes[CODES + (d + 1) * 16 + v_byte(t)] = (unsigned char)(vc >> 8);
-            } else {
-                codes[k_byte<HD>(t, d)] = (unsigned char)to_e4m3x2(k[i][half] * ki, 0.f);
-                codes[CODES + d * 16 + v_byte(t)] = (unsigned char)to_e4m3x2(v[i][half] * vi, 0.f);
+            for (int e = 0; e < 2; ++e)
+                c[e] = to_e4m3x2(k[i][4 * e] * ki, k[i][4 * e + 1] * ki) |
+                       (uint32_t)to_e4m3x2(k[i][4 * e + 2] * ki, k[i][4 * e + 3] * ki) << 16;
+            *reinterpret_cast<uint2*>(kc + k_byte<HD>(t, d)) = make_uint2(c[0], c[1]);
+            unsigned char* to = vc + v_row(d) + v_byte(t);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const uint16_t x = to_e4m3x2(v[i][e] * vi, v[i][e + 1] * vi);
+                to[16 * e] = (unsigned char)x;
+                to[16 * e + 16] = (unsigned char)(x >> 8);
             }
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2 * CODES / 16 / kAppendThreads; ++i)
-        reinterpret_cast<uint4*>(rec)[tid + i * kAppendThreads] = reinterpret_cast<const uint4*>(codes)[tid + i * kAppendThreads];
+    for (int i = 0; i < PIECES; ++i) {
+        const int at = (tid + i * kThreads) * 16;
+        reinterpret_cast<uint4*>(rec)[tid + i * kThreads] =
+            *reinterpret_cast<const uint4*>(at < CODES ? kc + at : vc + v_row((at - CODES) / 16));
+    }
     if (tid == 0) *reinterpret_cast<float2*>(rec + 2 * CODES) = make_float2(ks, vs);
+    __syncthreads();                                 // before the next block
 }
 
-// One CTA per (block slot, KV head): the record through shared memory, a
-// token's dims per warp and step.
-template <int HD, typename T>
-__global__ void __launch_bounds__(kAppendThreads) kv8_read_kernel(const Kv8Args a, T* k_out, T* v_out, int64_t row_ld,
-                                                                  int64_t head_ld) {
-    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD;
-    const int tid = threadIdx.x, h = blockIdx.y;
+// CTAs (., y) of a block's tokens: y below hk take KV head y, the others
+// kQHeads query heads each.  HD / 16 threads share a head vector, each with eight
+// neighbouring dims of the first half and their partners of the second, so that
+// every access is 16 bytes and 128 contiguous ones a vector half.  Bound by bytes
+// in flight: a query thread loads four vectors (two of fp32) before it rotates
+// the first.
+//
+// A KV head's new rows go from registers, quantised, into a copy of the block's
+// record in shared memory, and from there out in 16-byte pieces.  A block that
+// goes on keeps its old tokens (their record is read while the new rows are);
+// the tokens behind the last one are zeros.
+template <int HD, typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 6) kv8_append_kernel(const Kv8Args a, const Kv8RowArgs r) {
+    constexpr int TH = HD / 16, GROUPS = kThreads / TH;
+    if (a.stop && *a.stop) return;
+    const int tid = threadIdx.x;
+    const int group = tid / TH, d0 = tid % TH * 8, d1 = d0 + HD / 2;
     Kv8Slot w;
-    if (!kv8_slot(a, blockIdx.x, w)) return;
-    const unsigned char* rec = kv8_record_at(a, w.s, w.blk, h, REC);
-    if (!rec && tid == 0) kv8_flag(a, kKv8BadPage);
-    __shared__ __align__(16) unsigned char codes[2 * CODES];
-    float2 sc = make_float2(1.f, 1.f);
-    if (rec) sc = *reinterpret_cast<const float2*>(rec + 2 * CODES);
+    Kv8Blocks blocks(a);
+    if ((int)blockIdx.y >= a.hk) {
+        const int h0 = ((int)blockIdx.y - a.hk) * kQHeads, heads = min(kQHeads, r.hq - h0);
+        for (; blocks.get(w); blocks.b += blocks.step) {
+            // a thread stays with one token; a block of few tokens has more threads for its heads
+            const int tokens = w.last - w.first, ts = tokens > 8 ? 16 : tokens > 4 ? 8 : tokens > 2 ? 4 : tokens;
+            const int t = w.first + (group & (ts - 1)), pos = w.blk * kKv8Block + t, step = GROUPS / ts;
+            if (t >= w.last) continue;
+            constexpr int U = sizeof(T) == 2 ? 4 : 2;
+            const T* src = static_cast<const T*>(r.q) + (int64_t)(w.row + t) * r.q_row;
+            __nv_bfloat16* out = r.q_out + (int64_t)(w.row + t) * r.q_out_row;
+            const bool turn = r.rope != nullptr, past = turn && pos >= r.rope_rows;
+            float2 cs[8];
+            if (turn && !past) load_angles<WIDE>(r.rope + (size_t)pos * HD, d0, cs);
+            for (int i = group / ts; i < heads; i += U * step) {
+                Raw8<T> xs[U], ys[U];
 #pragma unroll
-    for (int i = 0; i < 2 * CODES / 16 / kAppendThreads; ++i)
-        reinterpret_cast<uint4*>(codes)[tid + i * kAppendThreads] =
-            rec ? reinterpret_cast<const uint4*>(rec)[tid + i * kAppendThreads] : make_uint4(0, 0, 0, 0);
-    __syncthreads();
-    constexpr int DP = HD / 2;     // pairs of dims
-    for (int i = tid; i < kKv8Block * DP; i += kAppendThreads) {
-        const int t = i / DP, d = 2 * (i % DP);
-        if (t < w.first || t >= w.last) continue;
-        const float2 kv = from_e4m3x2(*reinterpret_cast<const uint16_t*>(codes + k_byte<HD>(t, d)));
-        const unsigned char* vc = codes + CODES + d * 16 + v_byte(t);
-        const float2 vv = from_e4m3x2((uint16_t)(vc[0] | vc[16] << 8));
-        const int64_t o = (int64_t)(w.row + t) * row_ld + (int64_t)h * head_ld + d;
-        k_out[o] = from_float<T>(kv.x * sc.x);
-        k_out[o + 1] = from_float<T>(kv.y * sc.x);
-        v_out[o] = from_float<T>(vv.x * sc.y);
-        v_out[o + 1] = from_float<T>(vv.y * sc.y);
+                for (int u = 0; u < U; ++u)
+                    if (i + u * step < heads) {
+                        const T* p = src + (int64_t)(h0 + i + u * step) * r.q_head;
+                        load8<WIDE>(p + d0, xs[u]);
+                        load8<WIDE>(p + d1, ys[u]);
+                    }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (i + u * step < heads) {
+                        float x[8], y[8];
+                        xs[u].get(x);
+                        ys[u].get(y);
+                        if (past) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
+                        } else if (turn) {
+                            rotate8(cs, x, y);
+                        }
+                        __nv_bfloat16* o = out + (int64_t)(h0 + i + u * step) * r.q_out_head;
+                        store8<WIDE>(o + d0, x);
+                        store8<WIDE>(o + d1, y);
+                    }
+            }
+        }
+        return;
+    }
+    for (; blocks.get(w); blocks.b += blocks.step) append_block<HD, T, WIDE>(a, r, w, group, d0, d1);
+}
+
+// A CTA per block and KV head: the record through shared memory, eight dims of a
+// token a thread.
+template <int HD, typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads) kv8_read_kernel(const Kv8Args a, T* k_out, T* v_out, int64_t row_ld,
+                                                            int64_t head_ld) {
+    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, PIECES = 2 * HD / kThreads, TH = HD / 8;
+    const int tid = threadIdx.x, h = blockIdx.y, d = tid % TH * 8;
+    __shared__ __align__(16) unsigned char kc[CODES], vc[CODES + HD * 2];
+    Kv8Slot w;
+    for (Kv8Blocks blocks(a); blocks.get(w); blocks.b += blocks.step) {
+        const unsigned char* rec = kv8_record_at(a, w.s, w.blk, h, REC);
+        if (!rec && tid == 0) kv8_flag(a, kKv8BadPage);
+        float2 sc = make_float2(1.f, 1.f);
+        if (rec) sc = *reinterpret_cast<const float2*>(rec + 2 * CODES);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int at = (tid + i * kThreads) * 16;
+            *reinterpret_cast<uint4*>(at < CODES ? kc + at : vc + v_row((at - CODES) / 16)) =
+                rec ? reinterpret_cast<const uint4*>(rec)[tid + i * kThreads] : make_uint4(0, 0, 0, 0);
+        }
+        __syncthreads();
+        for (int t = w.first + tid / TH; t < w.last; t += kThreads / TH) {
+            const int64_t o = (int64_t)(w.row + t) * row_ld + (int64_t)h * head_ld + d;
+            const uint2 c = *reinterpret_cast<const uint2*>(kc + k_byte<HD>(t, d));
+            const unsigned char* vb = vc + v_row(d) + v_byte(t);
+            float x[8], y[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 kv = from_e4m3x2((uint16_t)((e < 2 ? c.x : c.y) >> (e & 1) * 16));
+                const float2 vv = from_e4m3x2((uint16_t)(vb[32 * e] | vb[32 * e + 16] << 8));
+                x[2 * e] = kv.x * sc.x; x[2 * e + 1] = kv.y * sc.x;
+                y[2 * e] = vv.x * sc.y; y[2 * e + 1] = vv.y * sc.y;
+            }
+            store8<WIDE>(k_out + o, x);
+            store8<WIDE>(v_out + o, y);
+        }
+        __syncthreads();
     }
 }
 
-template <int HD>
-cudaError_t append_hd(int dtype, const Kv8Args& a, const Kv8RowArgs& r, cudaStream_t s) {
-    const dim3 grid(a.n_rows / kKv8Block + 2 * a.n_seqs,
-                    a.hk + (r.q ? (r.hq + kAppendQHeads - 1) / kAppendQHeads : 0));
-    if (dtype == KS_DTYPE_BF16) kv8_append_kernel<HD, __nv_bfloat16><<<grid, kAppendThreads, 0, s>>>(a, r);
-    else kv8_append_kernel<HD, float><<<grid, kAppendThreads, 0, s>>>(a, r);
+// Sequences along x, two CTAs for their blocks, where they have at most a block's
+// rows on average; else a slot a block (see Kv8Blocks).  96 sequences of 1 to 11
+// rows, append and read back: 22.6 us by sequence, 24.8 us by slots; one prompt of
+// 4096 rows would give all its blocks to two CTAs a head by sequence.
+dim3 block_grid(Kv8Args& a, int y) {
+    a.by_seq = a.n_rows <= (int64_t)kKv8Block * a.n_seqs;
+    return a.by_seq ? dim3(a.n_seqs, y, 2) : dim3(a.n_rows / kKv8Block + 2 * a.n_seqs, y);
+}
+
+// 16-byte aligned, elements of es bytes, all strides whole 16 bytes
+bool wide(size_t es, std::initializer_list<const void*> ptrs, std::initializer_list<int64_t> strides) {
+    for (const void* p : ptrs)
+        if (reinterpret_cast<uintptr_t>(p) & 15) return false;
+    for (int64_t s : strides)
+        if (s * es & 15) return false;
+    return true;
+}
+
+template <int HD, typename T>
+cudaError_t append_hd(Kv8Args a, const Kv8RowArgs& r, cudaStream_t s) {
+    const dim3 grid = block_grid(a, a.hk + (r.q ? (r.hq + kQHeads - 1) / kQHeads : 0));
+    const bool w = wide(sizeof(T), {r.k, r.v, r.q, r.rope}, {r.k_row, r.k_head, r.v_row, r.v_head, r.q_row, r.q_head}) &&
+                   wide(2, {r.q_out}, {r.q_out_row, r.q_out_head});
+    if (w) kv8_append_kernel<HD, T, true><<<grid, kThreads, 0, s>>>(a, r);
+    else kv8_append_kernel<HD, T, false><<<grid, kThreads, 0, s>>>(a, r);
     return cudaGetLastError();
 }
 template <int HD, typename T>
-cudaError_t read_hd(const Kv8Args& a, void* k, void* v, int64_t row_ld, int64_t head_ld, cudaStream_t s) {
-    const dim3 grid(a.n_rows / kKv8Block + 2 * a.n_seqs, a.hk);
-    kv8_read_kernel<HD, T><<<grid, kAppendThreads, 0, s>>>(a, static_cast<T*>(k), static_cast<T*>(v), row_ld, head_ld);
+cudaError_t read_hd(Kv8Args a, void* k, void* v, int64_t row_ld, int64_t head_ld, cudaStream_t s) {
+    const dim3 grid = block_grid(a, a.hk);
+    T *ko = static_cast<T*>(k), *vo = static_cast<T*>(v);
+    if (wide(sizeof(T), {k, v}, {row_ld, head_ld})) kv8_read_kernel<HD, T, true><<<grid, kThreads, 0, s>>>(a, ko, vo, row_ld, head_ld);
+    else kv8_read_kernel<HD, T, false><<<grid, kThreads, 0, s>>>(a, ko, vo, row_ld, head_ld);
     return cudaGetLastError();
 }
 
@@ -330,7 +473,8 @@ ks_status launched(cudaError_t e, const char* who) {
 }  // namespace
 
 cudaError_t launch_kv8_append(int dtype, const Kv8Args& a, const Kv8RowArgs& r, cudaStream_t s) {
-    return a.hd == 128 ? append_hd<128>(dtype, a, r, s) : append_hd<64>(dtype, a, r, s);
+    if (dtype == KS_DTYPE_BF16) return a.hd == 128 ? append_hd<128, __nv_bfloat16>(a, r, s) : append_hd<64, __nv_bfloat16>(a, r, s);
+    return a.hd == 128 ? append_hd<128, float>(a, r, s) : append_hd<64, float>(a, r, s);
 }
 
 }  // namespace ks

@@ -101,28 +101,46 @@ KS_DEV unsigned char* kv8_record_at(const Kv8Args& a, int s, int b, int h, int r
     return a.data + (((size_t)page * a.hk + h) * a.bpp + b % a.bpp) * rec;
 }
 
-// The touched blocks of a batch: block slots of sequence s begin at
-// row0 / 16 + 2 s, which leaves room for every block that its rows can touch
-// (r rows touch at most (r + 30) / 16 of them) without a sum over the
-// sequences.
+// The touched blocks of a batch, over the grid's x and z.  Batches of few rows a
+// sequence (by_seq): x is the sequence, z counts its blocks, so that a CTA reads
+// the sequence's numbers at once.  Others: x is a block slot; the slots of
+// sequence s begin at row0 / 16 + 2 s, which leaves room for every block that its
+// rows can touch (r rows touch at most (r + 30) / 16) without a sum over the
+// sequences, and the sequence is searched for.
 struct Kv8Slot {
     int s, blk, first, last;   // sequence, block; tokens [first, last) of the block are the batch's rows
     int row;                   // batch row of the block's token 0 (it may be before the sequence's rows)
 };
-KS_DEV bool kv8_slot(const Kv8Args& a, int slot, Kv8Slot& w) {
-    w.s = kv8_find(a.n_seqs, slot, [&](int s) { return kv8_row0(a, s) / kKv8Block + 2 * s; });
-    const Kv8Seq q = kv8_seq(a, w.s);   // of the first sequence for slots before its own
-    const int start = max(q.len - q.rows, 0), b = slot - (q.row0 / kKv8Block + 2 * w.s);
-    w.blk = start / kKv8Block + b;
-    if (b == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-        if (kv8_seq_bad(a, w.s)) kv8_flag(a, kKv8BadBatch);
-        if (q.len < q.rows) kv8_flag(a, kKv8BadPosition);
+struct Kv8Blocks {
+    Kv8Seq q;
+    int s, start, b, step;
+    KS_DEV Kv8Blocks(const Kv8Args& a) {
+        if (a.by_seq) {
+            s = blockIdx.x;
+            b = blockIdx.z;
+            step = gridDim.z;
+        } else {
+            auto first = [&](int i) { return kv8_row0(a, i) / kKv8Block + 2 * i; };
+            s = kv8_find(a.n_seqs, blockIdx.x, first);
+            b = (int)blockIdx.x - first(s);      // below 0 for slots before the first sequence's
+            step = 1 << 30;
+        }
+        q = kv8_seq(a, s);
+        start = max(q.len - q.rows, 0);
+        if (b == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+            if (kv8_seq_bad(a, s)) kv8_flag(a, kKv8BadBatch);
+            if (q.len < q.rows) kv8_flag(a, kKv8BadPosition);
+        }
     }
-    if (b < 0 || q.rows == 0 || w.blk * kKv8Block >= q.len) return false;
-    w.first = max(start - w.blk * kKv8Block, 0);
-    w.last = min(q.len - w.blk * kKv8Block, kKv8Block);
-    w.row = q.row0 + w.blk * kKv8Block - (q.len - q.rows);
-    return true;
-}
+    KS_DEV bool get(Kv8Slot& w) const {
+        w.s = s;
+        w.blk = start / kKv8Block + b;
+        if (b < 0 || q.rows == 0 || b >= 1 << 28 || w.blk * kKv8Block >= q.len) return false;
+        w.first = max(start - w.blk * kKv8Block, 0);
+        w.last = min(q.len - w.blk * kKv8Block, kKv8Block);
+        w.row = q.row0 + w.blk * kKv8Block - (q.len - q.rows);
+        return true;
+    }
+};
 
 }  // namespace ks
