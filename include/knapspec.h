@@ -255,6 +255,24 @@ ks_status ks_decode_greedy(ks_model* m, int32_t n_tokens, int32_t* out);
 /* Committed length p and the pending token. */
 ks_status ks_model_position(const ks_model* m, int32_t* committed, int32_t* pending);
 
+/* An 8-bit cache for the drafts (an addition of this library; the paper's
+ * drafts read the target's cache).  With one, the attention of the draft
+ * passes of ks_draft, ks_draft_dynamic, ks_draft_sample and
+ * ks_generate_speculative reads an 8-bit copy of the model's K/V cache (the
+ * format below, 256-token pages) and half the bytes; what the target computes,
+ * greedy output among it, stays bit for bit what it is without, and only the
+ * drafts, so the number accepted, may differ.  Each draft pass takes the rows
+ * that a layer's copy lacks from the model's cache, so the copy follows
+ * prefills, verifies and rewinds by itself, and after every verify a layer's
+ * unfinished block is taken anew.  ks_draft_cache: memory (dev, 256-byte
+ * aligned, ks_draft_cache_bytes(cfg) bytes, borrowed until the model is
+ * destroyed or the cache replaced or taken away; needs no initial value), or
+ * NULL to go back to the bf16 cache; waits for the stream.
+ * ks_draft_cache_bytes: 0, and ks_draft_cache KS_ERR_UNSUPPORTED, for fp32
+ * models. */
+size_t ks_draft_cache_bytes(const ks_config* cfg);
+ks_status ks_draft_cache(ks_model* m, void* memory, size_t bytes);
+
 /* ------------------------------------------------------------ cosine (a4) */
 
 /* Sec. 2 matrix cosine for n_pairs pairs of [rows, d] matrices:

@@ -439,7 +439,56 @@ struct ks_model {
     CUtensorMap wide_lm, wide_xg, wide_q, wide_ao, wide_act, wide_kv;
     CUtensorMap map_lm, map_xg[16], map_xg2[16], map_attn_out[16], map_act[16];  // [R - 1]: boxes of R rows
     KlassTiming timing[kKlasses];
+    // 8-bit draft cache: null data = drafts attend over the cache above
+    struct Draft8 {
+        char* data = nullptr;        // [n_layers] caches of layer_bytes
+        size_t layer_bytes = 0;
+        int32_t *table, *pairs, *count;   // page i of token range i; (0, n) at 2 n; n at n
+        void* work;
+        std::vector<int> valid;      // a layer's leading positions that hold the bf16 cache's rows
+    } draft8;
 };
+
+// The 8-bit draft cache's memory: one sequence on pages in order, and the
+// batch arrays of every length as constants, so that no call uploads any.
+constexpr int kDraftPage = 256;      // tokens
+struct Draft8Layout {
+    size_t layer, table, pairs, count, work, total;
+    int pages;
+};
+static Kv8Args draft8_args(const ks_config& c) {
+    Kv8Args a{};
+    a.n_pages = (c.max_seq + kDraftPage - 1) / kDraftPage;
+    a.bpp = kDraftPage / 16;
+    a.hk = c.n_kv_heads;
+    a.hd = c.head_dim;
+    a.n_seqs = 1;
+    a.table_ld = a.n_pages;
+    a.n_rows = 1;
+    a.capacity = a.n_pages * kDraftPage;
+    return a;
+}
+static bool draft8_layout(const ks_config& c, Draft8Layout& L) {
+    if (c.dtype != KS_DTYPE_BF16) return false;      // the operators take more query heads than a model
+    const Kv8Args a = draft8_args(c);
+    L.pages = a.n_pages;
+    L.layer = align_up(ks_kv8_bytes(a.n_pages, kDraftPage, c.n_kv_heads, c.head_dim), 256);
+    if (L.layer == 0 || !kv8_attention_fits(a, c.n_q_heads)) return false;
+    size_t off = L.layer * c.n_layers;
+    auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
+    L.table = take(sizeof(int32_t) * L.pages);
+    L.pairs = take(sizeof(int32_t) * 2 * ((size_t)c.max_seq + 1));
+    L.count = take(sizeof(int32_t) * ((size_t)c.max_seq + 1));
+    L.work = take(kv8_attention_workspace(c.head_dim, c.n_q_heads / c.n_kv_heads, 1));
+    L.total = off;
+    return true;
+}
+// The bf16 cache of layer l is written from position p0 on: the 8-bit cache has
+// to take those rows again, from their block's start (so that a scale which a
+// rejected draft raised does not stay).
+static void draft8_stale(ks_model* m, int l, int p0) {
+    if (m->draft8.data) m->draft8.valid[l] = std::min(m->draft8.valid[l], p0 / 16 * 16);
+}
 
 // ----------------------------------------------------------------- plumbing
 static ks_status cuda_fail(cudaError_t e, const char* what) {
@@ -498,13 +547,54 @@ static void* vcache(ks_model* m, int layer) {
     return m->kv + (size_t)(2 * layer + 1) * per;
 }
 
+// The attention core of a draft pass over the 8-bit cache, after the query prep
+// wrote the row's key and value to the bf16 cache: take the rows that the 8-bit
+// cache lacks from there (the row itself, and in a layer's first pass after a
+// verify, or after passes whose mask skipped it, those committed since), then
+// attend.  qbuf holds q log2(e) / sqrt(hd); the operator's scale is natural.
+static ks_status draft8_attention(ks_model* m, int l, int p0, const int* stop) {
+    const ks_config& c = m->cfg;
+    const int hd = c.head_dim;
+    int& valid = m->draft8.valid[l];
+    if (valid > p0) valid = p0 / 16 * 16;      // drafted again without a verify
+    const int first = valid;
+    Kv8Args a = draft8_args(c);
+    a.data = reinterpret_cast<unsigned char*>(m->draft8.data + (size_t)l * m->draft8.layer_bytes);
+    a.table = m->draft8.table;
+    a.lengths = m->draft8.count + p0 + 1;
+    a.status = m->err;
+    a.stop = stop;
+    a.n_rows = p0 + 1 - first;
+    a.offsets = m->draft8.pairs + 2 * (size_t)a.n_rows;
+    Kv8RowArgs r{};
+    r.k = static_cast<char*>(kcache(m, l)) + (size_t)first * hd * m->es;
+    r.v = static_cast<char*>(vcache(m, l)) + (size_t)first * hd * m->es;
+    r.k_row = r.v_row = hd;
+    r.k_head = r.v_head = (int64_t)c.max_seq * hd;
+    KS_TRY(launch(m, K_PREP, [&] { return launch_kv8_append(KS_DTYPE_BF16, a, r, m->stream); }, "8-bit draft rows"));
+    a.n_rows = 1;
+    a.offsets = m->draft8.pairs + 2;
+    Kv8AttnArgs t{};
+    t.q = m->qbuf;
+    t.q_row = t.out_row = (int64_t)c.n_q_heads * hd;
+    t.q_head = t.out_head = hd;
+    t.out = static_cast<__nv_bfloat16*>(m->attn_out);
+    t.hq = c.n_q_heads;
+    t.scale = 0.6931471805599453f;
+    t.workspace = m->draft8.work;
+    KS_TRY(launch(m, K_ATTN, [&] { return launch_kv8_attention(a, t, m->stream); }, "8-bit draft attention"));
+    valid = p0 + 1;
+    return KS_OK;
+}
+
 // One pass of f^(S) over R consecutive rows at positions p0..p0+R-1.
 // tok: device token ids of the rows.  mask: host uint8[2L] or null (all).
 // capture_slot >= 0: write X^(i) of every row into the history slot (all
 // sublayers must run).  argmax: device int32[R] for the LM head argmax, or
-// null to skip the LM head.
+// null to skip the LM head.  draft: a draft pass, whose attention reads the
+// 8-bit draft cache if the model has one.
 static ks_status forward(ks_model* m, const int32_t* tok, int R, int p0, const uint8_t* mask,
-                         int capture_slot, int32_t* argmax, const int* stop = nullptr) {
+                         int capture_slot, int32_t* argmax, const int* stop = nullptr, bool draft = false) {
     const ks_config& c = m->cfg;
     const int d = c.d_model, hd = c.head_dim;
     const int nqkv = (c.n_q_heads + 2 * c.n_kv_heads) * hd;
@@ -588,7 +678,9 @@ static ks_status forward(ks_model* m, const int32_t* tok, int R, int p0, const u
             at.kv_row_v = (2 * l + 1) * c.n_kv_heads * c.max_seq;
             at.q = m->qbuf;
             KS_TRY(launch(m, K_PREP, [&] { return launch_attn_prep(at, s); }, "attention query prep"));
+            if (draft && m->draft8.data) return draft8_attention(m, l, p0, stop);
         }
+        draft8_stale(m, l, p0);
         KS_TRY(launch(m, K_ATTN, [&] { return launch_attention(dt, at, s); }, "attention"));
         KS_TRY(launch(m, K_MERGE, [&] { return launch_attn_merge(dt, at, s); }, "attention merge"));
         return KS_OK;
@@ -763,6 +855,7 @@ static ks_status wide_forward(ks_model* m, const int32_t* tok, int M, int p0, in
                       2.0 * K * (double)(kind == WK_SWIGLU ? 2 * N : N));
     };
     for (int l = 0; l < L; ++l) {
+        draft8_stale(m, l, p0);
         g.kcache = reinterpret_cast<__nv_bfloat16*>(kcache(m, l));
         g.vcache = reinterpret_cast<__nv_bfloat16*>(vcache(m, l));
         g.q_norm = c.qk_norm ? bf(m->q_norm[l]) : nullptr;
@@ -800,7 +893,7 @@ static ks_status sync(ks_model* m, const char* what) {
     if (e != cudaSuccess) return cuda_fail(e, what);
     e = cudaStreamSynchronize(m->stream);
     if (e != cudaSuccess) return cuda_fail(e, what);
-    if (*hs == 1) {
+    if (*hs == 1 || *hs == KS_KV8_TIMEOUT) {
         set_error("%s: a kernel gave up waiting for an asynchronous copy", what);
         return KS_ERR_TIMEOUT;
     }
@@ -1069,6 +1162,65 @@ ks_status ks_model_destroy(ks_model* m) {
     return KS_OK;
 }
 
+size_t ks_draft_cache_bytes(const ks_config* cfg) {
+    Draft8Layout L;
+    return config_ok(cfg) && draft8_layout(*cfg, L) ? L.total : 0;
+}
+
+ks_status ks_draft_cache(ks_model* m, void* memory, size_t bytes) {
+    if (!m) {
+        set_error("ks_draft_cache: null model");
+        return KS_ERR_INVALID_ARG;
+    }
+    const ks_config& c = m->cfg;
+    if (!memory) {
+        KS_CUDA(cudaStreamSynchronize(m->stream), "ks_draft_cache");   // drafts in flight use the memory
+        m->draft8.data = nullptr;
+        return KS_OK;
+    }
+    Draft8Layout L;
+    if (!draft8_layout(c, L)) {
+        set_error("ks_draft_cache: needs a bf16 model");
+        return KS_ERR_UNSUPPORTED;
+    }
+    if (reinterpret_cast<uintptr_t>(memory) & 255) {
+        set_error("ks_draft_cache: memory must be 256-byte aligned");
+        return KS_ERR_INVALID_ARG;
+    }
+    if (bytes < L.total) {
+        set_error("ks_draft_cache: memory %zu < required %zu", bytes, L.total);
+        return KS_ERR_WORKSPACE;
+    }
+    char* b = static_cast<char*>(memory);
+    auto& d = m->draft8;
+    std::vector<int32_t> host;
+    std::vector<int> valid;
+    try {
+        host.assign((L.work - L.table) / sizeof(int32_t), 0);
+        valid.assign(c.n_layers, 0);
+    } catch (const std::bad_alloc&) {
+        set_error("ks_draft_cache: out of host memory");
+        return KS_ERR_WORKSPACE;
+    }
+    d.data = nullptr;
+    for (int i = 0; i < L.pages; ++i) host[i] = i;
+    for (int i = 0; i <= c.max_seq; ++i) {
+        host[(L.pairs - L.table) / sizeof(int32_t) + 2 * (size_t)i + 1] = i;
+        host[(L.count - L.table) / sizeof(int32_t) + i] = i;
+    }
+    KS_CUDA(cudaMemcpyAsync(b + L.table, host.data(), host.size() * sizeof(int32_t), cudaMemcpyHostToDevice, m->stream),
+            "draft cache arrays");
+    KS_CUDA(cudaStreamSynchronize(m->stream), "draft cache arrays");
+    d.layer_bytes = L.layer;
+    d.table = reinterpret_cast<int32_t*>(b + L.table);
+    d.pairs = reinterpret_cast<int32_t*>(b + L.pairs);
+    d.count = reinterpret_cast<int32_t*>(b + L.count);
+    d.work = b + L.work;
+    d.valid.swap(valid);
+    d.data = b;
+    return KS_OK;
+}
+
 // The history after a prefill: one entry holding the last hist_init_rows of
 // the prompt's final chunk (lastlen rows captured in slot 0).
 static void reset_history(ks_model* m, int lastlen) {
@@ -1220,7 +1372,7 @@ ks_status ks_draft(ks_model* m, const uint8_t* mask, int32_t gamma, int32_t* dra
         return KS_ERR_CAPACITY;
     }
     for (int t = 0; t < gamma; ++t)
-        KS_TRY(forward(m, m->rows + t, 1, m->p + t, mask, -1, m->rows + t + 1));
+        KS_TRY(forward(m, m->rows + t, 1, m->p + t, mask, -1, m->rows + t + 1, nullptr, true));
     m->last_gamma = gamma;
     m->last_dynamic = false;
     m->last_sampled = false;
@@ -1256,7 +1408,7 @@ ks_status ks_draft_dynamic(ks_model* m, const uint8_t* mask, int32_t gamma, floa
     // a new step: no pass has run and none has stopped (stop and n_drafted are adjacent)
     KS_CUDA(cudaMemsetAsync(m->stop, 0, 2 * sizeof(int), s), "dynamic-exit reset");
     for (int t = 0; t < gamma; ++t) {
-        KS_TRY(forward(m, m->rows + t, 1, m->p + t, mask, -1, m->rows + t + 1, m->stop));
+        KS_TRY(forward(m, m->rows + t, 1, m->p + t, mask, -1, m->rows + t + 1, m->stop, true));
         KS_TRY(launch(m, K_ACCEPT, [&]() -> cudaError_t {
             top1_kernel<<<kTop1Ctas, kTop1Threads, 0, s>>>(m->logits, m->cfg.vocab, m->rows + t + 1, tau_conf, t,
                                                            m->stop, m->n_drafted, m->conf, m->top1_part,
@@ -1403,7 +1555,7 @@ ks_status ks_draft_sample(ks_model* m, const uint8_t* mask, int32_t gamma, const
         return KS_ERR_CAPACITY;
     }
     for (int t = 0; t < gamma; ++t) {
-        KS_TRY(forward(m, m->rows + t, 1, m->p + t, mask, -1, m->rows + t + 1));
+        KS_TRY(forward(m, m->rows + t, 1, m->p + t, mask, -1, m->rows + t + 1, nullptr, true));
         FilterArgs f{};
         f.logits = m->logits; f.ld = m->cfg.vocab; f.vocab = m->cfg.vocab;
         f.inv_t = 1.f / sp->temperature; f.top_k = sp->top_k; f.top_p = sp->top_p;

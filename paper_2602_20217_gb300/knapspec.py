@@ -136,6 +136,8 @@ _SIGS = {
     "ks_kernel_bytes": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_double)]),
     "ks_launch_count": (C.c_int64, [C.c_void_p]),
     "ks_transfer_bytes": (C.c_int, [C.c_void_p, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]),
+    "ks_draft_cache_bytes": (C.c_size_t, [C.POINTER(KsConfig)]),
+    "ks_draft_cache": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t]),
     "ks_kv8_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
     "ks_kv8_append": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Rows), C.c_void_p]),
     "ks_kv8_read": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.c_void_p, C.c_void_p, C.c_int32,
@@ -448,6 +450,14 @@ def ks_select_tpt(h: int, lat: "KsLatency", n_sublayers: int, n_candidates: int,
 
 
 # ------------------------------------------------- 8-bit paged cache
+def ks_draft_cache_bytes(cfg: KsConfig) -> int:
+    return int(load().ks_draft_cache_bytes(C.byref(cfg)))
+
+
+def ks_draft_cache(h: int, memory, nbytes: int):
+    check(load().ks_draft_cache(h, _ptr(memory), nbytes), "ks_draft_cache")
+
+
 KV8_BAD_PAGE, KV8_BAD_BATCH, KV8_BAD_POSITION, KV8_TIMEOUT = 1, 2, 4, 8
 
 

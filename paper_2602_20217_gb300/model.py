@@ -55,6 +55,18 @@ class Model:
     def decode_greedy(self, n_tokens: int):
         return ks.ks_decode_greedy(self.h, n_tokens)
 
+    def draft_cache(self, on: bool = True):
+        """Give the drafts an 8-bit copy of the K/V cache (bf16 models), or take it away."""
+        import torch
+        memory = None
+        if on:
+            nbytes = ks.ks_draft_cache_bytes(self.cfg)
+            if nbytes == 0:
+                raise ks.KsError(ks.KS_ERR_UNSUPPORTED, "draft_cache", "no 8-bit draft cache for this shape")
+            memory = torch.empty(nbytes, dtype=torch.uint8, device=self.workspace.device)
+        ks.ks_draft_cache(self.h, memory, 0 if memory is None else memory.numel())
+        self.draft_memory = memory
+
     def position(self):
         return ks.ks_model_position(self.h)
 
