@@ -274,6 +274,8 @@ KS_DEV void append_block(const Kv8Args& a, const Kv8RowArgs& r, const Kv8Slot& w
 template <int HD, typename T, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 6) kv8_append_kernel(const Kv8Args a, const Kv8RowArgs r) {
     constexpr int TH = HD / 16, GROUPS = kThreads / TH;
+    grid_dependency_wait();
+    grid_launch_dependents();
     if (a.stop && *a.stop) return;
     const int tid = threadIdx.x;
     const int group = tid / TH, d0 = tid % TH * 8, d1 = d0 + HD / 2;
@@ -332,6 +334,8 @@ __global__ void __launch_bounds__(kThreads) kv8_read_kernel(const Kv8Args a, T* 
     constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, PIECES = 2 * HD / kThreads, TH = HD / 8;
     const int tid = threadIdx.x, h = blockIdx.y, d = tid % TH * 8;
     __shared__ __align__(16) unsigned char kc[CODES], vc[CODES + HD * 2];
+    grid_dependency_wait();
+    grid_launch_dependents();
     Kv8Slot w;
     for (Kv8Blocks blocks(a); blocks.get(w); blocks.b += blocks.step) {
         const unsigned char* rec = kv8_record_at(a, w.s, w.blk, h, REC);
@@ -387,17 +391,15 @@ cudaError_t append_hd(Kv8Args a, const Kv8RowArgs& r, cudaStream_t s) {
     const dim3 grid = block_grid(a, a.hk + (r.q ? (r.hq + kQHeads - 1) / kQHeads : 0));
     const bool w = wide(sizeof(T), {r.k, r.v, r.q, r.rope}, {r.k_row, r.k_head, r.v_row, r.v_head, r.q_row, r.q_head}) &&
                    wide(2, {r.q_out}, {r.q_out_row, r.q_out_head});
-    if (w) kv8_append_kernel<HD, T, true><<<grid, kThreads, 0, s>>>(a, r);
-    else kv8_append_kernel<HD, T, false><<<grid, kThreads, 0, s>>>(a, r);
-    return cudaGetLastError();
+    return launch_kv8(w ? kv8_append_kernel<HD, T, true> : kv8_append_kernel<HD, T, false>, grid, kThreads, 0, s, a, r);
 }
 template <int HD, typename T>
 cudaError_t read_hd(Kv8Args a, void* k, void* v, int64_t row_ld, int64_t head_ld, cudaStream_t s) {
     const dim3 grid = block_grid(a, a.hk);
     T *ko = static_cast<T*>(k), *vo = static_cast<T*>(v);
-    if (wide(sizeof(T), {k, v}, {row_ld, head_ld})) kv8_read_kernel<HD, T, true><<<grid, kThreads, 0, s>>>(a, ko, vo, row_ld, head_ld);
-    else kv8_read_kernel<HD, T, false><<<grid, kThreads, 0, s>>>(a, ko, vo, row_ld, head_ld);
-    return cudaGetLastError();
+    const bool w = wide(sizeof(T), {k, v}, {row_ld, head_ld});
+    return launch_kv8(w ? kv8_read_kernel<HD, T, true> : kv8_read_kernel<HD, T, false>, grid, kThreads, 0, s, a, ko, vo,
+                      row_ld, head_ld);
 }
 
 // ------------------------------------------------------------ entry points

@@ -12,7 +12,6 @@
 #pragma once
 
 #include "kv8.cuh"
-#include "tma.cuh"
 
 namespace ks {
 
@@ -186,22 +185,6 @@ struct Rows {
         pos0 = q.len - q.rows + t0;
     }
 };
-
-// Programmatic launch: the kernel waits for what is before it by itself.
-template <class K, class... Args>
-cudaError_t launch_kv8(K kern, dim3 grid, int threads, int smem, cudaStream_t s, const Args&... args) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, args...);
-}
 
 cudaError_t launch_kv8_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s);   // kv8_tc.cu
 
