@@ -44,17 +44,8 @@ constexpr float kQuiet = 1.f / 16384.f;
 
 // Values' scales are taken relative to vref, which follows the tiles of a
 // segment in order: four times the loudest block seen, raised when one passes
-// it.  Both the converting warps and the streams compute it.
-KS_DEV float next_vref(float vref, const float2* scale, int have) {
-    float top = 0.f;
-#pragma unroll
-    for (int c = 0; c < kBlocks; ++c)
-        if (have >> c & 1) top = fmaxf(top, scale[c].y);
-    return top > vref ? 4.f * top : vref;
-}
-// The part of a block's relative scale that the f16 values carry: codes of 2^-9
-// and more stay exact down to 2^-14.  Quieter blocks have the rest in the weights.
-KS_DEV float value_factor(float scale, float vinv) { return fmaxf(scale * vinv, kQuiet); }
+// it.  The f16 values carry a block's relative scale down to 2^-14 (codes of
+// 2^-9 and more stay exact there), the weights the rest of a quieter block's.
 KS_DEV uint32_t f16_times(uint32_t v, __half2 f) {
     const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&v), f);
     return *reinterpret_cast<const uint32_t*>(&r);
@@ -68,13 +59,14 @@ struct Smem {
     unsigned char v[kRing][TILE];               // [key / 16][HD][16]
     unsigned char v16[2][2 * TILE];             // f16 [key / 8][HD][8]
     float2 scale[kNear][kBlocks];               // key scale, value scale
+    __half2 factor[kNear][kBlocks];             // of the values
     float4 join[2][kRows];                      // m, l, vref of a stream
     float qf[kRows];
     float vref[kNear];                          // of a tile; negative: one of its blocks is quiet
     int nan_from[4][HD];                        // first key whose value is NaN, a segment each
     int any_nan[4];
     int present[kNear];
-    uint64_t scales[kNear], vref_set[kNear], k_full[kRing], k_free[kRing], v_full[kRing], v_free[kRing], v16_full[2], v16_free[2];
+    uint64_t scales[kNear], k_full[kRing], k_free[kRing], v_full[kRing], v_free[kRing], v16_full[2], v16_free[2];
     uint64_t q_full, s_full[2], p_full[2], o_full[2], o_free;
     uint32_t tmem;
 };
@@ -147,10 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (warp == kProductWarp) tmem_alloc<1>(&sm.tmem, 512);
     if (tid == 0) {
-        for (int i = 0; i < kNear; ++i) {
-            mbar_init(&sm.scales[i], 1);
-            mbar_init(&sm.vref_set[i], 1);
-        }
+        for (int i = 0; i < kNear; ++i) mbar_init(&sm.scales[i], 1);
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&sm.k_full[i], 1);
             mbar_init(&sm.k_free[i], 1);
@@ -200,6 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int r = lane % kBlocks;
         const unsigned heads = p.run == 8 ? 0x01u : p.run == 4 ? 0x11u : p.run == 2 ? 0x55u : 0xffu;
         int it = 0, tile = at.tile, page = pages(at, tile);
+        float vref = 0.f;
         bool alive = true, more = true;
         while (more && alive) {
             Segment next = at;
@@ -215,6 +205,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             float2 scale = make_float2(0.f, 0.f);
             if (record >= 0) scale = __ldg(reinterpret_cast<const float2*>(a.data + (size_t)record * REC + 2 * PART));
             const unsigned have = __ballot_sync(0xffffffffu, record >= 0);
+            float top = scale.y;                     // of the lane's tile
+#pragma unroll
+            for (int o = 1; o < kBlocks; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if (tile == at.tile) vref = 0.f;
             for (int i = 0; i < TILES && tile + i < at.end; ++i, ++it) {
                 const int st = it % kRing, near = it % kNear, odd = ((it / kRing) & 1) ^ 1;
                 const unsigned mask = have >> (i * kBlocks) & ((1u << kBlocks) - 1);
@@ -230,13 +224,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_expect_tx(&sm.v_full[st], bytes);
                 }
                 __syncwarp();
-                if (lane / kBlocks == i && record >= 0) {
-                    if (heads >> r & 1) {
-                        tma_2d(sm.k[st] + r * PART, &map, 0, record, &sm.k_full[st]);
-                        tma_2d(sm.v[st] + r * PART, &map, PART / 8, record, &sm.v_full[st]);
-                    }
-                    sm.scale[near][r] = scale;
+                if (lane / kBlocks == i && record >= 0 && (heads >> r & 1)) {
+                    tma_2d(sm.k[st] + r * PART, &map, 0, record, &sm.k_full[st]);
+                    tma_2d(sm.v[st] + r * PART, &map, PART / 8, record, &sm.v_full[st]);
                 }
+                const float loudest = __shfl_sync(0xffffffffu, top, i * kBlocks);
+                if (loudest > vref) vref = 4.f * loudest;
+                const float rel = scale.y * inverse_pow2(vref);
+                const bool own = lane / kBlocks == i && record >= 0;
+                const unsigned quiet = __ballot_sync(0xffffffffu, own && rel < kQuiet);
+                if (own) {
+                    sm.scale[near][r] = scale;
+                    sm.factor[near][r] = __float2half2_rn(fmaxf(rel, kQuiet));
+                }
+                if (lane == 0) sm.vref[near] = quiet ? -vref : vref;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.scales[near]);
             }
@@ -264,13 +265,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     ok = ok && mbar_wait(&sm.k_full[st], ((it0 + j) / kRing) & 1, kWaitLimitNs);
                     if (!ok) return;
                     umma_fence_after();
-                    const uint32_t kb = smem_u32(sm.k[st]);
+                    // hi, then lo; a step of 256 bytes is 16 in a descriptor
+                    const uint64_t q0 = desc_plain(smem_u32(sm.q[0]), 128, 8 * HD), k0 = desc_plain(smem_u32(sm.k[st]), 128, 8 * HD);
 #pragma unroll
-                    for (int part = 0; part < 2; ++part)
-#pragma unroll
-                        for (int c = 0; c < HD / 32; ++c)
-                            umma_e4m3(tmem + 128 * (j & 1), desc_plain(smem_u32(sm.q[part]) + 256 * c, 128, 8 * HD),
-                                      desc_plain(kb + 256 * c, 128, 8 * HD), kIdS, part > 0 || c > 0);
+                    for (int c = 0; c < HD / 16; ++c) {
+                        const int k = c % (HD / 32);
+                        umma_e4m3(tmem + 128 * (j & 1), q0 + (c / (HD / 32) * (kRows * HD / 16) + 16 * k), k0 + 16 * k, kIdS, c > 0);
+                    }
                     umma_commit(&sm.k_free[st]);
                     umma_commit(&sm.s_full[j & 1]);
                 };
@@ -284,11 +285,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (!ok) break;
                     ++n[i];
                     umma_fence_after();
-                    const uint32_t vb = smem_u32(sm.v16[b]);
+                    const uint64_t v0 = desc_plain(smem_u32(sm.v16[b]), 16 * HD, 128);
 #pragma unroll
                     for (int c = 0; c < kTile / 16; ++c)
-                        umma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 8 * c, desc_plain(vb + 32 * HD * c, 16 * HD, 128),
-                                kIdO, j > 1 || c > 0);
+                        umma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 8 * c, v0 + 2 * HD * c, kIdO, j > 1 || c > 0);
                     umma_commit(&sm.v16_free[b]);
                     umma_commit(&sm.o_full[i]);
                     mbar_arrive(&sm.o_full[i]);
@@ -308,24 +308,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         int it = 0, seg = 0;
         do {
             const Rows rows(at.q, p.tq, at.g, G);
-            float vref = 0.f;
             for (int tile = at.tile; tile < at.end; ++tile, ++it) {
                 const int st = it % kRing, b = it & 1, near = it % kNear;
-                alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs);
-                const int have = present[near];
-                vref = next_vref(vref, sm.scale[near], have);
-                const float vinv = inverse_pow2(vref);
-                if (b == mine) {
-                    if (ct == 0) {
-                        bool quiet = false;
-#pragma unroll
-                        for (int c = 0; c < kBlocks; ++c)
-                            quiet = quiet || ((have >> c & 1) && sm.scale[near][c].y * vinv < kQuiet);
-                        sm.vref[near] = quiet ? -vref : vref;
-                        mbar_arrive(&sm.vref_set[near]);
-                    }
-                    alive = alive && mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
-                }
+                if (b == mine) alive = alive && mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
                 if (tile == at.tile) {
                     // Clear the next segment's marks.  The products of the tile two before are done, so those of
                     // the segment two back have begun and the readers of the one three back, who had this
@@ -337,6 +322,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     convert_sync();
                 }
                 if (b != mine) continue;
+                alive = alive && mbar_wait(&sm.scales[near], (it / kNear) & 1, kWaitLimitNs);
+                const int have = present[near];
                 alive = alive && mbar_wait(&sm.v_full[st], (it / kRing) & 1, kWaitLimitNs);
                 const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
                 const unsigned char* src = sm.v[st];
@@ -352,25 +339,25 @@ __global__ void __launch_bounds__(kThreads, 1)
                     *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                     *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 };
-                auto factor = [&](int r) { return __float2half2_rn(value_factor(sm.scale[near][r].y, vinv)); };
                 constexpr int STEP = 16 * kConvertWarps, N = kBlocks * HD / STEP, PER = HD / STEP;   // passes a record
                 if (!edge) {
-                    // all loads first: they wait behind the products' reads of shared memory
-                    uint4 x[N];
-                    __half2 f[kBlocks];
+                    // the next loads first: they wait behind the products' reads of shared memory
+                    constexpr int AHEAD = 4;
+                    uint4 x[AHEAD], next[AHEAD];
+                    auto load = [&](int c) {
 #pragma unroll
-                    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const uint4*>(src + (i * STEP + ct) * 16);
-#pragma unroll
-                    for (int r = 0; r < kBlocks; ++r) f[r] = factor(r);
+                        for (int i = 0; i < AHEAD; ++i)
+                            next[i] = *reinterpret_cast<const uint4*>(src + ((c + i) * STEP + ct) * 16);
+                    };
+                    load(0);
 #pragma unroll 1
-                    for (int c = 0; c < N; c += 8) {
+                    for (int c = 0; c < N; c += AHEAD) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            convert((c + i) / PER, (i % PER) * STEP + ct, x[i], f[i / PER]);
+                        for (int i = 0; i < AHEAD; ++i) x[i] = next[i];
+                        if (c + AHEAD < N) load(c + AHEAD);
 #pragma unroll
-                        for (int i = 0; i + 8 < N; ++i) x[i] = x[i + 8];
-#pragma unroll
-                        for (int r = 0; r + 8 / PER < kBlocks; ++r) f[r] = f[r + 8 / PER];
+                        for (int i = 0; i < AHEAD; ++i)
+                            convert((c + i) / PER, (i % PER) * STEP + ct, x[i], sm.factor[near][(c + i) / PER]);
                     }
                 } else {
 #pragma unroll 1
@@ -394,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                         }
                         if (have >> r & 1) {
-                            convert(r, d, make_uint4(w[0], w[1], w[2], w[3]), factor(r));
+                            convert(r, d, make_uint4(w[0], w[1], w[2], w[3]), sm.factor[near][r]);
                         } else {
                             *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) = make_uint4(0, 0, 0, 0);
                             *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(0, 0, 0, 0);
@@ -503,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             for (int j = i; j < cnt; j += 2, ++n) {
                 const int tile = at.tile + j, near = (it0 + j) % kNear;
-                alive = alive && mbar_wait(&sm.vref_set[near], ((it0 + j) / kNear) & 1, kWaitLimitNs);
+                alive = alive && mbar_wait(&sm.scales[near], ((it0 + j) / kNear) & 1, kWaitLimitNs);
                 // read before the scores are there: shared memory is the products' while they run, and a load
                 // between them takes hundreds of clocks
                 float f[kBlocks];
