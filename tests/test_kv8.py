@@ -170,3 +170,12 @@ def test_python_face_checks_its_tensors(lib):
     assert c.data.numel() == c.nbytes == 4 * 8 * 4 * 4128
     with pytest.raises(KsError):
         c.attention_workspace(12, 1, 1)
+
+
+def test_more_tiles_than_a_call_counts(lib):
+    """Rows times tokens past what 32 bits count are refused."""
+    from paper_2602_20217_gb300 import knapspec as ks
+    cache, batch, rows, attn = good(ks)
+    cache.page_tokens, batch.table_ld, batch.n_rows = 1 << 20, 1023, 2000
+    assert lib.ks_kv8_attention(C.byref(cache), C.byref(batch), C.byref(attn), None) == ks.KS_ERR_UNSUPPORTED
+    assert "too much for one call" in lib.ks_last_error().decode()
