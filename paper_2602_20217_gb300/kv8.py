@@ -77,9 +77,11 @@ class Cache8:
         self.c = ks.KsKv8Cache(data.data_ptr(), n_pages, page_tokens, n_kv_heads, head_dim)
 
     def _stream(self, stream):
-        if self.device.index != _cuda.current_device():
+        index = _cuda.current_device()
+        if self.device.index != index:
             raise ValueError(f"the cache is on {self.device}, not on the current device")
-        return _cuda.current_stream().cuda_stream if stream is None else ks._stream_ptr(stream)
+        # the address alone: torch.cuda.current_stream() builds an object in 2.8 us, a quarter of a small call
+        return torch._C._cuda_getCurrentRawStream(index) if stream is None else ks._stream_ptr(stream)
 
     def _rows(self, t, name, kinds, batch, heads=None):
         """Row and head stride of a [rows, heads, head_dim] tensor, after its checks."""
