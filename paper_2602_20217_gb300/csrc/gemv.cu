@@ -17,6 +17,7 @@
 // residual's producer wrote, in group order.
 #include "common.cuh"
 #include "internal.h"
+#include "kv8.h"
 #include "tma.cuh"
 
 #include <cudaTypedefs.h>

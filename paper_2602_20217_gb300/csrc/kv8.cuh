@@ -13,7 +13,7 @@
 #include <cuda_fp16.h>
 
 #include "common.cuh"
-#include "internal.h"
+#include "kv8.h"
 #include "tma.cuh"
 
 namespace ks {
@@ -128,9 +128,11 @@ struct Kv8Blocks {
         }
         q = kv8_seq(a, s);
         start = max(q.len - q.rows, 0);
-        if (b == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-            if (kv8_seq_bad(a, s)) kv8_flag(a, kKv8BadBatch);
-            if (q.len < q.rows) kv8_flag(a, kKv8BadPosition);
+        // x is at least n_seqs wide either way, and offsets that decrease may hide a sequence from the search
+        if ((int)blockIdx.x < a.n_seqs && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
+            const Kv8Seq own = kv8_seq(a, blockIdx.x);
+            if (kv8_seq_bad(a, blockIdx.x)) kv8_flag(a, kKv8BadBatch);
+            if (own.len < own.rows) kv8_flag(a, kKv8BadPosition);
         }
     }
     KS_DEV bool get(Kv8Slot& w) const {

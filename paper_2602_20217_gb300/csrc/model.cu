@@ -13,6 +13,7 @@
 #include "../../include/knapspec.h"
 #include "common.cuh"
 #include "internal.h"
+#include "kv8.h"
 
 #include <cmath>
 #include <cstdarg>

@@ -305,3 +305,20 @@ def test_append_many_blocks_of_few_sequences():
         blk = want[0, t // 16, 1]
         assert np.array_equal(ko[o0 + t - 50, 1].cpu().numpy(), O.VALUES[blk[0][t % 16]] * blk[2])
         assert np.array_equal(vo[o0 + t - 50, 1].cpu().numpy(), O.VALUES[blk[1][t % 16]] * blk[3])
+
+
+@pytest.mark.parametrize("offsets", [[100, 3, 60], [0, 80, 70], [-3, 50, 100], [0, 50, 101]])
+def test_append_flags_offsets_in_batches_of_many_rows(offsets):
+    import torch
+    pool = Pool([100, 100], 1, 64, 16, seed=24).fill()
+    d = pool.device([50, 50])
+    d["offsets"].copy_(torch.tensor(offsets, dtype=torch.int32))
+    x = torch.randn(100, 2, 64, device="cuda").to(torch.bfloat16)
+    d["cache"].append(d["batch"], x[:, :1], x[:, 1:])
+    torch.cuda.synchronize()
+    assert int(d["status"]) & 2
+    d["status"].zero_()
+    out = torch.empty(2, 100, 1, 64, device="cuda")
+    d["cache"].read(d["batch"], out[0], out[1])
+    torch.cuda.synchronize()
+    assert int(d["status"]) & 2
