@@ -498,6 +498,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int c = 0; c < kBlocks; ++c) f[c] = fmaxf(qf * sm.scale[near][c].x, 1e-36f);   // above zero: -inf stays
                 const int have = present[near];
                 const float vnow = sm.vref[near], vnew = fabsf(vnow);
+                const bool edge = have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0;
+                const bool fresh = __any_sync(0xffffffffu, m == -INFINITY);
+                const bool special = edge || fresh || vnew != vref;
                 alive = alive && mbar_wait(&sm.s_full[i], n & 1, kWaitLimitNs);
                 __syncwarp();
                 umma_fence_after();
@@ -505,38 +508,40 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (lane == 0) mbar_arrive(&sm.p_full[i]);
                     continue;
                 }
-                if (have != (1 << kBlocks) - 1 || tile * kTile + kTile - 1 > rows.pos0) {
-                    // what a row does not see becomes -inf where it lies, so that the pass below needs no mask
+                if (special) {
+                    if (edge) {
+                        // what a row does not see becomes -inf where it lies, so that the pass below needs no mask
 #pragma unroll 1
-                    for (int c = c0; c < c1; ++c) {
-                        uint32_t x[32];
-                        tmem_ld32(x, s_at + 32 * c);
-                        tmem_wait_ld();
-                        tmem_pin(x);
+                        for (int c = c0; c < c1; ++c) {
+                            uint32_t x[32];
+                            tmem_ld32(x, s_at + 32 * c);
+                            tmem_wait_ld();
+                            tmem_pin(x);
 #pragma unroll
-                        for (int q = 0; q < 32; ++q)
-                            if (tile * kTile + 32 * c + q > lim || !(have >> (2 * c + q / 16) & 1)) x[q] = 0xff800000u;
-                        tmem_st32(s_at + 32 * c, x);
+                            for (int q = 0; q < 32; ++q)
+                                if (tile * kTile + 32 * c + q > lim || !(have >> (2 * c + q / 16) & 1)) x[q] = 0xff800000u;
+                            tmem_st32(s_at + 32 * c, x);
+                        }
+                        tmem_wait_st();
                     }
-                    tmem_wait_st();
-                }
-                if (vnew != vref) {
-                    if (!first) rescale(vref * inverse_pow2(vnew));
-                    vref = vnew;
-                }
-                if (__any_sync(0xffffffffu, m == -INFINITY)) {
-                    float top = m;
+                    if (vnew != vref) {
+                        if (!first) rescale(vref * inverse_pow2(vnew));
+                        vref = vnew;
+                    }
+                    if (fresh) {
+                        float top = m;
 #pragma unroll 1
-                    for (int c = c0; c < c1; ++c) {
-                        uint32_t x[32];
-                        tmem_ld32(x, s_at + 32 * c);
-                        const float f0 = pick(f, 2 * c), f1 = pick(f, 2 * c + 1);
-                        tmem_wait_ld();
-                        tmem_pin(x);
+                        for (int c = c0; c < c1; ++c) {
+                            uint32_t x[32];
+                            tmem_ld32(x, s_at + 32 * c);
+                            const float f0 = pick(f, 2 * c), f1 = pick(f, 2 * c + 1);
+                            tmem_wait_ld();
+                            tmem_pin(x);
 #pragma unroll
-                        for (int q = 0; q < 32; ++q) top = fmaxf(top, __uint_as_float(x[q]) * (q < 16 ? f0 : f1));
+                            for (int q = 0; q < 32; ++q) top = fmaxf(top, __uint_as_float(x[q]) * (q < 16 ? f0 : f1));
+                        }
+                        if (m == -INFINITY) m = ceilf(top);          // l and O are still zero
                     }
-                    if (m == -INFINITY) m = ceilf(top);          // l and O are still zero
                 }
                 // 32 scores at a time, in a loop that stays one: unrolled, the roles' code together no longer fits
                 // the instruction cache, and a tile of the softmax takes up to 6700 clocks.
