@@ -8,6 +8,12 @@
 // relative rounding is 2^-4 at any scale, and it makes the growth of a scale
 // exact: when a later token raises it, the stored codes are multiplied by a
 // power of two, which rounds only where a code becomes subnormal.
+//
+// Bytes bound both kernels where there are many rows: nine prompts of 40k tokens
+// in all (64 query heads over 8, hd 128), append 291 us and read 45 us, both 5.4
+// TB/s; one prompt of 4096 tokens (32 heads) 33 us for both.  Batches of few rows
+// are a chain of four dependent loads (sequence, page, record and rows, angles):
+// 4 us for one token, 11 us a kernel for 96 sequences of 1 to 11 rows.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>

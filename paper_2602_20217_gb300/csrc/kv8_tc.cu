@@ -27,6 +27,17 @@
 // more than 2^15.5.  So most tiles need no maximum at all, no weight passes f16,
 // and weights count down to f16's 2^-24: 2^-34 of the largest, or 2^-39 where
 // the reference lags behind it.
+//
+// Measured: 2001 rows of a prompt at 8150 tokens (64 query heads over 8, hd 128)
+// 670 us, 700 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 84 us, 3.2
+// TB/s; 24 sequences of 2 to 11 rows at up to 16000 tokens 142 us.  What bounds
+// it is the round trip of a stream's tile, products to softmax and back, 5800
+// clocks of which the products are 1400 and the softmax 2600; the two streams
+// hide half of it.  Taking out the conversion, half of Q K^T and most of P V
+// together saves 15 %, all but a quarter of the weights 22 % more.  A third
+// stream has no TMEM (S and O of two fill it).  Other arrangements of two were
+// slower: tiles of 64 keys, two threads a row on one tile, the two products
+// issued by two warps, 64 scores at a time or 16.
 #include "kv8_plan.cuh"
 #include "umma.cuh"
 
