@@ -469,7 +469,8 @@ typedef struct {
  * decrease or pass n_rows, or a length below 0 or above the pages (taken as the
  * nearest possible value); bit 2: a token before position 0 or past the RoPE
  * table (not appended, or stored as zeros); bit 3: a bounded wait gave up.
- * No two sequences of a call may append to the same block. */
+ * No two blocks that a call appends to may be one (of two sequences, or of one
+ * whose table names a page twice); reading and attending may share pages. */
 #define KS_KV8_BAD_PAGE 1
 #define KS_KV8_BAD_BATCH 2
 #define KS_KV8_BAD_POSITION 4
@@ -478,7 +479,7 @@ typedef struct {
     const int32_t* page_table;   /* dev [n_seqs][table_ld]                      */
     const int32_t* row_offsets;  /* dev [n_seqs + 1], row_offsets[0] usually 0  */
     const int32_t* lengths;      /* dev [n_seqs], at most table_ld page_tokens  */
-    int32_t n_seqs, table_ld, n_rows;
+    int32_t n_seqs, table_ld, n_rows;   /* table_ld page_tokens at most 2^30     */
     int32_t* status;             /* dev, or NULL                                */
 } ks_kv8_batch;
 

@@ -409,7 +409,8 @@ cudaError_t read_hd(Kv8Args a, void* k, void* v, int64_t row_ld, int64_t head_ld
 }
 
 // ------------------------------------------------------------ entry points
-constexpr int kMaxRows = 1 << 24, kMaxSeqs = 1 << 20, kMaxHeads = 1024;
+// kMaxTokens: of a sequence; positions a tile past the last one still are ints
+constexpr int kMaxRows = 1 << 24, kMaxSeqs = 1 << 20, kMaxHeads = 1024, kMaxTokens = 1 << 30;
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -436,7 +437,7 @@ ks_status kv8_args(const char* who, const ks_kv8_cache* c, const ks_kv8_batch* b
         return KS_ERR_INVALID_ARG;
     }
     if (b->n_seqs > 0) {
-        if (b->table_ld < 1 || (int64_t)b->table_ld * c->page_tokens > INT32_MAX) {
+        if (b->table_ld < 1 || (int64_t)b->table_ld * c->page_tokens > kMaxTokens) {
             set_error("%s: a page table of %d pages of %d tokens", who, b->table_ld, c->page_tokens);
             return KS_ERR_INVALID_ARG;
         }

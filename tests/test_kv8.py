@@ -179,3 +179,17 @@ def test_more_tiles_than_a_call_counts(lib):
     cache.page_tokens, batch.table_ld, batch.n_rows = 1 << 20, 1023, 2000
     assert lib.ks_kv8_attention(C.byref(cache), C.byref(batch), C.byref(attn), None) == ks.KS_ERR_UNSUPPORTED
     assert "too much for one call" in lib.ks_last_error().decode()
+
+
+def test_longest_sequence(lib):
+    """Page tables of up to 2^30 tokens."""
+    from paper_2602_20217_gb300 import knapspec as ks
+    cache, batch, rows, attn = good(ks)
+    batch.n_rows = 0
+    batch.table_ld = 1 << 24
+    assert lib.ks_kv8_append(C.byref(cache), C.byref(batch), C.byref(rows), None) == 0
+    batch.table_ld += 1
+    for status in (lib.ks_kv8_append(C.byref(cache), C.byref(batch), C.byref(rows), None),
+                   lib.ks_kv8_attention(C.byref(cache), C.byref(batch), C.byref(attn), None),
+                   lib.ks_kv8_read(C.byref(cache), C.byref(batch), A, A, 1, 1024, 128, None)):
+        assert status == ks.KS_ERR_INVALID_ARG
