@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         if (tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
-    const int G = t.hq / a.hk;
+    const int G = p.G;
 
     if (warp == kConsumers) {
         // ------------------------------------------------------- producer
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
             const int b = tile * kBlocks + lane;
             const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
             if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
-            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + b / a.bpp);
+            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + p.page_of(b, a.bpp));
             return page >= 0 && page < a.n_pages ? page : -2;
         };
         int it = 0, tile = at.tile, page = pages(at, tile);
@@ -190,7 +190,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
             if (page == -2) kv8_flag(a, kKv8BadPage);
             const int b = tile * kBlocks + lane;
             const unsigned char* rec =
-                page >= 0 ? a.data + (((size_t)page * a.hk + at.h) * a.bpp + b % a.bpp) * REC : nullptr;
+                page >= 0 ? a.data + (((size_t)page * a.hk + at.h) * a.bpp + b - p.page_of(b, a.bpp) * a.bpp) * REC
+                          : nullptr;
             const unsigned have = __ballot_sync(0xffffffffu, rec != nullptr);
             // one copy for records that follow each other: the lane of the first one makes it
             const unsigned char* before = reinterpret_cast<const unsigned char*>(
@@ -232,12 +233,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         uint32_t qa[S::Q ? 1 : NQ][S::Q ? 1 : KJ][4];
         float qf[NQ];
         int lim[NQ];                                             // last key that the row sees
-        const int lim_first = rows.pos0, lim_last = rows.pos0 + (rows.n - 1) / G;
+        const int lim_first = rows.pos0, lim_last = rows.pos0 + rows.tokens - 1;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int m = 8 * n + g;
             const bool valid = m < rows.n;
-            const int tok = valid ? m / G : 0, head = at.h * G + (valid ? m - tok * G : 0);
+            const int tok = valid ? p.token(m) : 0, head = at.h * G + (valid ? m - tok * G : 0);
             const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head;
             lim[n] = valid ? rows.pos0 + tok : INT32_MAX;
             float x[KJ * 2][4], top = 0.f;
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     const float f = __shfl_sync(0xffffffffu, inv, 8 * q4 + 4 * e);
                     const int r = 8 * n + 2 * q4 + e;
                     if (any_nan) {
-                        const int seen = rows.pos0 + r / G;
+                        const int seen = rows.pos0 + p.token(r);
                         for (int i = 0; i < DT / 4; ++i)
                             for (int c = 0; c < 2; ++c)
                                 if (sm.nan_from[buf][16 * (dt0 + i) + 8 * c + g] <= seen)
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     }
                     if (r >= rows.n) continue;
                     if (whole) {
-                        const int tok = r / G;
+                        const int tok = p.token(r);
                         __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row +
                                              (int64_t)(at.h * G + r - tok * G) * t.out_head + 16 * dt0 + g;
 #pragma unroll
@@ -469,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     if (!whole) {
                         *reinterpret_cast<float2*>(slot + (size_t)m_row * (HD + 4)) = make_float2(m[n], l[n]);
                     } else if (t.lse) {
-                        const int tok = m_row / G;
+                        const int tok = p.token(m_row);
                         t.lse[(size_t)(rows.row0 + tok) * t.hq + at.h * G + m_row - tok * G] =
                             l[n] == 0.f ? -INFINITY : (m[n] + log2f(l[n])) * kLn2;
                     }
@@ -504,7 +505,7 @@ __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args 
     __shared__ int counts[kMergeThreads / 32];
     __shared__ int4 unit;
     __shared__ int run_x;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp % MW, G = t.hq / a.hk;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp % MW, G = p.G;
     if (tid == 0) unit = make_int4(0, 0, 0, 0);
     grid_dependency_wait();
     if (a.stop && *a.stop) return;
@@ -573,7 +574,7 @@ __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args 
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = fmaf(acc_s[rr][i][V * lane + j], f, acc[j]);
     }
-    const int tok = r / G, head = u.z * G + r - tok * G;
+    const int tok = p.token(r), head = u.z * G + r - tok * G;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     __nv_bfloat16* out = t.out + (int64_t)(u.x + tok) * t.out_row + (int64_t)head * t.out_head + V * lane;
 #pragma unroll
@@ -604,7 +605,7 @@ cudaError_t launch_few(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p,
 
 template <int HD>
 cudaError_t launch_merge(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, int64_t units, cudaStream_t s) {
-    const int x = (int)std::min<int64_t>(p.ctas, units), rows = p.tq * (t.hq / a.hk);
+    const int x = (int)std::min<int64_t>(p.ctas, units), rows = p.tq * p.G;
     if (units * units < p.ctas)
         return launch_kv8(kv8_merge_kernel<HD, 8>, dim3(x, (rows + 1) / 2), kMergeThreads, 0, s, a, t, p);
     return launch_kv8(kv8_merge_kernel<HD, 2>, dim3(x, (rows + 7) / 8), kMergeThreads, 0, s, a, t, p);
@@ -615,10 +616,15 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& ti
     const int G = hq / a.hk;
     p = Kv8Plan{};
     p.rg = rows_of_unit(G, a.n_rows, a.n_seqs);
+    p.G = G;
+    p.token_mul = (65536 + G - 1) / G;
     p.tq = p.rg / G;
-    p.tile = p.rg == kKv8TcRows ? 128 : kTile;
-    p.cost = 128 * kUnitCost / p.tile;
-    tiles = (a.capacity + (int64_t)p.tile - 1) / p.tile;
+    p.tile_log = p.rg == kKv8TcRows ? 7 : 6;
+    p.cost = (128 * kUnitCost) >> p.tile_log;
+    p.block_log = -1;
+    for (int i = 0; i < 31; ++i)
+        if (a.bpp == 1 << i) p.block_log = i;
+    tiles = (a.capacity + (1ll << p.tile_log) - 1) >> p.tile_log;
     units = (int64_t)a.hk * (a.n_rows / p.tq + a.n_seqs);
     return units * (tiles + p.cost) <= INT32_MAX;
 }

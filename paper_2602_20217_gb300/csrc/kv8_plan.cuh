@@ -23,7 +23,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kUnitCost = 2;
 
 struct Kv8Plan {
-    int tile;           // keys of a tile
+    int tile_log;       // keys of a tile
+    int block_log;      // blocks of a page, -1: no power of two
+    int G;              // query heads a KV head
+    int token_mul;      // see token()
     int cost;           // a unit's fixed cost in tiles
     int tq;             // tokens of a group
     int rg;             // rows of a group, at least tq query groups
@@ -33,18 +36,23 @@ struct Kv8Plan {
     float* part;        // [2 ctas][rg][HD + 4]: m, l, -, -, o
     int4* desc;         // [ctas]: the unit that begins in this CTA's run and ends in a later one's: first batch row,
                         // query rows (0: no such unit), KV head, last CTA
+    // The kernels' fixed steps are chains of a few hundred clocks each, in which a division by a number that is not
+    // known when compiling takes about 150: tiles and pages go by shifts, and row r < 128 of a group is of token
+    // r / G = r token_mul >> 16, token_mul = 2^16 / G rounded up (r (G - 1) < 2^16).
+    KS_DEV int token(int r) const { return r * token_mul >> 16; }
+    KS_DEV int page_of(int block, int bpp) const { return block_log >= 0 ? block >> block_log : block / bpp; }
 };
 
 // Tiles of group g; a group whose rows see nothing has one as well (its rows get zeros).
 KS_DEV int group_tiles(const Kv8Seq& q, const Kv8Plan& p, int g) {
     const int last = q.len - q.rows + min(q.rows, (g + 1) * p.tq) - 1;
-    return last < 0 ? 1 : (unsigned)last / (unsigned)p.tile + 1;
+    return last < 0 ? 1 : (last >> p.tile_log) + 1;
 }
-KS_DEV int groups_of(const Kv8Seq& q, int tq) { return (q.rows + tq - 1) / tq; }
+KS_DEV int groups_of(const Kv8Seq& q, int tq) { return q.rows <= tq ? q.rows > 0 : (q.rows + tq - 1) / tq; }
 // What the units of one head of a sequence take on the line of all units.
 KS_DEV int head_length(const Kv8Seq& q, const Kv8Plan& p) {
     int n = 0;
-    for (int g = 0; g < groups_of(q, p.tq); ++g) n += group_tiles(q, p, g) + p.cost;
+    for (int g = 0, groups = groups_of(q, p.tq); g < groups; ++g) n += group_tiles(q, p, g) + p.cost;
     return n;
 }
 
@@ -100,6 +108,7 @@ struct Segment {
 KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     Kv8Seq mine{};
+    int head = 0;                                // length of one of its heads' units
     auto load = [&](int c) {
         const int s = c + lane;
         if (s >= a.n_seqs) {
@@ -107,7 +116,8 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
             return 0;
         }
         mine = kv8_seq(a, s);
-        return a.hk * head_length(mine, p);
+        head = head_length(mine, p);
+        return a.hk * head;
     };
     int total = 0, v = 0;
     for (int c = 0; c < a.n_seqs; c += 32) {
@@ -117,7 +127,7 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
     }
     r.cut(total, p.ctas, cta);
     if (cta >= r.ctas) return false;
-    int start = 0;                               // of the sequence's units on the line
+    int start = 0, len = 0;                      // of the sequence's units on the line; a head's length
     for (int c = 0;; c += 32) {
         if (a.n_seqs > 32) v = load(c);
         int u = v;                               // inclusive sums
@@ -133,12 +143,12 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
             k.q.row0 = __shfl_sync(0xffffffffu, mine.row0, i);
             k.q.rows = __shfl_sync(0xffffffffu, mine.rows, i);
             k.q.len = __shfl_sync(0xffffffffu, mine.len, i);
+            len = __shfl_sync(0xffffffffu, head, i);
             start += __shfl_sync(0xffffffffu, u - v, i);
             break;
         }
         start += __shfl_sync(0xffffffffu, u, 31);
     }
-    const int len = head_length(k.q, p);
     k.h = (r.x0 - start) / len;
     start += k.h * len;
     k.g = 0;
@@ -175,12 +185,14 @@ KS_DEV float exp2_approx(float x) {
 }
 // A unit's rows, as its segments and the merge see them.
 struct Rows {
+    int tokens;
     int n;              // query rows: tokens x G
     int row0;           // batch row of the first token
     int pos0;           // its position; negative positions see nothing
     KS_DEV Rows(const Kv8Seq& q, int tq, int g, int G) {
-        const int t0 = g * tq, t = min(q.rows - t0, tq);
-        n = t * G;
+        const int t0 = g * tq;
+        tokens = min(q.rows - t0, tq);
+        n = tokens * G;
         row0 = q.row0 + t0;
         pos0 = q.len - q.rows + t0;
     }

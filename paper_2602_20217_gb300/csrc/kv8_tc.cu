@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool stopped = a.stop && *a.stop;
     const bool work = !stopped && find_run(a, p, run, at);
     if (!work && !stopped && tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
-    const int G = t.hq / a.hk;
+    const int G = p.G;
 
     if (!work) {
         // nothing in this run
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int b = tile * kBlocks + lane;
             const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
             if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
-            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + b / a.bpp);
+            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + p.page_of(b, a.bpp));
             return page >= 0 && page < a.n_pages ? page : -2;
         };
         // a run of p.run records is one copy of keys and one of values
@@ -211,7 +211,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const int next_page = more ? pages(next, next_tile) : -1;
             if (page == -2) kv8_flag(a, kKv8BadPage);
-            const int record = page >= 0 ? (page * a.hk + at.h) * a.bpp + (tile * kBlocks + lane) % a.bpp : -1;
+            const int b = tile * kBlocks + lane;
+            const int record = page >= 0 ? (page * a.hk + at.h) * a.bpp + b - p.page_of(b, a.bpp) * a.bpp : -1;
             // the scales come by ordinary loads, behind the first copies
             float2 scale = make_float2(0.f, 0.f);
             if (record >= 0) scale = __ldg(reinterpret_cast<const float2*>(a.data + (size_t)record * REC + 2 * PART));
@@ -428,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // the unit's queries in two codes: two threads a row
                 const int qr = tid >> 1, half = tid & 1, ur = qr & (kRows / copies - 1);
                 const bool valid = ur < rows.n;
-                const int tok = valid ? ur / G : 0, head = at.h * G + (valid ? ur - tok * G : 0);
+                const int tok = valid ? p.token(ur) : 0, head = at.h * G + (valid ? ur - tok * G : 0);
                 const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head + half * (HD / 2);
                 uint4 raw[HD / 16];
                 if (p.q_wide) {
@@ -480,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) mbar_arrive(&sm.q_full);
             }
             const float qf = sm.qf[row];
-            const int lim = row < rows.n ? rows.pos0 + row / G : INT32_MAX;
+            const int lim = row < rows.n ? rows.pos0 + p.token(row) : INT32_MAX;
             float m = -INFINITY, l = 0.f, vref = 0.f;
             bool first = true;
             auto rescale = [&](float fac) {           // O, once the products before are in it
@@ -641,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool whole = at.tile == 0 && at.end == at.tiles;
             const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
             const bool valid = row < rows.n, any_nan = sm.any_nan[seg & 3];
-            const int tok = valid ? row / G : 0, head = at.h * G + (valid ? row - tok * G : 0);
+            const int tok = valid ? p.token(row) : 0, head = at.h * G + (valid ? row - tok * G : 0);
             float* slot = p.part + ((size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg + row) * (HD + 4);
             __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row + (int64_t)head * t.out_head;
             float* pile = reinterpret_cast<float*>(sm.q);        // free: every product with it is done
