@@ -26,9 +26,9 @@
 // The record's layout makes every operand a run of ldmatrix rows without bank
 // conflicts and P's accumulator layout the next product's operand.
 //
-// Measured: one row of 64 query heads over 8 (hd 128) at 65537 tokens 33 us, 4.1
+// Measured: one row of 64 query heads over 8 (hd 128) at 65537 tokens 31.5 us, 4.3
 // TB/s; 64 sequences of up to 16000 tokens, 32 heads over 8, 73 us, 5.2 TB/s; at
-// 4099 tokens 14 us.  Past about 10 us of launches, first loads and the merge the
+// 4099 tokens 12 us.  Past about 10 us of launches, first loads and the merge the
 // bytes bound it (6.6 TB/s between the two contexts above); under 4k tokens those
 // fixed steps are all of it.
 #include <algorithm>
@@ -492,8 +492,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 
 // Merge of the units that lie in several runs: CTA (x, y) takes the x-th such
 // unit and 16 / MW of its rows.  The MW warps of a row take every so many of its
-// segments, each with its own maximum, and meet in shared memory: 8 where there
-// are fewer units than segments of one, else 2.
+// segments, each with its own maximum, and meet in shared memory.  A row of few
+// units is up to 64 segments, 34 KB that one SM takes 0.5 us for: all 16 warps are
+// one row's while there are at most as many rows as SMs, 8 where there are fewer
+// units than segments of one, else 2.  Attention and merge in us with 16, 8 and 2:
+// one row at 64k tokens 31.5, 31.9, -; five rows (128 of a unit) at 128k 82.9, 80.1,
+// 80.9; a batch of 64 sequences 90.7, 80.5, 72.9.
 constexpr int kMergeThreads = 512;
 template <int HD, int MW>
 __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
@@ -606,6 +610,8 @@ cudaError_t launch_few(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p,
 template <int HD>
 cudaError_t launch_merge(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, int64_t units, cudaStream_t s) {
     const int x = (int)std::min<int64_t>(p.ctas, units), rows = p.tq * p.G;
+    if (units * rows <= kKv8Sms)
+        return launch_kv8(kv8_merge_kernel<HD, 16>, dim3(x, rows), kMergeThreads, 0, s, a, t, p);
     if (units * units < p.ctas)
         return launch_kv8(kv8_merge_kernel<HD, 8>, dim3(x, (rows + 1) / 2), kMergeThreads, 0, s, a, t, p);
     return launch_kv8(kv8_merge_kernel<HD, 2>, dim3(x, (rows + 7) / 8), kMergeThreads, 0, s, a, t, p);
