@@ -29,8 +29,8 @@
 // the reference lags behind it.
 //
 // Measured: 2001 rows of a prompt at 8150 tokens (64 query heads over 8, hd 128)
-// 670 us, 700 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 84 us, 3.2
-// TB/s; 24 sequences of 2 to 11 rows at up to 16000 tokens 142 us.  What bounds
+// 650 us, 720 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 80 us, 3.4
+// TB/s; 24 sequences of 2 to 11 rows at up to 16000 tokens 137 us.  What bounds
 // it is the round trip of a stream's tile, products to softmax and back, 5800
 // clocks of which the products are 1400 and the softmax 2600; the two streams
 // hide half of it.  Taking out the conversion, half of Q K^T and most of P V
