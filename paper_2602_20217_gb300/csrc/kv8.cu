@@ -10,10 +10,10 @@
 // power of two, which rounds only where a code becomes subnormal.
 //
 // Bytes bound both kernels where there are many rows: nine prompts of 40k tokens
-// in all (64 query heads over 8, hd 128), append 291 us and read 45 us, both 5.4
-// TB/s; one prompt of 4096 tokens (32 heads) 33 us for both.  Batches of few rows
+// in all (64 query heads over 8, hd 128), append 277 us, 5.6 TB/s, and read 46 us,
+// 5.3 TB/s; one prompt of 4096 tokens (32 heads) 31 us for both.  Batches of few rows
 // are a chain of four dependent loads (sequence, page, record and rows, angles):
-// 4 us for one token, 11 us a kernel for 96 sequences of 1 to 11 rows.
+// 4 us for one token, 10 us a kernel for 96 sequences of 1 to 11 rows.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -25,7 +25,7 @@ namespace ks {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kQHeads = 16;          // query heads of a CTA that rotates queries
+constexpr int kQHeads = 8;           // query heads of a CTA that rotates queries
 
 // Four codes times a power of two at most 1.
 KS_DEV uint32_t rescale4(uint32_t v, float f) {
@@ -270,15 +270,17 @@ KS_DEV void append_block(const Kv8Args& a, const Kv8RowArgs& r, const Kv8Slot& w
 // kQHeads query heads each.  HD / 16 threads share a head vector, each with eight
 // neighbouring dims of the first half and their partners of the second, so that
 // every access is 16 bytes and 128 contiguous ones a vector half.  Bound by bytes
-// in flight: a query thread loads four vectors (two of fp32) before it rotates
-// the first.
+// in flight: a query thread loads two vectors before it rotates the first.  Four
+// of bf16 and six CTAs an SM: nine prompts, append and read, 339 us instead of 329;
+// one and ten: 373.  16 heads a CTA instead of 8: 96 sequences of a few fp32 rows
+// 22.6 us instead of 20.5, 32 heads 28.7.
 //
 // A KV head's new rows go from registers, quantised, into a copy of the block's
 // record in shared memory, and from there out in 16-byte pieces.  A block that
 // goes on keeps its old tokens (their record is read while the new rows are);
 // the tokens behind the last one are zeros.
 template <int HD, typename T, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 6) kv8_append_kernel(const Kv8Args a, const Kv8RowArgs r) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 6) kv8_append_kernel(const Kv8Args a, const Kv8RowArgs r) {
     constexpr int TH = HD / 16, GROUPS = kThreads / TH;
     grid_dependency_wait();
     grid_launch_dependents();
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 6) kv8_append_kernel(const Kv8Args a
             const int tokens = w.last - w.first, ts = tokens > 8 ? 16 : tokens > 4 ? 8 : tokens > 2 ? 4 : tokens;
             const int t = w.first + (group & (ts - 1)), pos = w.blk * kKv8Block + t, step = GROUPS / ts;
             if (t >= w.last) continue;
-            constexpr int U = sizeof(T) == 2 ? 4 : 2;
+            constexpr int U = 2;
             const T* src = static_cast<const T*>(r.q) + (int64_t)(w.row + t) * r.q_row;
             __nv_bfloat16* out = r.q_out + (int64_t)(w.row + t) * r.q_out_row;
             const bool turn = r.rope != nullptr, past = turn && pos >= r.rope_rows;
@@ -376,8 +378,9 @@ __global__ void __launch_bounds__(kThreads) kv8_read_kernel(const Kv8Args a, T* 
 
 // Sequences along x, two CTAs for their blocks, where they have at most a block's
 // rows on average; else a slot a block (see Kv8Blocks).  96 sequences of 1 to 11
-// rows, append and read back: 22.6 us by sequence, 24.8 us by slots; one prompt of
-// 4096 rows would give all its blocks to two CTAs a head by sequence.
+// rows, append and read back, with 16 query heads a CTA: 22.6 us by sequence, 24.8
+// us by slots; one prompt of 4096 rows would give all its blocks to two CTAs a head
+// by sequence.
 dim3 block_grid(Kv8Args& a, int y) {
     a.by_seq = a.n_rows <= (int64_t)kKv8Block * a.n_seqs;
     return a.by_seq ? dim3(a.n_seqs, y, 2) : dim3(a.n_rows / kKv8Block + 2 * a.n_seqs, y);
