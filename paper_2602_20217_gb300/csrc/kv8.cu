@@ -104,13 +104,13 @@ KS_DEV void load_angles(const float* row, int j, float2 (&cs)[8]) {
     if constexpr (WIDE) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float4 v = __ldg(reinterpret_cast<const float4*>(p) + i);
+            const float4 v = reinterpret_cast<const float4*>(p)[i];
             cs[2 * i] = make_float2(v.x, v.y);
             cs[2 * i + 1] = make_float2(v.z, v.w);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) cs[i] = __ldg(p + i);
+        for (int i = 0; i < 8; ++i) cs[i] = p[i];
     }
 }
 KS_DEV void rotate8(const float2 (&cs)[8], float (&a)[8], float (&b)[8]) {

@@ -65,9 +65,9 @@ KS_DEV void kv8_flag(const Kv8Args& a, int code) {
 struct Kv8Seq {
     int row0, rows, len;
 };
-KS_DEV int kv8_row0(const Kv8Args& a, int s) { return min(max(__ldg(a.offsets + s), 0), a.n_rows); }
+KS_DEV int kv8_row0(const Kv8Args& a, int s) { return min(max(a.offsets[s], 0), a.n_rows); }
 KS_DEV Kv8Seq kv8_seq(const Kv8Args& a, int s) {
-    const int o0 = __ldg(a.offsets + s), o1 = __ldg(a.offsets + s + 1), n = __ldg(a.lengths + s);
+    const int o0 = a.offsets[s], o1 = a.offsets[s + 1], n = a.lengths[s];
     Kv8Seq q;
     q.row0 = min(max(o0, 0), a.n_rows);
     q.rows = min(max(o1, q.row0), a.n_rows) - q.row0;
@@ -75,7 +75,7 @@ KS_DEV Kv8Seq kv8_seq(const Kv8Args& a, int s) {
     return q;
 }
 KS_DEV bool kv8_seq_bad(const Kv8Args& a, int s) {
-    const int o0 = __ldg(a.offsets + s), o1 = __ldg(a.offsets + s + 1), n = __ldg(a.lengths + s);
+    const int o0 = a.offsets[s], o1 = a.offsets[s + 1], n = a.lengths[s];
     return o0 < 0 || o1 < o0 || o1 > a.n_rows || n < 0 || n > a.capacity;
 }
 
@@ -97,7 +97,7 @@ KS_DEV int kv8_find(int n_seqs, int x, F&& first) {
 // The record of block b of sequence s and head h, or null for a page that the
 // pool does not have.
 KS_DEV unsigned char* kv8_record_at(const Kv8Args& a, int s, int b, int h, int rec) {
-    const int page = __ldg(a.table + (size_t)s * a.table_ld + b / a.bpp);
+    const int page = a.table[(size_t)s * a.table_ld + b / a.bpp];
     if (page < 0 || page >= a.n_pages) return nullptr;
     return a.data + (((size_t)page * a.hk + h) * a.bpp + b % a.bpp) * rec;
 }
@@ -146,7 +146,9 @@ struct Kv8Blocks {
     }
 };
 
-// Programmatic launch: the kernel waits for what is before it by itself.
+// Programmatic launch: the kernel waits for what is before it by itself.  It may
+// be resident while its predecessor still writes, so nothing that a caller may
+// write is read by non-coherent loads.
 template <class K, class... Args>
 cudaError_t launch_kv8(K kern, dim3 grid, int threads, int smem, cudaStream_t s, const Args&... args) {
     cudaLaunchConfig_t cfg{};

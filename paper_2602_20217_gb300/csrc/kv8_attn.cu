@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
             const int b = tile * kBlocks + lane;
             const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
             if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
-            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + p.page_of(b, a.bpp));
+            const int page = a.table[(size_t)k.s * a.table_ld + p.page_of(b, a.bpp)];
             return page >= 0 && page < a.n_pages ? page : -2;
         };
         int it = 0, tile = at.tile, page = pages(at, tile);

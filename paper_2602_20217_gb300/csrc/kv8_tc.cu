@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int b = tile * kBlocks + lane;
             const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
             if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
-            const int page = __ldg(a.table + (size_t)k.s * a.table_ld + p.page_of(b, a.bpp));
+            const int page = a.table[(size_t)k.s * a.table_ld + p.page_of(b, a.bpp)];
             return page >= 0 && page < a.n_pages ? page : -2;
         };
         // a run of p.run records is one copy of keys and one of values
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int record = page >= 0 ? (page * a.hk + at.h) * a.bpp + b - p.page_of(b, a.bpp) * a.bpp : -1;
             // the scales come by ordinary loads, behind the first copies
             float2 scale = make_float2(0.f, 0.f);
-            if (record >= 0) scale = __ldg(reinterpret_cast<const float2*>(a.data + (size_t)record * REC + 2 * PART));
+            if (record >= 0) scale = *reinterpret_cast<const float2*>(a.data + (size_t)record * REC + 2 * PART);
             const unsigned have = __ballot_sync(0xffffffffu, record >= 0);
             float top = scale.y;                     // of the lane's tile
 #pragma unroll

@@ -322,3 +322,52 @@ def test_append_flags_offsets_in_batches_of_many_rows(offsets):
     d["cache"].read(d["batch"], out[0], out[1])
     torch.cuda.synchronize()
     assert int(d["status"]) & 2
+
+
+@pytest.mark.parametrize("rows", [1, 20])
+def test_calls_in_a_row_see_each_others_writes(rows):
+    """Steps of append and attention without a pause between launches give the bits of steps with one after each
+    call: scales that grow, rows written over, a workspace and query buffer used by every step, a layer after the
+    other."""
+    import torch
+    from paper_2602_20217_gb300 import kv8
+    hq, hk, hd, page, steps, layers = 8, 2, 128, 32, 40, 3
+    n_pages = (rows * steps + 200) // page + 1
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    x = torch.randn(steps, layers, rows, hq + 2 * hk, hd, generator=g, device="cuda")
+    x *= torch.exp2(torch.arange(steps, device="cuda") % 7 - 3.0)[:, None, None, None, None]
+    x = x.to(torch.bfloat16)
+    table = torch.tensor(angles(rows * steps + 200, hd), device="cuda")
+    pages = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)[None]
+    offsets = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def run(pause):
+        caches = [kv8.Cache8(n_pages, page, hk, hd, data=torch.zeros(kv8.Cache8(n_pages, page, hk, hd).nbytes,
+                                                                    dtype=torch.uint8, device="cuda"))
+                  for _ in range(layers)]
+        lengths = torch.full((1,), 100, dtype=torch.int32, device="cuda")
+        batch = kv8.Batch8(pages, offsets, lengths, rows, status)
+        work = caches[0].attention_workspace(hq, 1, rows)
+        q = torch.empty(rows, hq, hd, dtype=torch.bfloat16, device="cuda")
+        outs = torch.zeros(steps, layers, rows, hq, hd, dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        for s in range(steps):
+            lengths += rows if s % 3 else rows - rows // 2      # every third step writes over half of the last one
+            for i, c in enumerate(caches):
+                y = x[s, i]
+                c.append(batch, y[:, hq:hq + hk], y[:, hq + hk:], rope=table, q=y[:, :hq], q_out=q)
+                if pause:
+                    torch.cuda.synchronize()
+                c.attention(batch, q, out=outs[s, i], workspace=work)
+                if pause:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return outs, torch.stack([c.data for c in caches])
+
+    want = run(True)
+    for _ in range(3):
+        got = run(False)
+        assert torch.equal(got[0].view(torch.int16), want[0].view(torch.int16)) and torch.equal(got[1], want[1])
+    assert int(status) == 0
