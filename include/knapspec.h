@@ -520,7 +520,8 @@ ks_status ks_kv8_read(const ks_kv8_cache* cache, const ks_kv8_batch* batch, void
  * query head h reads KV head h / (n_q_heads / n_kv_heads), at most 64 query
  * heads a KV head.  q, out: bf16, strides in elements.  lse (dev float
  * [n_rows][n_q_heads], or NULL): the logarithm of the sum of exponentials.  A
- * row that sees no token gives zeros and lse -inf.  A NaN key makes the rows
+ * row that sees no token gives zeros and lse -inf.  A weight below 2^-30 of the
+ * row's largest may count as zero in out.  A NaN key makes the rows
  * that see it NaN, a NaN value that dim of them; unseen ones do nothing.
  * workspace: dev, 256-byte aligned, ks_kv8_attention_workspace() bytes for
  * the call's n_seqs and n_rows or more; its contents matter to no later call,

@@ -20,13 +20,14 @@
 // keys, values and scales go to three places, keys and values of a tile
 // contiguous, which is the layout that the descriptors without a swizzle take.
 //
-// The weights are 2^(x - m + 10) with a reference m that is the maximum seen when
+// The weights are 2^(x - m + 7) with a reference m that is the maximum seen when
 // it was set, rounded up to a whole number, not the running one: a row's m is
 // raised (and its l, O and the weights of the tile so far multiplied down by a
 // power of two, without rounding) only when its weights of 32 keys add up to
 // more than 2^15.5.  So most tiles need no maximum at all, no weight passes f16,
-// and weights count down to f16's 2^-24: 2^-34 of the largest, or 2^-39 where
-// the reference lags behind it.
+// and weights count down to f16's 2^-24, at least 2^-30 of the largest (2^-39
+// where the reference lags behind it): what 128k keys below that add up to is
+// under 2^-13 of the row, a sixteenth of the output's rounding.
 //
 // Measured: 2001 rows of a prompt at 8150 tokens (64 query heads over 8, hd 128)
 // 650 us, 720 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 80 us, 3.4
