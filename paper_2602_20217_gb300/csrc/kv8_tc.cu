@@ -111,6 +111,23 @@ KS_DEV float2 add2(float2 a, float2 b) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
 }
+// Whether three phases have ended, without waiting: a look takes a hundred clocks, the three overlap.
+KS_DEV void mbar_look(const uint64_t* a, int pa, const uint64_t* b, int pb, const uint64_t* c, int pc, bool& ra, bool& rb,
+                      bool& rc) {
+    uint32_t x, y, z;
+    asm volatile(
+        "{ .reg .pred p, q, r;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%3], %4;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 q, [%5], %6;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 r, [%7], %8;\n"
+        "selp.u32 %0, 1, 0, p;\nselp.u32 %1, 1, 0, q;\nselp.u32 %2, 1, 0, r; }"
+        : "=r"(x), "=r"(y), "=r"(z)
+        : "r"(smem_u32(a)), "r"(pa), "r"(smem_u32(b)), "r"(pb), "r"(smem_u32(c)), "r"(pc)
+        : "memory");
+    ra = x;
+    rb = y;
+    rc = z;
+}
 KS_DEV void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // v[i] of a register array, for an i that is not known when compiling
 KS_DEV float pick(const float (&v)[kBlocks], int i) {
@@ -273,9 +290,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             do {
                 const int cnt = at.end - at.tile;
                 ok = mbar_wait(&sm.q_full, seg & 1, kWaitLimitNs);
-                auto scores = [&](int j) {
+                auto scores = [&](int j, bool here) {
                     const int st = (it0 + j) % kRing;
-                    ok = ok && mbar_wait(&sm.k_full[st], ((it0 + j) / kRing) & 1, kWaitLimitNs);
+                    ok = ok && (here || mbar_wait(&sm.k_full[st], ((it0 + j) / kRing) & 1, kWaitLimitNs));
                     if (!ok) return;
                     umma_fence_after();
                     // hi, then lo; a step of 256 bytes is 16 in a descriptor
@@ -288,13 +305,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     umma_commit(&sm.k_free[st]);
                     umma_commit(&sm.s_full[j & 1]);
                 };
-                scores(0);
-                if (cnt > 1) scores(1);
+                scores(0, false);
+                if (cnt > 1) scores(1, false);
                 if (seg > 0) ok = ok && mbar_wait(&sm.o_free, (seg - 1) & 1, kWaitLimitNs);
                 for (int j = 0; j < cnt && ok; ++j) {
                     const int i = j & 1, b = (it0 + j) & 1;
-                    ok = mbar_wait(&sm.p_full[i], n[i] & 1, kWaitLimitNs) &&
-                         mbar_wait(&sm.v16_full[b], ((it0 + j) >> 1) & 1, kWaitLimitNs);
+                    const int next = it0 + j + 2;
+                    bool weights, values, keys;
+                    mbar_look(&sm.p_full[i], n[i] & 1, &sm.v16_full[b], ((it0 + j) >> 1) & 1, &sm.k_full[next % kRing],
+                              (next / kRing) & 1, weights, values, keys);
+                    ok = (values || mbar_wait(&sm.v16_full[b], ((it0 + j) >> 1) & 1, kWaitLimitNs)) &&
+                         (weights || mbar_wait(&sm.p_full[i], n[i] & 1, kWaitLimitNs));
                     if (!ok) break;
                     ++n[i];
                     umma_fence_after();
@@ -305,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     umma_commit(&sm.v16_free[b]);
                     umma_commit(&sm.o_full[i]);
                     mbar_arrive(&sm.o_full[i]);
-                    if (j + 2 < cnt) scores(j + 2);
+                    if (j + 2 < cnt) scores(j + 2, keys);
                 }
                 it0 += cnt;
                 ++seg;
