@@ -302,7 +302,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const int k = c % (HD / 32);
                         umma_e4m3(tmem + 128 * (j & 1), q0 + (c / (HD / 32) * (kRows * HD / 16) + 16 * k), k0 + 16 * k, kIdS, c > 0);
                     }
-                    umma_commit(&sm.k_free[st]);
                     umma_commit(&sm.s_full[j & 1]);
                 };
                 scores(0, false);
@@ -537,6 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool special = edge || fresh || vnew != vref;
                 alive = alive && mbar_wait(&sm.s_full[i], n & 1, kWaitLimitNs);
                 __syncwarp();
+                if (quad == 0 && lane == 0) mbar_arrive(&sm.k_free[(it0 + j) % kRing]);      // spares the issuing thread a commit
                 umma_fence_after();
                 if (32 * (quad % per) >= rows.n) {   // no row: P stays what it is, in lanes that nobody reads
                     if (lane == 0) mbar_arrive(&sm.p_full[i]);
