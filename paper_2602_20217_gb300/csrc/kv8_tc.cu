@@ -12,10 +12,10 @@
 // padding the rows up to 128 costs nothing that bytes do not; with all 128 rows
 // in use the tensor pipe has 1024 clocks of work and the softmax about as many.
 //
-// Warps 0..3 and 4..7 are two softmax streams, a thread per row each: even tiles
-// of a segment and odd ones, with a maximum, a sum and an accumulator each
-// (TMEM: S0 S1 O0 O1, P in the first half of its S), joined at the segment's
-// end, so that one stream's softmax runs under the other's products.  Warps 8
+// Warps 0..3 and 4..7 are two softmax streams, a thread per row each: the CTA's
+// even tiles and the odd ones, with a maximum, a sum and an accumulator each
+// (TMEM: S0 S1 O0 O1, P in the first half of its S), joined at a segment's end,
+// so that one stream's softmax runs under the other's products.  Warps 8
 // to 11 convert V, warp 12 issues the products, warp 13 the copies: a record's
 // keys, values and scales go to three places, keys and values of a tile
 // contiguous, which is the layout that the descriptors without a swizzle take.
@@ -78,7 +78,7 @@ struct Smem {
     int nan_from[4][HD];                        // first key whose value is NaN, a segment each
     int any_nan[4];
     int present[kNear];
-    uint64_t scales[kNear], k_full[kRing], k_free[kRing], v_full[kRing], v_free[kRing], v16_full[2], v16_free[2];
+    uint64_t scales[kNear], k_full[kRing], k_free[kRing], v_full[kRing], v_free[kRing], v16_full[2];
     uint64_t q_full, s_full[2], p_full[2], o_full[2], o_free;
     uint32_t tmem;
 };
@@ -177,7 +177,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm.v16_full[i], kConvertWarps / 2);
-            mbar_init(&sm.v16_free[i], 1);
             mbar_init(&sm.s_full[i], 1);
             mbar_init(&sm.p_full[i], 4);
             mbar_init(&sm.o_full[i], 2);        // the products' commit, and an arrival that orders nan_from before it
@@ -291,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int cnt = at.end - at.tile;
                 ok = mbar_wait(&sm.q_full, seg & 1, kWaitLimitNs);
                 auto scores = [&](int j, bool here) {
-                    const int st = (it0 + j) % kRing;
+                    const int st = (it0 + j) % kRing, i = (it0 + j) & 1;
                     ok = ok && (here || mbar_wait(&sm.k_full[st], ((it0 + j) / kRing) & 1, kWaitLimitNs));
                     if (!ok) return;
                     umma_fence_after();
@@ -300,29 +299,28 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int c = 0; c < HD / 16; ++c) {
                         const int k = c % (HD / 32);
-                        umma_e4m3(tmem + 128 * (j & 1), q0 + (c / (HD / 32) * (kRows * HD / 16) + 16 * k), k0 + 16 * k, kIdS, c > 0);
+                        umma_e4m3(tmem + 128 * i, q0 + (c / (HD / 32) * (kRows * HD / 16) + 16 * k), k0 + 16 * k, kIdS, c > 0);
                     }
-                    umma_commit(&sm.s_full[j & 1]);
+                    umma_commit(&sm.s_full[i]);
                 };
                 scores(0, false);
                 if (cnt > 1) scores(1, false);
                 if (seg > 0) ok = ok && mbar_wait(&sm.o_free, (seg - 1) & 1, kWaitLimitNs);
                 for (int j = 0; j < cnt && ok; ++j) {
-                    const int i = j & 1, b = (it0 + j) & 1;
+                    const int i = (it0 + j) & 1;
                     const int next = it0 + j + 2;
                     bool weights, values, keys;
-                    mbar_look(&sm.p_full[i], n[i] & 1, &sm.v16_full[b], ((it0 + j) >> 1) & 1, &sm.k_full[next % kRing],
+                    mbar_look(&sm.p_full[i], n[i] & 1, &sm.v16_full[i], ((it0 + j) >> 1) & 1, &sm.k_full[next % kRing],
                               (next / kRing) & 1, weights, values, keys);
-                    ok = (values || mbar_wait(&sm.v16_full[b], ((it0 + j) >> 1) & 1, kWaitLimitNs)) &&
+                    ok = (values || mbar_wait(&sm.v16_full[i], ((it0 + j) >> 1) & 1, kWaitLimitNs)) &&
                          (weights || mbar_wait(&sm.p_full[i], n[i] & 1, kWaitLimitNs));
                     if (!ok) break;
                     ++n[i];
                     umma_fence_after();
-                    const uint64_t v0 = desc_plain(smem_u32(sm.v16[b]), 16 * HD, 128);
+                    const uint64_t v0 = desc_plain(smem_u32(sm.v16[i]), 16 * HD, 128);
 #pragma unroll
                     for (int c = 0; c < kTile / 16; ++c)
                         umma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 8 * c, v0 + 2 * HD * c, kIdO, j > 1 || c > 0);
-                    umma_commit(&sm.v16_free[b]);
                     umma_commit(&sm.o_full[i]);
                     mbar_arrive(&sm.o_full[i]);
                     if (j + 2 < cnt) scores(j + 2, keys);
@@ -343,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Rows rows(at.q, p.tq, at.g, G);
             for (int tile = at.tile; tile < at.end; ++tile, ++it) {
                 const int st = it % kRing, b = it & 1, near = it % kNear;
-                if (b == mine) alive = alive && mbar_wait(&sm.v16_free[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
+                if (b == mine) alive = alive && mbar_wait(&sm.o_full[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
                 if (tile == at.tile) {
                     // Clear the next segment's marks.  The products of the tile two before are done, so those of
                     // the segment two back have begun and the readers of the one three back, who had this
@@ -521,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tmem_wait_st();
             };
-            for (int j = i; j < cnt; j += 2, ++n) {
+            for (int j = (it0 ^ i) & 1; j < cnt; j += 2, ++n) {
                 const int tile = at.tile + j, near = (it0 + j) % kNear;
                 alive = alive && mbar_wait(&sm.scales[near], ((it0 + j) / kNear) & 1, kWaitLimitNs);
                 // read before the scores are there: shared memory is the products' while they run, and a load
@@ -643,7 +641,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) mbar_arrive(&sm.p_full[i]);
             }
             // ---------------------------------------------- segment's end
-            const bool mine = cnt > i;               // this stream had a tile
+            const bool mine = cnt > ((it0 ^ i) & 1);                     // this stream had a tile
+            const bool has0 = cnt > 1 || !(it0 & 1), has1 = cnt > 1 || (it0 & 1);
             if (mine) alive = alive && mbar_wait(&sm.o_full[i], (n - 1) & 1, kWaitLimitNs);
             sm.join[i][lane_row] = make_float4(m, l, vref, 0.f);
             umma_fence_before();
@@ -679,8 +678,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_pin(y);
 #pragma unroll
                 for (int q = 0; q < 32; ++q) {
-                    float v = __uint_as_float(x[q]) * o0;
-                    if (cnt > 1) v = fmaf(__uint_as_float(y[q]), o1, v);
+                    float v = has0 ? __uint_as_float(x[q]) * o0 : 0.f;   // a stream without a tile has no O
+                    if (has1) v = fmaf(__uint_as_float(y[q]), o1, v);
                     x[q] = __float_as_uint(v);
                 }
                 // add the copies, half of them at a time: 32 x 32 values a warp
