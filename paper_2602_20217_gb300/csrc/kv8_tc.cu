@@ -626,13 +626,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_st16(s_at + 16 * c, pk);    // over scores that are used
                     ++c;
                 }
-                if (copies > 1) {
-                    uint32_t zero[16];
+                if (copies > 1) {                    // zeros for the other chunks: one pair, and half of the own one
+                    uint32_t zero[32], half[16];
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) zero[q] = 0;
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c)
-                        if (c < c0 || c >= c1) tmem_st16(s_at + 16 * c, zero);
+                    for (int q = 0; q < 32; ++q) zero[q] = half[q / 2] = 0;
+                    tmem_st32(s_at + 32 * (c0 < 2), zero);
+                    if (per == 1) tmem_st16(s_at + 16 * (c0 ^ 1), half);
                 }
                 first = false;
                 tmem_wait_st();
