@@ -575,56 +575,71 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (m == -INFINITY) m = ceilf(top);          // l and O are still zero
                     }
                 }
-                // 32 scores at a time, in a loop that stays one: unrolled, the roles' code together no longer fits
-                // the instruction cache, and a tile of the softmax takes up to 6700 clocks.
+                // 32 scores at a time, in a short loop: unrolled, or with what is rare in it, the roles' code together
+                // no longer fits the instruction cache, and a tile of the softmax takes up to 6700 clocks.
+                for (int c = c0;;) {
+                    bool raise = false;
 #pragma unroll 1
-                for (int c = c0; c < c1;) {
-                    uint32_t s[32], pk[16];
+                    for (; c < c1; ++c) {
+                        uint32_t s[32], pk[16];
+                        tmem_ld32(s, s_at + 32 * c);
+                        const float f0 = pick(f, 2 * c), f1 = pick(f, 2 * c + 1);
+                        const float ref = (m == -INFINITY ? 0.f : m) - kUp;
+                        tmem_wait_ld();
+                        tmem_pin(s);
+                        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                        for (int q = 0; q < 32; q += 2) {
+                            const float fq = q < 16 ? f0 : f1;
+                            const float2 x = fma2(make_float2(__uint_as_float(s[q]), __uint_as_float(s[q + 1])),
+                                                  make_float2(fq, fq), make_float2(-ref, -ref));
+                            const float2 y = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                            part[q / 2 & 1] = add2(part[q / 2 & 1], y);
+                            pk[q / 2] = f16_pack(y.x, y.y);
+                        }
+                        part[0] = add2(part[0], part[1]);
+                        const float sum = part[0].x + part[0].y;
+                        raise = sum > kMost;         // else no weight passes f16; just raised, it is at most 2^12
+                        if (__any_sync(0xffffffffu, raise)) break;
+                        l += sum;
+                        tmem_st16(s_at + 16 * c, pk);                    // over scores that are used
+                    }
+                    if (c >= c1) break;
+                    // only this row's own reference moves, to a whole number: the factor is exact
+                    uint32_t s[32];
                     tmem_ld32(s, s_at + 32 * c);
                     const float f0 = pick(f, 2 * c), f1 = pick(f, 2 * c + 1);
-                    const float ref = (m == -INFINITY ? 0.f : m) - kUp;
                     tmem_wait_ld();
                     tmem_pin(s);
-                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    float top = m;
 #pragma unroll
-                    for (int q = 0; q < 32; q += 2) {
-                        const float fq = q < 16 ? f0 : f1;
-                        const float2 x = fma2(make_float2(__uint_as_float(s[q]), __uint_as_float(s[q + 1])),
-                                              make_float2(fq, fq), make_float2(-ref, -ref));
-                        const float2 y = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-                        part[q / 2 & 1] = add2(part[q / 2 & 1], y);
-                        pk[q / 2] = f16_pack(y.x, y.y);
-                    }
-                    part[0] = add2(part[0], part[1]);
-                    const float sum = part[0].x + part[0].y;
-                    const bool raise = sum > kMost;              // else no weight passes f16; just raised, it is at most 2^12
-                    if (__any_sync(0xffffffffu, raise)) {
-                        float top = m;
-#pragma unroll
-                        for (int q = 0; q < 32; ++q) top = fmaxf(top, __uint_as_float(s[q]) * (q < 16 ? f0 : f1));
-                        // only this row's own reference moves, to a whole number: the factor is exact
-                        const float mnew = raise ? fmaxf(m, ceilf(top)) : m;
-                        const float fac = m == mnew ? 1.f : pow2_below(m - mnew);
-                        l *= fac;
-                        m = mnew;
-                        if (!first) rescale(fac);
-                        scale_weights(s_at + 16 * c0, c - c0, fac);      // of this tile so far
-                        continue;
-                    }
-                    l += sum;
-                    if (vnow < 0.f) {                // a quiet block
-                        const float vinv = inverse_pow2(vref);
+                    for (int q = 0; q < 32; ++q) top = fmaxf(top, __uint_as_float(s[q]) * (q < 16 ? f0 : f1));
+                    const float mnew = raise ? fmaxf(m, ceilf(top)) : m;
+                    const float fac = m == mnew ? 1.f : pow2_below(m - mnew);
+                    l *= fac;
+                    m = mnew;
+                    if (!first) rescale(fac);
+                    scale_weights(s_at + 16 * c0, c - c0, fac);          // of this tile so far
+                }
+                if (vnow < 0.f) {                    // a quiet block
+                    const float vinv = inverse_pow2(vref);
+#pragma unroll 1
+                    for (int c = c0; c < c1; ++c) {
+                        uint32_t x[16];
+                        tmem_wait_st();
+                        tmem_ld16(x, s_at + 16 * c);
+                        tmem_wait_ld();
+                        tmem_pin(x);
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int b = 2 * c + e;
                             const float y = have >> b & 1 ? sm.scale[near][b].y * vinv : 1.f;
                             const __half2 w = __float2half2_rn(fminf(y * (1.f / kQuiet), 1.f));
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) pk[8 * e + q] = f16_times(pk[8 * e + q], w);
+                            for (int q = 0; q < 8; ++q) x[8 * e + q] = f16_times(x[8 * e + q], w);
                         }
+                        tmem_st16(s_at + 16 * c, x);
                     }
-                    tmem_st16(s_at + 16 * c, pk);    // over scores that are used
-                    ++c;
                 }
                 if (copies > 1) {                    // zeros for the other chunks: one pair, and half of the own one
                     uint32_t zero[32], half[16];
