@@ -371,53 +371,54 @@ __global__ void __launch_bounds__(kThreads, 1)
                     *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 };
                 constexpr int STEP = 16 * kConvertWarps, N = kBlocks * HD / STEP, PER = HD / STEP;   // passes a record
-                if (!edge) {
-                    // the next loads first: they wait behind the products' reads of shared memory
-                    constexpr int AHEAD = 4;
-                    uint4 x[AHEAD], next[AHEAD];
-                    auto load = [&](int c) {
+                // the next loads first: they wait behind the products' reads of shared memory
+                constexpr int AHEAD = 4;
+                uint4 x[AHEAD], next[AHEAD];
+                auto load = [&](int c) {
 #pragma unroll
-                        for (int i = 0; i < AHEAD; ++i)
-                            next[i] = *reinterpret_cast<const uint4*>(src + ((c + i) * STEP + ct) * 16);
-                    };
-                    load(0);
+                    for (int i = 0; i < AHEAD; ++i)
+                        next[i] = *reinterpret_cast<const uint4*>(src + ((c + i) * STEP + ct) * 16);
+                };
+                load(0);
 #pragma unroll 1
-                    for (int c = 0; c < N; c += AHEAD) {
+                for (int c = 0; c < N; c += AHEAD) {
+                    __half2 f[AHEAD];
 #pragma unroll
-                        for (int i = 0; i < AHEAD; ++i) x[i] = next[i];
-                        if (c + AHEAD < N) load(c + AHEAD);
-#pragma unroll
-                        for (int i = 0; i < AHEAD; ++i)
-                            convert((c + i) / PER, (i % PER) * STEP + ct, x[i], sm.factor[near][(c + i) / PER]);
+                    for (int i = 0; i < AHEAD; ++i) {
+                        x[i] = next[i];
+                        f[i] = sm.factor[near][(c + i) / PER];
                     }
-                } else {
-#pragma unroll 1
-                    for (int i = ct; i < kBlocks * HD; i += STEP) {
-                        const int r = i / HD, d = i % HD;
-                        // a NaN that not every row sees would pass through a weight of zero: it is taken out, and
-                        // the rows that do see it get their NaN at the end
-                        uint4 x = *reinterpret_cast<const uint4*>(src + i * 16);
-                        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    if (c + AHEAD < N) load(c + AHEAD);
+                    if (edge) {
+                        // absent records are zeros; a NaN that not every row sees would pass through a weight of
+                        // zero: it is taken out, and the rows that do see it get their NaN at the end
+                        uint32_t any = 0;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (!(have >> r & 1)) w[j] = 0;
-                            const uint32_t nan = ((w[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-                            if (nan) {
-                                sm.any_nan[seg & 3] = 1;
-                                for (int c = 0; c < 4; ++c)
-                                    if (nan >> (8 * c + 7) & 1)
-                                        atomicMin(&sm.nan_from[seg & 3][d],
-                                                  tile * kTile + 16 * r + 2 * j + (c & 1) + 8 * (c >> 1));
+                        for (int i = 0; i < AHEAD; ++i) {
+                            const bool here = have >> (c + i) / PER & 1;
+                            uint32_t* w = reinterpret_cast<uint32_t*>(&x[i]);
+                            if (!here) f[i] = __half2(0.f, 0.f);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (!here) w[j] = 0;
+                                const uint32_t nan = ((w[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                                any |= nan;
                                 w[j] &= ~((nan >> 7) * 0xffu);
                             }
                         }
-                        if (have >> r & 1) {
-                            convert(r, d, make_uint4(w[0], w[1], w[2], w[3]), sm.factor[near][r]);
-                        } else {
-                            *reinterpret_cast<uint4*>(dst + (2 * r * HD + d) * 16) = make_uint4(0, 0, 0, 0);
-                            *reinterpret_cast<uint4*>(dst + ((2 * r + 1) * HD + d) * 16) = make_uint4(0, 0, 0, 0);
+                        if (any) {
+                            sm.any_nan[seg & 3] = 1;
+#pragma unroll 1
+                            for (int k = 0; k < 16 * AHEAD; ++k) {           // bytes: tokens in the records' order
+                                const int at = (c + k / 16) * STEP + ct, r = at / HD, byte = k & 15;
+                                if ((have >> r & 1) && (src[at * 16 + byte] & 0x7f) == 0x7f)
+                                    atomicMin(&sm.nan_from[seg & 3][at % HD], tile * kTile + 16 * r + 2 * (byte >> 2) +
+                                                                                  (byte & 1) + 8 * (byte >> 1 & 1));
+                            }
                         }
                     }
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i) convert((c + i) / PER, (i % PER) * STEP + ct, x[i], f[i]);
                 }
                 fence_async_smem();
                 __syncwarp();
