@@ -30,14 +30,16 @@
 // under 2^-13 of the row, a sixteenth of the output's rounding.
 //
 // Measured: 2001 rows of a prompt at 8150 tokens (64 query heads over 8, hd 128)
-// 650 us, 720 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 80 us, 3.4
-// TB/s; 24 sequences of 2 to 11 rows at up to 16000 tokens 137 us.  What bounds
-// it is the round trip of a stream's tile, products to softmax and back, 5800
-// clocks of which the products are 1400 and the softmax 2600; the two streams
-// hide half of it.  Taking out the conversion, half of Q K^T and most of P V
-// together saves 15 %, all but a quarter of the weights 22 % more.  A third
-// stream has no TMEM (S and O of two fill it).  Other arrangements of two were
-// slower: tiles of 64 keys, two threads a row on one tile, the two products
+// 582 us, 805 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 75 us, 3.6
+// TB/s; 24 sequences of 2 to 11 rows at up to 16000 tokens 123 us.  What bounds
+// it is the round trip of a stream's tile, products to softmax and back, about
+// 5000 clocks of which the two products are 1350 and the softmax 2200; the two
+// streams hide half.  Taking out the conversion, half of Q K^T and most of P V
+// together saves 19 % of the prompt, three quarters of the weights another 26 %.
+// All roles share the instruction cache: code in the loops that seldom runs cost
+// more than anything it did (raises and quiet blocks in the softmax loop 6 %).  A
+// third stream has no TMEM (S and O of two fill it).  Other arrangements of two
+// were slower: tiles of 64 keys, two threads a row on one tile, the two products
 // issued by two warps, 64 scores at a time or 16.
 #include "kv8_plan.cuh"
 #include "umma.cuh"
