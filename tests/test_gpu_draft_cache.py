@@ -224,3 +224,30 @@ def test_refusals():
     with pytest.raises(ks.KsError):
         tiny.draft_cache()
     tiny.close()
+
+
+@pytest.mark.parametrize("kind", ["tpt", "dp"])
+def test_target_output_under_the_selection_stages(kind):
+    """The selection stages run between drafts; the DP one writes over the history's rows and puts them back."""
+    from paper_2602_20217_gb300 import knapspec as ks
+    m = _model(_shape(L=4), 300)
+    want = m.decode_greedy(40)
+    m.rewind()
+    args = {"tpt": dict(latency=ks.latency(0, 0.279, 0.735e-4, 0.279), resolve_every=2, tpt=(4, 5)),
+            "dp": dict(latency=ks.latency(1, units=[2, 1] * 4), resolve_every=2, dp=(5, 0.5, 16, 8))}[kind]
+    out, stats, _ = m.generate(40, 4, **args)
+    assert np.array_equal(np.asarray(out)[:40], want)
+    m.close()
+
+
+def test_sampled_jobs_repeat():
+    """The same seed gives the same sampled tokens again; drafts are taken from the copy."""
+    from paper_2602_20217_gb300 import knapspec as ks
+    m = _model(_shape(), 100)
+    samp = ks.sampling(0.7, 50, 0.95, seed=9)
+    first, _, _ = m.generate(40, 4, mask=np.ones(4, np.uint8), sampling=samp)
+    m.rewind()
+    again, _, _ = m.generate(40, 4, mask=np.ones(4, np.uint8), sampling=samp)
+    assert np.array_equal(first, again)
+    assert first.min() >= 0 and first.max() < 2000
+    m.close()
