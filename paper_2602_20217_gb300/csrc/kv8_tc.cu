@@ -55,6 +55,7 @@ constexpr int kRing = 3;            // tiles of keys, and of values
 constexpr int kNear = 8;            // tiles whose scales are kept
 constexpr float kUp = 7.f, kMost = 46340.f;
 constexpr float kQuiet = 1.f / 16384.f;
+constexpr float kFar = 4194304.f;   // 2^22
 
 // Values' scales are taken relative to vref, which follows the tiles of a
 // segment in order: four times the loudest block seen, raised when one passes
@@ -156,6 +157,11 @@ KS_DEV void scale_weights(uint32_t at, int n, float f) {
         tmem_st16(at + 16 * c, x);
     }
 }
+// Whether the weights of a row with this reference need products that are rounded
+// before the reference is taken off.  s f - (m - 7) in one rounding keeps the whole
+// product, and m came from rounded ones: that differs by half a unit in the last
+// place of the product, 16 at scores of 2^28, and m - 7 is m from there on.
+KS_DEV bool far(float m) { return fabsf(m) >= kFar && m != -INFINITY; }
 KS_DEV void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 KS_DEV void convert_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 
@@ -580,7 +586,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 // 32 scores at a time, in a short loop: unrolled, or with what is rare in it, the roles' code together
                 // no longer fits the instruction cache, and a tile of the softmax takes up to 6700 clocks.
-                for (int c = c0;;) {
+                for (int c = c0; c < c1; ++c) {
+                    // no sum of weights is below zero: a row of far scores leaves the loop at every chunk
+                    const float most = far(m) ? -1.f : kMost;
                     bool raise = false;
 #pragma unroll 1
                     for (; c < c1; ++c) {
@@ -602,27 +610,59 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         part[0] = add2(part[0], part[1]);
                         const float sum = part[0].x + part[0].y;
-                        raise = sum > kMost;         // else no weight passes f16; just raised, it is at most 2^12
+                        raise = sum > most;          // else no weight passes f16
                         if (__any_sync(0xffffffffu, raise)) break;
                         l += sum;
                         tmem_st16(s_at + 16 * c, pk);                    // over scores that are used
                     }
                     if (c >= c1) break;
-                    // only this row's own reference moves, to a whole number: the factor is exact
-                    uint32_t s[32];
-                    tmem_ld32(s, s_at + 32 * c);
-                    const float f0 = pick(f, 2 * c), f1 = pick(f, 2 * c + 1);
-                    tmem_wait_ld();
-                    tmem_pin(s);
+                    // A chunk in which a row is raised is done here, whatever comes of it: one visit a chunk.  Only that
+                    // row's own reference moves, to a whole number: the factor is exact.  A product below 2^22 rounds by a
+                    // quarter at most, so no weight of the row is above 2^(kUp + 1/4) then; those of far scores (see far())
+                    // come from rounded products, as the reference did, and are at most 2^kUp.  A block at a time keeps
+                    // this short: 32 scores in one go take the batch of verify passes from 127 to 130 us.
                     float top = m;
+#pragma unroll 1
+                    for (int b = 2 * c; b < 2 * c + 2; ++b) {
+                        uint32_t s[16];
+                        tmem_ld16(s, s_at + 16 * b);
+                        const float fq = pick(f, b);
+                        tmem_wait_ld();
+                        tmem_pin(s);
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) top = fmaxf(top, __uint_as_float(s[q]) * (q < 16 ? f0 : f1));
+                        for (int q = 0; q < 16; ++q) top = fmaxf(top, __uint_as_float(s[q]) * fq);
+                    }
                     const float mnew = raise ? fmaxf(m, ceilf(top)) : m;
                     const float fac = m == mnew ? 1.f : pow2_below(m - mnew);
                     l *= fac;
                     m = mnew;
                     if (!first) rescale(fac);
                     scale_weights(s_at + 16 * c0, c - c0, fac);          // of this tile so far
+                    const float base = m == -INFINITY ? 0.f : m, ref = base - kUp;
+                    const bool apart = far(m);
+                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+                    for (int b = 2 * c; b < 2 * c + 2; ++b) {
+                        uint32_t s[16], pk[8];
+                        tmem_ld16(s, s_at + 16 * b);
+                        const float fq = pick(f, b);
+                        tmem_wait_ld();
+                        tmem_pin(s);
+#pragma unroll
+                        for (int q = 0; q < 16; q += 2) {
+                            const float s0 = __uint_as_float(s[q]), s1 = __uint_as_float(s[q + 1]);
+                            float2 x = fma2(make_float2(s0, s1), make_float2(fq, fq), make_float2(-ref, -ref));
+                            if (apart)
+                                x = make_float2(__fsub_rn(__fmul_rn(s0, fq), base) + kUp,
+                                                __fsub_rn(__fmul_rn(s1, fq), base) + kUp);
+                            const float2 y = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                            part[q / 2 & 1] = add2(part[q / 2 & 1], y);
+                            pk[q / 2] = f16_pack(y.x, y.y);
+                        }
+                        tmem_st8(s_at + 8 * b, pk);
+                    }
+                    part[0] = add2(part[0], part[1]);                    // as in the loop: a row's sum is its own affair
+                    l += part[0].x + part[0].y;
                 }
                 if (vnow < 0.f) {                    // a quiet block
                     const float vinv = inverse_pow2(vref);
