@@ -467,8 +467,9 @@ typedef struct {
  * (never cleared by a call), bit 0: a page outside the pool (its tokens are not
  * written, read as zeros, and unseen by the attention); bit 1: offsets that
  * decrease or pass n_rows, or a length below 0 or above the pages (taken as the
- * nearest possible value); bit 2: a token before position 0 or past the RoPE
- * table (not appended, or stored as zeros); bit 3: a bounded wait gave up.
+ * nearest possible value; where offsets decrease the attention writes nothing);
+ * bit 2: a token before position 0 or past the RoPE table (not appended, or
+ * stored as zeros); bit 3: a bounded wait gave up.
  * No two blocks that a call appends to may be one (of two sequences, or of one
  * whose table names a page twice); reading and attending may share pages. */
 #define KS_KV8_BAD_PAGE 1

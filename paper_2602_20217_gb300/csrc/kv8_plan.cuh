@@ -104,7 +104,9 @@ struct Segment {
 };
 
 // This CTA's run and its first segment; false if it has none.  Every warp finds
-// it by itself, 32 sequences at a time.
+// it by itself, 32 sequences at a time.  Where offsets decrease, no CTA has one:
+// sequences that share rows could be more units than the host counted, and their
+// line longer than an int.
 KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     Kv8Seq mine{};
@@ -120,11 +122,14 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
         return a.hk * head;
     };
     int total = 0, v = 0;
+    bool falls = false;
     for (int c = 0; c < a.n_seqs; c += 32) {
         v = load(c);
         if (cta == 0 && c + lane < a.n_seqs && kv8_seq_bad(a, c + lane)) kv8_flag(a, kKv8BadBatch);
+        falls = falls || (c + lane < a.n_seqs && a.offsets[c + lane + 1] < a.offsets[c + lane]);
         total += __reduce_add_sync(0xffffffffu, v);
     }
+    if (__any_sync(0xffffffffu, falls)) return false;
     r.cut(total, p.ctas, cta);
     if (cta >= r.ctas) return false;
     int start = 0, len = 0;                      // of the sequence's units on the line; a head's length
