@@ -10,7 +10,9 @@ library's CUDA kernels.
 
 A Batch8 holds addresses, so it serves every layer of a step and, as the
 kernels read the arrays themselves, every later step that updates them in
-place.  Calls go to torch's current stream unless one is given.
+place.  Calls go to torch's current stream unless one is given; what attention()
+allocates by itself then belongs to that stream, as it does under
+torch.cuda.stream().
 """
 from __future__ import annotations
 
@@ -80,6 +82,8 @@ class Cache8:
         index = _cuda.current_device()
         if self.device.index != index:
             raise ValueError(f"the cache is on {self.device}, not on the current device")
+        if isinstance(stream, _cuda.Stream) and stream.device != self.device:
+            raise ValueError(f"the cache is on {self.device}, the stream on {stream.device}")
         # the address alone: torch.cuda.current_stream() builds an object in 2.8 us, a quarter of a small call
         return torch._C._cuda_getCurrentRawStream(index) if stream is None else ks._stream_ptr(stream)
 
@@ -143,8 +147,17 @@ class Cache8:
 
     def attention(self, batch: Batch8, q, scale=None, out=None, lse=None, workspace=None, stream=None):
         """Causal attention of the batch's rows: q, out [n_rows, n_q_heads, head_dim] bf16, lse [n_rows, n_q_heads]
-        fp32.  scale: head_dim ** -0.5 if not given.  Returns out."""
+        fp32.  scale: head_dim ** -0.5 if not given.  Returns out.  The address of a stream that is not the current
+        one needs out and workspace with it: torch cannot allocate for an address."""
         s = self._stream(stream)
+        if stream is not None and (out is None or workspace is None) and \
+                s != torch._C._cuda_getCurrentRawStream(self.device.index):
+            if not isinstance(stream, _cuda.Stream):
+                raise ValueError("out and workspace: to be given with the address of a stream")
+            # what the current stream allocates it may still write, the zeros below among it, and hand out again
+            # while the call runs
+            with _cuda.stream(stream):
+                return self.attention(batch, q, scale, out, lse, workspace)
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
         q_row, q_head = self._rows(q, "q", _BF16, batch)
