@@ -64,6 +64,8 @@ class Model:
             if nbytes == 0:
                 raise ks.KsError(ks.KS_ERR_UNSUPPORTED, "draft_cache", "no 8-bit draft cache for this shape")
             memory = torch.empty(nbytes, dtype=torch.uint8, device=self.workspace.device)
+            # what the current stream still writes there (tensors that are freed already) ends before the model's does
+            torch.cuda.current_stream(memory.device).synchronize()
         ks.ks_draft_cache(self.h, memory, 0 if memory is None else memory.numel())
         self.draft_memory = memory
 
