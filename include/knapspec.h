@@ -572,8 +572,9 @@ ks_status ks_debug_set_status(ks_model* m, int32_t code);
 /* Per-kernel timing with CUDA events on the model's stream.  While enabled,
  * every launch of the kernel class `klass` (0 QKV, 1 attention, 2 merge,
  * 3 O-proj, 4 gate/up, 5 down, 6 LM head, 7 embed, 8 accept, 9 chained
- * projections, 10 bf16 attention query prep) is bracketed by events; ks_kernel_time returns the launches
- * and total milliseconds since enabling.  Enabling resets the counters.
+ * projections, 10 bf16 attention query prep, and with an 8-bit draft cache
+ * also a draft's append to it) is bracketed by events; ks_kernel_time returns
+ * the launches and total milliseconds since enabling.  Enabling resets the counters.
  * bf16 models run the projections between two attention cores as one chained
  * launch (class 9); while any of classes 0, 3, 4, 5, 6 is enabled they run
  * one projection per launch instead, so that each can be timed alone.

@@ -633,5 +633,8 @@ extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_ba
     t.hq = attn->n_q_heads;
     t.scale = attn->scale;
     t.workspace = attn->workspace;
-    return launched(launch_kv8_attention(a, t, static_cast<cudaStream_t>(stream)), "ks_kv8_attention");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = launch_kv8_attention(a, t, s);
+    if (e == cudaSuccess && kv8_attention_merges(a, t.hq)) e = launch_kv8_merge(a, t, s);
+    return launched(e, "ks_kv8_attention");
 }

@@ -635,6 +635,17 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& ti
     return units * (tiles + p.cost) <= INT32_MAX;
 }
 
+// The plan with what depends on the launch's pointers and device.
+bool make_launch(const Kv8Args& a, const Kv8AttnArgs& t, Kv8Plan& p, int64_t& units, int64_t& tiles) {
+    if (!make_plan(a, t.hq, p, units, tiles)) return false;
+    p.ctas = (int)std::min<int64_t>(std::min(sm_count(), kKv8Sms) * resident(p.rg), units * (tiles + p.cost));
+    p.q_wide = reinterpret_cast<uintptr_t>(t.q) % 16 == 0 && t.q_row % 8 == 0 && t.q_head % 8 == 0;
+    p.out_wide = reinterpret_cast<uintptr_t>(t.out) % 16 == 0 && t.out_row % 8 == 0 && t.out_head % 8 == 0;
+    p.desc = static_cast<int4*>(t.workspace);
+    p.part = reinterpret_cast<float*>(p.desc + kKv8MaxCtas);
+    return true;
+}
+
 }  // namespace
 
 size_t kv8_attention_workspace(int hd, int group, int n_rows) {
@@ -652,23 +663,28 @@ bool kv8_attention_fits(const Kv8Args& a, int hq) {
     return make_plan(a, hq, p, units, tiles);
 }
 
+bool kv8_attention_merges(const Kv8Args& a, int hq) {
+    Kv8Plan p;
+    int64_t units, tiles;
+    return make_plan(a, hq, p, units, tiles) && tiles > 1;
+}
+
 cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s) {
     Kv8Plan p;
     int64_t units, tiles;
-    if (!make_plan(a, t.hq, p, units, tiles)) return cudaErrorInvalidValue;
-    p.ctas = (int)std::min<int64_t>(std::min(sm_count(), kKv8Sms) * resident(p.rg), units * (tiles + p.cost));
-    p.q_wide = reinterpret_cast<uintptr_t>(t.q) % 16 == 0 && t.q_row % 8 == 0 && t.q_head % 8 == 0;
-    p.out_wide = reinterpret_cast<uintptr_t>(t.out) % 16 == 0 && t.out_row % 8 == 0 && t.out_head % 8 == 0;
-    p.desc = static_cast<int4*>(t.workspace);
-    p.part = reinterpret_cast<float*>(p.desc + kKv8MaxCtas);
-    cudaError_t e;
+    if (!make_launch(a, t, p, units, tiles)) return cudaErrorInvalidValue;
     auto few = [&](auto hd) {
         constexpr int HD = decltype(hd)::value;
         return p.rg == 8 ? launch_few<HD, 1>(a, t, p, s) : launch_few<HD, 2>(a, t, p, s);
     };
-    if (p.rg == kKv8TcRows) e = launch_kv8_tc(a, t, p, s);
-    else e = a.hd == 128 ? few(std::integral_constant<int, 128>{}) : few(std::integral_constant<int, 64>{});
-    if (e != cudaSuccess || tiles <= 1) return e;       // no unit has a tile to cut off
+    if (p.rg == kKv8TcRows) return launch_kv8_tc(a, t, p, s);
+    return a.hd == 128 ? few(std::integral_constant<int, 128>{}) : few(std::integral_constant<int, 64>{});
+}
+
+cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s) {
+    Kv8Plan p;
+    int64_t units, tiles;
+    if (!make_launch(a, t, p, units, tiles)) return cudaErrorInvalidValue;
     return a.hd == 128 ? launch_merge<128>(a, t, p, units, s) : launch_merge<64>(a, t, p, units, s);
 }
 

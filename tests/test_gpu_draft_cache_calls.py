@@ -40,3 +40,35 @@ def test_memory_that_the_current_stream_still_writes():
         _check_copy(m, l, 123, 5)
     assert list(m.draft(mask, 5)) == first
     m.close()
+
+
+@pytest.mark.parametrize("mask", [[1, 1, 1, 1], [0, 1, 1, 1]])
+def test_every_launch_is_counted(mask):
+    """A draft's Attn sublayer over the copy: query prep, append, attention and its merge; the first, third and
+    fourth over the bf16 cache."""
+    from paper_2602_20217_gb300 import knapspec as ks
+    from paper_2602_20217_gb300 import synth
+    from paper_2602_20217_gb300.model import Model
+    shape, mask, gamma = _shape(), np.array(mask, np.uint8), 3
+    sublayers = gamma * int(mask[::2].sum())
+    counts, timed = {}, {}
+    for cached in (False, True):
+        m = Model(shape, max_seq=MAX_SEQ)
+        if cached:
+            m.draft_cache()
+        m.prefill(synth.prompt_tokens(shape, 123, seed=1))
+        m.draft(mask, gamma)                         # the copy takes the prompt
+        before = ks.ks_launch_count(m.h)
+        m.draft(mask, gamma)
+        counts[cached] = ks.ks_launch_count(m.h) - before
+        for klass in (1, 2, 10):
+            ks.ks_kernel_timing(m.h, klass, 1)
+            m.draft(mask, gamma)
+            timed[cached, klass] = ks.ks_kernel_time(m.h, klass)[0]
+            ks.ks_kernel_timing(m.h, klass, 0)
+        m.close()
+    assert counts[True] - counts[False] == sublayers
+    for klass, per in ((1, 1), (2, 1), (10, 1)):
+        assert timed[False, klass] == per * sublayers
+    for klass, per in ((1, 1), (2, 1), (10, 2)):
+        assert timed[True, klass] == per * sublayers
