@@ -521,9 +521,18 @@ ks_status ks_kv8_read(const ks_kv8_cache* cache, const ks_kv8_batch* batch, void
  * query head h reads KV head h / (n_q_heads / n_kv_heads), at most 64 query
  * heads a KV head.  q, out: bf16, strides in elements.  lse (dev float
  * [n_rows][n_q_heads], or NULL): the logarithm of the sum of exponentials.  A
- * row that sees no token gives zeros and lse -inf.  A weight below 2^-30 of the
- * row's largest may count as zero in out.  A NaN key makes the rows
+ * row that sees no token gives zeros and lse -inf.  A NaN key makes the rows
  * that see it NaN, a NaN value that dim of them; unseen ones do nothing.
+ * Scores, statistics and sums are fp32 (scores that pass fp32 make a row NaN).
+ * Fewer bits have:
+ *  - a query's elements: exact down to 2^-9 of the largest of its row and head,
+ *    off by at most 2^-17 of that below;
+ *  - the weights, 11 bits.  Let w be a key's weight relative to the row's
+ *    largest and s its block's value scale relative to the largest among the
+ *    blocks that the call reads of the sequence and KV head.  Below w = 2^-20 or
+ *    w s = 2^-28 a key has fewer bits, below w = 2^-30 or w s = 2^-38 it may
+ *    count as zero in out, even where w is 1: a value that lies that far below
+ *    others of its sequence does not come through next to them.
  * workspace: dev, 256-byte aligned, ks_kv8_attention_workspace() bytes for
  * the call's n_seqs and n_rows or more; its contents matter to no later call,
  * and calls that run at the same time need one each. */

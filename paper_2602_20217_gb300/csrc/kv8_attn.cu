@@ -13,16 +13,17 @@
 //     tensor cores as they are (4000 multiply-adds per SM and clock in this
 //     instruction, 1024 in its f16 form), and the 16 rows of the A operand are
 //     the queries' 8 rows in two codes each, hi = e4m3(q 2^-e), lo = e4m3(q
-//     2^-e - hi), which hold every bf16 query down to 2^-10 of its row's
+//     2^-e - hi), which hold every bf16 query down to 2^-9 of its row's
 //     largest element exactly;
 //   online softmax in fp32, base 2, the keys' block scale folded into the
 //     scores;
 //   O^T (dims x 8 rows) += V^T P^T by m16n8k16 f16: P in 11 bits, times the
 //     values' block scale relative to the largest seen so far and 2^14, so
-//     that weights down to 2^-39 of the largest count; V^T codes converted
-//     to f16 exactly in registers.  (Weights as e4m3 pairs would run at twice
-//     the rate but lose everything under 2^-18 of the row's maximum, half of
-//     the output where one key outweighs a flat context of 128k.)
+//     that weight times relative scale counts down to 2^-39 and has 11 bits down
+//     to 2^-28; V^T codes converted to f16 exactly in registers.  (Weights as
+//     e4m3 pairs would run at twice the rate but lose everything under 2^-18 of
+//     the row's maximum, half of the output where one key outweighs a flat
+//     context of 128k.)
 // The record's layout makes every operand a run of ldmatrix rows without bank
 // conflicts and P's accumulator layout the next product's operand.
 //

@@ -60,7 +60,8 @@ constexpr float kFar = 4194304.f;   // 2^22
 // Values' scales are taken relative to vref, which follows the tiles of a
 // segment in order: four times the loudest block seen, raised when one passes
 // it.  The f16 values carry a block's relative scale down to 2^-14 (codes of
-// 2^-9 and more stay exact there), the weights the rest of a quieter block's.
+// 2^-9 and more stay exact there), the weights the rest of a quieter block's:
+// with a weight of 1 it has 11 bits down to 2^-32 of the loudest block's.
 KS_DEV uint32_t f16_times(uint32_t v, __half2 f) {
     const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&v), f);
     return *reinterpret_cast<const uint32_t*>(&r);
