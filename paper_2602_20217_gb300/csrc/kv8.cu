@@ -634,7 +634,8 @@ extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_ba
     t.scale = attn->scale;
     t.workspace = attn->workspace;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_kv8_attention(a, t, s);
-    if (e == cudaSuccess && kv8_attention_merges(a, t.hq)) e = launch_kv8_merge(a, t, s);
+    bool merge;
+    cudaError_t e = launch_kv8_attention(a, t, s, merge);
+    if (e == cudaSuccess && merge) e = launch_kv8_merge(a, t, s);
     return launched(e, "ks_kv8_attention");
 }

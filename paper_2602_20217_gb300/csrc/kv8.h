@@ -42,10 +42,9 @@ constexpr int kKv8MaxGroup = 64;    // query heads a KV head
 cudaError_t launch_kv8_append(int dtype, const Kv8Args& a, const Kv8RowArgs& r, cudaStream_t s);
 size_t kv8_attention_workspace(int hd, int group, int n_rows);
 bool kv8_attention_fits(const Kv8Args& a, int hq);     // false: too many units and tiles for one call
-// A call is two launches: the units' runs, and the merge of units that lie in several (kv8_attention_merges; a pool
-// whose sequences are one tile long has none).  The second comes directly behind the first.
-cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s);
-bool kv8_attention_merges(const Kv8Args& a, int hq);
+// A call is two launches: the units' runs, and directly behind it the merge of units that lie in several, if the
+// first says that there can be any (merge; not where sequences are at most a tile long).
+cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, bool& merge);
 cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s);
 // Map of the 8-bit cache's records (gemv.cu): boxes of box_records records' keys, or values.
 bool make_kv8_map(CUtensorMap* map, const void* base, uint64_t records, uint32_t hd, uint32_t box_records);

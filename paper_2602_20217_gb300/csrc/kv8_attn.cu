@@ -628,9 +628,7 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& ti
     p.tq = p.rg / G;
     p.tile_log = p.rg == kKv8TcRows ? 7 : 6;
     p.cost = (128 * kUnitCost) >> p.tile_log;
-    p.block_log = -1;
-    for (int i = 0; i < 31; ++i)
-        if (a.bpp == 1 << i) p.block_log = i;
+    p.block_log = (a.bpp & (a.bpp - 1)) == 0 ? __builtin_ctz(a.bpp) : -1;
     tiles = (a.capacity + (1ll << p.tile_log) - 1) >> p.tile_log;
     units = (int64_t)a.hk * (a.n_rows / p.tq + a.n_seqs);
     return units * (tiles + p.cost) <= INT32_MAX;
@@ -664,16 +662,12 @@ bool kv8_attention_fits(const Kv8Args& a, int hq) {
     return make_plan(a, hq, p, units, tiles);
 }
 
-bool kv8_attention_merges(const Kv8Args& a, int hq) {
+cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, bool& merge) {
     Kv8Plan p;
     int64_t units, tiles;
-    return make_plan(a, hq, p, units, tiles) && tiles > 1;
-}
-
-cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s) {
-    Kv8Plan p;
-    int64_t units, tiles;
+    merge = false;
     if (!make_launch(a, t, p, units, tiles)) return cudaErrorInvalidValue;
+    merge = tiles > 1;
     auto few = [&](auto hd) {
         constexpr int HD = decltype(hd)::value;
         return p.rg == 8 ? launch_few<HD, 1>(a, t, p, s) : launch_few<HD, 2>(a, t, p, s);

@@ -583,8 +583,9 @@ static ks_status draft8_attention(ks_model* m, int l, int p0, const int* stop) {
     t.hq = c.n_q_heads;
     t.scale = 0.6931471805599453f;
     t.workspace = m->draft8.work;
-    KS_TRY(launch(m, K_ATTN, [&] { return launch_kv8_attention(a, t, m->stream); }, "8-bit draft attention"));
-    if (kv8_attention_merges(a, t.hq))
+    bool merge;
+    KS_TRY(launch(m, K_ATTN, [&] { return launch_kv8_attention(a, t, m->stream, merge); }, "8-bit draft attention"));
+    if (merge)
         KS_TRY(launch(m, K_MERGE, [&] { return launch_kv8_merge(a, t, m->stream); }, "8-bit draft attention merge"));
     valid = p0 + 1;
     return KS_OK;
