@@ -111,6 +111,7 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     Kv8Seq mine{};
     int head = 0;                                // length of one of its heads' units
+    bool falls = false;
     auto load = [&](int c) {
         const int s = c + lane;
         if (s >= a.n_seqs) {
@@ -118,15 +119,14 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
             return 0;
         }
         mine = kv8_seq(a, s);
+        falls |= a.offsets[s + 1] < a.offsets[s];
         head = head_length(mine, p);
         return a.hk * head;
     };
     int total = 0, v = 0;
-    bool falls = false;
     for (int c = 0; c < a.n_seqs; c += 32) {
         v = load(c);
         if (cta == 0 && c + lane < a.n_seqs && kv8_seq_bad(a, c + lane)) kv8_flag(a, kKv8BadBatch);
-        falls = falls || (c + lane < a.n_seqs && a.offsets[c + lane + 1] < a.offsets[c + lane]);
         total += __reduce_add_sync(0xffffffffu, v);
     }
     if (__any_sync(0xffffffffu, falls)) return false;
