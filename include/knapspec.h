@@ -264,7 +264,9 @@ ks_status ks_model_position(const ks_model* m, int32_t* committed, int32_t* pend
  * drafts, so the number accepted, may differ.  Each draft pass takes the rows
  * that a layer's copy lacks from the model's cache, so the copy follows
  * prefills, verifies and rewinds by itself, and after every verify a layer's
- * unfinished block is taken anew.  ks_draft_cache: memory (dev, 256-byte
+ * unfinished block is taken anew.  An Attn sublayer of a draft costs other
+ * times then: a ks_latency for the selection stages is to be fitted with the
+ * cache on (classes 1, 2 and 10 of ks_kernel_timing).  ks_draft_cache: memory (dev, 256-byte
  * aligned, ks_draft_cache_bytes(cfg) bytes, borrowed until the model is
  * destroyed or the cache replaced or taken away; needs no initial value), or
  * NULL to go back to the bf16 cache; waits for the stream.
@@ -533,6 +535,8 @@ ks_status ks_kv8_read(const ks_kv8_cache* cache, const ks_kv8_batch* batch, void
  *    w s = 2^-28 a key has fewer bits, below w = 2^-30 or w s = 2^-38 it may
  *    count as zero in out, even where w is 1: a value that lies that far below
  *    others of its sequence does not come through next to them.
+ * A call is cut by its mean rows a sequence; one prompt's chunk among many
+ * single rows is faster in a call of its own.
  * workspace: dev, 256-byte aligned, ks_kv8_attention_workspace() bytes for
  * the call's n_seqs and n_rows or more; its contents matter to no later call,
  * and calls that run at the same time need one each. */

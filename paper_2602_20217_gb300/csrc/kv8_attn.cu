@@ -591,7 +591,10 @@ __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args 
 // least G (whole tokens): 8 or 16 for this file's kernel, else the tcgen05
 // kernel's 128.  On the Qwen3-32B shape at 64k, 16 rows take 41 us here and 49 us
 // there; 24 rows take 74 us here (three row tiles of registers spill), 32 in two
-// warps of 16 rows 65 us, and 56 us there.
+// warps of 16 rows 65 us, and 56 us there.  One size serves the whole call, so an
+// uneven batch costs more than its parts: 200 single rows at 4000 tokens 268 us,
+// one sequence of 2000 rows at 4000 tokens 201 us, both in one call 811 us (32
+// heads over 8); two calls over disjoint sequences are faster there.
 int rows_of_unit(int G, int64_t n_rows, int64_t n_seqs) {
     const int64_t avg = n_seqs > 0 ? (n_rows * G + n_seqs - 1) / n_seqs : 0;
     const int64_t need = std::max<int64_t>(avg, G);

@@ -24,14 +24,15 @@
 // it was set, rounded up to a whole number, not the running one: a row's m is
 // raised (and its l, O and the weights of the tile so far multiplied down by a
 // power of two, without rounding) only when its weights of 32 keys add up to
-// more than 2^15.5.  So most tiles need no maximum at all, no weight passes f16,
-// and weights count down to f16's 2^-24, at least 2^-30 of the largest (2^-39
-// where the reference lags behind it): what 128k keys below that add up to is
-// under 2^-13 of the row, a sixteenth of the output's rounding.
+// more than 2^15.5.  A raise finishes its 32 keys itself, so no score, however
+// far, keeps a row raising.  So most tiles need no maximum at all, no weight
+// passes f16, and weights count down to f16's 2^-24, at least 2^-30 of the
+// largest (2^-39 where the reference lags behind it): what 128k keys below that
+// add up to is under 2^-13 of the row, a sixteenth of the output's rounding.
 //
 // Measured: 2001 rows of a prompt at 8150 tokens (64 query heads over 8, hd 128)
-// 582 us, 805 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 75 us, 3.6
-// TB/s; 24 sequences of 2 to 11 rows at up to 16000 tokens 123 us.  What bounds
+// 592 us, 790 TFLOP/s; 5 rows of 32 heads over 8 at 131077 tokens 75 us, 3.6
+// TB/s; 24 sequences of 2 to 11 rows at up to 16000 tokens 125 us.  What bounds
 // it is the round trip of a stream's tile, products to softmax and back, about
 // 5000 clocks of which the two products are 1350 and the softmax 2200; the two
 // streams hide half.  Taking out the conversion, half of Q K^T and most of P V
