@@ -115,3 +115,26 @@ def test_equal_far_scores_share_the_weight(rows, exponent):
         seen = pool.kv[0][1, :N - rows + i + 1, 0]
         ref, mag = seen.mean(0), np.abs(seen).mean(0)
         assert np.all(np.abs(got[i] - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -10 * mag)
+
+
+@pytest.mark.parametrize("rows,seqs", [(1, 300), (4, 300), (5, 200), (12, 100), (45, 40)])
+@pytest.mark.parametrize("order", ["mixed", "rising", "falling"])
+@pytest.mark.parametrize("exponent", [22, 28, 60])
+def test_far_scores_in_runs_of_many_tiles(rows, seqs, order, exponent):
+    """So many sequences of the same pages that a CTA's run holds several tiles of one: raises move what is summed."""
+    pool, q = inputs(rows, exponent, 1.0, order)
+    pool.lens, pool.kv, pool.table = [N] * seqs, pool.kv * seqs, np.repeat(pool.table, seqs, 0)
+    import torch
+    d = pool.device([rows] * seqs)
+    qt = torch.tensor(np.tile(q, (seqs, 1, 1)), dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(rows * seqs, HQ, device="cuda")
+    got = d["cache"].attention(d["batch"], qt, scale=1.0, lse=lse)
+    torch.cuda.synchronize()
+    assert int(d["status"]) == 0
+    told, out, want_lse, bound = expected(pool, rows, qt[:rows].double().cpu().numpy(), 1.0)
+    assert told.mean() >= 0.75
+    got = got.double().cpu().numpy().reshape(seqs, rows, HQ, HD)
+    lse = lse.double().cpu().numpy().reshape(seqs, rows, HQ)
+    assert np.isfinite(got).all()
+    assert np.all(np.abs(got - out)[:, told] <= (2.0 ** -8 + 2.0 ** -10) * np.abs(out)[told])
+    assert np.all(np.abs(lse - want_lse)[:, told] <= bound[told])
