@@ -464,7 +464,8 @@ typedef struct {
  * token lengths[s] - r + i.  Rows from row_offsets[n_seqs] on (padding up to
  * n_rows) belong to no sequence: nothing is read or written for them.  All
  * arrays are device memory and read by the kernels, so a captured call follows
- * their contents; n_seqs, table_ld and n_rows are fixed by the call.
+ * their contents; they are read more than once, so none may change while a call
+ * runs.  n_seqs, table_ld and n_rows are fixed by the call.
  * What the host cannot check is checked on the device and ORed into *status
  * (never cleared by a call), bit 0: a page outside the pool (its tokens are not
  * written, read as zeros, and unseen by the attention); bit 1: offsets that

@@ -134,6 +134,7 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
     if (cta >= r.ctas) return false;
     int start = 0, len = 0;                      // of the sequence's units on the line; a head's length
     for (int c = 0;; c += 32) {
+        if (c >= a.n_seqs) return false;         // not with arrays that stay what they are
         if (a.n_seqs > 32) v = load(c);
         int u = v;                               // inclusive sums
 #pragma unroll

@@ -36,7 +36,8 @@ def _check(t, name: str, dtypes, ndim: int, device):
 
 class Batch8:
     """The sequences of a call: page_table int32 [n_seqs, pages], row_offsets int32 [n_seqs + 1],
-    lengths int32 [n_seqs] on the device; status: int32 [1] for what only the device can see."""
+    lengths int32 [n_seqs] on the device; status: int32 [1] for what only the device can see.  Calls read the arrays
+    while they run: update them in the calls' stream, or after them."""
 
     def __init__(self, page_table, row_offsets, lengths, n_rows: int, status=None):
         dev = page_table.device
