@@ -555,6 +555,47 @@ typedef struct {
 size_t ks_kv8_attention_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_rows);
 ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_attn* attn, void* stream);
 
+/* ---------------------------------------------------- token log probabilities */
+
+/* What a serving interface reports beside its tokens (an addition of this
+ * library), from the logits x of a row, z = (x - max x) / temperature:
+ *   logprobs[row][j] = z[tokens[row][j]] - log sum exp z    (NaN for a token outside 0 .. vocab - 1)
+ *   entropy[row]     = -sum p log p, in nats
+ *   top_ids, top_logprobs[row][0 .. n_top - 1]: the tokens with the largest
+ *                      logits, larger first, ties by the lower id.
+ * A logit of -inf has no probability; a row of nothing else gives log
+ * probabilities of -inf, entropy 0 and the lowest ids.  A NaN or +inf among a
+ * row's logits makes its numbers NaN and its top_ids -1.
+ * logits: dev, fp32 or bf16, row r at r * row_stride elements.  All other
+ * arrays are dev, contiguous, and may be NULL where they have no elements
+ * (entropy always).  vocab up to 2^22, n_tokens and n_top up to 64, n_top at most
+ * vocab.  Sums are fp32; an exponential is off by at
+ * most 2^-22 relative, and none where it is below 2^-126. */
+typedef struct {
+    const void* logits;
+    int32_t dtype;           /* KS_DTYPE_F32 or KS_DTYPE_BF16 */
+    int32_t rows, vocab;
+    int64_t row_stride;
+    const int32_t* tokens;   /* [rows][n_tokens] */
+    int32_t n_tokens, n_top;
+    float temperature;
+    float* logprobs;         /* [rows][n_tokens] */
+    float* entropy;          /* [rows] */
+    int32_t* top_ids;        /* [rows][n_top] */
+    float* top_logprobs;     /* [rows][n_top] */
+} ks_logprobs;
+ks_status ks_token_logprobs(const ks_logprobs* args, void* stream);
+
+/* The same for rows first_row .. of the model's last prompt, draft or verify
+ * pass, on the model's stream: args gives tokens, n_tokens, n_top, temperature,
+ * rows and the results, all dev; its logits, dtype, vocab and stride are not
+ * read.  Row i of a verify pass holds the logits of the token after its input
+ * row i, so those of the tokens that ks_verify returned are rows 0 .. n_out - 1;
+ * after a prefill the last row's is the pending token's.  Does not wait.
+ * KS_ERR_STATE before a prefill, KS_ERR_INVALID_ARG for rows that the pass did
+ * not have.  A layer selection may replace the logits (see ks_debug_read). */
+ks_status ks_model_logprobs(ks_model* m, int32_t first_row, const ks_logprobs* args);
+
 /* ------------------------------------------------------------ diagnostics */
 
 /* Copy a window of device state to the caller (for tests):

@@ -1,0 +1,435 @@
+// Log probabilities of given tokens under rows of logits, the rows' entropies
+// and their most likely tokens, in one pass over the logits.
+//
+// With m the row's largest logit and x' = (x - m) / T:
+//   log p(x) = x' - log Z,  Z = sum exp x',  H = log Z - (sum x' exp x') / Z.
+// The largest logit is left out of the sums and counted instead, Z = n + tail,
+// so that a likely token's logarithm, -log1p(tail), keeps its digits.
+//
+// A cluster takes a row, each CTA every so many segments of it.  A warp reads a
+// segment, 32 kVec 16-byte vectors, at a time into registers and keeps the row's
+// maximum so far for all of its lanes: a segment that holds no larger logit,
+// nearly every one, adds to the sums without a look at single maxima.  The
+// segments' maxima stay in shared memory.  The n_top largest logits are in the
+// n_top segments with the largest maxima (ties: the earlier one; every logit of
+// another segment is behind each of those maxima), and at least as large as the
+// least of these maxima: those segments are read again, from L2, and the few
+// candidates ranked against each other.
+#include <cmath>
+
+#include "internal.h"
+#include "tma.cuh"
+#include "umma.cuh"
+
+namespace ks {
+
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kVec = 4;             // 16-byte vectors of a lane and segment
+constexpr int kMaxVocab = 1 << 22;
+constexpr int kMaxTop = 64, kMaxTokens = 64;
+constexpr int kCand = 1024;         // candidates that are ranked in one go
+constexpr int kMaxCluster = 8;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLeast = -200.f;    // below it 2^u is 0: -inf must not be multiplied by that
+
+struct LogprobArgs {
+    const void* logits;
+    int64_t ld;
+    int rows, vocab;
+    int n_tokens, n_top;
+    float temperature;
+    const int32_t* tokens;
+    float *logprobs, *entropy, *top_logprobs;
+    int32_t* top_ids;
+};
+
+// Larger float, larger key; the two zeros are one, and nothing is 0.
+KS_DEV unsigned order_key(float v) {
+    const unsigned b = __float_as_uint(v + 0.f);
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+KS_DEV float order_value(unsigned k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
+// Larger first, then the lower id.
+KS_DEV unsigned long long pair_key(float v, int id) {
+    return ((unsigned long long)order_key(v) << 32) | (0xFFFFFFFFu - (unsigned)id);
+}
+KS_DEV int pair_id(unsigned long long k) { return (int)(0xFFFFFFFFu - (unsigned)k); }
+KS_DEV float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Sums relative to a maximum m, u = (x - m) log2(e) / T: n logits equal to it, the
+// sum of 2^u over the others and of u 2^u.
+struct Sums {
+    float m, t, s;
+    int n;
+    // the same relative to a larger maximum
+    KS_DEV void raise(float top, float k) {
+        if (top == m) return;
+        const float u = (m - top) * k, f = exp2_approx(u), z = t + (float)n;
+        s = f > 0.f ? f * fmaf(u, z, s) : 0.f;       // u may be -inf
+        t = f * z;
+        n = 0;
+        m = top;
+    }
+};
+
+// A row as 16-byte vectors from the boundary at or before its first logit on:
+// position p of them is logit p - shift.
+template <typename T>
+struct Row {
+    static constexpr int E = 16 / sizeof(T), SEG = 32 * kVec * E;
+    const T* base;
+    int shift, end;                 // positions [shift, end) are the row's
+    KS_DEV Row(const LogprobArgs& a, int row) {
+        const T* p = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+        shift = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+        base = p - shift;
+        end = shift + a.vocab;
+    }
+    KS_DEV int segments() const { return (end + SEG - 1) / SEG; }
+    KS_DEV int position(int seg, int v) const { return seg * SEG + (v * 32 + (int)(threadIdx.x & 31)) * E; }
+    // a lane's part of a segment; what is not the row's is -inf
+    KS_DEV void load(int seg, float (&x)[kVec * E]) const {
+        uint4 raw[kVec];
+        if (seg * SEG >= shift && (seg + 1) * SEG <= end) {
+#pragma unroll
+            for (int v = 0; v < kVec; ++v) raw[v] = *reinterpret_cast<const uint4*>(base + position(seg, v));
+#pragma unroll
+            for (int v = 0; v < kVec; ++v) widen(raw[v], x + v * E);
+        } else {
+#pragma unroll
+            for (int v = 0; v < kVec; ++v)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int p = position(seg, v) + e;
+                    x[v * E + e] = p >= shift && p < end ? to_float(base[p]) : -INFINITY;
+                }
+        }
+    }
+    static KS_DEV void widen(const uint4& r, float* x) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E == 4) {
+                x[i] = __uint_as_float(w[i]);
+            } else {
+                x[2 * i] = bf16_lo(w[i]);
+                x[2 * i + 1] = bf16_hi(w[i]);
+            }
+        }
+    }
+};
+
+KS_DEV void store_cluster(void* p, int rank, unsigned long long v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_addr(p, rank)), "l"(v) : "memory");
+}
+
+struct Smem {
+    unsigned long long cand[kCand];
+    unsigned long long best[kMaxCluster][kMaxTop];      // the first CTA: every CTA's largest
+    unsigned long long sums[kMaxCluster][2];            // the first CTA: (m, n), (t, s) of each
+    Sums warp[kWarps];
+    int counts[2][kWarps];
+    unsigned bound;
+    int n_cand, n_chosen;
+    int chosen[kMaxTop];
+    float log_z, m;
+    bool bad;
+};
+
+// The K largest pairs (value, id) among the segments at `mine`, in order, to
+// out[K] (0: fewer).  maxima: the segments' largest keys, n of them, segment i
+// being first + i step of the row.
+template <typename T>
+KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigned* maxima, int K, Smem& sm,
+                    unsigned long long* out) {
+    using R = Row<T>;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        sm.n_cand = 0;
+        sm.bound = 0;
+    }
+    __syncthreads();
+    // the K segments with the largest maxima
+    for (int i = tid; i < n; i += kThreads) {
+        const unsigned k = maxima[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += maxima[j] > k || (maxima[j] == k && j < i);
+        if (rank < K) sm.chosen[rank] = i;
+        if (rank == K - 1) sm.bound = k;
+    }
+    __syncthreads();
+    const int chosen = min(n, K);
+    const unsigned bound = sm.bound;
+    auto each = [&](auto&& f) {
+        for (int c = warp; c < chosen; c += kWarps) {
+            const int seg = first + sm.chosen[c] * step;
+            float x[kVec * R::E];
+            row.load(seg, x);
+#pragma unroll
+            for (int v = 0; v < kVec; ++v)
+#pragma unroll
+                for (int e = 0; e < R::E; ++e) {
+                    const int p = row.position(seg, v) + e;
+                    if (p >= row.shift && p < row.end) f(x[v * R::E + e], p - row.shift);
+                }
+        }
+    };
+    each([&](float x, int id) {
+        if (order_key(x) >= bound) {
+            const int at = atomicAdd(&sm.n_cand, 1);
+            if (at < kCand) sm.cand[at] = pair_key(x, id);
+        }
+    });
+    __syncthreads();
+    int found = sm.n_cand;
+    if (found > kCand) {
+        // too many for one go: the K-th largest pair, bit by bit (all pairs differ)
+        unsigned long long least = 0;
+        for (int bit = 63, turn = 0; bit >= 0; --bit, turn ^= 1) {
+            const unsigned long long t = least | (1ull << bit);
+            int c = 0;
+            each([&](float x, int id) { c += pair_key(x, id) >= t; });
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (lane == 0) sm.counts[turn][warp] = c;
+            __syncthreads();
+            c = __reduce_add_sync(0xffffffffu, lane < kWarps ? sm.counts[turn][lane] : 0);
+            if (c >= K) least = t;
+            if (c == K) break;
+        }
+        if (tid == 0) sm.n_cand = 0;
+        __syncthreads();
+        each([&](float x, int id) {
+            const unsigned long long k = pair_key(x, id);
+            if (k >= least) sm.cand[atomicAdd(&sm.n_cand, 1)] = k;
+        });
+        __syncthreads();
+        found = sm.n_cand;
+    }
+    for (int i = tid; i < found; i += kThreads) {
+        const unsigned long long k = sm.cand[i];
+        int rank = 0;
+        for (int j = 0; j < found; ++j) rank += sm.cand[j] > k;
+        if (rank < K) out[rank] = k;
+    }
+    if (tid >= found && tid < K) out[tid] = 0ull;
+    __syncthreads();
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs a, int ctas) {
+    using R = Row<T>;
+    constexpr int N = kVec * R::E;
+    extern __shared__ unsigned maxima[];
+    __shared__ Smem sm;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = (int)blockIdx.x % ctas;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int r = (int)blockIdx.x / ctas;
+    const R row(a, r);
+    const int segs = row.segments(), mine = segs > rank ? (segs - rank - 1) / ctas + 1 : 0;
+    const float k = kLog2e / a.temperature;
+    if (ctas > 1) cluster_sync();                    // every CTA runs: the first one's shared memory may be written
+
+    Sums sum{-INFINITY, 0.f, 0.f, 0};                // m is the warp's, the rest the lane's
+    for (int i = warp; i < mine; i += kWarps) {
+        float x[N];
+        row.load(rank + i * ctas, x);
+        float top = x[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) top = fmaxf(top, x[j]);
+        const unsigned key = __reduce_max_sync(0xffffffffu, order_key(top));
+        if (lane == 0) maxima[i] = key;
+        top = order_value(key);
+        if (top >= sum.m) {
+            sum.raise(top, k);
+            const float ref = sum.m == -INFINITY ? 0.f : sum.m;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float u = (x[j] - ref) * k, e = exp2_approx(u);
+                if (x[j] == sum.m) {
+                    ++sum.n;
+                } else {
+                    sum.t += e;
+                    sum.s = fmaf(e, fmaxf(u, kLeast), sum.s);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float u = (x[j] - sum.m) * k, e = exp2_approx(u);
+                sum.t += e;
+                sum.s = fmaf(e, fmaxf(u, kLeast), sum.s);
+            }
+        }
+    }
+    sum.t = warp_sum(sum.t);
+    sum.s = warp_sum(sum.s);
+    sum.n = __reduce_add_sync(0xffffffffu, sum.n);
+    if (lane == 0) sm.warp[warp] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        float top = -INFINITY;
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm.warp[w].m);
+        Sums all{top, 0.f, 0.f, 0};
+        for (int w = 0; w < kWarps; ++w) {
+            Sums u = sm.warp[w];
+            u.raise(top, k);
+            all.t += u.t;
+            all.s += u.s;
+            all.n += u.n;
+        }
+        const unsigned long long lo = __float_as_uint(all.m) | (unsigned long long)(unsigned)all.n << 32;
+        const unsigned long long hi = __float_as_uint(all.t) | (unsigned long long)__float_as_uint(all.s) << 32;
+        if (ctas > 1) {
+            store_cluster(&sm.sums[rank][0], 0, lo);
+            store_cluster(&sm.sums[rank][1], 0, hi);
+        } else {
+            sm.sums[0][0] = lo;
+            sm.sums[0][1] = hi;
+        }
+    }
+    if (a.n_top) {
+        // this CTA's largest, in best[0] unless they go to the first CTA
+        largest(row, rank, ctas, mine, maxima, a.n_top, sm, sm.best[rank]);
+        if (ctas > 1 && rank > 0 && tid < a.n_top) store_cluster(&sm.best[rank][tid], 0, sm.best[rank][tid]);
+    }
+    if (ctas > 1) {
+        cluster_sync();
+        if (rank != 0) return;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        Sums all{-INFINITY, 0.f, 0.f, 0};
+        for (int c = 0; c < ctas; ++c) all.m = fmaxf(all.m, __uint_as_float((unsigned)sm.sums[c][0]));
+        for (int c = 0; c < ctas; ++c) {
+            Sums u{__uint_as_float((unsigned)sm.sums[c][0]), __uint_as_float((unsigned)sm.sums[c][1]),
+                   __uint_as_float((unsigned)(sm.sums[c][1] >> 32)), (int)(sm.sums[c][0] >> 32)};
+            u.raise(all.m, k);
+            all.t += u.t;
+            all.s += u.s;
+            all.n += u.n;
+        }
+        // NaN logits are in t, an infinite one is the maximum; a row of -inf alone has no distribution
+        const bool empty = all.m == -INFINITY;
+        const float log_z = all.n == 1 ? log1pf(all.t) : logf((float)all.n + all.t);
+        sm.bad = all.t != all.t || all.m == INFINITY;
+        sm.m = all.m;
+        sm.log_z = sm.bad ? __uint_as_float(0x7fc00000u) : empty ? INFINITY : log_z;
+        if (a.entropy)
+            a.entropy[r] = sm.bad ? __uint_as_float(0x7fc00000u)
+                                  : empty ? 0.f : log_z - all.s * kLn2 / ((float)all.n + all.t);
+    }
+    __syncthreads();
+    const float m = sm.m == -INFINITY ? 0.f : sm.m, log_z = sm.log_z;
+    for (int i = tid; i < a.n_tokens; i += kThreads) {
+        const int id = a.tokens[(size_t)r * a.n_tokens + i];
+        const bool inside = id >= 0 && id < a.vocab;
+        const float x = inside ? to_float(row.base[row.shift + id]) : __uint_as_float(0x7fc00000u);
+        a.logprobs[(size_t)r * a.n_tokens + i] = (x - m) / a.temperature - log_z;
+    }
+    if (a.n_top == 0) return;
+    // the CTAs' largest against each other
+    const int n = ctas * a.n_top;
+    for (int i = tid; i < n; i += kThreads) {
+        const unsigned long long key = sm.best[i / a.n_top][i % a.n_top];
+        if (key == 0ull) continue;
+        int at = 0;
+        for (int c = 0; c < ctas; ++c)
+            for (int j = 0; j < a.n_top; ++j) at += sm.best[c][j] > key;
+        if (at >= a.n_top) continue;
+        const size_t o = (size_t)r * a.n_top + at;
+        a.top_ids[o] = sm.bad ? -1 : pair_id(key);
+        a.top_logprobs[o] = (order_value((unsigned)(key >> 32)) - m) / a.temperature - log_z;
+    }
+}
+
+template <typename T>
+cudaError_t launch(const LogprobArgs& a, cudaStream_t s) {
+    auto kern = logprob_kernel<T>;
+    const int ctas = 1;
+    const int segs = (a.vocab + Row<T>::E - 1 + Row<T>::SEG - 1) / Row<T>::SEG;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)a.rows * ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(unsigned) * ((segs + ctas - 1) / ctas);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, a, ctas);
+}
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+}  // namespace
+
+}  // namespace ks
+
+using namespace ks;
+
+extern "C" ks_status ks_token_logprobs(const ks_logprobs* p, void* stream) {
+    if (!p) {
+        set_error("ks_token_logprobs: null argument");
+        return KS_ERR_INVALID_ARG;
+    }
+    if (p->dtype != KS_DTYPE_F32 && p->dtype != KS_DTYPE_BF16) {
+        set_error("ks_token_logprobs: unknown dtype %d", p->dtype);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (p->rows < 0 || p->rows > 1 << 24 || p->vocab < 1) {
+        set_error("ks_token_logprobs: %d rows of %d logits", p->rows, p->vocab);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (p->vocab > kMaxVocab || p->n_tokens > kMaxTokens || p->n_top > kMaxTop) {
+        set_error("ks_token_logprobs: %d logits, %d tokens, %d alternatives (at most %d, %d, %d)", p->vocab, p->n_tokens,
+                  p->n_top, kMaxVocab, kMaxTokens, kMaxTop);
+        return KS_ERR_UNSUPPORTED;
+    }
+    if (p->n_tokens < 0 || p->n_top < 0 || p->n_top > p->vocab) {
+        set_error("ks_token_logprobs: %d tokens, %d alternatives of %d", p->n_tokens, p->n_top, p->vocab);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (!std::isfinite(p->temperature) || !(p->temperature > 0.f)) {
+        set_error("ks_token_logprobs: the temperature is not a positive number");
+        return KS_ERR_INVALID_ARG;
+    }
+    if (p->rows == 0) return KS_OK;
+    const size_t es = p->dtype == KS_DTYPE_BF16 ? 2 : 4;
+    if (!p->logits || !aligned(p->logits, es) || (p->rows > 1 && p->row_stride < p->vocab) ||
+        p->row_stride < 0 || p->row_stride > (int64_t)1 << 40) {
+        set_error("ks_token_logprobs: null or misaligned logits, or a bad stride");
+        return KS_ERR_INVALID_ARG;
+    }
+    if ((p->n_tokens && (!p->tokens || !p->logprobs || !aligned(p->tokens, 4) || !aligned(p->logprobs, 4))) ||
+        (p->n_top && (!p->top_ids || !p->top_logprobs || !aligned(p->top_ids, 4) || !aligned(p->top_logprobs, 4))) ||
+        !aligned(p->entropy, 4)) {
+        set_error("ks_token_logprobs: null or misaligned tokens or results");
+        return KS_ERR_INVALID_ARG;
+    }
+    LogprobArgs a{};
+    a.logits = p->logits;
+    a.ld = p->row_stride;
+    a.rows = p->rows; a.vocab = p->vocab;
+    a.n_tokens = p->n_tokens; a.n_top = p->n_top;
+    a.temperature = p->temperature;
+    a.tokens = p->tokens;
+    a.logprobs = p->logprobs; a.entropy = p->entropy;
+    a.top_ids = p->top_ids; a.top_logprobs = p->top_logprobs;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = p->dtype == KS_DTYPE_BF16 ? launch<__nv_bfloat16>(a, s) : launch<float>(a, s);
+    if (e == cudaSuccess) return KS_OK;
+    set_error("ks_token_logprobs: %s", cudaGetErrorString(e));
+    return KS_ERR_CUDA;
+}

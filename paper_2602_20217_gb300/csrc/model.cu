@@ -2374,6 +2374,29 @@ ks_status ks_debug_set_status(ks_model* m, int32_t code) {
     return KS_OK;
 }
 
+ks_status ks_model_logprobs(ks_model* m, int32_t first_row, const ks_logprobs* args) {
+    if (!m || !args) {
+        set_error("ks_model_logprobs: null argument");
+        return KS_ERR_INVALID_ARG;
+    }
+    if (!m->have_seq) {
+        set_error("ks_model_logprobs: no sequence (call ks_prefill first)");
+        return KS_ERR_STATE;
+    }
+    if (first_row < 0 || args->rows < 0 || (int64_t)first_row + args->rows > m->last_pass_rows) {
+        set_error("ks_model_logprobs: rows %d .. of a pass of %d rows", first_row, m->last_pass_rows);
+        return KS_ERR_INVALID_ARG;
+    }
+    ks_logprobs a = *args;
+    a.logits = m->logits + (size_t)first_row * m->cfg.vocab;
+    a.dtype = KS_DTYPE_F32;
+    a.vocab = m->cfg.vocab;
+    a.row_stride = m->cfg.vocab;
+    const ks_status st = ks_token_logprobs(&a, m->stream);
+    if (st == KS_OK && a.rows > 0) m->launches++;
+    return st;
+}
+
 ks_status ks_debug_read(ks_model* m, int32_t what, int32_t layer, int32_t start, int32_t count, void* dst,
                         size_t bytes) {
     if (!m || !dst) return KS_ERR_INVALID_ARG;

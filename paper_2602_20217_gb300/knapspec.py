@@ -85,6 +85,13 @@ class KsKv8Attn(C.Structure):
                 ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class KsLogprobs(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32),
+                ("row_stride", C.c_int64), ("tokens", C.c_void_p), ("n_tokens", C.c_int32), ("n_top", C.c_int32),
+                ("temperature", C.c_float), ("logprobs", C.c_void_p), ("entropy", C.c_void_p),
+                ("top_ids", C.c_void_p), ("top_logprobs", C.c_void_p)]
+
+
 class KsError(RuntimeError):
     def __init__(self, status: int, where: str, msg: str):
         super().__init__(f"{where}: {_status_name(status)}: {msg}")
@@ -144,6 +151,8 @@ _SIGS = {
                               C.c_int64, C.c_int64, C.c_void_p]),
     "ks_kv8_attention_workspace": (C.c_size_t, [C.POINTER(KsKv8Cache), C.c_int32, C.c_int32, C.c_int32]),
     "ks_kv8_attention": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Attn), C.c_void_p]),
+    "ks_token_logprobs": (C.c_int, [C.POINTER(KsLogprobs), C.c_void_p]),
+    "ks_model_logprobs": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(KsLogprobs)]),
     "ks_status_str": (C.c_char_p, [C.c_int]),
     "ks_last_error": (C.c_char_p, []),
 }
@@ -482,6 +491,14 @@ def ks_kv8_attention_workspace(cache: KsKv8Cache, n_q_heads: int, n_seqs: int, n
 def ks_kv8_attention(cache: KsKv8Cache, batch: KsKv8Batch, attn: KsKv8Attn, stream=None):
     check(load().ks_kv8_attention(C.byref(cache), C.byref(batch), C.byref(attn), _stream_ptr(stream)),
           "ks_kv8_attention")
+
+
+def ks_token_logprobs(args: KsLogprobs, stream=None):
+    check(load().ks_token_logprobs(C.byref(args), _stream_ptr(stream)), "ks_token_logprobs")
+
+
+def ks_model_logprobs(h: int, first_row: int, args: KsLogprobs):
+    check(load().ks_model_logprobs(h, first_row, C.byref(args)), "ks_model_logprobs")
 
 
 def ks_launch_count(h: int) -> int:

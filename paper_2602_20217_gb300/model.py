@@ -134,6 +134,22 @@ class Model:
         lat, _u = latency
         return ks.ks_select_tpt(self.h, lat, self.shape.n_sublayers, n_candidates, max_gamma)
 
+    def logprobs(self, tokens, n_top: int = 0, first_row: int = 0, temperature: float = 1.0):
+        """Log probabilities of tokens [rows] or [rows, n] under rows first_row .. of the last pass, with the rows'
+        entropies and n_top best tokens: a logprobs.LogProbs of numpy arrays."""
+        import torch
+
+        from . import logprobs as lp
+        t = np.ascontiguousarray(tokens, dtype=np.int32)
+        if t.ndim not in (1, 2):
+            raise ValueError(f"tokens: {t.ndim} dimensions, 1 or 2 expected")
+        with torch.cuda.stream(self.stream):
+            dev = torch.from_numpy(t.reshape(len(t), -1)).to(self.workspace.device)
+            out = lp.empty(dev.shape[0], dev.shape[1], n_top, device=self.workspace.device)
+            ks.ks_model_logprobs(self.h, first_row, lp.marshal(None, 0, 0, 0, dev, n_top, temperature, out))
+            got = lp.LogProbs(*(x.cpu().numpy() for x in out))
+        return got if t.ndim == 2 else got._replace(logprobs=got.logprobs[:, 0])
+
     def history_similarities(self):
         import torch
         sims = torch.empty(self.shape.n_sublayers, dtype=torch.float32, device=self.workspace.device)
