@@ -555,6 +555,32 @@ typedef struct {
 size_t ks_kv8_attention_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_rows);
 ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_attn* attn, void* stream);
 
+/* The same attention for sequences that come in groups with a common
+ * beginning, several samples of one prompt for instance: what a group has in
+ * common is read once for all of its rows.  Sequences group_offsets[g] ..
+ * group_offsets[g + 1] - 1 begin with the same tokens[g] tokens, whole pages
+ * (a part of one is left out), on the pages that the first of them names; what
+ * the others' tables say of these pages is not read.  lengths count them.  A
+ * sequence in no group shares nothing.  Tokens that are among the batch's rows
+ * are never taken as common: a group with a sequence that short shares so much
+ * less.  group_offsets, tokens: dev int32 [n_groups + 1], [n_groups], read like
+ * the batch's arrays; status bit 1 also for offsets of groups that decrease or
+ * leave 0 .. n_seqs (no group shares anything then) and for tokens below 0 or
+ * above the pages (taken as the nearest possible value).
+ * Results, types and limits are ks_kv8_attention's; a value counts relative to
+ * the loudest of its own part, the common or the sequence's own.  Groups of one
+ * sequence, or a few common tokens, cost more than ks_kv8_attention.
+ * workspace: ks_kv8_shared_workspace() bytes for the call's sizes or larger ones. */
+typedef struct {
+    const int32_t* group_offsets;
+    const int32_t* tokens;
+    int32_t n_groups;
+} ks_kv8_shared;
+size_t ks_kv8_shared_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_rows,
+                               int32_t n_groups);
+ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_shared* shared,
+                                  const ks_kv8_attn* attn, void* stream);
+
 /* ---------------------------------------------------- token log probabilities */
 
 /* What a serving interface reports beside its tokens (an addition of this

@@ -586,48 +586,52 @@ extern "C" size_t ks_kv8_attention_workspace(const ks_kv8_cache* cache, int32_t 
     return kv8_attention_workspace(cache->head_dim, n_q_heads / cache->n_kv_heads, n_rows);
 }
 
-extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_attn* attn,
-                                      void* stream) {
-    Kv8Args a;
-    ks_status st = kv8_args("ks_kv8_attention", cache, batch, a);
+namespace {
+
+// Checks of an attention call, and the kernels' form of it.  More: what the call needs beside the batch's limits,
+// the workspace's bytes (0: too much for one call).
+template <class More>
+ks_status attention_args(const char* who, const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_attn* attn,
+                         Kv8Args& a, Kv8AttnArgs& t, More&& more) {
+    const ks_status st = kv8_args(who, cache, batch, a);
     if (st != KS_OK) return st;
     if (!attn) {
-        set_error("ks_kv8_attention: null argument");
+        set_error("%s: null argument", who);
         return KS_ERR_INVALID_ARG;
     }
     if (attn->n_q_heads < 1 || attn->n_q_heads > kMaxHeads || attn->n_q_heads % a.hk) {
-        set_error("ks_kv8_attention: %d query heads over %d KV heads", attn->n_q_heads, a.hk);
+        set_error("%s: %d query heads over %d KV heads", who, attn->n_q_heads, a.hk);
         return KS_ERR_INVALID_ARG;
     }
     if (attn->n_q_heads / a.hk > kKv8MaxGroup) {
-        set_error("ks_kv8_attention: %d query heads a KV head (at most %d)", attn->n_q_heads / a.hk, kKv8MaxGroup);
+        set_error("%s: %d query heads a KV head (at most %d)", who, attn->n_q_heads / a.hk, kKv8MaxGroup);
         return KS_ERR_UNSUPPORTED;
     }
     if (!std::isfinite(attn->scale)) {
-        set_error("ks_kv8_attention: the scale is not finite");
+        set_error("%s: the scale is not finite", who);
         return KS_ERR_INVALID_ARG;
     }
     if (a.n_seqs == 0 || a.n_rows == 0) return KS_OK;
     if (!attn->q || !attn->out || !aligned(attn->q, 2) || !aligned(attn->out, 2) || !aligned(attn->lse, 4) ||
         !strides_ok(attn->q_row, attn->q_head) || !strides_ok(attn->out_row, attn->out_head) ||
         (attn->out_row < a.hd && a.n_rows > 1) || (attn->out_head < a.hd && attn->n_q_heads > 1)) {
-        set_error("ks_kv8_attention: null or misaligned queries or output, or bad strides");
+        set_error("%s: null or misaligned queries or output, or bad strides", who);
         return KS_ERR_INVALID_ARG;
     }
-    if (!kv8_attention_fits(a, attn->n_q_heads)) {
-        set_error("ks_kv8_attention: %d rows over up to %d tokens are too much for one call", a.n_rows, a.capacity);
+    const size_t need = more();
+    if (need == 0) {
+        set_error("%s: %d rows over up to %d tokens are too much for one call", who, a.n_rows, a.capacity);
         return KS_ERR_UNSUPPORTED;
     }
-    const size_t need = kv8_attention_workspace(a.hd, attn->n_q_heads / a.hk, a.n_rows);
     if (!attn->workspace || !aligned(attn->workspace, 256)) {
-        set_error("ks_kv8_attention: null or misaligned workspace");
+        set_error("%s: null or misaligned workspace", who);
         return KS_ERR_INVALID_ARG;
     }
     if (attn->workspace_bytes < need) {
-        set_error("ks_kv8_attention: a workspace of %zu bytes, %zu needed", attn->workspace_bytes, need);
+        set_error("%s: a workspace of %zu bytes, %zu needed", who, attn->workspace_bytes, need);
         return KS_ERR_WORKSPACE;
     }
-    Kv8AttnArgs t{};
+    t = Kv8AttnArgs{};
     t.q = static_cast<const __nv_bfloat16*>(attn->q);
     t.q_row = attn->q_row; t.q_head = attn->q_head;
     t.out = static_cast<__nv_bfloat16*>(attn->out);
@@ -636,9 +640,52 @@ extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_ba
     t.hq = attn->n_q_heads;
     t.scale = attn->scale;
     t.workspace = attn->workspace;
+    return KS_OK;
+}
+
+}  // namespace
+
+extern "C" ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_attn* attn,
+                                      void* stream) {
+    Kv8Args a;
+    Kv8AttnArgs t;
+    const ks_status st = attention_args("ks_kv8_attention", cache, batch, attn, a, t, [&]() -> size_t {
+        if (!kv8_attention_fits(a, attn->n_q_heads)) return 0;
+        return kv8_attention_workspace(a.hd, attn->n_q_heads / a.hk, a.n_rows);
+    });
+    if (st != KS_OK || a.n_seqs == 0 || a.n_rows == 0) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     bool merge;
     cudaError_t e = launch_kv8_attention(a, t, s, merge);
     if (e == cudaSuccess && merge) e = launch_kv8_merge(a, t, s);
     return launched(e, "ks_kv8_attention");
+}
+
+extern "C" size_t ks_kv8_shared_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_rows,
+                                          int32_t n_groups) {
+    if (ks_kv8_attention_workspace(cache, n_q_heads, n_seqs, n_rows) == 0 || n_groups < 0 || n_groups > kMaxSeqs) return 0;
+    return kv8_shared_workspace(cache->head_dim, cache->n_kv_heads, n_q_heads, n_seqs, n_rows, n_groups);
+}
+
+extern "C" ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch,
+                                             const ks_kv8_shared* shared, const ks_kv8_attn* attn, void* stream) {
+    const char* who = "ks_kv8_shared_attention";
+    if (!shared) {
+        set_error("%s: null argument", who);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (shared->n_groups < 1 || shared->n_groups > kMaxSeqs || !shared->group_offsets || !shared->tokens ||
+        !aligned(shared->group_offsets, 4) || !aligned(shared->tokens, 4)) {
+        set_error("%s: %d groups, or null or misaligned arrays of them", who, shared->n_groups);
+        return KS_ERR_INVALID_ARG;
+    }
+    const Kv8SharedArgs g{shared->group_offsets, shared->tokens, shared->n_groups};
+    Kv8Args a;
+    Kv8AttnArgs t;
+    const ks_status st = attention_args(who, cache, batch, attn, a, t, [&]() -> size_t {
+        if (!kv8_shared_fits(a, g, attn->n_q_heads)) return 0;
+        return kv8_shared_workspace(a.hd, a.hk, attn->n_q_heads, a.n_seqs, a.n_rows, g.n_groups);
+    });
+    if (st != KS_OK || a.n_seqs == 0 || a.n_rows == 0) return st;
+    return launched(launch_kv8_shared(a, g, t, static_cast<cudaStream_t>(stream)), who);
 }

@@ -17,6 +17,7 @@ struct Kv8Args {            // cache and batch
     int* status;            // or null
     bool by_seq;            // append, read: how the grid counts blocks (set by the launch)
     const int* stop;        // draft passes: the launch does nothing when *stop != 0 (null: always runs)
+    const int64_t* first_page;  // attention in two parts: where in the table a sequence's pages begin
 };
 struct Kv8RowArgs {         // the rows to append; strides in elements
     const void *k, *v, *q;
@@ -36,6 +37,19 @@ struct Kv8AttnArgs {
     int hq;
     float scale;
     void* workspace;
+    // attention in two parts: what the rows' groups have in common gives normalised outputs and sums' logarithms to
+    // base 2, which the rows of sequences with cut[s] > 0 take in
+    float* common_out;      // [n_rows][hq][hd]
+    float* common_lse;      // [n_rows][hq]
+    const int32_t* cut;     // [n_seqs]
+};
+// Which part of the keys a launch attends to: all of a sequence's, those that a group of sequences has in common (its
+// "sequences" are the groups, whose rows all see all of them), or what a sequence has behind these.
+enum Kv8Part { kWhole = 0, kCommon = 1, kTail = 2 };
+struct Kv8SharedArgs {      // groups of sequences with a common beginning
+    const int32_t* groups;  // [n_groups + 1] first sequence of each
+    const int32_t* tokens;  // [n_groups] common tokens
+    int n_groups;
 };
 
 constexpr int kKv8MaxGroup = 64;    // query heads a KV head
@@ -44,8 +58,13 @@ size_t kv8_attention_workspace(int hd, int group, int n_rows);
 bool kv8_attention_fits(const Kv8Args& a, int hq);     // false: too many units and tiles for one call
 // A call is two launches: the units' runs, and directly behind it the merge of units that lie in several, if the
 // first says that there can be any (merge; not where sequences are at most a tile long).
-cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, bool& merge);
-cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s);
+cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, bool& merge,
+                                 Kv8Part part = kWhole);
+cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, Kv8Part part = kWhole);
+// Attention of groups with a common beginning (kv8_shared.cu); t.workspace has room for both parts.
+size_t kv8_shared_workspace(int hd, int hk, int hq, int n_seqs, int n_rows, int n_groups);
+bool kv8_shared_fits(const Kv8Args& a, const Kv8SharedArgs& g, int hq);
+cudaError_t launch_kv8_shared(const Kv8Args& a, const Kv8SharedArgs& g, const Kv8AttnArgs& t, cudaStream_t s);
 // Map of the 8-bit cache's records (gemv.cu): boxes of box_records records' keys, or values.
 bool make_kv8_map(CUtensorMap* map, const void* base, uint64_t records, uint32_t hd, uint32_t box_records);
 

@@ -134,7 +134,7 @@ KS_DEV int join(float (&o)[NQ][DT][4], float (&m)[NQ], float (&l)[NQ], float* co
     return upper ? H : 0;
 }
 
-template <int HD, int NQ>
+template <int HD, int NQ, int PART>
 __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     kv8_attention_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
     using S = Smem<HD, NQ>;
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     grid_launch_dependents();
     if (a.stop && *a.stop) return;
     Run run;
-    Segment at;
+    Segment<PART> at;
     if (!find_run(a, p, run, at)) {
         if (tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
@@ -170,18 +170,17 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         // Page numbers are read a group of tiles ahead, across segments: under
         // load such a read takes microseconds.
         constexpr int TILES = 32 / kBlocks;                      // tiles of a group, a block per lane
-        auto pages = [&](const Segment& k, int tile) {
+        auto pages = [&](const Segment<PART>& k, int tile) {
             const int b = tile * kBlocks + lane;
-            const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
-            if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
-            const int page = a.table[(size_t)k.s * a.table_ld + p.page_of(b, a.bpp)];
+            if (b * kKv8Block > last_key<PART>(k.q, p, k.g) || tile + lane / kBlocks >= k.end) return -1;
+            const int page = pages_of<PART>(a, k.s)[p.page_of(b, a.bpp)];
             return page >= 0 && page < a.n_pages ? page : -2;
         };
         int it = 0, tile = at.tile, page = pages(at, tile);
         bool alive = true, more = true;
         while (more && alive) {
             // the group after this one
-            Segment next = at;
+            Segment<PART> next = at;
             int next_tile = tile + TILES;
             if (next_tile >= at.end) {
                 more = next.next(a, run, p);
@@ -229,19 +228,19 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     int it = 0;
     bool alive = true, began = false;
     for (int buf = 0;; buf = buf == 2 ? 0 : buf + 1) {
-        const Rows rows(at.q, p.tq, at.g, G);
+        const Rows rows(at, p.tq, G);
         // this warp's queries, in two codes
         uint32_t qa[S::Q ? 1 : NQ][S::Q ? 1 : KJ][4];
         float qf[NQ];
         int lim[NQ];                                             // last key that the row sees
-        const int lim_first = rows.pos0, lim_last = rows.pos0 + rows.tokens - 1;
+        const int lim_first = rows.pos0, lim_last = rows.pos0 + (rows.tokens - 1) * rows.step;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int m = 8 * n + g;
             const bool valid = m < rows.n;
             const int tok = valid ? p.token(m) : 0, head = at.h * G + (valid ? m - tok * G : 0);
             const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head;
-            lim[n] = valid ? rows.pos0 + tok : INT32_MAX;
+            lim[n] = valid ? rows.pos0 + tok * rows.step : INT32_MAX;
             float x[KJ * 2][4], top = 0.f;
             // all loads first, without a branch between them
             uint2 raw[KJ * 2];
@@ -431,24 +430,55 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         dt0 += join<NQ, DT, DT / 2>(o, m, l, sm.comb[0], sm.ml[0], warp, warp ^ 1, warp & 1);
         const bool whole = at.tile == 0 && at.end == at.tiles;
         const bool any_nan = sm.any_nan[buf];
+        bool joins = false;                                      // with what its group has in common
+        if constexpr (PART == kTail) joins = t.cut[at.s] > 0;
         {
             float* slot = p.part + (size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg * (HD + 4);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                const float inv = whole ? (l[n] == 0.f ? 0.f : 1.f / l[n]) : 1.f;
+                float inv = whole ? (l[n] == 0.f ? 0.f : 1.f / l[n]) : 1.f, other = 0.f, joined = 0.f;
+                if constexpr (PART == kTail) {
+                    if (whole && joins) {
+                        const int m_row = min(8 * n + g, rows.n - 1), tok = p.token(m_row);
+                        const Joined j(m[n], l[n], t.common_lse[(size_t)(rows.row0 + tok) * t.hq + at.h * G + m_row - tok * G]);
+                        inv = j.own;
+                        other = j.other;
+                        joined = j.lse;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float f = __shfl_sync(0xffffffffu, inv, 8 * q4 + 4 * e);
+                    const float fc = PART == kTail ? __shfl_sync(0xffffffffu, other, 8 * q4 + 4 * e) : 0.f;
                     const int r = 8 * n + 2 * q4 + e;
                     if (any_nan) {
-                        const int seen = rows.pos0 + p.token(r);
+                        const int seen = rows.pos0 + p.token(r) * rows.step;
                         for (int i = 0; i < DT / 4; ++i)
                             for (int c = 0; c < 2; ++c)
                                 if (sm.nan_from[buf][16 * (dt0 + i) + 8 * c + g] <= seen)
                                     set_nan<DT>(o[n], i, 2 * c + e);
                     }
                     if (r >= rows.n) continue;
-                    if (whole) {
+                    if (PART == kCommon && whole) {
+                        const int tok = p.token(r);
+                        float* out = t.common_out + ((size_t)(rows.row0 + tok) * t.hq + at.h * G + r - tok * G) * HD +
+                                     16 * dt0 + g;
+#pragma unroll
+                        for (int i = 0; i < DT / 4; ++i) {
+                            out[16 * i] = o[n][i][e] * f;
+                            out[16 * i + 8] = o[n][i][2 + e] * f;
+                        }
+                    } else if (PART == kTail && whole && joins) {
+                        const int tok = p.token(r);
+                        const int64_t row = rows.row0 + tok, head = at.h * G + r - tok * G;
+                        const float* c = t.common_out + (row * t.hq + head) * HD + 16 * dt0 + g;
+                        __nv_bfloat16* out = t.out + row * t.out_row + head * t.out_head + 16 * dt0 + g;
+#pragma unroll
+                        for (int i = 0; i < DT / 4; ++i) {
+                            out[16 * i] = __float2bfloat16_rn(fmaf(o[n][i][e], f, c[16 * i] * fc));
+                            out[16 * i + 8] = __float2bfloat16_rn(fmaf(o[n][i][2 + e], f, c[16 * i + 8] * fc));
+                        }
+                    } else if (whole) {
                         const int tok = p.token(r);
                         __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row +
                                              (int64_t)(at.h * G + r - tok * G) * t.out_head + 16 * dt0 + g;
@@ -470,6 +500,13 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                 if (warp == 0 && q4 == 0 && m_row < rows.n) {
                     if (!whole) {
                         *reinterpret_cast<float2*>(slot + (size_t)m_row * (HD + 4)) = make_float2(m[n], l[n]);
+                    } else if (PART == kCommon) {
+                        const int tok = p.token(m_row);
+                        t.common_lse[(size_t)(rows.row0 + tok) * t.hq + at.h * G + m_row - tok * G] =
+                            l[n] == 0.f ? -INFINITY : m[n] + log2f(l[n]);
+                    } else if (PART == kTail && joins) {
+                        const int tok = p.token(m_row);
+                        if (t.lse) t.lse[(size_t)(rows.row0 + tok) * t.hq + at.h * G + m_row - tok * G] = joined * kLn2;
                     } else if (t.lse) {
                         const int tok = p.token(m_row);
                         t.lse[(size_t)(rows.row0 + tok) * t.hq + at.h * G + m_row - tok * G] =
@@ -481,7 +518,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         if (!whole && at.tile == 0) {
             began = true;
             if (tid == 0)
-                p.desc[blockIdx.x] = make_int4(rows.row0, rows.n, at.h, run.cta_of(at.first + at.tiles - 1));
+                p.desc[blockIdx.x] =
+                    make_int4(rows.row0, rows.n, joins ? ~at.h : at.h, run.cta_of(at.first + at.tiles - 1));
         }
         if (!at.next(a, run, p)) break;
     }
@@ -500,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 // one row at 64k tokens 31.5, 31.9, -; five rows (128 of a unit) at 128k 82.9, 80.1,
 // 80.9; a batch of 64 sequences 90.7, 80.5, 72.9.
 constexpr int kMergeThreads = 512;
-template <int HD, int MW>
+template <int HD, int MW, int PART>
 __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p) {
     constexpr int V = HD / 32, BATCH = 8, RW = kMergeThreads / 32 / MW;
     using Vec = typename std::conditional<V == 4, float4, float2>::type;
@@ -579,8 +617,26 @@ __global__ void __launch_bounds__(kMergeThreads) kv8_merge_kernel(const Kv8Args 
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = fmaf(acc_s[rr][i][V * lane + j], f, acc[j]);
     }
-    const int tok = p.token(r), head = u.z * G + r - tok * G;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const bool joins = PART == kTail && u.z < 0;     // a head below zero: ~head, see the units' end
+    const int tok = p.token(r), head = (joins ? ~u.z : u.z) * G + r - tok * G;
+    float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if constexpr (PART == kCommon) {
+        const size_t at = (size_t)(u.x + tok) * t.hq + head;
+#pragma unroll
+        for (int i = 0; i < V; ++i) t.common_out[at * HD + V * lane + i] = acc[i] * inv;
+        if (lane == 0) t.common_lse[at] = sum == 0.f ? -INFINITY : top + log2f(sum);
+        return;
+    }
+    if (joins) {
+        const size_t at = (size_t)(u.x + tok) * t.hq + head;
+        const Joined j(top, sum, t.common_lse[at]);
+        __nv_bfloat16* out = t.out + (int64_t)(u.x + tok) * t.out_row + (int64_t)head * t.out_head + V * lane;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            out[i] = __float2bfloat16_rn(fmaf(acc[i], j.own, t.common_out[at * HD + V * lane + i] * j.other));
+        if (t.lse && lane == 0) t.lse[at] = j.lse * kLn2;
+        return;
+    }
     __nv_bfloat16* out = t.out + (int64_t)(u.x + tok) * t.out_row + (int64_t)head * t.out_head + V * lane;
 #pragma unroll
     for (int i = 0; i < V; ++i) out[i] = __float2bfloat16_rn(acc[i] * inv);
@@ -603,22 +659,22 @@ int rows_of_unit(int G, int64_t n_rows, int64_t n_seqs) {
 // CTAs of an SM
 int resident(int rg) { return rg == kKv8TcRows ? 1 : rg == 8 ? 3 : 2; }
 
-template <int HD, int NQ>
+template <int HD, int NQ, int PART>
 cudaError_t launch_few(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s) {
-    auto kern = kv8_attention_kernel<HD, NQ>;
+    auto kern = kv8_attention_kernel<HD, NQ, PART>;
     constexpr int bytes = sizeof(Smem<HD, NQ>);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, s, a, t, p);
 }
 
-template <int HD>
+template <int HD, int PART>
 cudaError_t launch_merge(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, int64_t units, cudaStream_t s) {
     const int x = (int)std::min<int64_t>(p.ctas, units), rows = p.tq * p.G;
     if (units * rows <= kKv8Sms)
-        return launch_kv8(kv8_merge_kernel<HD, 16>, dim3(x, rows), kMergeThreads, 0, s, a, t, p);
+        return launch_kv8(kv8_merge_kernel<HD, 16, PART>, dim3(x, rows), kMergeThreads, 0, s, a, t, p);
     if (units * units < p.ctas)
-        return launch_kv8(kv8_merge_kernel<HD, 8>, dim3(x, (rows + 1) / 2), kMergeThreads, 0, s, a, t, p);
-    return launch_kv8(kv8_merge_kernel<HD, 2>, dim3(x, (rows + 7) / 8), kMergeThreads, 0, s, a, t, p);
+        return launch_kv8(kv8_merge_kernel<HD, 8, PART>, dim3(x, (rows + 1) / 2), kMergeThreads, 0, s, a, t, p);
+    return launch_kv8(kv8_merge_kernel<HD, 2, PART>, dim3(x, (rows + 7) / 8), kMergeThreads, 0, s, a, t, p);
 }
 
 // The plan of a call; false if its line of tiles is too long for 32 bits.
@@ -665,25 +721,45 @@ bool kv8_attention_fits(const Kv8Args& a, int hq) {
     return make_plan(a, hq, p, units, tiles);
 }
 
-cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, bool& merge) {
+namespace {
+
+// f with the part as a constant
+template <class F>
+cudaError_t with_part(Kv8Part part, F&& f) {
+    switch (part) {
+        case kCommon: return f(std::integral_constant<int, kCommon>{});
+        case kTail: return f(std::integral_constant<int, kTail>{});
+        default: return f(std::integral_constant<int, kWhole>{});
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, bool& merge, Kv8Part part) {
     Kv8Plan p;
     int64_t units, tiles;
     merge = false;
     if (!make_launch(a, t, p, units, tiles)) return cudaErrorInvalidValue;
     merge = tiles > 1;
-    auto few = [&](auto hd) {
-        constexpr int HD = decltype(hd)::value;
-        return p.rg == 8 ? launch_few<HD, 1>(a, t, p, s) : launch_few<HD, 2>(a, t, p, s);
-    };
-    if (p.rg == kKv8TcRows) return launch_kv8_tc(a, t, p, s);
-    return a.hd == 128 ? few(std::integral_constant<int, 128>{}) : few(std::integral_constant<int, 64>{});
+    if (p.rg == kKv8TcRows) return launch_kv8_tc(a, t, p, s, part);
+    return with_part(part, [&](auto c) {
+        constexpr int PART = decltype(c)::value;
+        auto few = [&](auto hd) {
+            constexpr int HD = decltype(hd)::value;
+            return p.rg == 8 ? launch_few<HD, 1, PART>(a, t, p, s) : launch_few<HD, 2, PART>(a, t, p, s);
+        };
+        return a.hd == 128 ? few(std::integral_constant<int, 128>{}) : few(std::integral_constant<int, 64>{});
+    });
 }
 
-cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s) {
+cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, Kv8Part part) {
     Kv8Plan p;
     int64_t units, tiles;
     if (!make_launch(a, t, p, units, tiles)) return cudaErrorInvalidValue;
-    return a.hd == 128 ? launch_merge<128>(a, t, p, units, s) : launch_merge<64>(a, t, p, units, s);
+    return with_part(part, [&](auto c) {
+        constexpr int PART = decltype(c)::value;
+        return a.hd == 128 ? launch_merge<128, PART>(a, t, p, units, s) : launch_merge<64, PART>(a, t, p, units, s);
+    });
 }
 
 }  // namespace ks

@@ -43,16 +43,36 @@ struct Kv8Plan {
     KS_DEV int page_of(int block, int bpp) const { return block_log >= 0 ? block >> block_log : block / bpp; }
 };
 
+// A sequence of a launch.  A group with nothing in common has no units.
+template <int PART>
+KS_DEV Kv8Seq seq_of(const Kv8Args& a, int s) {
+    Kv8Seq q = kv8_seq(a, s);
+    if (PART == kCommon && q.len == 0) q.rows = 0;
+    return q;
+}
+// Last key of group g.
+template <int PART>
+KS_DEV int last_key(const Kv8Seq& q, const Kv8Plan& p, int g) {
+    return PART == kCommon ? q.len - 1 : q.len - q.rows + min(q.rows, (g + 1) * p.tq) - 1;
+}
 // Tiles of group g; a group whose rows see nothing has one as well (its rows get zeros).
+template <int PART>
 KS_DEV int group_tiles(const Kv8Seq& q, const Kv8Plan& p, int g) {
-    const int last = q.len - q.rows + min(q.rows, (g + 1) * p.tq) - 1;
+    const int last = last_key<PART>(q, p, g);
     return last < 0 ? 1 : (last >> p.tile_log) + 1;
+}
+// Where a sequence's pages begin in the table.
+template <int PART>
+KS_DEV const int32_t* pages_of(const Kv8Args& a, int s) {
+    return a.table + (PART == kWhole ? (int64_t)s * a.table_ld : a.first_page[s]);
 }
 KS_DEV int groups_of(const Kv8Seq& q, int tq) { return q.rows <= tq ? q.rows > 0 : (q.rows + tq - 1) / tq; }
 // What the units of one head of a sequence take on the line of all units.
+template <int PART>
 KS_DEV int head_length(const Kv8Seq& q, const Kv8Plan& p) {
+    if (PART == kCommon) return groups_of(q, p.tq) * (group_tiles<PART>(q, p, 0) + p.cost);
     int n = 0;
-    for (int g = 0, groups = groups_of(q, p.tq); g < groups; ++g) n += group_tiles(q, p, g) + p.cost;
+    for (int g = 0, groups = groups_of(q, p.tq); g < groups; ++g) n += group_tiles<PART>(q, p, g) + p.cost;
     return n;
 }
 
@@ -75,11 +95,12 @@ struct Run {
 };
 
 // A segment: tiles [tile, end) of a unit, whose first tile is at `first` on the line.
+template <int PART = kWhole>
 struct Segment {
     int s, h, g, tile, end, tiles, first;
     Kv8Seq q;
     KS_DEV void at(const Run& r, const Kv8Plan& p, int start) {
-        tiles = group_tiles(q, p, g);
+        tiles = group_tiles<PART>(q, p, g);
         first = start + p.cost;
         tile = max(0, r.x0 - first);
         end = min(tiles, r.x1 - first);
@@ -94,7 +115,7 @@ struct Segment {
                 h = 0;
                 do {
                     if (++s >= a.n_seqs) return false;
-                    q = kv8_seq(a, s);
+                    q = seq_of<PART>(a, s);
                 } while (q.rows == 0);
             }
         }
@@ -107,7 +128,8 @@ struct Segment {
 // it by itself, 32 sequences at a time.  Where offsets decrease, no CTA has one:
 // sequences that share rows could be more units than the host counted, and their
 // line longer than an int.
-KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
+template <int PART>
+KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment<PART>& k) {
     const int lane = threadIdx.x & 31, cta = blockIdx.x;
     Kv8Seq mine{};
     int head = 0;                                // length of one of its heads' units
@@ -118,9 +140,9 @@ KS_DEV bool find_run(const Kv8Args& a, const Kv8Plan& p, Run& r, Segment& k) {
             mine = Kv8Seq{};
             return 0;
         }
-        mine = kv8_seq(a, s);
+        mine = seq_of<PART>(a, s);
         falls |= a.offsets[s + 1] < a.offsets[s];
-        head = head_length(mine, p);
+        head = head_length<PART>(mine, p);
         return a.hk * head;
     };
     int total = 0, v = 0;
@@ -195,15 +217,33 @@ struct Rows {
     int n;              // query rows: tokens x G
     int row0;           // batch row of the first token
     int pos0;           // its position; negative positions see nothing
-    KS_DEV Rows(const Kv8Seq& q, int tq, int g, int G) {
+    int step;           // from a token's position to the next one's: 0 where all see the same
+    template <int PART>
+    KS_DEV Rows(const Segment<PART>& at, int tq, int G) : step(PART != kCommon) {
+        const Kv8Seq& q = at.q;
+        const int g = at.g;
         const int t0 = g * tq;
         tokens = min(q.rows - t0, tq);
         n = tokens * G;
         row0 = q.row0 + t0;
-        pos0 = q.len - q.rows + t0;
+        pos0 = PART == kCommon ? q.len - 1 : q.len - q.rows + t0;
+    }
+};
+// A row's sums m, l (base 2) of its own part joined with the common part's: the factors of the two outputs (own not
+// normalised, the other normalised) and the sum's logarithm.
+struct Joined {
+    float own, other, lse;
+    KS_DEV Joined(float m, float l, float common) {
+        const float top = fmaxf(m, common), ref = top == -INFINITY ? 0.f : top;
+        const float a = exp2_approx(m - ref), b = exp2_approx(common - ref), sum = fmaf(a, l, b);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        own = a * inv;
+        other = b * inv;
+        lse = sum == 0.f ? -INFINITY : ref + log2f(sum);
     }
 };
 
-cudaError_t launch_kv8_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s);   // kv8_tc.cu
+// kv8_tc.cu
+cudaError_t launch_kv8_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s, Kv8Part part);
 
 }  // namespace ks

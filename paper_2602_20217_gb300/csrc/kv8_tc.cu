@@ -167,7 +167,7 @@ KS_DEV bool far(float m) { return fabsf(m) >= kFar && m != -INFINITY; }
 KS_DEV void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 KS_DEV void convert_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 
-template <int HD>
+template <int HD, int KIND>
 __global__ void __launch_bounds__(kThreads, 1)
     kv8_tc_kernel(const Kv8Args a, const Kv8AttnArgs t, const Kv8Plan p, const __grid_constant__ CUtensorMap map) {
     using S = Smem<HD>;
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_dependency_wait();
     grid_launch_dependents();
     Run run;
-    Segment at;
+    Segment<KIND> at;
     const bool stopped = a.stop && *a.stop;
     const bool work = !stopped && find_run(a, p, run, at);
     if (!work && !stopped && tid == 0) p.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
@@ -216,11 +216,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ---------------------------------------------------------- copies
         // Page numbers are read a group of tiles ahead, across segments.
         constexpr int TILES = 32 / kBlocks;
-        auto pages = [&](const Segment& k, int tile) {
+        auto pages = [&](const Segment<KIND>& k, int tile) {
             const int b = tile * kBlocks + lane;
-            const int last = k.q.len - k.q.rows + min(k.q.rows, (k.g + 1) * p.tq) - 1;   // of the unit's keys
-            if (b * kKv8Block > last || tile + lane / kBlocks >= k.end) return -1;
-            const int page = a.table[(size_t)k.s * a.table_ld + p.page_of(b, a.bpp)];
+            if (b * kKv8Block > last_key<KIND>(k.q, p, k.g) || tile + lane / kBlocks >= k.end) return -1;
+            const int page = pages_of<KIND>(a, k.s)[p.page_of(b, a.bpp)];
             return page >= 0 && page < a.n_pages ? page : -2;
         };
         // a run of p.run records is one copy of keys and one of values
@@ -230,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float vref = 0.f;
         bool alive = true, more = true;
         while (more && alive) {
-            Segment next = at;
+            Segment<KIND> next = at;
             int next_tile = tile + TILES;
             if (next_tile >= at.end) {
                 more = next.next(a, run, p);
@@ -348,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool alive = true;
         int it = 0, seg = 0;
         do {
-            const Rows rows(at.q, p.tq, at.g, G);
+            const Rows rows(at, p.tq, G);
             for (int tile = at.tile; tile < at.end; ++tile, ++it) {
                 const int st = it % kRing, b = it & 1, near = it % kNear;
                 if (b == mine) alive = alive && mbar_wait(&sm.o_full[b], ((it >> 1) & 1) ^ 1, kWaitLimitNs);
@@ -448,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool alive = true, began = false;
         int it0 = 0, seg = 0, n = 0;                 // tiles before the segment, segments, tiles of this stream
         for (;;) {
-            const Rows rows(at.q, p.tq, at.g, G);
+            const Rows rows(at, p.tq, G);
             const int cnt = at.end - at.tile;
             // Few rows: they stand in the 128 two or four times, and the warps of a copy take 64 or 32 of a tile's keys
             // (TMEM lanes belong to warps: the other warps could not help with them).  Their weights of the other
@@ -511,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) mbar_arrive(&sm.q_full);
             }
             const float qf = sm.qf[row];
-            const int lim = row < rows.n ? rows.pos0 + p.token(row) : INT32_MAX;
+            const int lim = row < rows.n ? rows.pos0 + p.token(row) * rows.step : INT32_MAX;
             float m = -INFINITY, l = 0.f, vref = 0.f;
             bool first = true;
             auto rescale = [&](float fac) {           // O, once the products before are in it
@@ -720,9 +719,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float4 u0 = sm.join[0][lane_row], u1 = sm.join[1][lane_row];
             const float o0 = exp2_approx(u0.x - ref) * u0.z, o1 = exp2_approx(u1.x - ref) * u1.z;
             const bool whole = at.tile == 0 && at.end == at.tiles;
-            const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+            float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
             const bool valid = row < rows.n, any_nan = sm.any_nan[seg & 3];
             const int tok = valid ? p.token(row) : 0, head = at.h * G + (valid ? row - tok * G : 0);
+            const size_t common_at = (size_t)(rows.row0 + tok) * t.hq + head;
+            bool joins = false;                      // with what its group has in common
+            float other = 0.f, joined = 0.f;
+            if constexpr (KIND == kTail) {
+                joins = t.cut[at.s] > 0;
+                if (whole && joins) {
+                    const Joined j(top - kUp, sum, t.common_lse[common_at]);
+                    inv = j.own;
+                    other = j.other;
+                    joined = j.lse;
+                }
+            }
             float* slot = p.part + ((size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg + row) * (HD + 4);
             __nv_bfloat16* out = t.out + (int64_t)(rows.row0 + tok) * t.out_row + (int64_t)head * t.out_head;
             float* pile = reinterpret_cast<float*>(sm.q);        // free: every product with it is done
@@ -764,6 +775,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (any_nan && sm.nan_from[seg & 3][d0 + q] <= lim) v = __uint_as_float(0x7fc00000u);
                     x[q] = __float_as_uint(v);
                 }
+                if constexpr (KIND == kCommon) {
+                    if (whole) {
+                        float* to = t.common_out + common_at * HD + d0;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            *reinterpret_cast<uint4*>(to + 4 * q) = make_uint4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                        continue;
+                    }
+                }
+                if constexpr (KIND == kTail) {
+                    if (whole && joins) {
+                        const float* from = t.common_out + common_at * HD + d0;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            const float4 u = *reinterpret_cast<const float4*>(from + 4 * q);
+                            x[4 * q] = __float_as_uint(fmaf(u.x, other, __uint_as_float(x[4 * q])));
+                            x[4 * q + 1] = __float_as_uint(fmaf(u.y, other, __uint_as_float(x[4 * q + 1])));
+                            x[4 * q + 2] = __float_as_uint(fmaf(u.z, other, __uint_as_float(x[4 * q + 2])));
+                            x[4 * q + 3] = __float_as_uint(fmaf(u.w, other, __uint_as_float(x[4 * q + 3])));
+                        }
+                    }
+                }
                 if (!whole) {
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
@@ -785,11 +818,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (valid && i == 0 && quad < per) {
                 // l and o carry the factor 2^kUp
                 if (!whole) *reinterpret_cast<float2*>(slot) = make_float2(top - kUp, sum);
-                else if (t.lse) t.lse[(size_t)(rows.row0 + tok) * t.hq + head] = sum == 0.f ? -INFINITY : (top - kUp + log2f(sum)) * kLn2;
+                else if (KIND == kCommon) t.common_lse[common_at] = sum == 0.f ? -INFINITY : top - kUp + log2f(sum);
+                else if (KIND == kTail && joins) {
+                    if (t.lse) t.lse[common_at] = joined * kLn2;
+                } else if (t.lse) t.lse[(size_t)(rows.row0 + tok) * t.hq + head] = sum == 0.f ? -INFINITY : (top - kUp + log2f(sum)) * kLn2;
             }
             if (!whole && at.tile == 0) {
                 began = true;
-                if (tid == 0) p.desc[blockIdx.x] = make_int4(rows.row0, rows.n, at.h, run.cta_of(at.first + at.tiles - 1));
+                if (tid == 0) p.desc[blockIdx.x] = make_int4(rows.row0, rows.n, joins ? ~at.h : at.h, run.cta_of(at.first + at.tiles - 1));
             }
             if (copies > 1) softmax_sync();          // the pile is read: the next queries may go there
             umma_fence_before();
@@ -812,9 +848,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-template <int HD>
+template <int HD, int KIND>
 cudaError_t launch_tc(const Kv8Args& a, const Kv8AttnArgs& t, Kv8Plan p, cudaStream_t s) {
-    auto kern = kv8_tc_kernel<HD>;
+    auto kern = kv8_tc_kernel<HD, KIND>;
     constexpr int bytes = sizeof(Smem<HD>);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
@@ -828,8 +864,12 @@ cudaError_t launch_tc(const Kv8Args& a, const Kv8AttnArgs& t, Kv8Plan p, cudaStr
 
 }  // namespace
 
-cudaError_t launch_kv8_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s) {
-    return a.hd == 128 ? launch_tc<128>(a, t, p, s) : launch_tc<64>(a, t, p, s);
+cudaError_t launch_kv8_tc(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& p, cudaStream_t s, Kv8Part part) {
+    switch (part) {
+        case kCommon: return a.hd == 128 ? launch_tc<128, kCommon>(a, t, p, s) : launch_tc<64, kCommon>(a, t, p, s);
+        case kTail: return a.hd == 128 ? launch_tc<128, kTail>(a, t, p, s) : launch_tc<64, kTail>(a, t, p, s);
+        default: return a.hd == 128 ? launch_tc<128, kWhole>(a, t, p, s) : launch_tc<64, kWhole>(a, t, p, s);
+    }
 }
 
 }  // namespace ks

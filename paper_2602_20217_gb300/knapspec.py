@@ -85,6 +85,10 @@ class KsKv8Attn(C.Structure):
                 ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class KsKv8Shared(C.Structure):
+    _fields_ = [("group_offsets", C.c_void_p), ("tokens", C.c_void_p), ("n_groups", C.c_int32)]
+
+
 class KsLogprobs(C.Structure):
     _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32),
                 ("row_stride", C.c_int64), ("tokens", C.c_void_p), ("n_tokens", C.c_int32), ("n_top", C.c_int32),
@@ -151,6 +155,9 @@ _SIGS = {
                               C.c_int64, C.c_int64, C.c_void_p]),
     "ks_kv8_attention_workspace": (C.c_size_t, [C.POINTER(KsKv8Cache), C.c_int32, C.c_int32, C.c_int32]),
     "ks_kv8_attention": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Attn), C.c_void_p]),
+    "ks_kv8_shared_workspace": (C.c_size_t, [C.POINTER(KsKv8Cache), C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "ks_kv8_shared_attention": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Shared),
+                                          C.POINTER(KsKv8Attn), C.c_void_p]),
     "ks_token_logprobs": (C.c_int, [C.POINTER(KsLogprobs), C.c_void_p]),
     "ks_model_logprobs": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(KsLogprobs)]),
     "ks_status_str": (C.c_char_p, [C.c_int]),
@@ -491,6 +498,15 @@ def ks_kv8_attention_workspace(cache: KsKv8Cache, n_q_heads: int, n_seqs: int, n
 def ks_kv8_attention(cache: KsKv8Cache, batch: KsKv8Batch, attn: KsKv8Attn, stream=None):
     check(load().ks_kv8_attention(C.byref(cache), C.byref(batch), C.byref(attn), _stream_ptr(stream)),
           "ks_kv8_attention")
+
+
+def ks_kv8_shared_workspace(cache: KsKv8Cache, n_q_heads: int, n_seqs: int, n_rows: int, n_groups: int) -> int:
+    return int(load().ks_kv8_shared_workspace(C.byref(cache), n_q_heads, n_seqs, n_rows, n_groups))
+
+
+def ks_kv8_shared_attention(cache: KsKv8Cache, batch: KsKv8Batch, shared: KsKv8Shared, attn: KsKv8Attn, stream=None):
+    check(load().ks_kv8_shared_attention(C.byref(cache), C.byref(batch), C.byref(shared), C.byref(attn),
+                                         _stream_ptr(stream)), "ks_kv8_shared_attention")
 
 
 def ks_token_logprobs(args: KsLogprobs, stream=None):

@@ -63,6 +63,24 @@ class Batch8:
                                int(n_rows), ks._ptr(status))
 
 
+class Shared8:
+    """Groups of a batch's sequences with a common beginning: group_offsets int32 [n_groups + 1], tokens int32
+    [n_groups] on the device, whole pages on those that a group's first sequence names."""
+
+    def __init__(self, group_offsets, tokens):
+        dev = group_offsets.device
+        _check(group_offsets, "group_offsets", (torch.int32,), 1, dev)
+        _check(tokens, "tokens", (torch.int32,), 1, dev)
+        n = tokens.shape[0]
+        if n < 1 or group_offsets.shape[0] != n + 1:
+            raise ValueError(f"{n} groups, {group_offsets.shape[0]} offsets")
+        if not (group_offsets.is_contiguous() and tokens.is_contiguous()):
+            raise ValueError("group_offsets and tokens have to be contiguous")
+        self._keep = (group_offsets, tokens)
+        self.device, self.n_groups = dev, n
+        self.c = ks.KsKv8Shared(group_offsets.data_ptr(), tokens.data_ptr(), n)
+
+
 class Cache8:
     """One layer's cache.  data: uint8, at least nbytes of it (allocated here if not given)."""
 
@@ -140,18 +158,23 @@ class Cache8:
         ks.ks_kv8_read(self.c, batch.c, k_out.data_ptr(), v_out.data_ptr(), code, *strides, s)
         return k_out, v_out
 
-    def attention_workspace(self, n_q_heads: int, n_seqs: int, n_rows: int):
+    def attention_workspace(self, n_q_heads: int, n_seqs: int, n_rows: int, shared: Shared8 | None = None):
         """A workspace of attention() for these sizes or smaller ones; calls that run at once need one each."""
-        n = ks.ks_kv8_attention_workspace(self.c, n_q_heads, n_seqs, n_rows)
+        if shared is None:
+            n = ks.ks_kv8_attention_workspace(self.c, n_q_heads, n_seqs, n_rows)
+        else:
+            n = ks.ks_kv8_shared_workspace(self.c, n_q_heads, n_seqs, n_rows, shared.n_groups)
         if n == 0:
             raise ks.KsError(ks.KS_ERR_INVALID_ARG, "attention_workspace", f"{n_q_heads} query heads over "
                              f"{self.n_kv_heads}, {n_seqs} sequences, {n_rows} rows")
         return torch.empty(n, dtype=torch.uint8, device=self.device)
 
-    def attention(self, batch: Batch8, q, scale=None, out=None, lse=None, workspace=None, stream=None):
+    def attention(self, batch: Batch8, q, scale=None, out=None, lse=None, workspace=None, stream=None,
+                  shared: Shared8 | None = None):
         """Causal attention of the batch's rows: q, out [n_rows, n_q_heads, head_dim] bf16, lse [n_rows, n_q_heads]
         fp32.  scale: head_dim ** -0.5 if not given.  Returns out.  The address of a stream that is not the current
-        one needs out and workspace with it: torch cannot allocate for an address."""
+        one needs out and workspace with it: torch cannot allocate for an address.  shared: groups of sequences with a
+        common beginning, which is read once a group."""
         s = self._stream(stream)
         if stream is not None and (out is None or workspace is None) and \
                 s != torch._C._cuda_getCurrentRawStream(self.device.index):
@@ -160,7 +183,7 @@ class Cache8:
             # what the current stream allocates it may still write, the zeros below among it, and hand out again
             # while the call runs
             with _cuda.stream(stream):
-                return self.attention(batch, q, scale, out, lse, workspace)
+                return self.attention(batch, q, scale, out, lse, workspace, shared=shared)
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
         q_row, q_head = self._rows(q, "q", _BF16, batch)
@@ -175,10 +198,15 @@ class Cache8:
                 raise ValueError(f"lse: shape {tuple(lse.shape)}")
             sums = lse.data_ptr()
         if workspace is None:
-            workspace = self.attention_workspace(hq, batch.n_seqs, batch.n_rows)
+            workspace = self.attention_workspace(hq, batch.n_seqs, batch.n_rows, shared)
         elif workspace.device != self.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
             raise ValueError("workspace: contiguous bytes on the cache's device expected")
         a = ks.KsKv8Attn(q.data_ptr(), q_row, q_head, out.data_ptr(), o_row, o_head, sums, hq,
                          self.head_dim ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel())
-        ks.ks_kv8_attention(self.c, batch.c, a, s)
+        if shared is None:
+            ks.ks_kv8_attention(self.c, batch.c, a, s)
+        else:
+            if shared.device != self.device:
+                raise ValueError(f"the groups are on {shared.device}, the cache on {self.device}")
+            ks.ks_kv8_shared_attention(self.c, batch.c, shared.c, a, s)
         return out
