@@ -501,6 +501,8 @@ typedef struct {
     int32_t rope_rows;
     void* q_out;
     int64_t q_out_row, q_out_head;
+    const int32_t* shift;        /* dev [n_seqs], or NULL: the row of the table is the token's place in the cache plus
+                                    shift[s] (sequences that have lost tokens, see ks_kv8_evict) */
 } ks_kv8_rows;
 
 /* Bytes of a cache; 0 for sizes that are not supported. */
@@ -580,6 +582,67 @@ size_t ks_kv8_shared_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int
                                int32_t n_groups);
 ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_shared* shared,
                                   const ks_kv8_attn* attn, void* stream);
+
+/* The attention weight that every cached token receives from the batch's rows:
+ * for sequence s, KV head h and its tokens t < lengths[s]
+ *   out[s][h][t] = decay scores[s][h][t] + sum of exp(scale q k_t - lse)
+ * over the sequence's rows that see t and the query heads of h, lse [n_rows]
+ * [n_q_heads] being what the attention of these rows returned.  The rows' own
+ * tokens begin anew: their scores are not read; nor are any with a decay of 0,
+ * and scores may be NULL then.  out may be scores.  Sequences without rows, and
+ * places from lengths[s] on, are left as they are.
+ * Scores and sums are fp32; queries as in ks_kv8_attention.  A row with lse -inf
+ * gives no weight, a token on a page outside the pool receives none (status bit
+ * 0), a NaN key, query or lse makes the weights it enters NaN.  Where offsets
+ * decrease nothing is written.  A token's sum has one order: the same bits from
+ * call to call. */
+typedef struct {
+    const void* q;           /* dev, bf16, strides in elements */
+    int64_t q_row, q_head;
+    int32_t n_q_heads;
+    float scale, decay;
+    const float* lse;
+    const float* scores;     /* dev, [n_seqs][n_kv_heads][score_ld], score_ld >= the tokens of a table row */
+    float* out;
+    int64_t score_ld;
+} ks_kv8_weights;
+ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_weights* weights,
+                                   void* stream);
+
+/* Eviction: of every sequence and KV head keep n = min(keep[s], lengths[s])
+ * tokens, the last `recent`, then the first `first`, then of those between the
+ * ones with the largest scores (ties: the earlier token; NaN below all), in
+ * their order, as tokens 0 .. n - 1 on the pages of page_table; lengths[s] = n.
+ *   kept[s][h][i]        where token i was
+ *   new_scores[s][h][i]  its score (or NULL)
+ * Codes and scales are what an append of the kept values would give: a code is
+ * rounded only where it becomes subnormal.  The batch's row offsets are not read.
+ * The new pages hold none that the call reads, and one sequence's are not
+ * another's, except that a sequence that keeps all of its tokens may keep its
+ * pages (the whole table row or pages of it): blocks that stay where they are are
+ * not written.  kept, new_scores and lengths overlap nothing that is read.
+ * Places from n on are left as they are, tokens of the last block from n on are
+ * zeros.  Status bit 0: a page outside the pool (its tokens are read as zeros, or
+ * not written); bit 1: keep[s] below 0 or n above the new pages' tokens (taken as
+ * the nearest possible value).
+ * Heads keep tokens of their own, so a token's place no longer is its position:
+ * later appends that rotate give shift[s] = the tokens that s has lost (see
+ * ks_kv8_rows).  Attention, weights, reads and later evictions go by places. */
+typedef struct {
+    const float* scores;     /* dev, [n_seqs][n_kv_heads][score_ld] */
+    int64_t score_ld;
+    const int32_t* keep;     /* dev, [n_seqs] */
+    int32_t first, recent;
+    const int32_t* page_table;   /* dev, [n_seqs][table_ld], table_ld * page_tokens at most 2^30 */
+    int32_t table_ld;
+    int32_t* lengths;        /* dev, [n_seqs] */
+    int32_t* kept;           /* dev, [n_seqs][n_kv_heads][kept_ld], kept_ld >= table_ld * page_tokens */
+    int64_t kept_ld;
+    float* new_scores;       /* dev, [n_seqs][n_kv_heads][new_score_ld], likewise */
+    int64_t new_score_ld;
+} ks_kv8_eviction;
+ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_eviction* eviction,
+                       void* stream);
 
 /* ---------------------------------------------------- token log probabilities */
 

@@ -126,6 +126,9 @@ KS_DEV void rotate8(const float2 (&cs)[8], float (&a)[8], float (&b)[8]) {
 // after every 8 dims: threads 8 dims apart use different banks.
 KS_DEV int v_row(int d) { return d * 16 + (d >> 3) * 16; }
 
+// Position of the token in place `at` of sequence s.
+KS_DEV int64_t rope_position(const Kv8RowArgs& r, int s, int at) { return r.shift ? (int64_t)at + r.shift[s] : at; }
+
 // A block of KV head blockIdx.y.
 template <int HD, typename T, bool WIDE>
 KS_DEV void append_block(const Kv8Args& a, const Kv8RowArgs& r, const Kv8Slot& w, int group, int d0, int d1) {
@@ -163,9 +166,10 @@ KS_DEV void append_block(const Kv8Args& a, const Kv8RowArgs& r, const Kv8Slot& w
         raw[2].get(v[0]);
         raw[3].get(v[1]);
         if (r.rope) {
-            if (pos0 + t < r.rope_rows) {
+            const int64_t pos = rope_position(r, w.s, pos0 + t);
+            if (pos >= 0 && pos < r.rope_rows) {
                 float2 cs[8];
-                load_angles<WIDE>(r.rope + (size_t)(pos0 + t) * HD, d0, cs);
+                load_angles<WIDE>(r.rope + (size_t)pos * HD, d0, cs);
                 rotate8(cs, k[0], k[1]);
             } else {
                 if (d0 == 0) kv8_flag(a, kKv8BadPosition);
@@ -294,12 +298,14 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 6) kv8_append_k
         for (; blocks.get(w); blocks.b += blocks.step) {
             // a thread stays with one token; a block of few tokens has more threads for its heads
             const int tokens = w.last - w.first, ts = tokens > 8 ? 16 : tokens > 4 ? 8 : tokens > 2 ? 4 : tokens;
-            const int t = w.first + (group & (ts - 1)), pos = w.blk * kKv8Block + t, step = GROUPS / ts;
+            const int t = w.first + (group & (ts - 1)), step = GROUPS / ts;
             if (t >= w.last) continue;
             constexpr int U = 2;
             const T* src = static_cast<const T*>(r.q) + (int64_t)(w.row + t) * r.q_row;
             __nv_bfloat16* out = r.q_out + (int64_t)(w.row + t) * r.q_out_row;
-            const bool turn = r.rope != nullptr, past = turn && pos >= r.rope_rows;
+            const bool turn = r.rope != nullptr;
+            const int64_t pos = turn ? rope_position(r, w.s, w.blk * kKv8Block + t) : 0;
+            const bool past = turn && (pos < 0 || pos >= r.rope_rows);
             float2 cs[8];
             if (turn && !past) load_angles<WIDE>(r.rope + (size_t)pos * HD, d0, cs);
             for (int i = group / ts; i < heads; i += U * step) {
@@ -530,6 +536,10 @@ extern "C" ks_status ks_kv8_append(const ks_kv8_cache* cache, const ks_kv8_batch
         set_error("ks_kv8_append: a RoPE table of %d rows, or a misaligned one", rows->rope_rows);
         return KS_ERR_INVALID_ARG;
     }
+    if (!aligned(rows->shift, 4)) {
+        set_error("ks_kv8_append: misaligned shifts");
+        return KS_ERR_INVALID_ARG;
+    }
     if (rows->q) {
         if (rows->n_q_heads < 1 || rows->n_q_heads > kMaxHeads || !rows->q_out || !aligned(rows->q_out, 2) ||
             !strides_ok(rows->q_row, rows->q_head) || !strides_ok(rows->q_out_row, rows->q_out_head) ||
@@ -547,6 +557,7 @@ extern "C" ks_status ks_kv8_append(const ks_kv8_cache* cache, const ks_kv8_batch
     r.rope = rows->rope; r.rope_rows = rows->rope_rows;
     r.q_out = static_cast<__nv_bfloat16*>(rows->q_out);
     r.q_out_row = rows->q_out_row; r.q_out_head = rows->q_out_head;
+    r.shift = rows->shift;
     return launched(launch_kv8_append(rows->dtype, a, r, static_cast<cudaStream_t>(stream)), "ks_kv8_append");
 }
 
@@ -688,4 +699,103 @@ extern "C" ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks
     });
     if (st != KS_OK || a.n_seqs == 0 || a.n_rows == 0) return st;
     return launched(launch_kv8_shared(a, g, t, static_cast<cudaStream_t>(stream)), who);
+}
+
+extern "C" ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const ks_kv8_batch* batch,
+                                              const ks_kv8_weights* w, void* stream) {
+    const char* who = "ks_kv8_attention_weights";
+    Kv8Args a;
+    const ks_status st = kv8_args(who, cache, batch, a);
+    if (st != KS_OK) return st;
+    if (!w) {
+        set_error("%s: null argument", who);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (w->n_q_heads < 1 || w->n_q_heads > kMaxHeads || w->n_q_heads % a.hk) {
+        set_error("%s: %d query heads over %d KV heads", who, w->n_q_heads, a.hk);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (w->n_q_heads / a.hk > kKv8MaxGroup) {
+        set_error("%s: %d query heads a KV head (at most %d)", who, w->n_q_heads / a.hk, kKv8MaxGroup);
+        return KS_ERR_UNSUPPORTED;
+    }
+    if (!std::isfinite(w->scale) || !std::isfinite(w->decay)) {
+        set_error("%s: the scale or the decay is not finite", who);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (a.n_seqs == 0 || a.n_rows == 0) return KS_OK;
+    if (!w->q || !w->lse || !aligned(w->q, 2) || !aligned(w->lse, 4) || !strides_ok(w->q_row, w->q_head)) {
+        set_error("%s: null or misaligned queries or sums, or bad strides", who);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (!w->out || !aligned(w->out, 4) || !aligned(w->scores, 4) || (!w->scores && w->decay != 0.f) ||
+        w->score_ld < a.capacity || w->score_ld > (int64_t)1 << 40) {
+        set_error("%s: null or misaligned scores, or %lld of them for %d tokens", who, (long long)w->score_ld, a.capacity);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (!kv8_weights_fits(a, w->n_q_heads)) {
+        set_error("%s: %d sequences of up to %d tokens are too much for one call", who, a.n_seqs, a.capacity);
+        return KS_ERR_UNSUPPORTED;
+    }
+    Kv8WeightArgs t{};
+    t.q = static_cast<const __nv_bfloat16*>(w->q);
+    t.q_row = w->q_row; t.q_head = w->q_head;
+    t.hq = w->n_q_heads;
+    t.scale = w->scale;
+    t.decay = w->decay;
+    t.lse = w->lse;
+    t.scores = w->scores;
+    t.out = w->out;
+    t.ld = w->score_ld;
+    return launched(launch_kv8_weights(a, t, static_cast<cudaStream_t>(stream)), who);
+}
+
+extern "C" ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_eviction* ev,
+                                  void* stream) {
+    const char* who = "ks_kv8_evict";
+    Kv8Args a;
+    const ks_status st = kv8_args(who, cache, batch, a);
+    if (st != KS_OK) return st;
+    if (!ev) {
+        set_error("%s: null argument", who);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (ev->first < 0 || ev->recent < 0) {
+        set_error("%s: the first %d and the last %d tokens stay", who, ev->first, ev->recent);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (a.n_seqs == 0) return KS_OK;
+    if (ev->table_ld < 1 || (int64_t)ev->table_ld * cache->page_tokens > kMaxTokens) {
+        set_error("%s: a page table of %d pages of %d tokens", who, ev->table_ld, cache->page_tokens);
+        return KS_ERR_INVALID_ARG;
+    }
+    for (const void* p : {(const void*)ev->scores, (const void*)ev->keep, (const void*)ev->page_table,
+                          (const void*)ev->lengths, (const void*)ev->kept})
+        if (!p || !aligned(p, 4)) {
+            set_error("%s: null or misaligned scores, counts, pages, lengths or places", who);
+            return KS_ERR_INVALID_ARG;
+        }
+    const int room = ev->table_ld * cache->page_tokens;
+    const int64_t most = (int64_t)1 << 40;
+    if (!aligned(ev->new_scores, 4) || ev->score_ld < a.capacity || ev->kept_ld < room ||
+        (ev->new_scores && ev->new_score_ld < room) || ev->score_ld > most || ev->kept_ld > most || ev->new_score_ld > most) {
+        set_error("%s: %lld scores for %d tokens, or %lld places and %lld scores for %d", who, (long long)ev->score_ld,
+                  a.capacity, (long long)ev->kept_ld, (long long)ev->new_score_ld, room);
+        return KS_ERR_INVALID_ARG;
+    }
+    Kv8EvictArgs t{};
+    t.scores = ev->scores;
+    t.ld = ev->score_ld;
+    t.keep = ev->keep;
+    t.first = ev->first;
+    t.recent = ev->recent;
+    t.new_table = ev->page_table;
+    t.new_table_ld = ev->table_ld;
+    t.new_capacity = room;
+    t.new_lengths = ev->lengths;
+    t.kept = ev->kept;
+    t.kept_ld = ev->kept_ld;
+    t.new_scores = ev->new_scores;
+    t.new_ld = ev->new_score_ld;
+    return launched(launch_kv8_evict(a, t, static_cast<cudaStream_t>(stream)), who);
 }

@@ -27,6 +27,7 @@ struct Kv8RowArgs {         // the rows to append; strides in elements
     int rope_rows;
     __nv_bfloat16* q_out;
     int64_t q_out_row, q_out_head;
+    const int32_t* shift;   // [n_seqs] what a token's position is ahead of its place in the cache, or null
 };
 struct Kv8AttnArgs {
     const __nv_bfloat16* q;
@@ -65,6 +66,32 @@ cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_
 size_t kv8_shared_workspace(int hd, int hk, int hq, int n_seqs, int n_rows, int n_groups);
 bool kv8_shared_fits(const Kv8Args& a, const Kv8SharedArgs& g, int hq);
 cudaError_t launch_kv8_shared(const Kv8Args& a, const Kv8SharedArgs& g, const Kv8AttnArgs& t, cudaStream_t s);
+struct Kv8WeightArgs {      // the weight that tokens receive; scores, out: [n_seqs][hk][ld]
+    const __nv_bfloat16* q;
+    int64_t q_row, q_head;
+    int hq;
+    float scale, decay;
+    const float* lse;       // [n_rows][hq]
+    const float* scores;
+    float* out;
+    int64_t ld;
+};
+bool kv8_weights_fits(const Kv8Args& a, int hq);
+cudaError_t launch_kv8_weights(const Kv8Args& a, const Kv8WeightArgs& t, cudaStream_t s);
+struct Kv8EvictArgs {       // eviction into the pages of new_table
+    const float* scores;    // [n_seqs][hk][ld]
+    int64_t ld;
+    const int32_t* keep;    // [n_seqs]
+    int first, recent;
+    const int32_t* new_table;   // [n_seqs][new_table_ld]
+    int new_table_ld, new_capacity;
+    int32_t* new_lengths;   // [n_seqs]
+    int32_t* kept;          // [n_seqs][hk][kept_ld]
+    int64_t kept_ld;
+    float* new_scores;      // [n_seqs][hk][new_ld] or null
+    int64_t new_ld;
+};
+cudaError_t launch_kv8_evict(const Kv8Args& a, const Kv8EvictArgs& t, cudaStream_t s);
 // Map of the 8-bit cache's records (gemv.cu): boxes of box_records records' keys, or values.
 bool make_kv8_map(CUtensorMap* map, const void* base, uint64_t records, uint32_t hd, uint32_t box_records);
 

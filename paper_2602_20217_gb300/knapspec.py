@@ -76,7 +76,8 @@ class KsKv8Rows(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("dtype", C.c_int32),
                 ("n_q_heads", C.c_int32), ("k_row", C.c_int64), ("k_head", C.c_int64), ("v_row", C.c_int64),
                 ("v_head", C.c_int64), ("q_row", C.c_int64), ("q_head", C.c_int64), ("rope", C.c_void_p),
-                ("rope_rows", C.c_int32), ("q_out", C.c_void_p), ("q_out_row", C.c_int64), ("q_out_head", C.c_int64)]
+                ("rope_rows", C.c_int32), ("q_out", C.c_void_p), ("q_out_row", C.c_int64), ("q_out_head", C.c_int64),
+                ("shift", C.c_void_p)]
 
 
 class KsKv8Attn(C.Structure):
@@ -87,6 +88,18 @@ class KsKv8Attn(C.Structure):
 
 class KsKv8Shared(C.Structure):
     _fields_ = [("group_offsets", C.c_void_p), ("tokens", C.c_void_p), ("n_groups", C.c_int32)]
+
+
+class KsKv8Weights(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64), ("n_q_heads", C.c_int32),
+                ("scale", C.c_float), ("decay", C.c_float), ("lse", C.c_void_p), ("scores", C.c_void_p),
+                ("out", C.c_void_p), ("score_ld", C.c_int64)]
+
+
+class KsKv8Eviction(C.Structure):
+    _fields_ = [("scores", C.c_void_p), ("score_ld", C.c_int64), ("keep", C.c_void_p), ("first", C.c_int32),
+                ("recent", C.c_int32), ("page_table", C.c_void_p), ("table_ld", C.c_int32), ("lengths", C.c_void_p),
+                ("kept", C.c_void_p), ("kept_ld", C.c_int64), ("new_scores", C.c_void_p), ("new_score_ld", C.c_int64)]
 
 
 class KsLogprobs(C.Structure):
@@ -158,6 +171,9 @@ _SIGS = {
     "ks_kv8_shared_workspace": (C.c_size_t, [C.POINTER(KsKv8Cache), C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
     "ks_kv8_shared_attention": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Shared),
                                           C.POINTER(KsKv8Attn), C.c_void_p]),
+    "ks_kv8_attention_weights": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Weights),
+                                           C.c_void_p]),
+    "ks_kv8_evict": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Eviction), C.c_void_p]),
     "ks_token_logprobs": (C.c_int, [C.POINTER(KsLogprobs), C.c_void_p]),
     "ks_model_logprobs": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(KsLogprobs)]),
     "ks_status_str": (C.c_char_p, [C.c_int]),
@@ -507,6 +523,15 @@ def ks_kv8_shared_workspace(cache: KsKv8Cache, n_q_heads: int, n_seqs: int, n_ro
 def ks_kv8_shared_attention(cache: KsKv8Cache, batch: KsKv8Batch, shared: KsKv8Shared, attn: KsKv8Attn, stream=None):
     check(load().ks_kv8_shared_attention(C.byref(cache), C.byref(batch), C.byref(shared), C.byref(attn),
                                          _stream_ptr(stream)), "ks_kv8_shared_attention")
+
+
+def ks_kv8_attention_weights(cache: KsKv8Cache, batch: KsKv8Batch, weights: KsKv8Weights, stream=None):
+    check(load().ks_kv8_attention_weights(C.byref(cache), C.byref(batch), C.byref(weights), _stream_ptr(stream)),
+          "ks_kv8_attention_weights")
+
+
+def ks_kv8_evict(cache: KsKv8Cache, batch: KsKv8Batch, eviction: KsKv8Eviction, stream=None):
+    check(load().ks_kv8_evict(C.byref(cache), C.byref(batch), C.byref(eviction), _stream_ptr(stream)), "ks_kv8_evict")
 
 
 def ks_token_logprobs(args: KsLogprobs, stream=None):

@@ -118,9 +118,10 @@ class Cache8:
                              f"{'any' if heads is None else heads} heads of {self.head_dim} contiguous values")
         return stride[0], stride[1]
 
-    def append(self, batch: Batch8, k, v, rope=None, q=None, q_out=None, stream=None):
+    def append(self, batch: Batch8, k, v, rope=None, q=None, q_out=None, stream=None, shift=None):
         """Append k, v [n_rows, n_kv_heads, head_dim] (fp32 or bf16); rope [positions, head_dim / 2, 2] fp32 rotates
-        the keys, and the queries q [n_rows, n_q_heads, head_dim] into q_out (bf16)."""
+        the keys, and the queries q [n_rows, n_q_heads, head_dim] into q_out (bf16).  shift: int32 [n_seqs], what a
+        sequence has lost by eviction: its tokens' positions are so far ahead of their places."""
         s = self._stream(stream)
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
@@ -134,6 +135,8 @@ class Cache8:
                     shape[1] != self.head_dim // 2 or shape[2] != 2 or not rope.is_contiguous():
                 raise ValueError(f"rope: {rope.dtype} of shape {tuple(shape)} on {rope.device}")
             angles, positions = rope.data_ptr(), shape[0]
+        if shift is not None:
+            self._per_seq(shift, "shift", batch)
         if q is None and q_out is None:
             r = ks.KsKv8Rows(k.data_ptr(), v.data_ptr(), None, code, 0, k_row, k_head, v_row, v_head, 0, 0, angles,
                              positions)
@@ -144,7 +147,22 @@ class Cache8:
             o_row, o_head = self._rows(q_out, "q_out", _BF16, batch, q.shape[1])
             r = ks.KsKv8Rows(k.data_ptr(), v.data_ptr(), q.data_ptr(), code, q.shape[1], k_row, k_head, v_row, v_head,
                              q_row, q_head, angles, positions, q_out.data_ptr(), o_row, o_head)
+        if shift is not None:
+            r.shift = shift.data_ptr()
         ks.ks_kv8_append(self.c, batch.c, r, s)
+
+    def _per_seq(self, t, name, batch):
+        _check(t, name, (torch.int32,), 1, self.device)
+        if t.shape[0] < batch.n_seqs or not t.is_contiguous():
+            raise ValueError(f"{name}: shape {tuple(t.shape)} for {batch.n_seqs} sequences")
+
+    def _per_token(self, t, name, dtype, batch, tokens):
+        """Tokens of a head in a [sequences, heads, tokens] tensor, after its checks."""
+        _check(t, name, (dtype,), 3, self.device)
+        if t.shape[0] < batch.n_seqs or t.shape[1] != self.n_kv_heads or t.shape[2] < tokens or not t.is_contiguous():
+            raise ValueError(f"{name}: shape {tuple(t.shape)} for {batch.n_seqs} sequences, {self.n_kv_heads} heads, "
+                             f"{tokens} tokens")
+        return t.shape[2]
 
     def read(self, batch: Batch8, k_out, v_out, stream=None):
         """The values of the batch's rows into k_out, v_out [n_rows, n_kv_heads, head_dim] (fp32 or bf16)."""
@@ -210,3 +228,51 @@ class Cache8:
                 raise ValueError(f"the groups are on {shared.device}, the cache on {self.device}")
             ks.ks_kv8_shared_attention(self.c, batch.c, shared.c, a, s)
         return out
+
+    def attention_weights(self, batch: Batch8, q, lse, scores, scale=None, decay=1.0, out=None, stream=None):
+        """Add the weight that each token receives from the batch's rows to scores [n_seqs, n_kv_heads, tokens of a
+        page table row] fp32, times decay: q [n_rows, n_q_heads, head_dim] bf16 and lse [n_rows, n_q_heads] as
+        attention() took and returned them.  Into out, or scores itself; scores may be None with a decay of 0 and an
+        out.  Returns out."""
+        s = self._stream(stream)
+        if batch.device != self.device:
+            raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
+        q_row, q_head = self._rows(q, "q", _BF16, batch)
+        hq = q.shape[1]
+        _check(lse, "lse", (torch.float32,), 2, self.device)
+        if lse.shape[0] < batch.n_rows or lse.shape[1] != hq or not lse.is_contiguous():
+            raise ValueError(f"lse: shape {tuple(lse.shape)}")
+        tokens = batch.c.table_ld * self.c.page_tokens
+        if out is None:
+            out = scores
+        if out is None or (scores is None and decay != 0):
+            raise ValueError("scores: to be given, unless there is an out and the decay is 0")
+        ld = self._per_token(out, "out", torch.float32, batch, tokens)
+        if scores is not None and self._per_token(scores, "scores", torch.float32, batch, tokens) != ld:
+            raise ValueError("scores and out differ in their tokens")
+        ks.ks_kv8_attention_weights(self.c, batch.c, ks.KsKv8Weights(
+            q.data_ptr(), q_row, q_head, hq, self.head_dim ** -0.5 if scale is None else scale, decay, lse.data_ptr(),
+            None if scores is None else scores.data_ptr(), out.data_ptr(), ld), s)
+        return out
+
+    def evict(self, batch: Batch8, scores, keep, page_table, lengths, kept, new_scores=None, first: int = 0,
+              recent: int = 0, stream=None):
+        """Keep min(keep[s], length) tokens of each sequence and head, the last `recent`, the first `first` and the ones
+        with the largest scores [n_seqs, n_kv_heads, tokens of a page table row], on the pages of page_table, whose
+        lengths come with them; kept int32 and new_scores fp32 [n_seqs, n_kv_heads, tokens of a row of page_table]
+        receive where the tokens were and their scores."""
+        s = self._stream(stream)
+        if batch.device != self.device:
+            raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
+        ld = self._per_token(scores, "scores", torch.float32, batch, batch.c.table_ld * self.c.page_tokens)
+        self._per_seq(keep, "keep", batch)
+        self._per_seq(lengths, "lengths", batch)
+        _check(page_table, "page_table", (torch.int32,), 2, self.device)
+        if page_table.shape[0] < batch.n_seqs or not page_table.is_contiguous():
+            raise ValueError(f"page_table: shape {tuple(page_table.shape)}, strides {page_table.stride()}")
+        tokens = page_table.shape[1] * self.c.page_tokens
+        kept_ld = self._per_token(kept, "kept", torch.int32, batch, tokens)
+        new_ld = 0 if new_scores is None else self._per_token(new_scores, "new_scores", torch.float32, batch, tokens)
+        ks.ks_kv8_evict(self.c, batch.c, ks.KsKv8Eviction(
+            scores.data_ptr(), ld, keep.data_ptr(), first, recent, page_table.data_ptr(), page_table.shape[1],
+            lengths.data_ptr(), kept.data_ptr(), kept_ld, None if new_scores is None else new_scores.data_ptr(), new_ld), s)
