@@ -591,9 +591,11 @@ ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks_kv8_batch*
  * tokens begin anew: their scores are not read; nor are any with a decay of 0,
  * and scores may be NULL then.  out may be scores.  Sequences without rows, and
  * places from lengths[s] on, are left as they are.
- * Scores and sums are fp32; queries as in ks_kv8_attention.  A row with lse -inf
- * gives no weight, a token on a page outside the pool receives none (status bit
- * 0), a NaN key, query or lse makes the weights it enters NaN.  Where offsets
+ * Scores and sums are fp32; queries as in ks_kv8_attention, or exact (in calls
+ * of many rows).  A row with lse -inf gives no weight to keys that are numbers, a
+ * token on a page outside the pool receives none (status bit 0), a NaN key, query
+ * or lse makes the weights it enters NaN (the lse of a row with an infinite query
+ * is NaN).  Where offsets
  * decrease nothing is written.  A token's sum has one order: the same bits from
  * call to call. */
 typedef struct {
@@ -605,7 +607,11 @@ typedef struct {
     const float* scores;     /* dev, [n_seqs][n_kv_heads][score_ld], score_ld >= the tokens of a table row */
     float* out;
     int64_t score_ld;
+    void* workspace;         /* dev, 256-byte aligned, ks_kv8_attention_weights_workspace() bytes for these query
+                                heads and rows (0 for few: NULL will do); calls that run at once need one each */
+    size_t workspace_bytes;
 } ks_kv8_weights;
+size_t ks_kv8_attention_weights_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_rows);
 ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const ks_kv8_batch* batch, const ks_kv8_weights* weights,
                                    void* stream);
 

@@ -15,7 +15,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libknapspec.so")
 SOURCES = ["chain.cu", "gemv.cu", "attn.cu", "select.cu", "sample.cu", "dp.cu", "model.cu", "wide.cu", "wide_attn.cu",
            "kv8.cu", "kv8_attn.cu", "kv8_tc.cu", "kv8_shared.cu", "kv8_weights.cu",
-           "kv8_evict.cu", "logprob.cu"]
+           "kv8_weights_tc.cu", "kv8_evict.cu", "logprob.cu"]
 HEADERS = ["common.cuh", "internal.h", "tma.cuh", "umma.cuh", "kv8.h", "kv8.cuh", "kv8_plan.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]

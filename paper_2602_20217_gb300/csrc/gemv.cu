@@ -275,6 +275,19 @@ bool make_kv8_map(CUtensorMap* map, const void* base, uint64_t records, uint32_t
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_kv8_query_map(CUtensorMap* map, const void* q, uint64_t n_rows, uint32_t hq, uint32_t hd, int64_t row, int64_t head,
+                        uint32_t box_heads, uint32_t box_rows) {
+    auto encode = tensor_map_encoder();
+    if (!encode || (reinterpret_cast<uintptr_t>(q) & 15) != 0 || row % 8 || head % 8 || row < hd || head < hd) return false;
+    const cuuint64_t dims[3] = {hd, hq, n_rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)head * 2, (cuuint64_t)row * 2};
+    const cuuint32_t box[3] = {64, box_heads, box_rows};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_wide_kv_map(CUtensorMap* map, const void* base, uint64_t rows, uint32_t hd) {
     auto encode = tensor_map_encoder();
     if (!encode || hd % 64 != 0 || (reinterpret_cast<uintptr_t>(base) & 15) != 0) return false;

@@ -701,6 +701,11 @@ extern "C" ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks
     return launched(launch_kv8_shared(a, g, t, static_cast<cudaStream_t>(stream)), who);
 }
 
+extern "C" size_t ks_kv8_attention_weights_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_rows) {
+    if (ks_kv8_attention_workspace(cache, n_q_heads, 1, n_rows) == 0) return 0;
+    return kv8_weights_workspace(n_q_heads / cache->n_kv_heads, n_rows, 1);
+}
+
 extern "C" ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const ks_kv8_batch* batch,
                                               const ks_kv8_weights* w, void* stream) {
     const char* who = "ks_kv8_attention_weights";
@@ -737,7 +742,17 @@ extern "C" ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const k
         set_error("%s: %d sequences of up to %d tokens are too much for one call", who, a.n_seqs, a.capacity);
         return KS_ERR_UNSUPPORTED;
     }
+    const size_t need = kv8_weights_workspace(w->n_q_heads / a.hk, a.n_rows, a.n_seqs);
+    if (need > 0 && (!w->workspace || !aligned(w->workspace, 256))) {
+        set_error("%s: null or misaligned workspace", who);
+        return KS_ERR_INVALID_ARG;
+    }
+    if (w->workspace_bytes < need) {
+        set_error("%s: a workspace of %zu bytes, %zu needed", who, w->workspace_bytes, need);
+        return KS_ERR_WORKSPACE;
+    }
     Kv8WeightArgs t{};
+    t.workspace = w->workspace;
     t.q = static_cast<const __nv_bfloat16*>(w->q);
     t.q_row = w->q_row; t.q_head = w->q_head;
     t.hq = w->n_q_heads;

@@ -75,8 +75,16 @@ struct Kv8WeightArgs {      // the weight that tokens receive; scores, out: [n_s
     const float* scores;
     float* out;
     int64_t ld;
+    void* workspace;        // kv8_weights_workspace() bytes
 };
 bool kv8_weights_fits(const Kv8Args& a, int hq);
+size_t kv8_weights_workspace(int group, int64_t n_rows, int64_t n_seqs);
+size_t kv8_weights_tc_workspace();
+// Many query rows a sequence (kv8_weights_tc.cu); taken: false where the queries are no operand of tensor copies.
+cudaError_t launch_kv8_weights_tc(const Kv8Args& a, const Kv8WeightArgs& t, cudaStream_t s, bool& taken);
+// Map of rows of queries: boxes of 64 dims x box_heads heads x box_rows rows with the 128-byte swizzle (gemv.cu).
+bool make_kv8_query_map(CUtensorMap* map, const void* q, uint64_t n_rows, uint32_t hq, uint32_t hd, int64_t row, int64_t head,
+                        uint32_t box_heads, uint32_t box_rows);
 cudaError_t launch_kv8_weights(const Kv8Args& a, const Kv8WeightArgs& t, cudaStream_t s);
 struct Kv8EvictArgs {       // eviction into the pages of new_table
     const float* scores;    // [n_seqs][hk][ld]

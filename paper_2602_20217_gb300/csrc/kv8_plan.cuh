@@ -211,6 +211,21 @@ KS_DEV float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two fp32 operations in one instruction.
+KS_DEV float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("{ .reg .b64 x, y, z; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; mov.b64 z, {%5, %6}; fma.rn.f32x2 %0, x, y, z; }"
+        : "=l"(r)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
+}
+KS_DEV float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("{ .reg .b64 x, y; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; add.rn.f32x2 %0, x, y; }"
+        : "=l"(r)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
+}
 // A unit's rows, as its segments and the merge see them.
 struct Rows {
     int tokens;

@@ -102,20 +102,6 @@ KS_DEV uint64_t desc_plain(uint32_t addr, uint32_t lbo, uint32_t sbo) {
 // fp32 accumulators; e4m3 for kind::f8f6f4 and f16 for kind::f16 are both type 0
 __host__ __device__ constexpr uint32_t idesc_of(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24); }
 
-KS_DEV float2 fma2(float2 a, float2 b, float2 c) {
-    uint64_t r;
-    asm("{ .reg .b64 x, y, z; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; mov.b64 z, {%5, %6}; fma.rn.f32x2 %0, x, y, z; }"
-        : "=l"(r)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
-}
-KS_DEV float2 add2(float2 a, float2 b) {
-    uint64_t r;
-    asm("{ .reg .b64 x, y; mov.b64 x, {%1, %2}; mov.b64 y, {%3, %4}; add.rn.f32x2 %0, x, y; }"
-        : "=l"(r)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return make_float2(__uint_as_float((uint32_t)r), __uint_as_float((uint32_t)(r >> 32)));
-}
 // Whether three phases have ended, without waiting: a look takes a hundred clocks, the three overlap.
 KS_DEV void mbar_look(const uint64_t* a, int pa, const uint64_t* b, int pb, const uint64_t* c, int pc, bool& ra, bool& rb,
                       bool& rc) {

@@ -137,28 +137,35 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_weights_kernel(const Kv8Args 
     do {
         const Rows rows(at, p.tq, G);
         const int chunks = (rows.n + kChunk - 1) / kChunk;
-        // the record of this warp's block kb of a tile, null if there is none
-        auto record = [&](int tile, int kb) -> const unsigned char* {
-            const int b = tile * (kTile / kKv8Block) + warp * kWarpBlocks + kb;
-            if (tile >= at.end || b * kKv8Block >= at.q.len) return nullptr;
-            const int page = a.table[(size_t)at.s * a.table_ld + p.page_of(b, a.bpp)];
-            if (page < 0 || page >= a.n_pages) {
-                if (lane == 0) kv8_flag(a, kKv8BadPage);
-                return nullptr;
+        // the pages of this warp's blocks of a tile (-1: no such block), two tiles ahead: an address that waits for
+        // its page holds up everything behind it
+        int page[kWarpBlocks];
+        auto look = [&](int tile) {
+#pragma unroll
+            for (int kb = 0; kb < kWarpBlocks; ++kb) {
+                const int b = tile * (kTile / kKv8Block) + warp * kWarpBlocks + kb;
+                page[kb] = -1;
+                if (tile < at.end && b * kKv8Block < at.q.len) {
+                    page[kb] = a.table[(size_t)at.s * a.table_ld + p.page_of(b, a.bpp)];
+                    if (page[kb] < 0) page[kb] = -2;
+                }
             }
-            return a.data + (((size_t)page * a.hk + at.h) * a.bpp + b - p.page_of(b, a.bpp) * a.bpp) * REC;
         };
         Keys<HD> next[kWarpBlocks];
         bool next_there[kWarpBlocks];
         auto fetch = [&](int tile) {
 #pragma unroll
             for (int kb = 0; kb < kWarpBlocks; ++kb) {
-                const unsigned char* rec = record(tile, kb);
-                next_there[kb] = rec != nullptr;
-                next[kb].load(rec);
+                const int b = tile * (kTile / kKv8Block) + warp * kWarpBlocks + kb;
+                next_there[kb] = page[kb] >= 0 && page[kb] < a.n_pages;
+                if (!next_there[kb] && page[kb] != -1 && lane == 0) kv8_flag(a, kKv8BadPage);
+                next[kb].load(next_there[kb] ? a.data + (((size_t)page[kb] * a.hk + at.h) * a.bpp + b -
+                                                         p.page_of(b, a.bpp) * a.bpp) * REC : nullptr);
             }
         };
+        look(at.tile);
         fetch(at.tile);
+        look(at.tile + 1);
         int held = -1;                               // chunk in shared memory
         for (int tile = at.tile; tile < at.end; ++tile) {
             Keys<HD> k[kWarpBlocks];
@@ -169,6 +176,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_weights_kernel(const Kv8Args 
                 there[kb] = next_there[kb];
             }
             fetch(tile + 1);
+            look(tile + 2);
             const int key0 = tile * kTile + warp * kWarpBlocks * kKv8Block;
             float sum[kWarpBlocks][2] = {};
             // rows before the tile's first key see nothing of it
@@ -259,7 +267,17 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p) {
     return total <= INT32_MAX;
 }
 
+// Query rows a KV head and sequence, on average, from which on the tcgen05 kernel takes the call.
+constexpr int kManyRows = 17;
+bool many_rows(int64_t group, int64_t n_rows, int64_t n_seqs) { return group * n_rows >= kManyRows * n_seqs; }
+
 }  // namespace
+
+size_t kv8_weights_workspace(int group, int64_t n_rows, int64_t n_seqs) {
+    // a call with fewer sequences may be one of many rows
+    (void)n_seqs;
+    return group * n_rows >= kManyRows ? kv8_weights_tc_workspace() : 0;
+}
 
 bool kv8_weights_fits(const Kv8Args& a, int hq) {
     const int64_t tiles = ((int64_t)a.capacity + kTile - 1) / kTile;
@@ -267,6 +285,11 @@ bool kv8_weights_fits(const Kv8Args& a, int hq) {
 }
 
 cudaError_t launch_kv8_weights(const Kv8Args& a, const Kv8WeightArgs& t, cudaStream_t s) {
+    if (many_rows(t.hq / a.hk, a.n_rows, a.n_seqs)) {
+        bool taken;
+        const cudaError_t e = launch_kv8_weights_tc(a, t, s, taken);
+        if (taken) return e;
+    }
     Kv8Plan p;
     if (!make_plan(a, t.hq, p)) return cudaErrorInvalidValue;
     const bool wide = reinterpret_cast<uintptr_t>(t.q) % 16 == 0 && t.q_row % 8 == 0 && t.q_head % 8 == 0;

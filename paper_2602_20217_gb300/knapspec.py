@@ -93,7 +93,7 @@ class KsKv8Shared(C.Structure):
 class KsKv8Weights(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64), ("n_q_heads", C.c_int32),
                 ("scale", C.c_float), ("decay", C.c_float), ("lse", C.c_void_p), ("scores", C.c_void_p),
-                ("out", C.c_void_p), ("score_ld", C.c_int64)]
+                ("out", C.c_void_p), ("score_ld", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 class KsKv8Eviction(C.Structure):
@@ -171,6 +171,7 @@ _SIGS = {
     "ks_kv8_shared_workspace": (C.c_size_t, [C.POINTER(KsKv8Cache), C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
     "ks_kv8_shared_attention": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Shared),
                                           C.POINTER(KsKv8Attn), C.c_void_p]),
+    "ks_kv8_attention_weights_workspace": (C.c_size_t, [C.POINTER(KsKv8Cache), C.c_int32, C.c_int32]),
     "ks_kv8_attention_weights": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Weights),
                                            C.c_void_p]),
     "ks_kv8_evict": (C.c_int, [C.POINTER(KsKv8Cache), C.POINTER(KsKv8Batch), C.POINTER(KsKv8Eviction), C.c_void_p]),
@@ -523,6 +524,10 @@ def ks_kv8_shared_workspace(cache: KsKv8Cache, n_q_heads: int, n_seqs: int, n_ro
 def ks_kv8_shared_attention(cache: KsKv8Cache, batch: KsKv8Batch, shared: KsKv8Shared, attn: KsKv8Attn, stream=None):
     check(load().ks_kv8_shared_attention(C.byref(cache), C.byref(batch), C.byref(shared), C.byref(attn),
                                          _stream_ptr(stream)), "ks_kv8_shared_attention")
+
+
+def ks_kv8_attention_weights_workspace(cache: KsKv8Cache, n_q_heads: int, n_rows: int) -> int:
+    return int(load().ks_kv8_attention_weights_workspace(C.byref(cache), n_q_heads, n_rows))
 
 
 def ks_kv8_attention_weights(cache: KsKv8Cache, batch: KsKv8Batch, weights: KsKv8Weights, stream=None):

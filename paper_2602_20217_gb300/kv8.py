@@ -229,11 +229,18 @@ class Cache8:
             ks.ks_kv8_shared_attention(self.c, batch.c, shared.c, a, s)
         return out
 
-    def attention_weights(self, batch: Batch8, q, lse, scores, scale=None, decay=1.0, out=None, stream=None):
+    def weights_workspace(self, n_q_heads: int, n_rows: int):
+        """A workspace of attention_weights() for these sizes or smaller ones (empty for few rows); calls that run at
+        once need one each."""
+        return torch.empty(ks.ks_kv8_attention_weights_workspace(self.c, n_q_heads, n_rows), dtype=torch.uint8,
+                           device=self.device)
+
+    def attention_weights(self, batch: Batch8, q, lse, scores, scale=None, decay=1.0, out=None, workspace=None,
+                          stream=None):
         """Add the weight that each token receives from the batch's rows to scores [n_seqs, n_kv_heads, tokens of a
         page table row] fp32, times decay: q [n_rows, n_q_heads, head_dim] bf16 and lse [n_rows, n_q_heads] as
         attention() took and returned them.  Into out, or scores itself; scores may be None with a decay of 0 and an
-        out.  Returns out."""
+        out.  Returns out.  The address of a stream that is not the current one needs a workspace with it."""
         s = self._stream(stream)
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
@@ -250,9 +257,19 @@ class Cache8:
         ld = self._per_token(out, "out", torch.float32, batch, tokens)
         if scores is not None and self._per_token(scores, "scores", torch.float32, batch, tokens) != ld:
             raise ValueError("scores and out differ in their tokens")
+        if workspace is None:
+            if s != torch._C._cuda_getCurrentRawStream(self.device.index):
+                if not isinstance(stream, _cuda.Stream):
+                    raise ValueError("workspace: to be given with the address of a stream")
+                with _cuda.stream(stream):           # its memory belongs to the stream it is used on
+                    workspace = self.weights_workspace(hq, batch.n_rows)
+            else:
+                workspace = self.weights_workspace(hq, batch.n_rows)
+        elif workspace.device != self.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+            raise ValueError("workspace: contiguous bytes on the cache's device expected")
         ks.ks_kv8_attention_weights(self.c, batch.c, ks.KsKv8Weights(
             q.data_ptr(), q_row, q_head, hq, self.head_dim ** -0.5 if scale is None else scale, decay, lse.data_ptr(),
-            None if scores is None else scores.data_ptr(), out.data_ptr(), ld), s)
+            None if scores is None else scores.data_ptr(), out.data_ptr(), ld, workspace.data_ptr(), workspace.numel()), s)
         return out
 
     def evict(self, batch: Batch8, scores, keep, page_table, lengths, kept, new_scores=None, first: int = 0,

@@ -22,7 +22,7 @@ def test_what_stays():
 
 
 def weights_args(ks):
-    return ks.KsKv8Weights(A, 4096, 128, 32, 0.1, 1.0, A, A, A, 256)
+    return ks.KsKv8Weights(A, 4096, 128, 32, 0.1, 1.0, A, A, A, 256, A, 1 << 30)
 
 
 def evict_args(ks):
@@ -32,7 +32,7 @@ def evict_args(ks):
 WEIGHTS = [("q", None, 1), ("q", A + 1, 1), ("q_row", -1, 1), ("n_q_heads", 12, 1), ("n_q_heads", 0, 1),
            ("n_q_heads", 1024, 6), ("scale", math.nan, 1), ("decay", math.inf, 1), ("lse", None, 1), ("lse", A + 2, 1),
            ("scores", None, 1), ("scores", A + 1, 1), ("out", None, 1), ("out", A + 2, 1), ("score_ld", 255, 1),
-           ("score_ld", 1 << 50, 1)]
+           ("score_ld", 1 << 50, 1), ("workspace", None, 1), ("workspace", A + 16, 1), ("workspace_bytes", 1000, 3)]
 EVICT = [("scores", None, 1), ("scores", A + 2, 1), ("score_ld", 255, 1), ("keep", None, 1), ("first", -1, 1),
          ("recent", -1, 1), ("page_table", None, 1), ("table_ld", 0, 1), ("table_ld", 1 << 28, 1), ("lengths", None, 1),
          ("kept", None, 1), ("kept", A + 1, 1), ("kept_ld", 127, 1), ("new_scores", A + 2, 1), ("new_score_ld", 127, 1)]
