@@ -5,23 +5,31 @@
 // select: the least kept score by a radix search over the scores' 32 bits, made
 // whole numbers in the scores' order, 11, 11 and 10 bits at a time, then one pass
 // that numbers what stays: scores above it, and as many equal ones, the earlier
-// first, as there is room for.
+// first, as there is room for.  A cluster of up to eight CTAs takes a sequence's
+// head, each a contiguous slice, eight neighbouring scores a thread, in registers
+// unless the slice is longer than that; the CTAs read each other's counts.
 //
 // gather: a CTA writes one block of 16 kept tokens.  Their codes come from up to 16
 // records with scales of their own; the new block's scale is the smallest power
 // of two for their values, as an append of them would choose it, and a code is
 // multiplied by a power of two, which rounds only where it becomes subnormal.  A
-// token's keys are 16-byte pieces of its record; its values are one byte of every
-// 16, so every sector of the record's second half is read.
+// token's keys are 16-byte pieces of its record, a thread each.  Its values are
+// one byte of every 16: a thread takes a dim, reads the 16 bytes of each record
+// that the block's tokens come from once, and has the new record's 16 bytes of the
+// dim together without any exchange.  The places and pages of a CTA's next block
+// are looked up while it works on one.
 #include <algorithm>
 
 #include "kv8.cuh"
+#include "umma.cuh"
 
 namespace ks {
 
 namespace {
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32, kBins = 2048;
+constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048, kPer = 8, kRound = kThreads * kPer;
+constexpr int kCopies = 4;          // of the first pass's bins: scores crowd into few of them
+constexpr int kMaxCluster = 8;
 
 // Larger score, larger key; the two zeros are one, and NaN is below everything.
 KS_DEV unsigned score_key(float v) {
@@ -59,15 +67,18 @@ KS_DEV int block_before(int v, int* sums, int& total) {
     return before + u - v;
 }
 
-__global__ void __launch_bounds__(kThreads) kv8_select_kernel(const Kv8Args a, const Kv8EvictArgs t) {
-    __shared__ int bins[kBins], sums[kWarps];
+KS_DEV int load_cluster(const int* p, int rank) { return (int)cluster_load(cluster_addr(p, (uint32_t)rank)); }
+
+// Grid: a cluster of `ctas` along x per head, sequences along y.
+__global__ void __launch_bounds__(kThreads) kv8_select_kernel(const Kv8Args a, const Kv8EvictArgs t, int ctas) {
+    __shared__ int bins[kCopies][kBins], sums[kWarps];       // a pass each; the first one uses all
     __shared__ unsigned s_prefix;
-    __shared__ int s_left;
-    const int tid = threadIdx.x, h = blockIdx.x, s = blockIdx.y;
+    __shared__ int s_left, counts[2];                // scores above the least one that stays (and protected ones), equal ones
+    const int tid = threadIdx.x, h = blockIdx.x / ctas, rank = blockIdx.x % ctas, s = blockIdx.y;
     grid_dependency_wait();
     grid_launch_dependents();
     const Stay w(a, t, s);
-    if (h == 0 && tid == 0) {
+    if (blockIdx.x == 0 && tid == 0) {
         const int len = a.lengths[s], keep = t.keep[s];
         if (len < 0 || len > a.capacity || keep < 0 || min(keep, len) > t.new_capacity) kv8_flag(a, kKv8BadBatch);
         t.new_lengths[s] = w.n;
@@ -75,37 +86,76 @@ __global__ void __launch_bounds__(kThreads) kv8_select_kernel(const Kv8Args a, c
     const float* score = t.scores + ((size_t)s * a.hk + h) * t.ld;
     int32_t* kept = t.kept + ((size_t)s * a.hk + h) * t.kept_ld;
     float* out = t.new_scores ? t.new_scores + ((size_t)s * a.hk + h) * t.new_ld : nullptr;
-    if (w.n == w.len) {
-        for (int i = tid; i < w.n; i += kThreads) {
+    if (w.n == w.len) {                              // the whole cluster
+        for (int i = rank * kThreads + tid; i < w.n; i += ctas * kThreads) {
             kept[i] = i;
             if (out) out[i] = score[i];
         }
         return;
     }
     const int lo = w.first, hi = w.len - w.recent, most = w.n - w.first - w.recent;      // most of [lo, hi) stay
+    const int slice = ((w.len + ctas - 1) / ctas + kPer - 1) / kPer * kPer, begin = rank * slice;
+    const int end = min(w.len, begin + slice), rounds = max(0, end - begin + kRound - 1) / kRound;
+    // this thread's scores of a round
+    float v[kPer];
+    auto load = [&](int round) {
+        const int i0 = begin + round * kRound + tid * kPer;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[e] = i0 + e < end ? score[i0 + e] : 0.f;
+    };
+    if (rounds > 0) load(0);
+    for (int i = tid; i < kCopies * kBins; i += kThreads) bins[0][i] = 0;
+    __syncthreads();
     // the least key that stays, and how many of those equal to it
     unsigned prefix = 0;
     int left = most;
     if (most > 0) {
 #pragma unroll 1
-        for (int shift = 21; shift >= 0; shift -= shift == 21 ? 11 : 10) {
-            const int width = shift == 0 ? 10 : 11;
-            const unsigned above = shift == 21 ? 0u : 0xffffffffu << (shift + width);
-            for (int i = tid; i < kBins; i += kThreads) bins[i] = 0;
-            __syncthreads();
-            for (int i = lo + tid; i < hi; i += kThreads) {
-                const unsigned k = score_key(score[i]);
-                if ((k & above) == prefix) atomicAdd(&bins[k >> shift & ((1u << width) - 1)], 1);
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+            const unsigned above = pass == 0 ? 0u : 0xffffffffu << (shift + width);
+            for (int round = 0; round < rounds; ++round) {
+                if (rounds > 1) load(round);
+                const int i0 = begin + round * kRound + tid * kPer;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const unsigned k = score_key(v[e]);
+                    if (i0 + e >= lo && i0 + e < min(hi, end) && (k & above) == prefix)
+                        atomicAdd(&bins[pass == 0 ? tid % kCopies : pass][k >> shift & ((1u << width) - 1)], 1);
+                }
             }
-            __syncthreads();
-            // bins from the largest down, two a thread: the one in which the count passes what is left
-            const int top = (1 << width) - 1, b0 = top - 2 * tid, c0 = b0 >= 0 ? bins[b0] : 0, c1 = b0 >= 1 ? bins[b0 - 1] : 0;
+            if (pass == 0) {
+                __syncthreads();
+                for (int i = tid; i < kBins; i += kThreads) {
+                    bins[0][i] += bins[1][i] + bins[2][i] + bins[3][i];
+                    bins[1][i] = bins[2][i] = 0;
+                }
+            }
+            if (ctas > 1) cluster_sync();
+            else __syncthreads();
+            // bins from the largest down, some neighbouring ones a thread: the one in which the count passes what is left
+            constexpr int OWN = kBins / kThreads;
+            const int b0 = (1 << width) - 1 - OWN * tid;
+            int c[OWN] = {}, mine = 0;
+            if (b0 > 0)
+                for (int r = 0; r < ctas; ++r)
+#pragma unroll
+                    for (int e = 0; e < OWN; ++e)
+                        c[e] += ctas > 1 ? load_cluster(&bins[pass][b0 - e], r) : bins[pass][b0 - e];
+#pragma unroll
+            for (int e = 0; e < OWN; ++e) mine += c[e];
             int total;
-            const int before = block_before(c0 + c1, sums, total);
-            if (before < left && before + c0 + c1 >= left) {
-                const bool second = before + c0 < left;
-                s_prefix = prefix | (unsigned)(second ? b0 - 1 : b0) << shift;
-                s_left = left - before - (second ? c0 : 0);
+            int before = block_before(mine, sums, total);
+            if (before < left && before + mine >= left) {
+                int e = 0;
+#pragma unroll
+                for (int i = 0; i < OWN - 1; ++i)
+                    if (e == i && before + c[i] < left) {
+                        before += c[i];
+                        ++e;
+                    }
+                s_prefix = prefix | (unsigned)(b0 - e) << shift;
+                s_left = left - before;
             }
             __syncthreads();
             prefix = s_prefix;
@@ -113,109 +163,266 @@ __global__ void __launch_bounds__(kThreads) kv8_select_kernel(const Kv8Args a, c
             __syncthreads();
         }
     }
-    int ties = 0, done = 0;                          // equal ones, and kept ones so far
-    for (int base = 0; base < w.len; base += kThreads) {
-        const int i = base + tid;
-        const bool inside = i >= lo && i < hi;
-        const float v = i < w.len && (inside || out) ? score[i] : 0.f;
-        const unsigned k = inside ? score_key(v) : 0u;
-        const bool equal = inside && most > 0 && k == prefix;
-        int total;
-        const int tie = ties + block_before(equal, sums, total);
-        ties += total;
-        const bool stays = i < w.len && (!inside || (most > 0 && (k > prefix || (equal && tie < left))));
-        const int o = done + block_before(stays, sums, total);
-        done += total;
-        if (stays) {
-            kept[o] = i;
-            if (out) out[o] = v;
-        }
-    }
-}
-
-template <int HD>
-__global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const Kv8EvictArgs t) {
-    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, TH = HD / 16, WARPS = HD / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, b = blockIdx.x, h = blockIdx.y;
-    __shared__ __align__(16) unsigned char vc[CODES + HD * 2];
-    __shared__ float top[2][WARPS];
-    grid_dependency_wait();
-    grid_launch_dependents();
-    for (int s = blockIdx.z; s < a.n_seqs; s += gridDim.z) {
-        const Stay w(a, t, s);
-        if (b * kKv8Block >= w.n) continue;
-        const int page = t.new_table[(size_t)s * t.new_table_ld + b / a.bpp];
-        if (page < 0 || page >= a.n_pages) {
-            if (tid == 0) kv8_flag(a, kKv8BadPage);
-            continue;
-        }
-        unsigned char* rec = a.data + (((size_t)page * a.hk + h) * a.bpp + b % a.bpp) * REC;
-        // a sequence that keeps all of its tokens may keep its pages
-        if (w.n == w.len && rec == kv8_record_at(a, s, b, h, REC)) continue;
-        const int tok = tid / TH, part = tid % TH, at = b * kKv8Block + tok;
-        float k[16], v[16], k_top = 0.f, v_top = 0.f;
+    // which of a thread's scores stay for sure, and which are equal to the least one
+    auto mark = [&](int round, unsigned& sure, unsigned& equal) {
+        sure = equal = 0;
+        const int i0 = begin + round * kRound + tid * kPer;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) k[i] = v[i] = 0.f;
-        if (at < w.n) {
-            const int from = t.kept[((size_t)s * a.hk + h) * t.kept_ld + at], ft = from % kKv8Block;
-            const unsigned char* src = kv8_record_at(a, s, from / kKv8Block, h, REC);
-            if (src) {
-                const float2 sc = *reinterpret_cast<const float2*>(src + 2 * CODES);
-                const uint4 c = *reinterpret_cast<const uint4*>(src + k_byte<HD>(ft, 16 * part));
-                const unsigned char* vb = src + CODES + 16 * part * 16 + v_byte(ft);
-                unsigned char e[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) e[i] = vb[16 * i];
-                const uint32_t words[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 kv = from_e4m3x2((uint16_t)(words[i / 2] >> 16 * (i & 1)));
-                    const float2 vv = from_e4m3x2((uint16_t)(e[2 * i] | e[2 * i + 1] << 8));
-                    k[2 * i] = kv.x * sc.x; k[2 * i + 1] = kv.y * sc.x;
-                    v[2 * i] = vv.x * sc.y; v[2 * i + 1] = vv.y * sc.y;
-                }
-            } else if (part == 0) {
-                kv8_flag(a, kKv8BadPage);            // read as zeros
+        for (int e = 0; e < kPer; ++e) {
+            const int i = i0 + e;
+            if (i >= end) continue;
+            if (i < lo || i >= hi) {
+                sure |= 1u << e;
+            } else if (most > 0) {
+                const unsigned k = score_key(v[e]);
+                sure |= (unsigned)(k > prefix) << e;
+                equal |= (unsigned)(k == prefix) << e;
             }
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if (finite(k[i])) k_top = fmaxf(k_top, fabsf(k[i]));
-            if (finite(v[i])) v_top = fmaxf(v_top, fabsf(v[i]));
+    };
+    int ties = 0, done = 0;                          // equal ones, and kept ones, before
+    unsigned sure, equal;
+    if (ctas > 1) {
+        int n_sure = 0, n_equal = 0;
+        for (int round = 0; round < rounds; ++round) {
+            if (rounds > 1) load(round);
+            mark(round, sure, equal);
+            n_sure += __popc(sure);
+            n_equal += __popc(equal);
         }
+        int total;
+        block_before(n_sure, sums, total);
+        if (tid == 0) counts[0] = total;
+        block_before(n_equal, sums, total);
+        if (tid == 0) counts[1] = total;
+        cluster_sync();
+        for (int r = 0; r < rank; ++r) {
+            const int n = load_cluster(&counts[0], r), e = load_cluster(&counts[1], r);
+            done += n + min(e, max(left - ties, 0));
+            ties += e;
+        }
+    }
+    for (int round = 0; round < rounds; ++round) {
+        if (rounds > 1) load(round);
+        mark(round, sure, equal);
+        int total;
+        const int before = block_before(__popc(equal), sums, total);
+        int take = min(max(left - ties - before, 0), __popc(equal));     // of the thread's equal ones, the first
+        ties += total;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if ((equal >> e & 1) && take > 0) {
+                sure |= 1u << e;
+                --take;
+            }
+        int o = done + block_before(__popc(sure), sums, total);
+        done += total;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (sure >> e & 1) {
+                kept[o] = begin + round * kRound + tid * kPer + e;
+                if (out) out[o] = v[e];
+                ++o;
+            }
+    }
+    if (ctas > 1) cluster_sync();                    // nobody leaves while its counts are read
+}
+
+// Where a block's token comes from.
+struct Source {
+    const unsigned char* rec;       // null: no such page, or no token
+    int token;                      // of the record
+    int fresh;                      // another record than the token before
+};
+// A power of two f <= 2^18 as two factors of f16; below 2^-24 a code times f rounds to 0 anyway.
+KS_DEV void two_factors(float f, __half& a, __half& b) {
+    f = fmaxf(f, 1.f / 16777216.f);
+    const float first = fminf(fmaxf(f, 1.f / 4096.f), 512.f);
+    a = __float2half_rn(first);
+    b = __float2half_rn(f * inverse_pow2(first));
+}
+KS_DEV uint32_t scaled(uint32_t halves, __half2 a, __half2 b) {
+    const __half2 x = __hmul2(__hmul2(*reinterpret_cast<const __half2*>(&halves), a), b);
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t*>(&x)));
+    return r;
+}
+KS_DEV uint32_t halves_of(uint32_t codes) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+    return h;
+}
+
+// A CTA takes blocks blockIdx.x, + gridDim.x, .. of a sequence's head.
+template <int HD>
+__global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const Kv8EvictArgs t) {
+    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, TH = HD / 16, WARPS = HD / 32, BATCH = 8;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, s = blockIdx.z;
+    __shared__ __align__(16) Source from[2][kKv8Block];
+    __shared__ float2 scales[kKv8Block];
+    __shared__ __align__(8) __half factors[2][kKv8Block];         // of the values, in the new record's order
+    __shared__ float top[2][WARPS];
+    __shared__ unsigned char* to[2];                 // the new record; null: none is to be written
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const Stay w(a, t, s);
+    const int blocks = (w.n + kKv8Block - 1) / kKv8Block;
+    // Lanes 0..15 of warp 0 look for a block's tokens, in two steps an iteration apart, lane 16 for its place.
+    auto place_of = [&](int b) {
+        const int at = b * kKv8Block + lane;
+        return warp == 0 && lane < kKv8Block && at < w.n ? t.kept[((size_t)s * a.hk + h) * t.kept_ld + at] : -1;
+    };
+    auto look = [&](int b, int place, Source& f, unsigned char*& rec) {
+        f.rec = nullptr;
+        f.token = 0;
+        f.fresh = 1;
+        rec = nullptr;
+        if (warp != 0 || b >= blocks) return;
+        if (place >= 0) {
+            f.token = place % kKv8Block;
+            f.rec = kv8_record_at(a, s, place / kKv8Block, h, REC);
+            if (!f.rec) kv8_flag(a, kKv8BadPage);    // read as zeros
+        }
+        const int block = place < 0 ? -1 : place / kKv8Block, before = __shfl_up_sync(0xffffffffu, block, 1);
+        f.fresh = lane % BATCH == 0 || before != block;
+        if (lane == kKv8Block) {
+            const int page = t.new_table[(size_t)s * t.new_table_ld + b / a.bpp];
+            if (page < 0 || page >= a.n_pages) kv8_flag(a, kKv8BadPage);
+            else rec = a.data + (((size_t)page * a.hk + h) * a.bpp + b % a.bpp) * REC;
+            // a sequence that keeps all of its tokens may keep its pages
+            if (rec && w.n == w.len && rec == kv8_record_at(a, s, b, h, REC)) rec = nullptr;
+        }
+    };
+    auto keep = [&](int buf, const Source& f, unsigned char* rec) {
+        if (warp != 0) return;
+        if (lane < kKv8Block) from[buf][lane] = f;
+        if (lane == kKv8Block) to[buf] = rec;
+    };
+    Source f;
+    unsigned char* rec;
+    look(blockIdx.x, place_of(blockIdx.x), f, rec);
+    keep(0, f, rec);
+    int place = place_of(blockIdx.x + gridDim.x);
+    __syncthreads();
+    int buf = 0;
+    const int tok = tid / TH, part = tid % TH;
+    for (int b = blockIdx.x; b < blocks; b += gridDim.x, buf ^= 1) {
+        float2 sc = make_float2(0.f, 0.f);
+        if (tid < kKv8Block && from[buf][tid].rec) sc = *reinterpret_cast<const float2*>(from[buf][tid].rec + 2 * CODES);
+        uint4 k = make_uint4(0, 0, 0, 0);
+        {
+            const Source u = from[buf][tok];         // of this thread's piece of keys
+            if (u.rec) k = *reinterpret_cast<const uint4*>(u.rec + k_byte<HD>(u.token, 16 * part));
+        }
+        uint32_t v[4];                               // the dim's codes in the new record's order
+#pragma unroll
+        for (int j0 = 0; j0 < kKv8Block; j0 += BATCH) {
+            uint4 raw[BATCH];
+            int token[BATCH];
+            bool fresh[BATCH];
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const Source u = from[buf][j0 + j];
+                token[j] = u.token;
+                fresh[j] = u.fresh;
+                if (u.fresh) {
+                    raw[j] = make_uint4(0, 0, 0, 0);
+                    if (u.rec) raw[j] = *reinterpret_cast<const uint4*>(u.rec + CODES + tid * 16);
+                }
+            }
+            uint32_t byte[BATCH];
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                if (j > 0 && !fresh[j]) raw[j] = raw[j - 1];
+                const int at = v_byte(token[j]);
+                const uint32_t lo = __byte_perm(raw[j].x, raw[j].y, at & 7), hi = __byte_perm(raw[j].z, raw[j].w, at & 7);
+                byte[j] = at & 8 ? hi : lo;
+            }
+            // tokens 2 w, 2 w + 1 are bytes 0, 1 of word w, 8 + 2 w and 9 + 2 w bytes 2, 3
+#pragma unroll
+            for (int w4 = 0; w4 < 4; ++w4) {
+                const uint32_t pair = __byte_perm(byte[2 * w4], byte[2 * w4 + 1], 0x0040);
+                v[w4] = j0 == 0 ? pair : __byte_perm(v[w4], pair, 0x5410);
+            }
+        }
+        look(b + gridDim.x, place, f, rec);          // the next block's
+        place = place_of(b + 2 * gridDim.x);
+        if (tid < kKv8Block) scales[tid] = sc;
+        __syncthreads();
+        // the largest values: NaN is passed over, infinities there are none
+        const uint32_t kw[4] = {k.x, k.y, k.z, k.w};
+        __half2 k_max = __half2(0.f, 0.f);
+        float v_top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t x = halves_of(kw[i / 2] >> 16 * (i & 1)), y = halves_of(v[i / 2] >> 16 * (i & 1));
+            k_max = __hmax2(k_max, __habs2(*reinterpret_cast<const __half2*>(&x)));
+            const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&y));
+            const int t0 = 8 * (i & 1) + 2 * (i / 2);
+            v_top = fmaxf(fmaxf(v_top, fabsf(z.x * scales[t0].y)), fabsf(z.y * scales[t0 + 1].y));
+        }
+        const float k_scale = scales[tok].x;
+        float k_top = fmaxf(__low2float(k_max), __high2float(k_max)) * k_scale;      // one scale a token
         k_top = warp_max(k_top);
         v_top = warp_max(v_top);
         if (lane == 0) {
             top[0][warp] = k_top;
             top[1][warp] = v_top;
         }
+        keep(buf ^ 1, f, rec);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < WARPS; ++i) {
             k_top = fmaxf(k_top, top[0][i]);
             v_top = fmaxf(v_top, top[1][i]);
         }
-        const float ks = scale_for(k_top), vs = scale_for(v_top), ki = inverse_pow2(ks), vi = inverse_pow2(vs);
-        uint32_t c[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            c[i] = to_e4m3x2(k[4 * i] * ki, k[4 * i + 1] * ki) | (uint32_t)to_e4m3x2(k[4 * i + 2] * ki, k[4 * i + 3] * ki) << 16;
-        *reinterpret_cast<uint4*>(rec + k_byte<HD>(tok, 16 * part)) = make_uint4(c[0], c[1], c[2], c[3]);
-        // 16 unused bytes after every 8 dims, as in an append
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const int d = 16 * part + i;
-            const uint16_t x = to_e4m3x2(v[i] * vi, v[i + 1] * vi);
-            unsigned char* to = vc + d * 16 + (d >> 3) * 16 + v_byte(tok);
-            to[0] = (unsigned char)x;
-            to[16] = (unsigned char)(x >> 8);
+        const float ks = scale_for(k_top), vs = scale_for(v_top);
+        // a factor is past 2^18 only where all codes are zeros
+        if (tid < kKv8Block) {
+            const int at = v_byte(tid);
+            two_factors(fminf(sc.y * inverse_pow2(vs), 262144.f), factors[0][at], factors[1][at]);
         }
+        __half ka, kb;
+        two_factors(fminf(k_scale * inverse_pow2(ks), 262144.f), ka, kb);
         __syncthreads();
-        *reinterpret_cast<uint4*>(rec + CODES + tid * 16) = *reinterpret_cast<const uint4*>(vc + tid * 16 + (tid >> 3) * 16);
-        if (tid == 0) *reinterpret_cast<float2*>(rec + 2 * CODES) = make_float2(ks, vs);
-        __syncthreads();
+        if (unsigned char* out = to[buf]) {
+            const __half2 ka2 = __half2(ka, ka), kb2 = __half2(kb, kb);
+            uint32_t c[4], d[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[i] = scaled(halves_of(kw[i]), ka2, kb2) | scaled(halves_of(kw[i] >> 16), ka2, kb2) << 16;
+                const __half2* f0 = reinterpret_cast<const __half2*>(factors[0] + 4 * i);
+                const __half2* f1 = reinterpret_cast<const __half2*>(factors[1] + 4 * i);
+                d[i] = scaled(halves_of(v[i]), f0[0], f1[0]) | scaled(halves_of(v[i] >> 16), f0[1], f1[1]) << 16;
+            }
+            *reinterpret_cast<uint4*>(out + k_byte<HD>(tok, 16 * part)) = make_uint4(c[0], c[1], c[2], c[3]);
+            *reinterpret_cast<uint4*>(out + CODES + tid * 16) = make_uint4(d[0], d[1], d[2], d[3]);
+            if (tid == 0) *reinterpret_cast<float2*>(out + 2 * CODES) = make_float2(ks, vs);
+        }
+        __syncthreads();                             // before the buffers' next turn
     }
 }
+
+// CTAs of a head: no more than a round of scores needs, nor than fill the GPU.
+cudaError_t launch_select(const Kv8Args& a, const Kv8EvictArgs& t, cudaStream_t s) {
+    int ctas = 1;
+    while (ctas < kMaxCluster && (int64_t)ctas * kRound < a.capacity && a.hk * a.n_seqs * ctas < sm_count()) ctas *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(a.hk * ctas, a.n_seqs);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kv8_select_kernel, a, t, ctas);
+}
+
+constexpr int kGatherBlocks = 4;
 
 }  // namespace
 
@@ -234,9 +441,12 @@ cudaError_t launch_kv8_evict(const Kv8Args& a, const Kv8EvictArgs& t, cudaStream
         u.new_lengths += s0;
         u.kept += (size_t)s0 * a.hk * t.kept_ld;
         if (u.new_scores) u.new_scores += (size_t)s0 * a.hk * t.new_ld;
-        e = launch_kv8(kv8_select_kernel, dim3(a.hk, b.n_seqs), kThreads, 0, s, b, u);
-        if (e != cudaSuccess || t.new_capacity == 0) return e;
-        const dim3 grid(t.new_capacity / kKv8Block, a.hk, b.n_seqs);
+        e = launch_select(b, u, s);
+        if (e != cudaSuccess) return e;
+        // a block a CTA while all are resident at once, else up to kGatherBlocks one after the other: sequences are uneven
+        const int64_t most = t.new_capacity / kKv8Block, resident = (int64_t)sm_count() * (a.hd == 128 ? 7 : 14);
+        const int64_t each = std::min(most, std::max((most + kGatherBlocks - 1) / kGatherBlocks, resident / a.hk / b.n_seqs));
+        const dim3 grid((unsigned)each, a.hk, b.n_seqs);
         e = a.hd == 128 ? launch_kv8(kv8_gather_kernel<128>, grid, 128, 0, s, b, u)
                         : launch_kv8(kv8_gather_kernel<64>, grid, 64, 0, s, b, u);
     }

@@ -3,17 +3,16 @@
 //   out[t] = decay scores[t] + sum over rows i >= t and query heads g of exp(scale q_ig k_t - lse_ig)
 // for a sequence and KV head, the softmax's own sums lse given by the attention.
 //
-// Only keys are read, and only once: a warp holds 32 of them, in registers, as
-// the A operand of m16n8k32 e4m3 products, and all rows of the sequence pass by
-// as B, eight at a time and in two codes each (see kv8_attn.cu).  A thread's
+// Only keys are read, and only once.  A CTA is a producer warp, which copies the
+// keys of 128 tokens at a time into a ring (a record's first half and its
+// scales), and four consumer warps, each with 32 of the keys in registers as the
+// A operand of m16n8k32 e4m3 products; all rows of the sequence pass by as B,
+// eight at a time and in two codes each (see kv8_attn.cu).  A thread's
 // accumulators are two rows' scores of each of its keys, so the sum over the
 // rows stays in the thread until the end; one warp writes a token, in an order
 // of its own: no atomics, and the same bits from call to call.
 //
-// The dot product goes over the dims in any order, as long as both operands have
-// the same: a lane's 16 contiguous bytes of a token are its four k-slices of four
-// products, so a record's keys come by 16-byte loads, all of a line used, and
-// straight from memory, without shared memory or ldmatrix.
+// Calls of many rows go to kv8_weights_tc.cu.
 #include <algorithm>
 #include <type_traits>
 
@@ -23,11 +22,12 @@ namespace ks {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kWarps = 4, kThreads = 32 * (kWarps + 1), kCtas = 2;  // consumers; CTAs an SM
 constexpr int kWarpBlocks = 2;                      // blocks of 16 keys a warp
-constexpr int kTileLog = 7, kTile = 1 << kTileLog;
-constexpr int kChunkBlocks = 8, kChunk = 8 * kChunkBlocks;      // queries in shared memory
-static_assert(kTile == kWarps * kWarpBlocks * kKv8Block, "a tile is what the warps hold");
+constexpr int kTileLog = 7, kTile = 1 << kTileLog, kBlocks = kTile / kKv8Block, kStages = 4;
+constexpr int kUnitTiles = 2;                       // a unit's fixed cost, in tiles
+constexpr int kChunkBlocks = 4, kChunk = 8 * kChunkBlocks;      // queries in shared memory
+static_assert(kBlocks == kWarps * kWarpBlocks && kWarpBlocks == 2, "a tile is what the warps hold, a key a lane");
 
 KS_DEV void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -35,32 +35,19 @@ KS_DEV void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Of a block of keys, or of eight queries in one code: 16 bytes of dims 64 i + 16 q4 .. of row g, and of row g + 8.
-template <int HD>
-struct Keys {
-    static constexpr int P = HD / 64;
-    uint4 x[2][P];              // [token half]
-    float scale;
-    KS_DEV void load(const unsigned char* rec) {
-        const int lane = threadIdx.x & 31, at = (lane & 3) * 128 + (lane >> 2) * 16;
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                x[half][i] = make_uint4(0, 0, 0, 0);
-                if (rec) x[half][i] = *reinterpret_cast<const uint4*>(rec + half * 8 * HD + i * 512 + at);
-            }
-        scale = rec ? *reinterpret_cast<const float*>(rec + 32 * HD) : 0.f;
-    }
-};
 KS_DEV uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 template <int HD>
 struct Smem {
-    uint4 code[kChunkBlocks][2][HD / 64][32];       // [hi, lo], a lane's dims as in Keys
+    unsigned char keys[kStages][kBlocks][kKv8Block * HD];
+    float4 scales[kStages][kBlocks];                // key scale, value scale, unused
+    uint4 code[kChunkBlocks][2][HD / 64][32];       // [hi, lo]: B operands of two products, as a lane holds them
     float2 factor[kChunk];                          // of the scores, and minus the sum's logarithm; base 2
     int lim[kChunk];                                // last key that the row sees
+    int present[kStages];                           // records that were copied
+    uint64_t full[kStages], empty[kStages];
 };
+KS_DEV void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
 
 // Queries first .. of a unit's n, eight a warp and turn, in two codes.
 template <int HD, bool WIDE>
@@ -110,8 +97,13 @@ KS_DEV void convert(Smem<HD>& sm, const Kv8Args& a, const Kv8WeightArgs& t, cons
                 lo[j] = to_e4m3x2(v[0] * inv - f0.x, v[1] * inv - f0.y) |
                         (uint32_t)to_e4m3x2(v[2] * inv - f1.x, v[3] * inv - f1.y) << 16;
             }
-            sm.code[b][0][p][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            sm.code[b][1][p][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            // dims 16 q4 + 4 j: the product's lane j of row g has them, as word q4 of its operands
+            uint32_t *hi_at = reinterpret_cast<uint32_t*>(sm.code[b][0][p]), *lo_at = reinterpret_cast<uint32_t*>(sm.code[b][1][p]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                hi_at[(4 * g + j) * 4 + q4] = hi[j];
+                lo_at[(4 * g + j) * 4 + q4] = lo[j];
+            }
         }
         if (q4 == 0) {
             const float lse = valid ? t.lse[(size_t)(rows.row0 + tok) * t.hq + head] : INFINITY;
@@ -124,67 +116,123 @@ KS_DEV void convert(Smem<HD>& sm, const Kv8Args& a, const Kv8WeightArgs& t, cons
 }
 
 template <int HD, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 4) kv8_weights_kernel(const Kv8Args a, const Kv8WeightArgs t, const Kv8Plan p) {
-    constexpr int REC = kv8_record(HD), P = HD / 64;
-    __shared__ Smem<HD> sm;
+__global__ void __launch_bounds__(kThreads, kCtas)
+    kv8_weights_kernel(const Kv8Args a, const Kv8WeightArgs t, const Kv8Plan p) {
+    constexpr int REC = kv8_record(HD), P = HD / 64, KEYS = kKv8Block * HD;
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    Smem<HD>& sm = *reinterpret_cast<Smem<HD>*>(smem_raw);
+    volatile int* present = sm.present;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], kWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
     grid_dependency_wait();
     grid_launch_dependents();
     Run run;
     Segment<> at;
     if (!find_run(a, p, run, at)) return;
     const int G = p.G;
+
+    if (warp == kWarps) {
+        // ------------------------------------------------------- producer
+        // Page numbers are read a group of tiles ahead, across segments.
+        constexpr int TILES = 32 / kBlocks;
+        auto pages = [&](const Segment<>& k, int tile) {             // -1: no such block, -2: no such page
+            const int b = tile * kBlocks + lane;
+            if (b * kKv8Block >= k.q.len || tile + lane / kBlocks >= k.end) return -1;
+            const int page = a.table[(size_t)k.s * a.table_ld + p.page_of(b, a.bpp)];
+            return page >= 0 && page < a.n_pages ? page : -2;
+        };
+        int it = 0, tile = at.tile, page = pages(at, tile);
+        bool alive = true, more = true;
+        while (more && alive) {
+            Segment<> next = at;
+            int next_tile = tile + TILES;
+            if (next_tile >= at.end) {
+                more = next.next(a, run, p);
+                next_tile = next.tile;
+            }
+            const int next_page = more ? pages(next, next_tile) : -1;
+            if (page == -2) kv8_flag(a, kKv8BadPage);
+            const int b = tile * kBlocks + lane;
+            const unsigned char* rec =
+                page >= 0 ? a.data + (((size_t)page * a.hk + at.h) * a.bpp + b - p.page_of(b, a.bpp) * a.bpp) * REC : nullptr;
+            const unsigned have = __ballot_sync(0xffffffffu, rec != nullptr);
+            for (int i = 0; i < TILES && tile + i < at.end; ++i, ++it) {
+                const int st = it % kStages;
+                const unsigned mask = have >> (i * kBlocks) & ((1u << kBlocks) - 1);
+                alive = mbar_wait(&sm.empty[st], ((it / kStages) & 1) ^ 1, kWaitLimitNs);
+                if (!__all_sync(0xffffffffu, alive)) {
+                    alive = false;
+                    break;
+                }
+                if (lane == 0) {
+                    present[st] = (int)mask;
+                    mbar_expect_tx(&sm.full[st], __popc(mask) * (KEYS + 16));
+                }
+                __syncwarp();
+                if (lane / kBlocks == i && rec != nullptr) {
+                    bulk_load(sm.keys[st][lane % kBlocks], rec, KEYS, &sm.full[st]);
+                    bulk_load(&sm.scales[st][lane % kBlocks], rec + 2 * KEYS, 16, &sm.full[st]);
+                }
+            }
+            at = next;
+            tile = next_tile;
+            page = next_page;
+        }
+        if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
+        // no copy may be in flight when the CTA ends
+        for (int i = max(0, it - kStages); i < it; ++i)
+            mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, kWaitLimitNs);
+        return;
+    }
+
+    // ----------------------------------------------------------- consumers
+    int it = 0;
+    bool alive = true;
     do {
         const Rows rows(at, p.tq, G);
         const int chunks = (rows.n + kChunk - 1) / kChunk;
-        // the pages of this warp's blocks of a tile (-1: no such block), two tiles ahead: an address that waits for
-        // its page holds up everything behind it
-        int page[kWarpBlocks];
-        auto look = [&](int tile) {
-#pragma unroll
-            for (int kb = 0; kb < kWarpBlocks; ++kb) {
-                const int b = tile * (kTile / kKv8Block) + warp * kWarpBlocks + kb;
-                page[kb] = -1;
-                if (tile < at.end && b * kKv8Block < at.q.len) {
-                    page[kb] = a.table[(size_t)at.s * a.table_ld + p.page_of(b, a.bpp)];
-                    if (page[kb] < 0) page[kb] = -2;
-                }
-            }
+        const size_t score0 = ((size_t)at.s * a.hk + at.h) * t.ld;
+        const int older = t.decay != 0.f ? at.q.len - at.q.rows : 0;         // tokens whose scores count
+        auto score_of = [&](int tile) {              // of this lane's key, a tile ahead
+            const int key = tile * kTile + warp * kWarpBlocks * kKv8Block + lane;
+            return tile < at.end && key < older ? t.scores[score0 + key] : 0.f;
         };
-        Keys<HD> next[kWarpBlocks];
-        bool next_there[kWarpBlocks];
-        auto fetch = [&](int tile) {
-#pragma unroll
-            for (int kb = 0; kb < kWarpBlocks; ++kb) {
-                const int b = tile * (kTile / kKv8Block) + warp * kWarpBlocks + kb;
-                next_there[kb] = page[kb] >= 0 && page[kb] < a.n_pages;
-                if (!next_there[kb] && page[kb] != -1 && lane == 0) kv8_flag(a, kKv8BadPage);
-                next[kb].load(next_there[kb] ? a.data + (((size_t)page[kb] * a.hk + at.h) * a.bpp + b -
-                                                         p.page_of(b, a.bpp) * a.bpp) * REC : nullptr);
-            }
-        };
-        look(at.tile);
-        fetch(at.tile);
-        look(at.tile + 1);
+        float next_old = score_of(at.tile);
         int held = -1;                               // chunk in shared memory
-        for (int tile = at.tile; tile < at.end; ++tile) {
-            Keys<HD> k[kWarpBlocks];
-            bool there[kWarpBlocks];
+        for (int tile = at.tile; tile < at.end; ++tile, ++it) {
+            const int st = it % kStages;
+            const float old = next_old;
+            next_old = score_of(tile + 1);
+            const int key0 = tile * kTile + warp * kWarpBlocks * kKv8Block;
+            if (alive) alive = mbar_wait(&sm.full[st], (it / kStages) & 1, kWaitLimitNs);
+            const int have = alive ? present[st] >> (warp * kWarpBlocks) : 0;
+            uint32_t k[kWarpBlocks][2 * P][4];
+            float scale[kWarpBlocks];
 #pragma unroll
             for (int kb = 0; kb < kWarpBlocks; ++kb) {
-                k[kb] = next[kb];
-                there[kb] = next_there[kb];
+                // matrices (tokens 0..7, dims 32 j ..), (tokens 8.., same), (tokens 0..7, dims 32 j + 16 ..), (tokens 8.., same)
+                const uint32_t base = smem_u32(sm.keys[st][warp * kWarpBlocks + kb]) + (lane >> 3 & 1) * (8 * HD) +
+                                      (lane >> 4) * 128 + (lane & 7) * 16;
+#pragma unroll
+                for (int j = 0; j < 2 * P; ++j) ldsm_x4(k[kb][j], base + j * 256);
+                scale[kb] = sm.scales[st][warp * kWarpBlocks + kb].x;
             }
-            fetch(tile + 1);
-            look(tile + 2);
-            const int key0 = tile * kTile + warp * kWarpBlocks * kKv8Block;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.empty[st]);
             float sum[kWarpBlocks][2] = {};
             // rows before the tile's first key see nothing of it
-            for (int c = max(0, tile * kTile - rows.pos0) * (int64_t)G / kChunk; c < chunks; ++c) {
+            for (int c = (int)(max(0, tile * kTile - rows.pos0) * (int64_t)G / kChunk); c < chunks; ++c) {
                 if (held != c) {
-                    __syncthreads();
+                    consumers_sync();
                     convert<HD, WIDE>(sm, a, t, rows, at.h, G, c * kChunk);
-                    __syncthreads();
+                    consumers_sync();
                     held = c;
                 }
                 const bool edge = key0 + kWarpBlocks * kKv8Block - 1 > rows.pos0 + c * kChunk / G;
@@ -208,15 +256,9 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_weights_kernel(const Kv8Args 
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int j = 0; j < 2 * P; ++j) {
-                                // two words of 16 bytes a product
-                                constexpr int W = 2;
-                                const int part16 = j / 2, w = j % 2 * W;
-                                const uint32_t ka[4] = {word(k[kb].x[0][part16], w), word(k[kb].x[1][part16], w),
-                                                        word(k[kb].x[0][part16], w + 1), word(k[kb].x[1][part16], w + 1)};
-                                mma_e4m3(s, ka, word(q[i][part16], w), word(q[i][part16], w + 1));
-                            }
-                        const float f0 = f.x * k[kb].scale, f1 = f.z * k[kb].scale;
+                            for (int j = 0; j < 2 * P; ++j)
+                                mma_e4m3(s, k[kb][j], word(q[i][j / 2], j % 2 * 2), word(q[i][j / 2], j % 2 * 2 + 1));
+                        const float f0 = f.x * scale[kb], f1 = f.z * scale[kb];
                         const int key = key0 + 16 * kb + g;
                         float x[4] = {fmaf(s[0], f0, f.y), fmaf(s[1], f1, f.w), fmaf(s[2], f0, f.y), fmaf(s[3], f1, f.w)};
                         if (edge) {
@@ -239,20 +281,19 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_weights_kernel(const Kv8Args 
             for (int kb = 0; kb < kWarpBlocks; ++kb)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    float v = sum[kb][half];
-                    v += __shfl_xor_sync(0xffffffffu, v, 1);
-                    v += __shfl_xor_sync(0xffffffffu, v, 2);
-                    const int key = key0 + 16 * kb + 8 * half + g;
-                    if (q4 == 0 && key < at.q.len) {
-                        const size_t o = ((size_t)at.s * a.hk + at.h) * t.ld + key;
-                        if (!there[kb]) v = 0.f;                 // its page is not there: unseen
-                        if (t.decay != 0.f && key < at.q.len - at.q.rows) v = fmaf(t.decay, t.scores[o], v);
-                        t.out[o] = v;
-                    }
+                    sum[kb][half] += __shfl_xor_sync(0xffffffffu, sum[kb][half], 1);
+                    sum[kb][half] += __shfl_xor_sync(0xffffffffu, sum[kb][half], 2);
+                    if (!(have >> kb & 1)) sum[kb][half] = 0.f;          // no such page: unseen
                 }
+            // a quad has the sums of keys g, g + 8, g + 16 and g + 24: one to each of its lanes, then lane i gets key i
+            float v = q4 < 2 ? (q4 == 0 ? sum[0][0] : sum[0][1]) : q4 == 2 ? sum[1][0] : sum[1][1];
+            v = __shfl_sync(0xffffffffu, v, 4 * (lane & 7) + (lane >> 3));
+            const int key = key0 + lane;
+            if (key < at.q.len) t.out[score0 + key] = key < older ? fmaf(t.decay, old, v) : v;
         }
-        __syncthreads();                             // the next segment's queries
+        consumers_sync();                            // the next segment's queries
     } while (at.next(a, run, p));
+    if (!alive && lane == 0) kv8_flag(a, kKv8Timeout);
 }
 
 bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p) {
@@ -260,10 +301,10 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p) {
     p.G = hq / a.hk;
     p.tq = INT32_MAX / 2;                            // a unit has all rows of its sequence
     p.tile_log = kTileLog;
-    p.cost = 1;
+    p.cost = kUnitTiles;
     p.block_log = (a.bpp & (a.bpp - 1)) == 0 ? __builtin_ctz(a.bpp) : -1;
     const int64_t tiles = ((int64_t)a.capacity + kTile - 1) / kTile, total = (int64_t)a.hk * a.n_seqs * (tiles + p.cost);
-    p.ctas = (int)std::min<int64_t>(sm_count() * 4, total);
+    p.ctas = (int)std::min<int64_t>(sm_count() * kCtas, total);
     return total <= INT32_MAX;
 }
 
@@ -281,7 +322,7 @@ size_t kv8_weights_workspace(int group, int64_t n_rows, int64_t n_seqs) {
 
 bool kv8_weights_fits(const Kv8Args& a, int hq) {
     const int64_t tiles = ((int64_t)a.capacity + kTile - 1) / kTile;
-    return hq > 0 && (int64_t)a.hk * a.n_seqs * (tiles + 1) <= INT32_MAX;
+    return hq > 0 && (int64_t)a.hk * a.n_seqs * (tiles + kUnitTiles) <= INT32_MAX;
 }
 
 cudaError_t launch_kv8_weights(const Kv8Args& a, const Kv8WeightArgs& t, cudaStream_t s) {
@@ -295,8 +336,10 @@ cudaError_t launch_kv8_weights(const Kv8Args& a, const Kv8WeightArgs& t, cudaStr
     const bool wide = reinterpret_cast<uintptr_t>(t.q) % 16 == 0 && t.q_row % 8 == 0 && t.q_head % 8 == 0;
     auto go = [&](auto hd) {
         constexpr int HD = decltype(hd)::value;
-        return launch_kv8(wide ? kv8_weights_kernel<HD, true> : kv8_weights_kernel<HD, false>, dim3(p.ctas), kThreads, 0, s,
-                          a, t, p);
+        auto kern = wide ? kv8_weights_kernel<HD, true> : kv8_weights_kernel<HD, false>;
+        constexpr int bytes = sizeof(Smem<HD>);
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, s, a, t, p);
     };
     return a.hd == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
 }

@@ -8,7 +8,7 @@
 // sum never leaves the thread.  So there is nothing to exchange between threads,
 // no maximum, and the only operand beside the scores is a column's lse.
 //
-// A CTA holds 512 keys (128 KB), four tiles with an S in TMEM and four warps each,
+// A CTA holds 512 keys (128 KB), four tiles with an S in TMEM each,
 // so that a chunk of queries, 32 KB from L2, is used 65536 times: at 128 keys the
 // chunks alone would ask L2 for 18 TB/s.  One warp copies chunks, one issues the
 // products.  A unit is (sequence, KV head, 512 keys), as long as it has chunks of
@@ -28,7 +28,7 @@ namespace {
 constexpr int kTiles = 4, kTile = 128, kUnit = kTiles * kTile;     // keys
 constexpr int kSoftmaxWarps = 4 * kTiles, kProductWarp = kSoftmaxWarps, kCopyWarp = kProductWarp + 1;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
-constexpr int kQueries = 128, kRing = 2;
+constexpr int kQueries = 128, kRing = 3, kSums = 5;
 constexpr int kUnitCost = 2;            // a unit's keys, in the time of chunks
 
 struct WeightsPlan {
@@ -45,7 +45,7 @@ template <int HD>
 struct Smem {
     unsigned char q[kRing][kQueries * HD * 2];  // [HD / 64][query][64], 128-byte swizzle
     unsigned char k[kTiles][kTile * HD * 2];    // [key / 8][HD / 8][8][8]
-    float lse[kRing][kQueries];                 // minus the sums' logarithms, base 2
+    float lse[kSums][kQueries];                 // minus the sums' logarithms, base 2
     uint64_t q_full[kRing], q_free[kRing], k_full[kTiles], s_full[kTiles], s_free[kTiles];
     uint32_t tmem;
 };
@@ -190,19 +190,19 @@ template <int HD>
 __global__ void __launch_bounds__(kThreads, 1)
     kv8_weights_tc_kernel(const Kv8Args a, const Kv8WeightArgs t, const WeightsPlan p, const __grid_constant__ CUtensorMap map) {
     constexpr int REC = kv8_record(HD);
-    extern __shared__ unsigned char smem_raw[];
-    Smem<HD>& sm = *reinterpret_cast<Smem<HD>*>(smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023));
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    Smem<HD>& sm = *reinterpret_cast<Smem<HD>*>(smem_raw);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (warp == kProductWarp) tmem_alloc<1>(&sm.tmem, 512);
     if (tid == 0) {
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&sm.q_full[i], 1);
-            mbar_init(&sm.q_free[i], 1 + kSoftmaxWarps);
+            mbar_init(&sm.q_free[i], 1);
         }
         for (int i = 0; i < kTiles; ++i) {
             mbar_init(&sm.k_full[i], 4);
-            mbar_init(&sm.s_full[i], 1);
-            mbar_init(&sm.s_free[i], 4);
+            mbar_init(&sm.s_full[i], 2);        // the products' commit, and an arrival that orders the sums before it
+            mbar_init(&sm.s_free[i], 8);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -249,9 +249,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     alive = false;
                     break;
                 }
+                // the products of chunk it - kRing waited until the scores of the chunk before were in registers, so
+                // the weights of the one before that, which had this place, are done
+                static_assert(kSums == kRing + 2, "sums outlive their queries by two chunks");
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sm.lse[st][32 * i + lane] = -x[i] * kLog2e;
+                    sm.lse[it % kSums][32 * i + lane] = -x[i] * kLog2e;
                     x[i] = next[i];
                 }
                 __syncwarp();
@@ -288,6 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             umma_ss<1>(tmem + kQueries * i, ka + 16 * j, qb + (j / 4 * (kQueries * 128) + j % 4 * 32) / 16, idesc,
                                        j > 0);
                         umma_commit(&sm.s_full[i]);
+                        mbar_arrive(&sm.s_full[i]);
                     }
                     umma_commit(&sm.q_free[st]);
                 }
@@ -297,102 +301,139 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
     } else {
-        const int i = warp >> 2, row = (warp & 3) * 32 + lane;           // tile, key of the tile
-        const uint32_t s_at = tmem + kQueries * i + ((uint32_t)(32 * (warp & 3)) << 16);
+        // Warps 0..7 take tiles 0 and 2, the others 1 and 3; four of the eight have the first 64 columns of a tile's
+        // scores, four the others: a tile's scores are used up in half the time that four warps take, which is what
+        // its next products wait for.
+        const int group = warp >> 3, half = warp >> 2 & 1, row = (warp & 3) * 32 + lane;
+        const int i = group + 2 * half;                                  // tile whose key this thread converts
+        const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         const float c2 = t.scale * kLog2e;
         bool alive = true, began = false;
         int it = 0;
+        // A unit's key of this thread; its page is looked up a unit ahead.
+        auto look = [&](const Segment& k) {          // -1: no such key, -2: no such page
+            const int key = k.u * kUnit + i * kTile + row;
+            if (key >= k.q.len) return -1;
+            const int page = a.table[(size_t)k.s * a.table_ld + p.page_of(key / kKv8Block, a.bpp)];
+            return page < 0 ? -2 : page;
+        };
+        int page = look(at);
         for (;;) {
             const int key = at.u * kUnit + i * kTile + row, pos0 = at.q.len - at.q.rows;
-            // the key, as bf16
-            bool there = false;
-            {
+            const bool here = page >= 0 && page < a.n_pages;
+            if (!here && page != -1) kv8_flag(a, kKv8BadPage);
+            uint4 raw[HD / 16];
+            float scale = 0.f;
+#pragma unroll
+            for (int j = 0; j < HD / 16; ++j) raw[j] = make_uint4(0, 0, 0, 0);
+            if (here) {
                 const int b = key / kKv8Block, tok = key % kKv8Block;
-                const unsigned char* rec = nullptr;
-                if (key < at.q.len) {
-                    const int page = a.table[(size_t)at.s * a.table_ld + p.page_of(b, a.bpp)];
-                    there = page >= 0 && page < a.n_pages;
-                    if (there) rec = a.data + (((size_t)page * a.hk + at.h) * a.bpp + b - p.page_of(b, a.bpp) * a.bpp) * REC;
-                    else kv8_flag(a, kKv8BadPage);
-                }
-                uint4 raw[HD / 16];
-                float scale = 0.f;
+                const unsigned char* rec =
+                    a.data + (((size_t)page * a.hk + at.h) * a.bpp + b - p.page_of(b, a.bpp) * a.bpp) * REC;
+                scale = *reinterpret_cast<const float*>(rec + 32 * HD);
 #pragma unroll
-                for (int j = 0; j < HD / 16; ++j) raw[j] = make_uint4(0, 0, 0, 0);
-                if (rec) {
-                    scale = *reinterpret_cast<const float*>(rec + 32 * HD);
-#pragma unroll
-                    for (int j = 0; j < HD / 16; ++j)
-                        raw[j] = *reinterpret_cast<const uint4*>(rec + (tok >> 3) * 8 * HD + j * 128 + (tok & 7) * 16);
-                }
-                unsigned char* to = sm.k[i] + (row >> 3) * (HD * 16) + (row & 7) * 16;
-#pragma unroll
-                for (int j = 0; j < HD / 16; ++j) {
-                    const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
-                    uint32_t o[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 v = from_e4m3x2((uint16_t)(w[e / 2] >> 16 * (e & 1)));
-                        o[e] = pack_bf16(v.x * scale, v.y * scale);
-                    }
-                    *reinterpret_cast<uint4*>(to + 256 * j) = make_uint4(o[0], o[1], o[2], o[3]);
-                    *reinterpret_cast<uint4*>(to + 256 * j + 128) = make_uint4(o[4], o[5], o[6], o[7]);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.k_full[i]);
+                for (int j = 0; j < HD / 16; ++j)
+                    raw[j] = *reinterpret_cast<const uint4*>(rec + (tok >> 3) * 8 * HD + j * 128 + (tok & 7) * 16);
             }
-            float sum = 0.f;
+            // as bf16
+            unsigned char* to = sm.k[i] + (row >> 3) * (HD * 16) + (row & 7) * 16;
+#pragma unroll
+            for (int j = 0; j < HD / 16; ++j) {
+                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+                uint32_t o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 v = from_e4m3x2((uint16_t)(w[e / 2] >> 16 * (e & 1)));
+                    o[e] = pack_bf16(v.x * scale, v.y * scale);
+                }
+                *reinterpret_cast<uint4*>(to + 256 * j) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4*>(to + 256 * j + 128) = make_uint4(o[4], o[5], o[6], o[7]);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.k_full[i]);
+            {
+                Segment next = at;                   // not kept: its registers are the scores'
+                const bool more = next.next(a, line.x0, line.x1, p);
+                page = more ? look(next) : -1;
+                if (page >= 0 && page < a.n_pages) { // into L2, a line a thread
+                    const int b = (next.u * kUnit + i * kTile + row) / kKv8Block;
+                    const unsigned char* line_of = a.data + (((size_t)page * a.hk + next.h) * a.bpp + b -
+                                                             p.page_of(b, a.bpp) * a.bpp) * REC + (row >> 3 & 1) * 8 * HD;
+                    if ((row & 7) * 128 < 8 * HD) asm volatile("prefetch.global.L2 [%0];" ::"l"(line_of + (row & 7) * 128));
+                }
+            }
+            float sum[2] = {0.f, 0.f};               // tiles group and group + 2
             for (int c = at.c; c < at.end; ++c, ++it) {
-                const int st = it % kRing, n = columns(at, c), tok0 = c * p.tq;
-                alive = alive && mbar_wait(&sm.s_full[i], it & 1, kWaitLimitNs) &&
-                        mbar_wait(&sm.q_full[st], (it / kRing) & 1, kWaitLimitNs);       // the sums, too
-                __syncwarp();
-                umma_fence_after();
-                const bool edge = key - lane + 31 > pos0 + tok0;         // a row of the chunk that does not see a key
-                float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                // columns of rows that see this key
-                const int d = max(0, key - pos0 - tok0), from = d >= p.tq ? n : d * p.G;
+                const int n = columns(at, c), tok0 = c * p.tq;
+                const float* lse = sm.lse[it % kSums] + 64 * half;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int tile = group + 2 * u, first = at.u * kUnit + tile * kTile + (warp & 3) * 32;       // key of lane 0
+                    alive = alive && mbar_wait(&sm.s_full[tile], it & 1, kWaitLimitNs);
+                    __syncwarp();
+                    umma_fence_after();
+                    const bool edge = first + 31 > pos0 + tok0;          // a row of the chunk that does not see a key
+                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    const uint32_t s_at = lanes + kQueries * tile + 64 * half;
+                    if (edge || n < 64 * half + 64) {
+                        // columns of rows that see this key
+                        const int d = max(0, first + lane - pos0 - tok0);
+                        const int from = (d >= p.tq ? n : d * p.G) - 64 * half, to = min(n - 64 * half, 64);
 #pragma unroll 1
-                for (int j = 0; j < n; j += 32) {
-                    uint32_t s[32];
-                    tmem_ld32(s, s_at + j);
-                    tmem_wait_ld();
-                    tmem_pin(s);
-                    if (edge || j + 32 > n) {
+                        for (int j = 0; j < to; j += 32) {
+                            uint32_t s[32];
+                            tmem_ld32(s, s_at + j);
+                            tmem_wait_ld();
+                            tmem_pin(s);
 #pragma unroll
-                        for (int q = 0; q < 32; ++q) {
-                            const float x = fmaf(__uint_as_float(s[q]), c2, sm.lse[st][j + q]);
-                            if (j + q >= from && j + q < n) part[0].x += exp2_approx(x);
+                            for (int q = 0; q < 32; ++q) {
+                                const float x = fmaf(__uint_as_float(s[q]), c2, lse[j + q]);
+                                if (j + q >= from && j + q < to) part[0].x += exp2_approx(x);
+                            }
                         }
+                        umma_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sm.s_free[tile]);
                     } else {
+                        // the scores go to registers in one piece, and their place to the next products
+                        uint32_t s[2][32];
+                        tmem_ld32(s[0], s_at);
+                        tmem_ld32(s[1], s_at + 32);
+                        tmem_wait_ld();
+                        tmem_pin(s[0]);
+                        tmem_pin(s[1]);
+                        umma_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sm.s_free[tile]);
 #pragma unroll
-                        for (int q = 0; q < 32; q += 4) {
-                            const float4 l = *reinterpret_cast<const float4*>(&sm.lse[st][j + q]);
-                            const float2 x = fma2(make_float2(__uint_as_float(s[q]), __uint_as_float(s[q + 1])),
+                        for (int q = 0; q < 64; q += 4) {
+                            const uint32_t* v = s[q / 32] + q % 32;
+                            const float4 l = *reinterpret_cast<const float4*>(&lse[q]);
+                            const float2 x = fma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])),
                                                   make_float2(c2, c2), make_float2(l.x, l.y));
-                            const float2 y = fma2(make_float2(__uint_as_float(s[q + 2]), __uint_as_float(s[q + 3])),
+                            const float2 y = fma2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])),
                                                   make_float2(c2, c2), make_float2(l.z, l.w));
                             part[0] = add2(part[0], make_float2(exp2_approx(x.x), exp2_approx(x.y)));
                             part[1] = add2(part[1], make_float2(exp2_approx(y.x), exp2_approx(y.y)));
                         }
                     }
+                    part[0] = add2(part[0], part[1]);
+                    sum[u] += part[0].x + part[0].y;
                 }
-                umma_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&sm.s_free[i]);
-                    mbar_arrive(&sm.q_free[st]);
-                }
-                part[0] = add2(part[0], part[1]);
-                sum += part[0].x + part[0].y;
             }
-            if (!there) sum = 0.f;                   // no such page: unseen
+            // Both halves' sums of a tile meet where its keys were: their products are done.
+            auto join = [&](int tile) { return reinterpret_cast<float*>(sm.k[tile]) + row; };
+            *join(group + 2 * (half ^ 1)) = half ? sum[0] : sum[1];
+            asm volatile("bar.sync %0, 256;" ::"r"(1 + group) : "memory");
+            float v = (half ? sum[1] : sum[0]) + *join(i);
+            asm volatile("bar.sync %0, 256;" ::"r"(1 + group) : "memory");       // before the next unit's keys
+            if (!here) v = 0.f;                      // no such page: unseen
             const bool begins = at.c == at.c0, whole = begins && at.end == at.chunks;
             if (whole) {
-                put(a, t, at.q, at.s, at.h, key, sum);
+                put(a, t, at.q, at.s, at.h, key, v);
             } else {
-                p.part[(size_t)(2 * blockIdx.x + begins) * kUnit + i * kTile + row] = sum;
+                p.part[(size_t)(2 * blockIdx.x + begins) * kUnit + i * kTile + row] = v;
                 if (begins) {
                     began = true;
                     if (tid == 0) p.desc[blockIdx.x] = make_int4(at.s, at.h, at.u, line.cta_of(at.past() - 1));
@@ -427,7 +468,8 @@ __global__ void __launch_bounds__(kUnit) kv8_weights_merge_kernel(const Kv8Args 
 template <int HD>
 cudaError_t launch_tc(const Kv8Args& a, const Kv8WeightArgs& t, const WeightsPlan& p, const CUtensorMap& map, cudaStream_t s) {
     auto kern = kv8_weights_tc_kernel<HD>;
-    constexpr int bytes = sizeof(Smem<HD>) + 1024;
+    constexpr int bytes = sizeof(Smem<HD>);
+    static_assert(bytes <= 227 * 1024, "what a CTA can have");
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     return e != cudaSuccess ? e : launch_kv8(kern, dim3(p.ctas), kThreads, bytes, s, a, t, p, map);
 }

@@ -7,7 +7,7 @@
 // so that a likely token's logarithm, -log1p(tail), keeps its digits.
 //
 // A cluster takes a row, each CTA every so many segments of it.  A warp reads a
-// segment, 32 kVec 16-byte vectors, at a time into registers and keeps the row's
+// segment, 512 logits, at a time into registers, the next one while it works on it, and keeps the row's
 // maximum so far for all of its lanes: a segment that holds no larger logit,
 // nearly every one, adds to the sums without a look at single maxima.  The
 // segments' maxima stay in shared memory.  The n_top largest logits are in the
@@ -26,7 +26,6 @@ namespace ks {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kVec = 4;             // 16-byte vectors of a lane and segment
 constexpr int kMaxVocab = 1 << 22;
 constexpr int kMaxTop = 64, kMaxTokens = 64;
 constexpr int kCand = 1024;         // candidates that are ranked in one go
@@ -82,7 +81,7 @@ struct Sums {
 // position p of them is logit p - shift.
 template <typename T>
 struct Row {
-    static constexpr int E = 16 / sizeof(T), SEG = 32 * kVec * E;
+    static constexpr int E = 16 / sizeof(T), kVec = 16 / E, SEG = 32 * kVec * E;         // 16 logits a lane
     const T* base;
     int shift, end;                 // positions [shift, end) are the row's
     KS_DEV Row(const LogprobArgs& a, int row) {
@@ -93,23 +92,35 @@ struct Row {
     }
     KS_DEV int segments() const { return (end + SEG - 1) / SEG; }
     KS_DEV int position(int seg, int v) const { return seg * SEG + (v * 32 + (int)(threadIdx.x & 31)) * E; }
-    // a lane's part of a segment; what is not the row's is -inf
-    KS_DEV void load(int seg, float (&x)[kVec * E]) const {
-        uint4 raw[kVec];
+    // A lane's part of a segment, as it lies in memory; what is not the row's is -inf.
+    KS_DEV void load(int seg, uint4 (&raw)[kVec]) const {
         if (seg * SEG >= shift && (seg + 1) * SEG <= end) {
 #pragma unroll
             for (int v = 0; v < kVec; ++v) raw[v] = *reinterpret_cast<const uint4*>(base + position(seg, v));
-#pragma unroll
-            for (int v = 0; v < kVec; ++v) widen(raw[v], x + v * E);
         } else {
 #pragma unroll
-            for (int v = 0; v < kVec; ++v)
+            for (int v = 0; v < kVec; ++v) {
+                uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int p = position(seg, v) + e;
-                    x[v * E + e] = p >= shift && p < end ? to_float(base[p]) : -INFINITY;
+                for (int i = 0; i < 4; ++i) {
+                    const int p = position(seg, v) + i * (E / 4);
+                    if constexpr (E == 4) {
+                        w[i] = 0xff800000u;
+                        if (p >= shift && p < end) w[i] = __float_as_uint(base[p]);
+                    } else {
+                        w[i] = 0xff80ff80u;
+                        const unsigned short* e = reinterpret_cast<const unsigned short*>(base);
+                        if (p >= shift && p < end) w[i] = (w[i] & 0xffff0000u) | e[p];
+                        if (p + 1 >= shift && p + 1 < end) w[i] = (w[i] & 0xffffu) | (uint32_t)e[p + 1] << 16;
+                    }
                 }
+                raw[v] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         }
+    }
+    static KS_DEV void widen(const uint4 (&raw)[kVec], float (&x)[16]) {
+#pragma unroll
+        for (int v = 0; v < kVec; ++v) widen(raw[v], x + v * E);
     }
     static KS_DEV void widen(const uint4& r, float* x) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -169,10 +180,12 @@ KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigne
     auto each = [&](auto&& f) {
         for (int c = warp; c < chosen; c += kWarps) {
             const int seg = first + sm.chosen[c] * step;
-            float x[kVec * R::E];
-            row.load(seg, x);
+            uint4 raw[R::kVec];
+            float x[16];
+            row.load(seg, raw);
+            R::widen(raw, x);
 #pragma unroll
-            for (int v = 0; v < kVec; ++v)
+            for (int v = 0; v < R::kVec; ++v)
 #pragma unroll
                 for (int e = 0; e < R::E; ++e) {
                     const int p = row.position(seg, v) + e;
@@ -222,9 +235,9 @@ KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigne
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs a, int ctas) {
+__global__ void __launch_bounds__(kThreads, 2) logprob_kernel(const LogprobArgs a, int ctas) {
     using R = Row<T>;
-    constexpr int N = kVec * R::E;
+    constexpr int N = 16;
     extern __shared__ unsigned maxima[];
     __shared__ Smem sm;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -238,9 +251,12 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs a, 
     if (ctas > 1) cluster_sync();                    // every CTA runs: the first one's shared memory may be written
 
     Sums sum{-INFINITY, 0.f, 0.f, 0};                // m is the warp's, the rest the lane's
+    uint4 next[R::kVec];
+    if (warp < mine) row.load(rank + warp * ctas, next);
     for (int i = warp; i < mine; i += kWarps) {
         float x[N];
-        row.load(rank + i * ctas, x);
+        R::widen(next, x);
+        if (i + kWarps < mine) row.load(rank + (i + kWarps) * ctas, next);
         float top = x[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) top = fmaxf(top, x[j]);
@@ -353,7 +369,9 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobArgs a, 
 template <typename T>
 cudaError_t launch(const LogprobArgs& a, cudaStream_t s) {
     auto kern = logprob_kernel<T>;
-    const int ctas = 1;
+    // few rows: as many CTAs a row as are resident at once
+    int ctas = 1;
+    while (ctas < kMaxCluster && (int64_t)a.rows * ctas * 2 <= 2 * sm_count() && ctas * 2 * Row<T>::SEG * 4 <= a.vocab) ctas *= 2;
     const int segs = (a.vocab + Row<T>::E - 1 + Row<T>::SEG - 1) / Row<T>::SEG;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)a.rows * ctas);
