@@ -6,8 +6,10 @@
 // whole numbers in the scores' order, 11, 11 and 10 bits at a time, then one pass
 // that numbers what stays: scores above it, and as many equal ones, the earlier
 // first, as there is room for.  A cluster of up to eight CTAs takes a sequence's
-// head, each a contiguous slice, eight neighbouring scores a thread, in registers
-// unless the slice is longer than that; the CTAs read each other's counts.
+// head, each a contiguous slice, in registers unless it is longer than 18 scores
+// a thread; a warp has neighbouring ones, so that a ballot numbers them.  The CTAs
+// add their counts that are not zero to the first one's (reading all of each
+// other's counts took 25000 clocks a pass, five times the rest of it).
 //
 // gather: a CTA writes one block of 16 kept tokens.  Their codes come from up to 16
 // records with scales of their own; the new block's scale is the smallest power
@@ -27,8 +29,8 @@ namespace ks {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048, kPer = 8, kRound = kThreads * kPer;
-constexpr int kCopies = 4;          // of the first pass's bins: scores crowd into few of them
+constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048, kPer = 18, kRound = kThreads * kPer;
+constexpr int kCopies = 2;          // of a CTA's bins: scores crowd into few of them
 constexpr int kMaxCluster = 8;
 
 // Larger score, larger key; the two zeros are one, and NaN is below everything.
@@ -49,8 +51,8 @@ struct Stay {
     }
 };
 
-// Sum over the CTA of the counts before this thread's; total: of all.
-KS_DEV int block_before(int v, int* sums, int& total) {
+// Sum over the CTA of the values before this thread's.
+KS_DEV int block_before(int v, int* sums) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int u = v;
 #pragma unroll
@@ -60,21 +62,24 @@ KS_DEV int block_before(int v, int* sums, int& total) {
     }
     if (lane == 31) sums[warp] = u;
     __syncthreads();
-    int w = lane < kWarps ? sums[lane] : 0;
-    total = __reduce_add_sync(0xffffffffu, w);
-    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
-    __syncthreads();
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums[lane] : 0);
     return before + u - v;
 }
-
-KS_DEV int load_cluster(const int* p, int rank) { return (int)cluster_load(cluster_addr(p, (uint32_t)rank)); }
+KS_DEV void add_cluster(int* p, int rank, int v) {
+    asm volatile("red.relaxed.cluster.shared::cluster.add.s32 [%0], %1;" ::"r"(cluster_addr(p, (uint32_t)rank)), "r"(v)
+                 : "memory");
+}
+KS_DEV void store_cluster(int* p, int rank, int v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(p, (uint32_t)rank)), "r"(v) : "memory");
+}
 
 // Grid: a cluster of `ctas` along x per head, sequences along y.
-__global__ void __launch_bounds__(kThreads) kv8_select_kernel(const Kv8Args a, const Kv8EvictArgs t, int ctas) {
-    __shared__ int bins[kCopies][kBins], sums[kWarps];       // a pass each; the first one uses all
-    __shared__ unsigned s_prefix;
-    __shared__ int s_left, counts[2];                // scores above the least one that stays (and protected ones), equal ones
-    const int tid = threadIdx.x, h = blockIdx.x / ctas, rank = blockIdx.x % ctas, s = blockIdx.y;
+__global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a, const Kv8EvictArgs t, int ctas) {
+    __shared__ int bins[kCopies][kBins], all[3][kBins];      // this CTA's counts; the first CTA: everybody's, a pass each
+    __shared__ int sums[kWarps], found[3][2];                // per pass: the least key's bits so far, what is left of its bin
+    __shared__ int counts[kMaxCluster][2], in_warp[kWarps][2];       // scores that stay for sure, and equal ones
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int h = blockIdx.x / ctas, rank = blockIdx.x % ctas, s = blockIdx.y;
     grid_dependency_wait();
     grid_launch_dependents();
     const Stay w(a, t, s);
@@ -94,18 +99,20 @@ __global__ void __launch_bounds__(kThreads) kv8_select_kernel(const Kv8Args a, c
         return;
     }
     const int lo = w.first, hi = w.len - w.recent, most = w.n - w.first - w.recent;      // most of [lo, hi) stay
-    const int slice = ((w.len + ctas - 1) / ctas + kPer - 1) / kPer * kPer, begin = rank * slice;
-    const int end = min(w.len, begin + slice), rounds = max(0, end - begin + kRound - 1) / kRound;
+    const int slice = (w.len + ctas - 1) / ctas, begin = rank * slice, end = min(w.len, begin + slice);
+    const int rounds = max(0, end - begin + kRound - 1) / kRound;
     // this thread's scores of a round
     float v[kPer];
+    auto place = [&](int round, int e) { return begin + round * kRound + (warp * kPer + e) * 32 + lane; };
     auto load = [&](int round) {
-        const int i0 = begin + round * kRound + tid * kPer;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) v[e] = i0 + e < end ? score[i0 + e] : 0.f;
+        for (int e = 0; e < kPer; ++e) v[e] = place(round, e) < end ? score[place(round, e)] : 0.f;
     };
     if (rounds > 0) load(0);
     for (int i = tid; i < kCopies * kBins; i += kThreads) bins[0][i] = 0;
-    __syncthreads();
+    for (int i = tid; i < 3 * kBins; i += kThreads) all[0][i] = 0;
+    if (ctas > 1) cluster_sync();
+    else __syncthreads();
     // the least key that stays, and how many of those equal to it
     unsigned prefix = 0;
     int left = most;
@@ -116,116 +123,138 @@ __global__ void __launch_bounds__(kThreads) kv8_select_kernel(const Kv8Args a, c
             const unsigned above = pass == 0 ? 0u : 0xffffffffu << (shift + width);
             for (int round = 0; round < rounds; ++round) {
                 if (rounds > 1) load(round);
-                const int i0 = begin + round * kRound + tid * kPer;
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
                     const unsigned k = score_key(v[e]);
-                    if (i0 + e >= lo && i0 + e < min(hi, end) && (k & above) == prefix)
-                        atomicAdd(&bins[pass == 0 ? tid % kCopies : pass][k >> shift & ((1u << width) - 1)], 1);
+                    const int i = place(round, e);
+                    if (i >= lo && i < min(hi, end) && (k & above) == prefix)
+                        atomicAdd(&bins[lane % kCopies][k >> shift & ((1u << width) - 1)], 1);
                 }
             }
-            if (pass == 0) {
-                __syncthreads();
-                for (int i = tid; i < kBins; i += kThreads) {
-                    bins[0][i] += bins[1][i] + bins[2][i] + bins[3][i];
-                    bins[1][i] = bins[2][i] = 0;
+            __syncthreads();
+            for (int i = tid; i < kBins; i += kThreads) {
+                const int c = bins[0][i] + bins[1][i];
+                bins[0][i] = bins[1][i] = 0;
+                if (ctas == 1) all[pass][i] = c;
+                else if (c) add_cluster(&all[pass][i], 0, c);
+            }
+            if (ctas > 1) cluster_sync();
+            else __syncthreads();
+            if (rank == 0) {
+                // bins from the largest down, four a thread: the one in which the count passes what is left
+                constexpr int OWN = kBins / kThreads;
+                const int b0 = (1 << width) - 1 - OWN * tid;
+                int c[OWN] = {}, mine = 0;
+                if (b0 > 0)
+#pragma unroll
+                    for (int e = 0; e < OWN; ++e) c[e] = all[pass][b0 - e];
+#pragma unroll
+                for (int e = 0; e < OWN; ++e) mine += c[e];
+                int before = block_before(mine, sums);
+                if (before < left && before + mine >= left) {
+                    int e = 0;
+#pragma unroll
+                    for (int i = 0; i < OWN - 1; ++i)
+                        if (e == i && before + c[i] < left) {
+                            before += c[i];
+                            ++e;
+                        }
+                    for (int r = 0; r < ctas; ++r) {
+                        store_cluster(&found[pass][0], r, (int)(prefix | (unsigned)(b0 - e) << shift));
+                        store_cluster(&found[pass][1], r, left - before);
+                    }
                 }
             }
             if (ctas > 1) cluster_sync();
             else __syncthreads();
-            // bins from the largest down, some neighbouring ones a thread: the one in which the count passes what is left
-            constexpr int OWN = kBins / kThreads;
-            const int b0 = (1 << width) - 1 - OWN * tid;
-            int c[OWN] = {}, mine = 0;
-            if (b0 > 0)
-                for (int r = 0; r < ctas; ++r)
-#pragma unroll
-                    for (int e = 0; e < OWN; ++e)
-                        c[e] += ctas > 1 ? load_cluster(&bins[pass][b0 - e], r) : bins[pass][b0 - e];
-#pragma unroll
-            for (int e = 0; e < OWN; ++e) mine += c[e];
-            int total;
-            int before = block_before(mine, sums, total);
-            if (before < left && before + mine >= left) {
-                int e = 0;
-#pragma unroll
-                for (int i = 0; i < OWN - 1; ++i)
-                    if (e == i && before + c[i] < left) {
-                        before += c[i];
-                        ++e;
-                    }
-                s_prefix = prefix | (unsigned)(b0 - e) << shift;
-                s_left = left - before;
-            }
-            __syncthreads();
-            prefix = s_prefix;
-            left = s_left;
-            __syncthreads();
+            prefix = (unsigned)found[pass][0];
+            left = found[pass][1];
         }
     }
-    // which of a thread's scores stay for sure, and which are equal to the least one
-    auto mark = [&](int round, unsigned& sure, unsigned& equal) {
-        sure = equal = 0;
-        const int i0 = begin + round * kRound + tid * kPer;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            const int i = i0 + e;
-            if (i >= end) continue;
-            if (i < lo || i >= hi) {
-                sure |= 1u << e;
-            } else if (most > 0) {
-                const unsigned k = score_key(v[e]);
-                sure |= (unsigned)(k > prefix) << e;
-                equal |= (unsigned)(k == prefix) << e;
-            }
-        }
+    // whether a score stays for sure, and whether it is equal to the least one that stays
+    auto mark = [&](int round, int e, bool& sure, bool& equal) {
+        const int i = place(round, e);
+        const unsigned k = score_key(v[e]);
+        const bool inside = i >= lo && i < hi;
+        sure = i < end && (!inside || (most > 0 && k > prefix));
+        equal = i < end && inside && most > 0 && k == prefix;
     };
     int ties = 0, done = 0;                          // equal ones, and kept ones, before
-    unsigned sure, equal;
     if (ctas > 1) {
         int n_sure = 0, n_equal = 0;
         for (int round = 0; round < rounds; ++round) {
             if (rounds > 1) load(round);
-            mark(round, sure, equal);
-            n_sure += __popc(sure);
-            n_equal += __popc(equal);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                bool sure, equal;
+                mark(round, e, sure, equal);
+                n_sure += sure;
+                n_equal += equal;
+            }
         }
-        int total;
-        block_before(n_sure, sums, total);
-        if (tid == 0) counts[0] = total;
-        block_before(n_equal, sums, total);
-        if (tid == 0) counts[1] = total;
+        n_sure = __reduce_add_sync(0xffffffffu, n_sure);
+        n_equal = __reduce_add_sync(0xffffffffu, n_equal);
+        if (lane == 0) {
+            in_warp[warp][0] = n_sure;
+            in_warp[warp][1] = n_equal;
+        }
+        __syncthreads();
+        if (tid < 2 * ctas) {                        // to CTA tid / 2
+            int n = 0;
+            for (int i = 0; i < kWarps; ++i) n += in_warp[i][tid % 2];
+            store_cluster(&counts[rank][tid % 2], tid / 2, n);
+        }
         cluster_sync();
         for (int r = 0; r < rank; ++r) {
-            const int n = load_cluster(&counts[0], r), e = load_cluster(&counts[1], r);
-            done += n + min(e, max(left - ties, 0));
-            ties += e;
+            done += counts[r][0] + min(counts[r][1], max(left - ties, 0));
+            ties += counts[r][1];
         }
     }
     for (int round = 0; round < rounds; ++round) {
         if (rounds > 1) load(round);
-        mark(round, sure, equal);
-        int total;
-        const int before = block_before(__popc(equal), sums, total);
-        int take = min(max(left - ties - before, 0), __popc(equal));     // of the thread's equal ones, the first
-        ties += total;
+        unsigned sure_of[kPer], equal_of[kPer];      // of the warp's 32 scores e
+        int n_sure = 0, n_equal = 0;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if ((equal >> e & 1) && take > 0) {
-                sure |= 1u << e;
-                --take;
+        for (int e = 0; e < kPer; ++e) {
+            bool sure, equal;
+            mark(round, e, sure, equal);
+            sure_of[e] = __ballot_sync(0xffffffffu, sure);
+            equal_of[e] = __ballot_sync(0xffffffffu, equal);
+            n_sure += __popc(sure_of[e]);
+            n_equal += __popc(equal_of[e]);
+        }
+        __syncthreads();                             // the counts of the round before are read
+        if (lane == 0) {
+            in_warp[warp][0] = n_sure;
+            in_warp[warp][1] = n_equal;
+        }
+        __syncthreads();
+        int o = done, tie = ties;                    // before this warp
+        for (int i = 0; i < kWarps; ++i) {
+            const int n = in_warp[i][0], q = in_warp[i][1], taken = min(q, max(left - ties, 0));
+            if (i < warp) {
+                o += n + taken;
+                tie += q;
             }
-        int o = done + block_before(__popc(sure), sums, total);
-        done += total;
+            done += n + taken;
+            ties += q;
+        }
+        const unsigned below = (1u << lane) - 1;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (sure >> e & 1) {
-                kept[o] = begin + round * kRound + tid * kPer + e;
-                if (out) out[o] = v[e];
-                ++o;
+        for (int e = 0; e < kPer; ++e) {
+            const int rest = max(left - tie, 0);     // equal ones that there is still room for: the first of them
+            const bool stays = (sure_of[e] >> lane & 1) || ((equal_of[e] >> lane & 1) && __popc(equal_of[e] & below) < rest);
+            const unsigned staying = __ballot_sync(0xffffffffu, stays);
+            if (stays) {
+                const int to = o + __popc(staying & below);
+                kept[to] = place(round, e);
+                if (out) out[to] = v[e];
             }
+            o += __popc(staying);
+            tie += __popc(equal_of[e]);
+        }
     }
-    if (ctas > 1) cluster_sync();                    // nobody leaves while its counts are read
+    if (ctas > 1) cluster_sync();                    // nobody leaves before what it is sent has arrived
 }
 
 // Where a block's token comes from.
@@ -376,6 +405,12 @@ __global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const K
             k_top = fmaxf(k_top, top[0][i]);
             v_top = fmaxf(v_top, top[1][i]);
         }
+        if (b + (int)gridDim.x < blocks) {           // the next block's records into L2, 16 lines of values each
+            const Source u = from[buf ^ 1][tok];
+            if (u.rec && u.fresh)
+                for (int l = part; l < CODES / 128; l += TH) asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + CODES + l * 128));
+            if (u.rec) asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + k_byte<HD>(u.token, 16 * part)));
+        }
         const float ks = scale_for(k_top), vs = scale_for(v_top);
         // a factor is past 2^18 only where all codes are zeros
         if (tid < kKv8Block) {
@@ -422,7 +457,7 @@ cudaError_t launch_select(const Kv8Args& a, const Kv8EvictArgs& t, cudaStream_t 
     return cudaLaunchKernelEx(&cfg, kv8_select_kernel, a, t, ctas);
 }
 
-constexpr int kGatherBlocks = 4;
+constexpr int kGatherBlocks = 8;
 
 }  // namespace
 
