@@ -99,6 +99,29 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
         return;
     }
     const int lo = w.first, hi = w.len - w.recent, most = w.n - w.first - w.recent;      // most of [lo, hi) stay
+    const unsigned below = (1u << lane) - 1;
+    if (w.len <= kThreads) {
+        // a token a thread, ranked against all between: 1000 clocks where the passes' fixed steps take 12000
+        if (rank > 0) return;
+        const bool inside = tid >= lo && tid < hi;
+        const float mine = tid < w.len && (inside || out) ? score[tid] : 0.f;
+        const unsigned key = inside ? score_key(mine) : 0u;
+        unsigned* keys = reinterpret_cast<unsigned*>(bins[0]);
+        keys[tid] = key;
+        __syncthreads();
+        int before = 0;
+        for (int i = lo; i < hi; ++i) before += keys[i] > key || (keys[i] == key && i < tid);
+        const bool stays = tid < w.len && (!inside || before < most);
+        const unsigned staying = __ballot_sync(0xffffffffu, stays);
+        if (lane == 0) sums[warp] = __popc(staying);
+        __syncthreads();
+        const int o = __reduce_add_sync(0xffffffffu, lane < warp ? sums[lane] : 0) + __popc(staying & below);
+        if (stays) {
+            kept[o] = tid;
+            if (out) out[o] = mine;
+        }
+        return;
+    }
     const int slice = (w.len + ctas - 1) / ctas, begin = rank * slice, end = min(w.len, begin + slice);
     const int rounds = max(0, end - begin + kRound - 1) / kRound;
     // this thread's scores of a round
@@ -239,7 +262,6 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
             done += n + taken;
             ties += q;
         }
-        const unsigned below = (1u << lane) - 1;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const int rest = max(left - tie, 0);     // equal ones that there is still room for: the first of them
@@ -259,9 +281,9 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
 
 // Where a block's token comes from.
 struct Source {
-    const unsigned char* rec;       // null: no such page, or no token
-    int token;                      // of the record
-    int fresh;                      // another record than the token before
+    const unsigned char* rec;       // where there is none (no such page, no token) the cache's first, and
+    uint32_t mask;                  // zeros instead of ones
+    int token;                      // of the record; its byte among a dim's 16 in bits 8 ..
 };
 // A power of two f <= 2^18 as two factors of f16; below 2^-24 a code times f rounds to 0 anyway.
 KS_DEV void two_factors(float f, __half& a, __half& b) {
@@ -285,10 +307,11 @@ KS_DEV uint32_t halves_of(uint32_t codes) {
 // A CTA takes blocks blockIdx.x, + gridDim.x, .. of a sequence's head.
 template <int HD>
 __global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const Kv8EvictArgs t) {
-    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, TH = HD / 16, WARPS = HD / 32, BATCH = 8;
+    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, TH = HD / 16, WARPS = HD / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, s = blockIdx.z;
     __shared__ __align__(16) Source from[2][kKv8Block];
-    __shared__ float2 scales[kKv8Block];
+    __shared__ float k_scales[2][kKv8Block];
+    __shared__ __align__(8) float v_scales[2][kKv8Block];    // in the new record's order
     __shared__ __align__(8) __half factors[2][kKv8Block];         // of the values, in the new record's order
     __shared__ float top[2][WARPS];
     __shared__ unsigned char* to[2];                 // the new record; null: none is to be written
@@ -301,19 +324,21 @@ __global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const K
         const int at = b * kKv8Block + lane;
         return warp == 0 && lane < kKv8Block && at < w.n ? t.kept[((size_t)s * a.hk + h) * t.kept_ld + at] : -1;
     };
-    auto look = [&](int b, int place, Source& f, unsigned char*& rec) {
-        f.rec = nullptr;
-        f.token = 0;
-        f.fresh = 1;
+    auto look = [&](int b, int place, Source& f, float2& sc, unsigned char*& rec) {
+        f = Source{a.data, 0u, 0};
+        sc = make_float2(0.f, 0.f);
         rec = nullptr;
         if (warp != 0 || b >= blocks) return;
         if (place >= 0) {
-            f.token = place % kKv8Block;
-            f.rec = kv8_record_at(a, s, place / kKv8Block, h, REC);
-            if (!f.rec) kv8_flag(a, kKv8BadPage);    // read as zeros
+            const unsigned char* at = kv8_record_at(a, s, place / kKv8Block, h, REC);
+            if (at) {
+                const int token = place % kKv8Block;
+                f = Source{at, 0xffffffffu, token | v_byte(token) << 8};
+                sc = *reinterpret_cast<const float2*>(at + 2 * CODES);
+            } else {
+                kv8_flag(a, kKv8BadPage);            // read as zeros
+            }
         }
-        const int block = place < 0 ? -1 : place / kKv8Block, before = __shfl_up_sync(0xffffffffu, block, 1);
-        f.fresh = lane % BATCH == 0 || before != block;
         if (lane == kKv8Block) {
             const int page = t.new_table[(size_t)s * t.new_table_ld + b / a.bpp];
             if (page < 0 || page >= a.n_pages) kv8_flag(a, kKv8BadPage);
@@ -322,64 +347,58 @@ __global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const K
             if (rec && w.n == w.len && rec == kv8_record_at(a, s, b, h, REC)) rec = nullptr;
         }
     };
-    auto keep = [&](int buf, const Source& f, unsigned char* rec) {
+    auto keep = [&](int buf, const Source& f, const float2& sc, unsigned char* rec) {
         if (warp != 0) return;
-        if (lane < kKv8Block) from[buf][lane] = f;
+        if (lane < kKv8Block) {
+            from[buf][lane] = f;
+            k_scales[buf][lane] = sc.x;
+            v_scales[buf][v_byte(lane)] = sc.y;
+        }
         if (lane == kKv8Block) to[buf] = rec;
     };
     Source f;
+    float2 sc;
     unsigned char* rec;
-    look(blockIdx.x, place_of(blockIdx.x), f, rec);
-    keep(0, f, rec);
+    look(blockIdx.x, place_of(blockIdx.x), f, sc, rec);
+    keep(0, f, sc, rec);
     int place = place_of(blockIdx.x + gridDim.x);
     __syncthreads();
     int buf = 0;
     const int tok = tid / TH, part = tid % TH;
     for (int b = blockIdx.x; b < blocks; b += gridDim.x, buf ^= 1) {
-        float2 sc = make_float2(0.f, 0.f);
-        if (tid < kKv8Block && from[buf][tid].rec) sc = *reinterpret_cast<const float2*>(from[buf][tid].rec + 2 * CODES);
-        uint4 k = make_uint4(0, 0, 0, 0);
+        uint4 k;
+        uint32_t k_mask;
         {
             const Source u = from[buf][tok];         // of this thread's piece of keys
-            if (u.rec) k = *reinterpret_cast<const uint4*>(u.rec + k_byte<HD>(u.token, 16 * part));
+            k = *reinterpret_cast<const uint4*>(u.rec + k_byte<HD>(u.token & 15, 16 * part));
+            k_mask = u.mask;
         }
         uint32_t v[4];                               // the dim's codes in the new record's order
 #pragma unroll
-        for (int j0 = 0; j0 < kKv8Block; j0 += BATCH) {
-            uint4 raw[BATCH];
-            int token[BATCH];
-            bool fresh[BATCH];
+        for (int half = 0; half < 2; ++half) {
+            uint4 raw[8];
 #pragma unroll
-            for (int j = 0; j < BATCH; ++j) {
-                const Source u = from[buf][j0 + j];
-                token[j] = u.token;
-                fresh[j] = u.fresh;
-                if (u.fresh) {
-                    raw[j] = make_uint4(0, 0, 0, 0);
-                    if (u.rec) raw[j] = *reinterpret_cast<const uint4*>(u.rec + CODES + tid * 16);
-                }
-            }
-            uint32_t byte[BATCH];
+            for (int j = 0; j < 8; ++j)              // neighbours of one record meet in L1
+                raw[j] = *reinterpret_cast<const uint4*>(from[buf][8 * half + j].rec + (CODES + tid * 16));
+            uint32_t byte[8];
 #pragma unroll
-            for (int j = 0; j < BATCH; ++j) {
-                if (j > 0 && !fresh[j]) raw[j] = raw[j - 1];
-                const int at = v_byte(token[j]);
+            for (int j = 0; j < 8; ++j) {
+                const uint2 u = *reinterpret_cast<const uint2*>(&from[buf][8 * half + j].mask);
+                const int at = (int)u.y >> 8;
                 const uint32_t lo = __byte_perm(raw[j].x, raw[j].y, at & 7), hi = __byte_perm(raw[j].z, raw[j].w, at & 7);
-                byte[j] = at & 8 ? hi : lo;
+                byte[j] = (at & 8 ? hi : lo) & u.x;
             }
             // tokens 2 w, 2 w + 1 are bytes 0, 1 of word w, 8 + 2 w and 9 + 2 w bytes 2, 3
 #pragma unroll
             for (int w4 = 0; w4 < 4; ++w4) {
                 const uint32_t pair = __byte_perm(byte[2 * w4], byte[2 * w4 + 1], 0x0040);
-                v[w4] = j0 == 0 ? pair : __byte_perm(v[w4], pair, 0x5410);
+                v[w4] = half == 0 ? pair : __byte_perm(v[w4], pair, 0x5410);
             }
         }
-        look(b + gridDim.x, place, f, rec);          // the next block's
+        look(b + gridDim.x, place, f, sc, rec);      // the next block's
         place = place_of(b + 2 * gridDim.x);
-        if (tid < kKv8Block) scales[tid] = sc;
-        __syncthreads();
         // the largest values: NaN is passed over, infinities there are none
-        const uint32_t kw[4] = {k.x, k.y, k.z, k.w};
+        const uint32_t kw[4] = {k.x & k_mask, k.y & k_mask, k.z & k_mask, k.w & k_mask};
         __half2 k_max = __half2(0.f, 0.f);
         float v_top = 0.f;
 #pragma unroll
@@ -387,10 +406,10 @@ __global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const K
             const uint32_t x = halves_of(kw[i / 2] >> 16 * (i & 1)), y = halves_of(v[i / 2] >> 16 * (i & 1));
             k_max = __hmax2(k_max, __habs2(*reinterpret_cast<const __half2*>(&x)));
             const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&y));
-            const int t0 = 8 * (i & 1) + 2 * (i / 2);
-            v_top = fmaxf(fmaxf(v_top, fabsf(z.x * scales[t0].y)), fabsf(z.y * scales[t0 + 1].y));
+            const float2 at = *reinterpret_cast<const float2*>(&v_scales[buf][2 * i]);
+            v_top = fmaxf(fmaxf(v_top, fabsf(z.x * at.x)), fabsf(z.y * at.y));
         }
-        const float k_scale = scales[tok].x;
+        const float k_scale = k_scales[buf][tok];
         float k_top = fmaxf(__low2float(k_max), __high2float(k_max)) * k_scale;      // one scale a token
         k_top = warp_max(k_top);
         v_top = warp_max(v_top);
@@ -398,7 +417,7 @@ __global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const K
             top[0][warp] = k_top;
             top[1][warp] = v_top;
         }
-        keep(buf ^ 1, f, rec);
+        keep(buf ^ 1, f, sc, rec);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < WARPS; ++i) {
@@ -407,15 +426,13 @@ __global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const K
         }
         if (b + (int)gridDim.x < blocks) {           // the next block's records into L2, 16 lines of values each
             const Source u = from[buf ^ 1][tok];
-            if (u.rec && u.fresh)
-                for (int l = part; l < CODES / 128; l += TH) asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + CODES + l * 128));
-            if (u.rec) asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + k_byte<HD>(u.token, 16 * part)));
+            for (int l = part; l < CODES / 128; l += TH) asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + CODES + l * 128));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + k_byte<HD>(u.token & 15, 16 * part)));
         }
         const float ks = scale_for(k_top), vs = scale_for(v_top);
         // a factor is past 2^18 only where all codes are zeros
         if (tid < kKv8Block) {
-            const int at = v_byte(tid);
-            two_factors(fminf(sc.y * inverse_pow2(vs), 262144.f), factors[0][at], factors[1][at]);
+            two_factors(fminf(v_scales[buf][tid] * inverse_pow2(vs), 262144.f), factors[0][tid], factors[1][tid]);
         }
         __half ka, kb;
         two_factors(fminf(k_scale * inverse_pow2(ks), 262144.f), ka, kb);
