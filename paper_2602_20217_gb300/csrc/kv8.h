@@ -47,6 +47,7 @@ struct Kv8AttnArgs {
 // Which part of the keys a launch attends to: all of a sequence's, those that a group of sequences has in common (its
 // "sequences" are the groups, whose rows all see all of them), or what a sequence has behind these.
 enum Kv8Part { kWhole = 0, kCommon = 1, kTail = 2 };
+bool kv8_attention_fits(const Kv8Args& a, int hq, Kv8Part part = kWhole);      // false: too many units and tiles for one call
 struct Kv8SharedArgs {      // groups of sequences with a common beginning
     const int32_t* groups;  // [n_groups + 1] first sequence of each
     const int32_t* tokens;  // [n_groups] common tokens
@@ -56,7 +57,6 @@ struct Kv8SharedArgs {      // groups of sequences with a common beginning
 constexpr int kKv8MaxGroup = 64;    // query heads a KV head
 cudaError_t launch_kv8_append(int dtype, const Kv8Args& a, const Kv8RowArgs& r, cudaStream_t s);
 size_t kv8_attention_workspace(int hd, int group, int n_rows);
-bool kv8_attention_fits(const Kv8Args& a, int hq);     // false: too many units and tiles for one call
 // A call is two launches: the units' runs, and directly behind it the merge of units that lie in several, if the
 // first says that there can be any (merge; not where sequences are at most a tile long).
 cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, bool& merge,

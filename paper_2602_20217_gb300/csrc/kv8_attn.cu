@@ -742,9 +742,12 @@ __global__ void __launch_bounds__(kMergeThreads) kv8_rows_merge_kernel(const Kv8
 // uneven batch costs more than its parts: 200 single rows at 4000 tokens 268 us,
 // one sequence of 2000 rows at 4000 tokens 201 us, both in one call 811 us (32
 // heads over 8); two calls over disjoint sequences are faster there.
-int rows_of_unit(int G, int64_t n_rows, int64_t n_seqs) {
+int rows_of_unit(int G, int64_t n_rows, int64_t n_seqs, Kv8Part part = kWhole) {
     const int64_t avg = n_seqs > 0 ? (n_rows * G + n_seqs - 1) / n_seqs : 0;
     const int64_t need = std::max<int64_t>(avg, G);
+    // What sequences have behind a common beginning is short: two units of 16 rows there read it twice, but begin
+    // sooner than one of 128 (see kv8_shared.cu).
+    if (part == kTail && G <= 16 && need > 16 && need <= 32) return 16;
     return need <= 8 ? 8 : need <= 16 ? 16 : kKv8TcRows;
 }
 // CTAs of an SM
@@ -774,10 +777,10 @@ cudaError_t launch_merge(const Kv8Args& a, const Kv8AttnArgs& t, const Kv8Plan& 
 }
 
 // The plan of a call; false if its line of tiles is too long for 32 bits.
-bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& tiles) {
+bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& tiles, Kv8Part part) {
     const int G = hq / a.hk;
     p = Kv8Plan{};
-    p.rg = rows_of_unit(G, a.n_rows, a.n_seqs);
+    p.rg = rows_of_unit(G, a.n_rows, a.n_seqs, part);
     p.G = G;
     p.token_mul = (65536 + G - 1) / G;
     p.tq = p.rg / G;
@@ -790,8 +793,8 @@ bool make_plan(const Kv8Args& a, int hq, Kv8Plan& p, int64_t& units, int64_t& ti
 }
 
 // The plan with what depends on the launch's pointers and device.
-bool make_launch(const Kv8Args& a, const Kv8AttnArgs& t, Kv8Plan& p, int64_t& units, int64_t& tiles) {
-    if (!make_plan(a, t.hq, p, units, tiles)) return false;
+bool make_launch(const Kv8Args& a, const Kv8AttnArgs& t, Kv8Plan& p, int64_t& units, int64_t& tiles, Kv8Part part) {
+    if (!make_plan(a, t.hq, p, units, tiles, part)) return false;
     p.ctas = (int)std::min<int64_t>(std::min(sm_count(), kKv8Sms) * resident(p.rg), units * (tiles + p.cost));
     p.q_wide = reinterpret_cast<uintptr_t>(t.q) % 16 == 0 && t.q_row % 8 == 0 && t.q_head % 8 == 0;
     p.out_wide = reinterpret_cast<uintptr_t>(t.out) % 16 == 0 && t.out_row % 8 == 0 && t.out_head % 8 == 0;
@@ -811,10 +814,10 @@ size_t kv8_attention_workspace(int hd, int group, int n_rows) {
     return sizeof(float) * rows * (hd + 4) + sizeof(int4) * kKv8MaxCtas;
 }
 
-bool kv8_attention_fits(const Kv8Args& a, int hq) {
+bool kv8_attention_fits(const Kv8Args& a, int hq, Kv8Part part) {
     Kv8Plan p;
     int64_t units, tiles;
-    return make_plan(a, hq, p, units, tiles);
+    return make_plan(a, hq, p, units, tiles, part);
 }
 
 namespace {
@@ -835,7 +838,7 @@ cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStr
     Kv8Plan p;
     int64_t units, tiles;
     merge = false;
-    if (!make_launch(a, t, p, units, tiles)) return cudaErrorInvalidValue;
+    if (!make_launch(a, t, p, units, tiles, part)) return cudaErrorInvalidValue;
     merge = tiles > 1;
     if (p.rg == kKv8TcRows) return launch_kv8_tc(a, t, p, s, part);
     return with_part(part, [&](auto c) {
@@ -851,7 +854,7 @@ cudaError_t launch_kv8_attention(const Kv8Args& a, const Kv8AttnArgs& t, cudaStr
 cudaError_t launch_kv8_merge(const Kv8Args& a, const Kv8AttnArgs& t, cudaStream_t s, Kv8Part part) {
     Kv8Plan p;
     int64_t units, tiles;
-    if (!make_launch(a, t, p, units, tiles)) return cudaErrorInvalidValue;
+    if (!make_launch(a, t, p, units, tiles, part)) return cudaErrorInvalidValue;
     return with_part(part, [&](auto c) {
         constexpr int PART = decltype(c)::value;
         return a.hd == 128 ? launch_merge<128, PART>(a, t, p, units, s) : launch_merge<64, PART>(a, t, p, units, s);

@@ -118,7 +118,7 @@ size_t kv8_shared_workspace(int hd, int hk, int hq, int n_seqs, int n_rows, int 
 bool kv8_shared_fits(const Kv8Args& a, const Kv8SharedArgs& g, int hq) {
     Kv8Args c = a;
     c.n_seqs = g.n_groups;
-    return kv8_attention_fits(a, hq) && kv8_attention_fits(c, hq);
+    return kv8_attention_fits(a, hq, kTail) && kv8_attention_fits(c, hq, kCommon);
 }
 
 cudaError_t launch_kv8_shared(const Kv8Args& a, const Kv8SharedArgs& g, const Kv8AttnArgs& t, cudaStream_t s) {

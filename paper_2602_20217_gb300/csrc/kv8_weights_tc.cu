@@ -410,15 +410,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int q = 0; q < 64; q += 4) {
                             const uint32_t* v = s[q / 32] + q % 32;
                             const float4 l = *reinterpret_cast<const float4*>(&lse[q]);
-                            const float2 x = fma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])),
+                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])),
                                                   make_float2(c2, c2), make_float2(l.x, l.y));
-                            const float2 y = fma2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])),
+                            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])),
                                                   make_float2(c2, c2), make_float2(l.z, l.w));
-                            part[0] = add2(part[0], make_float2(exp2_approx(x.x), exp2_approx(x.y)));
-                            part[1] = add2(part[1], make_float2(exp2_approx(y.x), exp2_approx(y.y)));
+                            part[0] = __fadd2_rn(part[0], make_float2(exp2_approx(x.x), exp2_approx(x.y)));
+                            part[1] = __fadd2_rn(part[1], make_float2(exp2_approx(y.x), exp2_approx(y.y)));
                         }
                     }
-                    part[0] = add2(part[0], part[1]);
+                    part[0] = __fadd2_rn(part[0], part[1]);
                     sum[u] += part[0].x + part[0].y;
                 }
             }

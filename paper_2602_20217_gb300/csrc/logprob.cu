@@ -7,7 +7,7 @@
 // so that a likely token's logarithm, -log1p(tail), keeps its digits.
 //
 // A cluster takes a row, each CTA every so many segments of it.  A warp reads a
-// segment, 512 logits, at a time into registers, the next one while it works on it, and keeps the row's
+// segment, 32 times 64 bytes, at a time into registers, the next one while it works on it, and keeps the row's
 // maximum so far for all of its lanes: a segment that holds no larger logit,
 // nearly every one, adds to the sums without a look at single maxima.  The
 // segments' maxima stay in shared memory.  The n_top largest logits are in the
@@ -25,12 +25,13 @@ namespace ks {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxVocab = 1 << 22;
 constexpr int kMaxTop = 64, kMaxTokens = 64;
 constexpr int kCand = 1024;         // candidates that are ranked in one go
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 8, kCtas = 4;            // CTAs of a row; of an SM
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kTame = 4096.f;     // of a maximum's |m k|
 constexpr float kLeast = -200.f;    // below it 2^u is 0: -inf must not be multiplied by that
 
 struct LogprobArgs {
@@ -77,11 +78,18 @@ struct Sums {
     }
 };
 
+// One warp: the sums of all lanes together.
+KS_DEV Sums merged(Sums u, float k) {
+    const float top = warp_max(u.m);
+    u.raise(top, k);
+    return Sums{top, warp_sum(u.t), warp_sum(u.s), (int)__reduce_add_sync(0xffffffffu, u.n)};
+}
+
 // A row as 16-byte vectors from the boundary at or before its first logit on:
 // position p of them is logit p - shift.
 template <typename T>
 struct Row {
-    static constexpr int E = 16 / sizeof(T), kVec = 16 / E, SEG = 32 * kVec * E;         // 16 logits a lane
+    static constexpr int E = 16 / sizeof(T), kVec = 4, SEG = 32 * kVec * E;
     const T* base;
     int shift, end;                 // positions [shift, end) are the row's
     KS_DEV Row(const LogprobArgs& a, int row) {
@@ -118,9 +126,38 @@ struct Row {
             }
         }
     }
-    static KS_DEV void widen(const uint4 (&raw)[kVec], float (&x)[16]) {
+    // The largest of a lane's logits; NaN is passed over.
+    template <int N>
+    static KS_DEV float largest(const uint4 (&raw)[N]) {
+        if constexpr (E == 4) {
+            float m = -INFINITY;
 #pragma unroll
-        for (int v = 0; v < kVec; ++v) widen(raw[v], x + v * E);
+            for (int v = 0; v < N; ++v)
+                m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(raw[v].x)), __uint_as_float(raw[v].y)),
+                          fmaxf(__uint_as_float(raw[v].z), __uint_as_float(raw[v].w)));
+            return m;
+        } else {
+            __nv_bfloat162 m = pair(raw[0].x);
+#pragma unroll
+            for (int v = 0; v < N; ++v)
+                m = __hmax2(__hmax2(__hmax2(m, pair(raw[v].x)), pair(raw[v].y)), __hmax2(pair(raw[v].z), pair(raw[v].w)));
+            return fmaxf(__low2float(m), __high2float(m));
+        }
+    }
+    static KS_DEV __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+    // What is below `floor`, -inf too, as that: the exponential is 0, and times the exponent still is.  NaN stays.
+    static KS_DEV uint4 raised(const uint4& r, float floor) {
+        uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E == 4) {
+                asm("max.NaN.f32 %0, %0, %1;" : "+r"(w[i]) : "r"(__float_as_uint(floor)));
+            } else {
+                const __nv_bfloat162 f = __float2bfloat162_rn(floor), m = __hmax2_nan(pair(w[i]), f);
+                w[i] = *reinterpret_cast<const uint32_t*>(&m);
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
     static KS_DEV void widen(const uint4& r, float* x) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -142,9 +179,10 @@ KS_DEV void store_cluster(void* p, int rank, unsigned long long v) {
 
 struct Smem {
     unsigned long long cand[kCand];
-    unsigned long long best[kMaxCluster][kMaxTop];      // the first CTA: every CTA's largest
+    __align__(16) unsigned long long best[kMaxCluster][kMaxTop];      // the first CTA: every CTA's largest
     unsigned long long sums[kMaxCluster][2];            // the first CTA: (m, n), (t, s) of each
     Sums warp[kWarps];
+    unsigned first[kWarps];
     int counts[2][kWarps];
     unsigned bound;
     int n_cand, n_chosen;
@@ -165,35 +203,80 @@ KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigne
         sm.n_cand = 0;
         sm.bound = 0;
     }
-    __syncthreads();
-    // the K segments with the largest maxima
-    for (int i = tid; i < n; i += kThreads) {
-        const unsigned k = maxima[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += maxima[j] > k || (maxima[j] == k && j < i);
-        if (rank < K) sm.chosen[rank] = i;
-        if (rank == K - 1) sm.bound = k;
+    __syncthreads();                                 // maxima, and the zeros behind them
+    // The K segments with the largest maxima.  Up to one a thread they are ranked against each other, which is soonest
+    // done; of more the K-th largest key is found bit by bit, by one warp: several microseconds, but in calls of many rows
+    // next to nothing beside what the SM's other CTAs do meanwhile (1500 rows of 151936 fp32 logits 157 us, ranked 171).
+    if (n <= kThreads) {
+        if (const int i = tid; i < n) {
+            const unsigned k = maxima[i];
+            const uint4* four = reinterpret_cast<const uint4*>(maxima);      // behind the last one: zeros
+            int rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < (n + 3) / 4; ++j) {
+                const uint4 o = four[j];
+                rank += (o.x > k) + (o.y > k) + (o.z > k) + (o.w > k);
+                // equal ones count where they are earlier
+                if (o.x == k || o.y == k || o.z == k || o.w == k)
+                    rank += (o.x == k && 4 * j < i) + (o.y == k && 4 * j + 1 < i) + (o.z == k && 4 * j + 2 < i) +
+                            (o.w == k && 4 * j + 3 < i);
+            }
+            if (rank < K) sm.chosen[rank] = i;
+            if (rank == K - 1) sm.bound = k;
+        }
+    } else if (warp == 0) {
+        unsigned least = 0;
+        int above = 0, at = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const unsigned t = least | (1u << bit);
+            int c = 0;
+            for (int i = lane; i < n; i += 32) c += maxima[i] >= t;
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (c >= K) least = t;
+            if (c == K) break;
+        }
+        for (int i = lane; i < n; i += 32) above += maxima[i] > least;
+        int equal = K - __reduce_add_sync(0xffffffffu, above);           // of those at `least`, the first
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const unsigned k = i0 + lane < n ? maxima[i0 + lane] : 0u, below = (1u << lane) - 1;
+            const unsigned same = __ballot_sync(0xffffffffu, i0 + lane < n && k == least);
+            const bool take = i0 + lane < n && (k > least || (k == least && __popc(same & below) < equal));
+            equal = max(0, equal - __popc(same));
+            const unsigned taken = __ballot_sync(0xffffffffu, take);
+            if (take) sm.chosen[at + __popc(taken & below)] = i0 + lane;
+            at += __popc(taken);
+        }
+        if (lane == 0) sm.bound = least;
     }
     __syncthreads();
     const int chosen = min(n, K);
     const unsigned bound = sm.bound;
-    auto each = [&](auto&& f) {
+    // f for each logit of the chosen segments, of lanes that have one at least as large as `from`
+    auto each = [&](float from, auto&& f) {
+        uint4 next[R::kVec];
+        if (warp < chosen) row.load(first + sm.chosen[warp] * step, next);
         for (int c = warp; c < chosen; c += kWarps) {
             const int seg = first + sm.chosen[c] * step;
             uint4 raw[R::kVec];
-            float x[16];
-            row.load(seg, raw);
-            R::widen(raw, x);
 #pragma unroll
-            for (int v = 0; v < R::kVec; ++v)
+            for (int v = 0; v < R::kVec; ++v) raw[v] = next[v];
+            if (c + kWarps < chosen) row.load(first + sm.chosen[c + kWarps] * step, next);
+            if (R::largest(raw) < from) continue;
+#pragma unroll
+            for (int v = 0; v < R::kVec; ++v) {
+                const uint4 one[1] = {raw[v]};
+                if (R::largest(one) < from) continue;
+                float x[R::E];
+                R::widen(raw[v], x);
 #pragma unroll
                 for (int e = 0; e < R::E; ++e) {
                     const int p = row.position(seg, v) + e;
-                    if (p >= row.shift && p < row.end) f(x[v * R::E + e], p - row.shift);
+                    if (p >= row.shift && p < row.end) f(x[e], p - row.shift);
                 }
+            }
         }
     };
-    each([&](float x, int id) {
+    each(order_value(bound), [&](float x, int id) {
         if (order_key(x) >= bound) {
             const int at = atomicAdd(&sm.n_cand, 1);
             if (at < kCand) sm.cand[at] = pair_key(x, id);
@@ -207,7 +290,7 @@ KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigne
         for (int bit = 63, turn = 0; bit >= 0; --bit, turn ^= 1) {
             const unsigned long long t = least | (1ull << bit);
             int c = 0;
-            each([&](float x, int id) { c += pair_key(x, id) >= t; });
+            each(-INFINITY, [&](float x, int id) { c += pair_key(x, id) >= t; });
             c = __reduce_add_sync(0xffffffffu, c);
             if (lane == 0) sm.counts[turn][warp] = c;
             __syncthreads();
@@ -217,7 +300,7 @@ KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigne
         }
         if (tid == 0) sm.n_cand = 0;
         __syncthreads();
-        each([&](float x, int id) {
+        each(-INFINITY, [&](float x, int id) {
             const unsigned long long k = pair_key(x, id);
             if (k >= least) sm.cand[atomicAdd(&sm.n_cand, 1)] = k;
         });
@@ -227,6 +310,7 @@ KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigne
     for (int i = tid; i < found; i += kThreads) {
         const unsigned long long k = sm.cand[i];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < found; ++j) rank += sm.cand[j] > k;
         if (rank < K) out[rank] = k;
     }
@@ -235,10 +319,9 @@ KS_DEV void largest(const Row<T>& row, int first, int step, int n, const unsigne
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) logprob_kernel(const LogprobArgs a, int ctas) {
+__global__ void __launch_bounds__(kThreads, kCtas) logprob_kernel(const LogprobArgs a, int ctas) {
     using R = Row<T>;
-    constexpr int N = 16;
-    extern __shared__ unsigned maxima[];
+    extern __shared__ __align__(16) unsigned maxima[];
     __shared__ Smem sm;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)blockIdx.x % ctas;
@@ -251,23 +334,74 @@ __global__ void __launch_bounds__(kThreads, 2) logprob_kernel(const LogprobArgs 
     if (ctas > 1) cluster_sync();                    // every CTA runs: the first one's shared memory may be written
 
     Sums sum{-INFINITY, 0.f, 0.f, 0};                // m is the warp's, the rest the lane's
+    // Sums of segments whose logits are all below m, u taken as x k - (m k rounded): `rest` is what the rounding left.
+    float2 quick_t = make_float2(0.f, 0.f), quick_s = quick_t;
+    float mk = 0.f, rest = 0.f;
+    bool tame = false;                               // whether m is small enough for that
+    const float floor = -2.f * kTame / k;            // 2^u is 0 from there down, beside any tame maximum
+    auto set = [&](float top) {
+        sum.raise(top, k);
+        mk = sum.m * k;
+        tame = fabsf(mk) < kTame && floor > -1e38f;
+        rest = tame ? fmaf(sum.m, k, -mk) : 0.f;
+    };
+    auto settle = [&] {
+        const float t = quick_t.x + quick_t.y, f = fmaf(-rest, kLn2, 1.f);       // 2^-rest, rest under 2^-12
+        sum.s = fmaf(fmaf(-rest, t, quick_s.x + quick_s.y), f, sum.s);
+        sum.t = fmaf(t, f, sum.t);
+        quick_t = quick_s = make_float2(0.f, 0.f);
+    };
     uint4 next[R::kVec];
     if (warp < mine) row.load(rank + warp * ctas, next);
+    // the tokens' logits, long before they are needed
+    const bool scores = rank == 0 && tid < a.n_tokens;
+    float token_x = __uint_as_float(0x7fc00000u);
+    if (scores) {
+        const int id = a.tokens[(size_t)r * a.n_tokens + tid];
+        if (id >= 0 && id < a.vocab) token_x = to_float(row.base[row.shift + id]);
+    }
+    // All warps begin with the largest logit of their first segments: on its own a warp would meet a larger one than so
+    // far in three of twelve segments, and looks at each of its logits then.
+    {
+        unsigned key = 0;                            // below that of any number
+        if (warp < mine) key = __reduce_max_sync(0xffffffffu, order_key(R::largest(next)));
+        if (lane == 0) sm.first[warp] = key;
+        __syncthreads();
+        key = __reduce_max_sync(0xffffffffu, sm.first[lane % kWarps]);
+        if (key != 0) set(order_value(key));
+    }
     for (int i = warp; i < mine; i += kWarps) {
-        float x[N];
-        R::widen(next, x);
+        uint4 raw[R::kVec];
+#pragma unroll
+        for (int v = 0; v < R::kVec; ++v) raw[v] = next[v];
         if (i + kWarps < mine) row.load(rank + (i + kWarps) * ctas, next);
-        float top = x[0];
-#pragma unroll
-        for (int j = 1; j < N; ++j) top = fmaxf(top, x[j]);
-        const unsigned key = __reduce_max_sync(0xffffffffu, order_key(top));
+        const unsigned key = __reduce_max_sync(0xffffffffu, order_key(R::largest(raw)));
         if (lane == 0) maxima[i] = key;
-        top = order_value(key);
-        if (top >= sum.m) {
-            sum.raise(top, k);
-            const float ref = sum.m == -INFINITY ? 0.f : sum.m;
+        const float top = order_value(key);
+        if (top < sum.m && tame) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
+            for (int v = 0; v < R::kVec; ++v) {
+                float x[R::E];
+                R::widen(R::raised(raw[v], floor), x);
+#pragma unroll
+                for (int j = 0; j < R::E; j += 2) {
+                    const float2 u = __ffma2_rn(make_float2(x[j], x[j + 1]), make_float2(k, k), make_float2(-mk, -mk));
+                    const float2 e = make_float2(exp2_approx(u.x), exp2_approx(u.y));
+                    quick_t = __fadd2_rn(quick_t, e);
+                    quick_s = __ffma2_rn(e, u, quick_s);
+                }
+            }
+            continue;
+        }
+        settle();
+        if (top >= sum.m) set(top);
+        const float ref = sum.m == -INFINITY ? 0.f : sum.m;
+#pragma unroll
+        for (int v = 0; v < R::kVec; ++v) {
+            float x[R::E];
+            R::widen(raw[v], x);
+#pragma unroll
+            for (int j = 0; j < R::E; ++j) {
                 const float u = (x[j] - ref) * k, e = exp2_approx(u);
                 if (x[j] == sum.m) {
                     ++sum.n;
@@ -276,39 +410,22 @@ __global__ void __launch_bounds__(kThreads, 2) logprob_kernel(const LogprobArgs 
                     sum.s = fmaf(e, fmaxf(u, kLeast), sum.s);
                 }
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float u = (x[j] - sum.m) * k, e = exp2_approx(u);
-                sum.t += e;
-                sum.s = fmaf(e, fmaxf(u, kLeast), sum.s);
-            }
         }
     }
+    settle();
     sum.t = warp_sum(sum.t);
     sum.s = warp_sum(sum.s);
     sum.n = __reduce_add_sync(0xffffffffu, sum.n);
     if (lane == 0) sm.warp[warp] = sum;
     __syncthreads();
-    if (tid == 0) {
-        float top = -INFINITY;
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm.warp[w].m);
-        Sums all{top, 0.f, 0.f, 0};
-        for (int w = 0; w < kWarps; ++w) {
-            Sums u = sm.warp[w];
-            u.raise(top, k);
-            all.t += u.t;
-            all.s += u.s;
-            all.n += u.n;
-        }
+    if (tid < 4 && mine + tid < (mine + 3) / 4 * 4) maxima[mine + tid] = 0;
+    if (warp == 0) {
+        const Sums all = merged(lane < kWarps ? sm.warp[lane] : Sums{-INFINITY, 0.f, 0.f, 0}, k);
         const unsigned long long lo = __float_as_uint(all.m) | (unsigned long long)(unsigned)all.n << 32;
         const unsigned long long hi = __float_as_uint(all.t) | (unsigned long long)__float_as_uint(all.s) << 32;
-        if (ctas > 1) {
-            store_cluster(&sm.sums[rank][0], 0, lo);
-            store_cluster(&sm.sums[rank][1], 0, hi);
-        } else {
-            sm.sums[0][0] = lo;
-            sm.sums[0][1] = hi;
+        if (lane < 2) {
+            if (ctas > 1) store_cluster(&sm.sums[rank][lane], 0, lane ? hi : lo);
+            else sm.sums[0][lane] = lane ? hi : lo;
         }
     }
     if (a.n_top) {
@@ -321,44 +438,45 @@ __global__ void __launch_bounds__(kThreads, 2) logprob_kernel(const LogprobArgs 
         if (rank != 0) return;
     }
     __syncthreads();
-    if (tid == 0) {
-        Sums all{-INFINITY, 0.f, 0.f, 0};
-        for (int c = 0; c < ctas; ++c) all.m = fmaxf(all.m, __uint_as_float((unsigned)sm.sums[c][0]));
-        for (int c = 0; c < ctas; ++c) {
-            Sums u{__uint_as_float((unsigned)sm.sums[c][0]), __uint_as_float((unsigned)sm.sums[c][1]),
-                   __uint_as_float((unsigned)(sm.sums[c][1] >> 32)), (int)(sm.sums[c][0] >> 32)};
-            u.raise(all.m, k);
-            all.t += u.t;
-            all.s += u.s;
-            all.n += u.n;
-        }
+    if (warp == 0) {
+        Sums u{-INFINITY, 0.f, 0.f, 0};
+        if (lane < ctas)
+            u = Sums{__uint_as_float((unsigned)sm.sums[lane][0]), __uint_as_float((unsigned)sm.sums[lane][1]),
+                     __uint_as_float((unsigned)(sm.sums[lane][1] >> 32)), (int)(sm.sums[lane][0] >> 32)};
+        const Sums all = merged(u, k);
         // NaN logits are in t, an infinite one is the maximum; a row of -inf alone has no distribution
         const bool empty = all.m == -INFINITY;
         const float log_z = all.n == 1 ? log1pf(all.t) : logf((float)all.n + all.t);
-        sm.bad = all.t != all.t || all.m == INFINITY;
-        sm.m = all.m;
-        sm.log_z = sm.bad ? __uint_as_float(0x7fc00000u) : empty ? INFINITY : log_z;
-        if (a.entropy)
-            a.entropy[r] = sm.bad ? __uint_as_float(0x7fc00000u)
+        const bool bad = all.t != all.t || all.m == INFINITY;
+        if (lane == 0) {
+            sm.bad = bad;
+            sm.m = all.m;
+            sm.log_z = bad ? __uint_as_float(0x7fc00000u) : empty ? INFINITY : log_z;
+        }
+        if (a.entropy && lane == 0)
+            a.entropy[r] = bad ? __uint_as_float(0x7fc00000u)
                                   : empty ? 0.f : log_z - all.s * kLn2 / ((float)all.n + all.t);
     }
     __syncthreads();
     const float m = sm.m == -INFINITY ? 0.f : sm.m, log_z = sm.log_z;
-    for (int i = tid; i < a.n_tokens; i += kThreads) {
-        const int id = a.tokens[(size_t)r * a.n_tokens + i];
-        const bool inside = id >= 0 && id < a.vocab;
-        const float x = inside ? to_float(row.base[row.shift + id]) : __uint_as_float(0x7fc00000u);
-        a.logprobs[(size_t)r * a.n_tokens + i] = (x - m) / a.temperature - log_z;
-    }
+    if (scores) a.logprobs[(size_t)r * a.n_tokens + tid] = (token_x - m) / a.temperature - log_z;
     if (a.n_top == 0) return;
     // the CTAs' largest against each other
     const int n = ctas * a.n_top;
     for (int i = tid; i < n; i += kThreads) {
         const unsigned long long key = sm.best[i / a.n_top][i % a.n_top];
         if (key == 0ull) continue;
-        int at = 0;
-        for (int c = 0; c < ctas; ++c)
-            for (int j = 0; j < a.n_top; ++j) at += sm.best[c][j] > key;
+        // each list is in order: how many of it are larger, all lists at once
+        int pos[kMaxCluster] = {}, at = 0;
+#pragma unroll
+        for (int step = kMaxTop; step > 0; step /= 2) {
+            if (step > a.n_top) continue;
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c)
+                if (c < ctas && pos[c] + step <= a.n_top && sm.best[c][pos[c] + step - 1] > key) pos[c] += step;
+        }
+#pragma unroll
+        for (int c = 0; c < kMaxCluster; ++c) at += pos[c];
         if (at >= a.n_top) continue;
         const size_t o = (size_t)r * a.n_top + at;
         a.top_ids[o] = sm.bad ? -1 : pair_id(key);
@@ -371,12 +489,12 @@ cudaError_t launch(const LogprobArgs& a, cudaStream_t s) {
     auto kern = logprob_kernel<T>;
     // few rows: as many CTAs a row as are resident at once
     int ctas = 1;
-    while (ctas < kMaxCluster && (int64_t)a.rows * ctas * 2 <= 2 * sm_count() && ctas * 2 * Row<T>::SEG * 4 <= a.vocab) ctas *= 2;
+    while (ctas < kMaxCluster && (int64_t)a.rows * ctas * 2 <= kCtas * sm_count() && ctas * 2 * Row<T>::SEG * 4 <= a.vocab) ctas *= 2;
     const int segs = (a.vocab + Row<T>::E - 1 + Row<T>::SEG - 1) / Row<T>::SEG;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)a.rows * ctas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(unsigned) * ((segs + ctas - 1) / ctas);
+    cfg.dynamicSmemBytes = sizeof(unsigned) * (((segs + ctas - 1) / ctas + 3) / 4 * 4);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
