@@ -11,15 +11,15 @@
 // add their counts that are not zero to the first one's (reading all of each
 // other's counts took 25000 clocks a pass, five times the rest of it).
 //
-// gather: a CTA writes one block of 16 kept tokens.  Their codes come from up to 16
+// gather: a warp writes one block of 16 kept tokens.  Their codes come from up to 16
 // records with scales of their own; the new block's scale is the smallest power
 // of two for their values, as an append of them would choose it, and a code is
 // multiplied by a power of two, which rounds only where it becomes subnormal.  A
-// token's keys are 16-byte pieces of its record, a thread each.  Its values are
-// one byte of every 16: a thread takes a dim, reads the 16 bytes of each record
-// that the block's tokens come from once, and has the new record's 16 bytes of the
-// dim together without any exchange.  The places and pages of a CTA's next block
-// are looked up while it works on one.
+// token's keys are 16-byte pieces of its record.  Its values are one byte of every
+// 16: a lane takes four dims (two of heads of 64), reads their bytes of each record
+// that the block's tokens come from once, and has the new record's bytes of its
+// dims together without any exchange.  Four warps a block, which wait for each
+// other, and 16 reads of each row took 75 us where this takes TIME.
 #include <algorithm>
 
 #include "kv8.cuh"
@@ -279,12 +279,6 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
     if (ctas > 1) cluster_sync();                    // nobody leaves before what it is sent has arrived
 }
 
-// Where a block's token comes from.
-struct Source {
-    const unsigned char* rec;       // where there is none (no such page, no token) the cache's first, and
-    uint32_t mask;                  // zeros instead of ones
-    int token;                      // of the record; its byte among a dim's 16 in bits 8 ..
-};
 // A power of two f <= 2^18 as two factors of f16; below 2^-24 a code times f rounds to 0 anyway.
 KS_DEV void two_factors(float f, __half& a, __half& b) {
     f = fmaxf(f, 1.f / 16777216.f);
@@ -304,155 +298,151 @@ KS_DEV uint32_t halves_of(uint32_t codes) {
     return h;
 }
 
-// A CTA takes blocks blockIdx.x, + gridDim.x, .. of a sequence's head.
+constexpr int kGatherWarps = 4;
+
 template <int HD>
-__global__ void __launch_bounds__(HD) kv8_gather_kernel(const Kv8Args a, const Kv8EvictArgs t) {
-    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, TH = HD / 16, WARPS = HD / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, s = blockIdx.z;
-    __shared__ __align__(16) Source from[2][kKv8Block];
-    __shared__ float k_scales[2][kKv8Block];
-    __shared__ __align__(8) float v_scales[2][kKv8Block];    // in the new record's order
-    __shared__ __align__(8) __half factors[2][kKv8Block];         // of the values, in the new record's order
-    __shared__ float top[2][WARPS];
-    __shared__ unsigned char* to[2];                 // the new record; null: none is to be written
+__global__ void __launch_bounds__(32 * kGatherWarps) kv8_gather_kernel(const Kv8Args a, const Kv8EvictArgs t) {
+    constexpr int REC = kv8_record(HD), CODES = kKv8Block * HD, D = HD / 32, PARTS = HD / 16;    // D: dims, and pieces, of a lane
+    constexpr unsigned ALL = 0xffffffffu;
+    const int lane = threadIdx.x & 31, b = blockIdx.x * kGatherWarps + (threadIdx.x >> 5), h = blockIdx.y, s = blockIdx.z;
     grid_dependency_wait();
     grid_launch_dependents();
     const Stay w(a, t, s);
-    const int blocks = (w.n + kKv8Block - 1) / kKv8Block;
-    // Lanes 0..15 of warp 0 look for a block's tokens, in two steps an iteration apart, lane 16 for its place.
-    auto place_of = [&](int b) {
-        const int at = b * kKv8Block + lane;
-        return warp == 0 && lane < kKv8Block && at < w.n ? t.kept[((size_t)s * a.hk + h) * t.kept_ld + at] : -1;
-    };
-    auto look = [&](int b, int place, Source& f, float2& sc, unsigned char*& rec) {
-        f = Source{a.data, 0u, 0};
-        sc = make_float2(0.f, 0.f);
-        rec = nullptr;
-        if (warp != 0 || b >= blocks) return;
-        if (place >= 0) {
-            const unsigned char* at = kv8_record_at(a, s, place / kKv8Block, h, REC);
-            if (at) {
-                const int token = place % kKv8Block;
-                f = Source{at, 0xffffffffu, token | v_byte(token) << 8};
-                sc = *reinterpret_cast<const float2*>(at + 2 * CODES);
-            } else {
-                kv8_flag(a, kKv8BadPage);            // read as zeros
-            }
-        }
-        if (lane == kKv8Block) {
-            const int page = t.new_table[(size_t)s * t.new_table_ld + b / a.bpp];
-            if (page < 0 || page >= a.n_pages) kv8_flag(a, kKv8BadPage);
-            else rec = a.data + (((size_t)page * a.hk + h) * a.bpp + b % a.bpp) * REC;
-            // a sequence that keeps all of its tokens may keep its pages
-            if (rec && w.n == w.len && rec == kv8_record_at(a, s, b, h, REC)) rec = nullptr;
-        }
-    };
-    auto keep = [&](int buf, const Source& f, const float2& sc, unsigned char* rec) {
-        if (warp != 0) return;
-        if (lane < kKv8Block) {
-            from[buf][lane] = f;
-            k_scales[buf][lane] = sc.x;
-            v_scales[buf][v_byte(lane)] = sc.y;
-        }
-        if (lane == kKv8Block) to[buf] = rec;
-    };
-    Source f;
-    float2 sc;
-    unsigned char* rec;
-    look(blockIdx.x, place_of(blockIdx.x), f, sc, rec);
-    keep(0, f, sc, rec);
-    int place = place_of(blockIdx.x + gridDim.x);
-    __syncthreads();
-    int buf = 0;
-    const int tok = tid / TH, part = tid % TH;
-    for (int b = blockIdx.x; b < blocks; b += gridDim.x, buf ^= 1) {
-        uint4 k;
-        uint32_t k_mask;
-        {
-            const Source u = from[buf][tok];         // of this thread's piece of keys
-            k = *reinterpret_cast<const uint4*>(u.rec + k_byte<HD>(u.token & 15, 16 * part));
-            k_mask = u.mask;
-        }
-        uint32_t v[4];                               // the dim's codes in the new record's order
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint4 raw[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)              // neighbours of one record meet in L1
-                raw[j] = *reinterpret_cast<const uint4*>(from[buf][8 * half + j].rec + (CODES + tid * 16));
-            uint32_t byte[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint2 u = *reinterpret_cast<const uint2*>(&from[buf][8 * half + j].mask);
-                const int at = (int)u.y >> 8;
-                const uint32_t lo = __byte_perm(raw[j].x, raw[j].y, at & 7), hi = __byte_perm(raw[j].z, raw[j].w, at & 7);
-                byte[j] = (at & 8 ? hi : lo) & u.x;
-            }
-            // tokens 2 w, 2 w + 1 are bytes 0, 1 of word w, 8 + 2 w and 9 + 2 w bytes 2, 3
-#pragma unroll
-            for (int w4 = 0; w4 < 4; ++w4) {
-                const uint32_t pair = __byte_perm(byte[2 * w4], byte[2 * w4 + 1], 0x0040);
-                v[w4] = half == 0 ? pair : __byte_perm(v[w4], pair, 0x5410);
-            }
-        }
-        look(b + gridDim.x, place, f, sc, rec);      // the next block's
-        place = place_of(b + 2 * gridDim.x);
-        // the largest values: NaN is passed over, infinities there are none
-        const uint32_t kw[4] = {k.x & k_mask, k.y & k_mask, k.z & k_mask, k.w & k_mask};
-        __half2 k_max = __half2(0.f, 0.f);
-        float v_top = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t x = halves_of(kw[i / 2] >> 16 * (i & 1)), y = halves_of(v[i / 2] >> 16 * (i & 1));
-            k_max = __hmax2(k_max, __habs2(*reinterpret_cast<const __half2*>(&x)));
-            const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&y));
-            const float2 at = *reinterpret_cast<const float2*>(&v_scales[buf][2 * i]);
-            v_top = fmaxf(fmaxf(v_top, fabsf(z.x * at.x)), fabsf(z.y * at.y));
-        }
-        const float k_scale = k_scales[buf][tok];
-        float k_top = fmaxf(__low2float(k_max), __high2float(k_max)) * k_scale;      // one scale a token
-        k_top = warp_max(k_top);
-        v_top = warp_max(v_top);
-        if (lane == 0) {
-            top[0][warp] = k_top;
-            top[1][warp] = v_top;
-        }
-        keep(buf ^ 1, f, sc, rec);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) {
-            k_top = fmaxf(k_top, top[0][i]);
-            v_top = fmaxf(v_top, top[1][i]);
-        }
-        if (b + (int)gridDim.x < blocks) {           // the next block's records into L2, 16 lines of values each
-            const Source u = from[buf ^ 1][tok];
-            for (int l = part; l < CODES / 128; l += TH) asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + CODES + l * 128));
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(u.rec + k_byte<HD>(u.token & 15, 16 * part)));
-        }
-        const float ks = scale_for(k_top), vs = scale_for(v_top);
-        // a factor is past 2^18 only where all codes are zeros
-        if (tid < kKv8Block) {
-            two_factors(fminf(v_scales[buf][tid] * inverse_pow2(vs), 262144.f), factors[0][tid], factors[1][tid]);
-        }
-        __half ka, kb;
-        two_factors(fminf(k_scale * inverse_pow2(ks), 262144.f), ka, kb);
-        __syncthreads();
-        if (unsigned char* out = to[buf]) {
-            const __half2 ka2 = __half2(ka, ka), kb2 = __half2(kb, kb);
-            uint32_t c[4], d[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c[i] = scaled(halves_of(kw[i]), ka2, kb2) | scaled(halves_of(kw[i] >> 16), ka2, kb2) << 16;
-                const __half2* f0 = reinterpret_cast<const __half2*>(factors[0] + 4 * i);
-                const __half2* f1 = reinterpret_cast<const __half2*>(factors[1] + 4 * i);
-                d[i] = scaled(halves_of(v[i]), f0[0], f1[0]) | scaled(halves_of(v[i] >> 16), f0[1], f1[1]) << 16;
-            }
-            *reinterpret_cast<uint4*>(out + k_byte<HD>(tok, 16 * part)) = make_uint4(c[0], c[1], c[2], c[3]);
-            *reinterpret_cast<uint4*>(out + CODES + tid * 16) = make_uint4(d[0], d[1], d[2], d[3]);
-            if (tid == 0) *reinterpret_cast<float2*>(out + 2 * CODES) = make_float2(ks, vs);
-        }
-        __syncthreads();                             // before the buffers' next turn
+    if (b * kKv8Block >= w.n) return;
+    // lanes 0..15: the block's tokens
+    const int at = b * kKv8Block + lane;
+    int place = -1;
+    if (lane < kKv8Block && at < w.n) place = t.kept[((size_t)s * a.hk + h) * t.kept_ld + at];
+    const int page = t.new_table[(size_t)s * t.new_table_ld + b / a.bpp];
+    unsigned char* to = nullptr;
+    if (page >= 0 && page < a.n_pages) to = a.data + (((size_t)page * a.hk + h) * a.bpp + b % a.bpp) * REC;
+    else if (lane == 0) kv8_flag(a, kKv8BadPage);
+    // a sequence that keeps all of its tokens may keep its pages
+    if (to == nullptr || (w.n == w.len && to == kv8_record_at(a, s, b, h, REC))) return;
+    const int block = place < 0 ? -1 : place / kKv8Block, token = place & (kKv8Block - 1);
+    const unsigned char* rec = nullptr;              // null: no such page, read as zeros, or no token
+    float2 scale = make_float2(0.f, 0.f);
+    if (block >= 0) {
+        rec = kv8_record_at(a, s, block, h, REC);
+        if (rec) scale = *reinterpret_cast<const float2*>(rec + 2 * CODES);
+        else kv8_flag(a, kKv8BadPage);
     }
+    const unsigned there = __ballot_sync(ALL, rec != nullptr);
+    const int before = __shfl_up_sync(ALL, block, 1);
+    const unsigned fresh = __ballot_sync(ALL, rec != nullptr && (lane == 0 || block != before));
+    auto rec_of = [&](int j) {
+        return reinterpret_cast<const unsigned char*>(__shfl_sync(ALL, reinterpret_cast<unsigned long long>(rec), j));
+    };
+    // values of dims D lane ..: 16 bytes each, of a record at a time, the next one's on their way
+    uint4 row[D], next[D];
+    uint32_t v[D][4];
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        row[i] = next[i] = make_uint4(0, 0, 0, 0);
+        v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0;
+    }
+    auto fetch = [&](int j) {                        // of the j-th token's record
+        const unsigned char* of = rec_of(j & 31) + CODES + lane * (16 * D);
+#pragma unroll
+        for (int i = 0; i < D; ++i) next[i] = *reinterpret_cast<const uint4*>(of + 16 * i);
+    };
+    unsigned rest = fresh;
+    if (rest) fetch(__ffs(rest) - 1);
+    // pieces of keys: token (lane + 32 i) / PARTS, dims 16 ((lane + 32 i) % PARTS) ..
+    uint4 k[D];
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        const int p = lane + 32 * i;
+        const unsigned char* of = rec_of(p / PARTS);
+        const int from = __shfl_sync(ALL, token, p / PARTS);
+        k[i] = make_uint4(0, 0, 0, 0);
+        if (of) k[i] = *reinterpret_cast<const uint4*>(of + k_byte<HD>(from, 16 * (p % PARTS)));
+    }
+    // the largest values: NaN is passed over, infinities there are none
+    float k_top = 0.f;
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        const uint32_t w4[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+        __half2 m = __half2(0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t x = halves_of(w4[e / 2] >> 16 * (e & 1));
+            m = __hmax2(m, __habs2(*reinterpret_cast<const __half2*>(&x)));
+        }
+        // one scale a token
+        k_top = fmaxf(k_top, fmaxf(__low2float(m), __high2float(m)) * __shfl_sync(ALL, scale.x, (lane + 32 * i) / PARTS));
+    }
+    k_top = warp_max(k_top);
+    const float ks = scale_for(k_top);
+    // lanes 0..15: both factors of a token; one past 2^18 only where all codes are zeros
+    auto factors = [&](float from, float to_scale) {
+        __half x, y;
+        two_factors(fminf(from * inverse_pow2(to_scale), 262144.f), x, y);
+        return __half2(x, y);
+    };
+    const __half2 kf = factors(scale.x, ks);
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        const int p = lane + 32 * i;
+        const uint32_t f = __shfl_sync(ALL, *reinterpret_cast<const uint32_t*>(&kf), p / PARTS);
+        const __half2 both = *reinterpret_cast<const __half2*>(&f), f0 = __low2half2(both), f1 = __high2half2(both);
+        const uint32_t w4[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+        uint32_t c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = scaled(halves_of(w4[e]), f0, f1) | scaled(halves_of(w4[e] >> 16), f0, f1) << 16;
+        *reinterpret_cast<uint4*>(to + k_byte<HD>(p / PARTS, 16 * (p % PARTS))) = make_uint4(c[0], c[1], c[2], c[3]);
+    }
+#pragma unroll
+    for (int j = 0; j < kKv8Block; ++j) {
+        if (fresh >> j & 1) {
+#pragma unroll
+            for (int i = 0; i < D; ++i) row[i] = next[i];
+            rest &= rest - 1;
+            if (rest) fetch(__ffs(rest) - 1);
+        }
+        if (there >> j & 1) {
+            const int byte = v_byte(__shfl_sync(ALL, token, j));
+            const int word = (j & 7) >> 1, place_of = 2 * (j >> 3) + (j & 1);        // where token j goes
+#pragma unroll
+            for (int i = 0; i < D; ++i) {
+                const uint32_t lo = __byte_perm(row[i].x, row[i].y, byte & 7), hi = __byte_perm(row[i].z, row[i].w, byte & 7);
+                v[i][word] |= ((byte & 8 ? hi : lo) & 0xffu) << 8 * place_of;
+            }
+        }
+    }
+    float v_top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {                    // tokens 2 w, 2 w + 1 of word w, then 8 + 2 w, 9 + 2 w
+        const int t0 = 8 * (e & 1) + 2 * (e / 2);
+        const float s0 = __shfl_sync(ALL, scale.y, t0), s1 = __shfl_sync(ALL, scale.y, t0 + 1);
+        __half2 m = __half2(0.f, 0.f);               // over the lane's dims, a token each
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const uint32_t x = halves_of(v[i][e / 2] >> 16 * (e & 1));
+            m = __hmax2(m, __habs2(*reinterpret_cast<const __half2*>(&x)));
+        }
+        v_top = fmaxf(v_top, fmaxf(__low2float(m) * s0, __high2float(m) * s1));
+    }
+    v_top = warp_max(v_top);
+    const float vs = scale_for(v_top);
+    const __half2 vf = factors(scale.y, vs);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int t0 = 8 * (e & 1) + 2 * (e / 2);
+        const uint32_t x = __shfl_sync(ALL, *reinterpret_cast<const uint32_t*>(&vf), t0),
+                       y = __shfl_sync(ALL, *reinterpret_cast<const uint32_t*>(&vf), t0 + 1);
+        const uint32_t g0 = __byte_perm(x, y, 0x5410), g1 = __byte_perm(x, y, 0x7632);
+        const __half2 f0 = *reinterpret_cast<const __half2*>(&g0), f1 = *reinterpret_cast<const __half2*>(&g1);
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const uint32_t c = scaled(halves_of(v[i][e / 2] >> 16 * (e & 1)), f0, f1);
+            v[i][e / 2] = e & 1 ? __byte_perm(v[i][e / 2], c, 0x5410) : __byte_perm(v[i][e / 2], c, 0x3254);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < D; ++i)
+        *reinterpret_cast<uint4*>(to + CODES + lane * (16 * D) + 16 * i) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
+    if (lane == 0) *reinterpret_cast<float2*>(to + 2 * CODES) = make_float2(ks, vs);
 }
 
 // CTAs of a head: no more than a round of scores needs, nor than fill the GPU.
@@ -474,7 +464,6 @@ cudaError_t launch_select(const Kv8Args& a, const Kv8EvictArgs& t, cudaStream_t 
     return cudaLaunchKernelEx(&cfg, kv8_select_kernel, a, t, ctas);
 }
 
-constexpr int kGatherBlocks = 8;
 
 }  // namespace
 
@@ -495,12 +484,10 @@ cudaError_t launch_kv8_evict(const Kv8Args& a, const Kv8EvictArgs& t, cudaStream
         if (u.new_scores) u.new_scores += (size_t)s0 * a.hk * t.new_ld;
         e = launch_select(b, u, s);
         if (e != cudaSuccess) return e;
-        // a block a CTA while all are resident at once, else up to kGatherBlocks one after the other: sequences are uneven
-        const int64_t most = t.new_capacity / kKv8Block, resident = (int64_t)sm_count() * (a.hd == 128 ? 7 : 14);
-        const int64_t each = std::min(most, std::max((most + kGatherBlocks - 1) / kGatherBlocks, resident / a.hk / b.n_seqs));
-        const dim3 grid((unsigned)each, a.hk, b.n_seqs);
-        e = a.hd == 128 ? launch_kv8(kv8_gather_kernel<128>, grid, 128, 0, s, b, u)
-                        : launch_kv8(kv8_gather_kernel<64>, grid, 64, 0, s, b, u);
+        const int blocks = t.new_capacity / kKv8Block;
+        const dim3 grid((blocks + kGatherWarps - 1) / kGatherWarps, a.hk, b.n_seqs);
+        e = a.hd == 128 ? launch_kv8(kv8_gather_kernel<128>, grid, 32 * kGatherWarps, 0, s, b, u)
+                        : launch_kv8(kv8_gather_kernel<64>, grid, 32 * kGatherWarps, 0, s, b, u);
     }
     return e;
 }

@@ -354,14 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) mbar_arrive(&sm.k_full[i]);
             {
                 Segment next = at;                   // not kept: its registers are the scores'
-                const bool more = next.next(a, line.x0, line.x1, p);
-                page = more ? look(next) : -1;
-                if (page >= 0 && page < a.n_pages) { // into L2, a line a thread
-                    const int b = (next.u * kUnit + i * kTile + row) / kKv8Block;
-                    const unsigned char* line_of = a.data + (((size_t)page * a.hk + next.h) * a.bpp + b -
-                                                             p.page_of(b, a.bpp) * a.bpp) * REC + (row >> 3 & 1) * 8 * HD;
-                    if ((row & 7) * 128 < 8 * HD) asm volatile("prefetch.global.L2 [%0];" ::"l"(line_of + (row & 7) * 128));
-                }
+                page = next.next(a, line.x0, line.x1, p) ? look(next) : -1;
             }
             float sum[2] = {0.f, 0.f};               // tiles group and group + 2
             for (int c = at.c; c < at.end; ++c, ++it) {
