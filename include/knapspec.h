@@ -626,7 +626,8 @@ ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const ks_kv8_batch
  * The new pages hold none that the call reads, and one sequence's are not
  * another's, except that a sequence that keeps all of its tokens may keep its
  * pages (the whole table row or pages of it): blocks that stay where they are are
- * not written.  kept, new_scores and lengths overlap nothing that is read.
+ * not written.  Arrays that are written may not overlap those that are read, the
+ * batch's among them.
  * Places from n on are left as they are, tokens of the last block from n on are
  * zeros.  Status bit 0: a page outside the pool (its tokens are read as zeros, or
  * not written); bit 1: keep[s] below 0 or n above the new pages' tokens (taken as
@@ -661,7 +662,7 @@ ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch* batch, con
  * A logit of -inf has no probability; a row of nothing else gives log
  * probabilities of -inf, entropy 0 and the lowest ids.  A NaN or +inf among a
  * row's logits makes its numbers NaN and its top_ids -1.
- * logits: dev, fp32 or bf16, row r at r * row_stride elements.  All other
+ * logits: dev, fp32 or bf16, row r at r * row_stride elements (at least vocab).  All other
  * arrays are dev, contiguous, and may be NULL where they have no elements
  * (entropy always).  vocab up to 2^22, n_tokens and n_top up to 64, n_top at most
  * vocab.  Sums are fp32; an exponential is off by at

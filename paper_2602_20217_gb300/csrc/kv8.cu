@@ -798,6 +798,22 @@ extern "C" ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch*
                   a.capacity, (long long)ev->kept_ld, (long long)ev->new_score_ld, room);
         return KS_ERR_INVALID_ARG;
     }
+    // what is written may not be what is read meanwhile
+    auto meet = [](const void* p, size_t n, const void* q, size_t m) {
+        const char *x = static_cast<const char*>(p), *y = static_cast<const char*>(q);
+        return p && q && x < y + m && y < x + n;
+    };
+    const size_t seqs = (size_t)a.n_seqs, heads = seqs * a.hk;
+    const struct { const void* p; size_t n; } writes[] = {{ev->lengths, 4 * seqs}, {ev->kept, 4 * heads * ev->kept_ld},
+                                                          {ev->new_scores, 4 * heads * ev->new_score_ld}},
+        reads[] = {{a.lengths, 4 * seqs}, {ev->keep, 4 * seqs}, {ev->scores, 4 * heads * ev->score_ld},
+                   {a.table, 4 * seqs * a.table_ld}, {ev->page_table, 4 * seqs * ev->table_ld}};
+    for (const auto& w : writes)
+        for (const auto& r : reads)
+            if (meet(w.p, w.n, r.p, r.n)) {
+                set_error("%s: results overlap what is read", who);
+                return KS_ERR_INVALID_ARG;
+            }
     Kv8EvictArgs t{};
     t.scores = ev->scores;
     t.ld = ev->score_ld;

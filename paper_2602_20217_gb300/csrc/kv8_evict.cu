@@ -6,7 +6,7 @@
 // whole numbers in the scores' order, 11, 11 and 10 bits at a time, then one pass
 // that numbers what stays: scores above it, and as many equal ones, the earlier
 // first, as there is room for.  A cluster of up to eight CTAs takes a sequence's
-// head, each a contiguous slice, in registers unless it is longer than 18 scores
+// head, each a contiguous slice, in registers unless it is longer than 17 scores
 // a thread; a warp has neighbouring ones, so that a ballot numbers them.  The CTAs
 // add their counts that are not zero to the first one's (reading all of each
 // other's counts took 25000 clocks a pass, five times the rest of it).
@@ -29,7 +29,7 @@ namespace ks {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048, kPer = 18, kRound = kThreads * kPer;
+constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048, kPer = 17, kRound = kThreads * kPer;
 constexpr int kCopies = 2;          // of a CTA's bins: scores crowd into few of them
 constexpr int kMaxCluster = 8;
 

@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 static_assert(kSums == kRing + 2, "sums outlive their queries by two chunks");
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sm.lse[it % kSums][32 * i + lane] = -x[i] * kLog2e;
+                    sm.lse[it % kSums][32 * i + lane] = x[i] == -INFINITY ? -INFINITY : -x[i] * kLog2e;    // no weight
                     x[i] = next[i];
                 }
                 __syncwarp();

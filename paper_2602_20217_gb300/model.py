@@ -143,7 +143,10 @@ class Model:
         t = np.ascontiguousarray(tokens, dtype=np.int32)
         if t.ndim not in (1, 2):
             raise ValueError(f"tokens: {t.ndim} dimensions, 1 or 2 expected")
-        with torch.cuda.stream(self.stream):
+        stream = self.stream
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.workspace.device)
+        with torch.cuda.stream(stream):
             dev = torch.from_numpy(t.reshape(len(t), -1)).to(self.workspace.device)
             out = lp.empty(dev.shape[0], dev.shape[1], n_top, device=self.workspace.device)
             ks.ks_model_logprobs(self.h, first_row, lp.marshal(None, 0, 0, 0, dev, n_top, temperature, out))

@@ -212,6 +212,40 @@ def test_long_sequence(n):
                                   O.kept(x[0, h].cpu().numpy(), n, keep, 3, 100, 1 << 30)), keep
 
 
+def test_more_sequences_than_a_grid_has():
+    """70000 sequences of at most 16 tokens, a page each."""
+    import torch
+
+    from paper_2602_20217_gb300 import kv8
+    n = 70000
+    cache = kv8.Cache8(2 * n, 16, 1, 64)
+    cache.data.random_(0, 100)
+    rec = cache.data.view(2 * n, 2080)
+    rec[:, -32:-24] = torch.ones(2, device="cuda").view(torch.uint8)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table = torch.arange(n, **i32)[:, None].contiguous()
+    lens = torch.randint(1, 17, (n,), **i32)
+    batch = kv8.Batch8(table, torch.arange(n + 1, **i32), lens, n, torch.zeros(1, **i32))
+    x = torch.rand(n, 1, 16, device="cuda")
+    kept, lengths = torch.full((n, 1, 16), -1, **i32), torch.zeros(n, **i32)
+    cache.evict(batch, x, torch.full((n,), 9, **i32), table + n, lengths, kept, recent=2)
+    assert torch.equal(lengths, lens.clamp(max=9)) and int(batch._keep[3]) == 0
+    t = torch.arange(16, device="cuda")
+    key = torch.where(t >= lens[:, None] - 2, 2.0, x[:, 0]).masked_fill(t >= lens[:, None], -1.0)
+    want = torch.where(t[:9] < lengths[:, None], key.topk(9).indices, 99).sort(1).values
+    assert torch.equal(kept[:, 0, :9].long().masked_fill(t[:9] >= lengths[:, None], 99), want)
+    k, v = (torch.zeros(n * 16, 1, 64, device="cuda") for _ in range(2))
+    offs = torch.cat((torch.zeros(1, **i32), lens.cumsum(0).int()))
+    cache.read(kv8.Batch8(table, offs, lens, n * 16), k, v)
+    k2, v2 = torch.zeros_like(k), torch.zeros_like(v)
+    offs2 = torch.cat((torch.zeros(1, **i32), lengths.cumsum(0).int()))
+    cache.read(kv8.Batch8((table + n).contiguous(), offs2, lengths, n * 16), k2, v2)
+    seq = torch.repeat_interleave(torch.arange(n, device="cuda"), lengths.long())
+    at = torch.arange(len(seq), device="cuda") - offs2.long()[seq]
+    src = offs.long()[seq] + kept[seq, 0, at].long()
+    assert torch.equal(k2[:len(seq)], k[src]) and torch.equal(v2[:len(seq)], v[src])
+
+
 def test_append_goes_on_at_the_old_positions():
     """After an eviction rows are rotated by their positions, and stored at their places."""
     import torch

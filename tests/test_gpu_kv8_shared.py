@@ -252,6 +252,32 @@ def test_graph_follows_the_groups_and_streams_have_their_own_workspaces():
     assert all(torch.equal(o, want) for o in outs)
 
 
+def test_thousands_of_groups():
+    """More groups than the preparation keeps in shared memory, of one and two sequences."""
+    import torch
+
+    from paper_2602_20217_gb300 import kv8
+    n_groups, page = 5000, 16
+    sizes = np.random.default_rng(0).integers(1, 3, n_groups)
+    groups = np.concatenate(([0], np.cumsum(sizes)))
+    n = int(groups[-1])
+    cache = kv8.Cache8(n_groups + n, page, 1, 64)
+    cache.data.random_(0, 100)
+    cache.data.view(-1, 2080)[:, -32:-24] = torch.full((2,), 2.0 ** -5, device="cuda").view(torch.uint8)
+    table = np.stack((np.repeat(np.arange(n_groups), sizes), n_groups + np.arange(n)), 1).astype(np.int32)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    lens = torch.randint(17, 33, (n,), **i32)
+    batch = kv8.Batch8(torch.tensor(table, device="cuda"), torch.arange(n + 1, **i32), lens, n, torch.zeros(1, **i32))
+    shared = kv8.Shared8(torch.tensor(groups, **i32), torch.full((n_groups,), 16, **i32))
+    q = torch.randn(n, 4, 64, device="cuda").to(torch.bfloat16)
+    out = cache.attention(batch, q, shared=shared)
+    plain = cache.attention(batch, q)
+    assert int(batch._keep[3]) == 0
+    v = 2.0 ** -5 * 448                              # the largest value that a code times the scale can be
+    a, b = out.double(), plain.double()
+    assert bool(((a - b).abs() <= 2.0 ** -8 * (a.abs() + b.abs()) + 2.0 ** -9 * v).all()) and bool((a != 0).any())
+
+
 def test_refusals_of_the_python_face():
     import torch
 

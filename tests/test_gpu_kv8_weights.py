@@ -182,6 +182,100 @@ def test_strides_streams_and_graphs():
     assert torch.equal(out[0], want[0]) and torch.equal(out[2], want[2]) and bool((out[1] == 0).all())
 
 
+def test_many_rows_of_many_sequences():
+    """Calls for the tcgen05 kernel with more sequences than a warp looks at in one go, some without rows or tokens."""
+    rng = np.random.default_rng(3)
+    lens = [int(x) for x in rng.integers(0, 700, 50)]
+    rows = [int(min(n, x)) for n, x in zip(lens, rng.integers(0, 60, 50))]
+    receive(Pool(lens, 2, 64, 16, seed=2).fill(), rows, 8, pad=2, decay=0.5)
+
+
+@pytest.mark.parametrize("n", [511, 512, 513, 1024, 1500])
+@pytest.mark.parametrize("rows", [40, 300])
+def test_units_of_512_keys(n, rows):
+    """Lengths around a unit of the tcgen05 kernel; rows in one chunk of queries and in several; runs that cut units."""
+    receive(Pool([n], 8, 128, 64, seed=n).fill(), [rows], 32, decay=0.9, place="same")
+
+
+def test_many_rows_out_of_range():
+    receive(Pool([90, 64, 50], 2, 64, 16).fill(), [20, 20, 20], 8, lengths=[90, -5, 50], status=2)
+    receive(Pool([96, 96], 2, 64, 16).fill(), [30, 8], 8, lengths=[96, 5000], status=2)
+    receive(Pool([90, 64, 50], 2, 64, 16).fill(), [20, 20, 20], 8, offsets=[0, 40, 20, 60], status=2)
+
+
+def test_many_rows_not_finite():
+    for what in ("key", "query", "lse"):
+        pool = Pool([700, 60], 2, 64, 16).fill()
+        q, lse = np.random.default_rng(0).standard_normal((90, 8, 64)), np.full((90, 8), 2.0)
+        if what == "key":
+            pool.block(0, 3)[1][0] = 0x7f
+            pool.kv[0][0, 48, 1, 0] = math.nan
+        if what == "query":
+            q[1, 2, 9] = q[70, 7, 0] = math.nan
+        if what == "lse":
+            lse[0, 0], lse[30, 3], lse[80, 5] = -math.inf, math.inf, math.nan
+        receive(pool, [50, 40], 8, lse=lse, q=q)
+
+
+def test_many_rows_with_pages_outside_the_pool():
+    import torch
+    pool = Pool([600], 2, 64, 16).fill()
+    lse = torch.full((40, 8), 3.0, device="cuda")
+    q = torch.randn(40, 8, 64, device="cuda").to(torch.bfloat16)
+    old = torch.rand(1, 2, pool.ld * 16, device="cuda")
+    d = pool.device([40])
+    want = d["cache"].attention_weights(d["batch"], q, lse, old, decay=0.5, out=torch.full_like(old, 7.0))
+    pool.table[0, 3], pool.table[0, 20] = 10 ** 6, -1
+    d = pool.device([40])
+    got = d["cache"].attention_weights(d["batch"], q, lse, old, decay=0.5, out=torch.full_like(old, 7.0))
+    torch.cuda.synchronize()
+    assert int(d["status"]) == 1
+    for a, b in ((48, 64), (320, 336)):
+        want[:, :, a:b] = 0.5 * old[:, :, a:b]
+    assert torch.equal(got, want)
+
+
+def test_many_rows_strides_streams_and_graphs():
+    """Queries that tensor copies cannot take go through the other kernel; calls at once have a workspace each."""
+    import torch
+    pool = Pool([900, 40, 333], 2, 64, 32).fill()
+    d, q, out = receive(pool, [100, 40, 33], 8)
+    n = q.shape[0]
+    lse = torch.full((n, 8), 3.0, device="cuda")
+    old = torch.rand(3, 2, pool.ld * 32, device="cuda")
+    want = d["cache"].attention_weights(d["batch"], q, lse, old, out=torch.zeros_like(old))
+    odd = torch.zeros(n, 9, 67, dtype=torch.bfloat16, device="cuda")[:, 1:, 1:65]
+    odd.copy_(q)
+    got = d["cache"].attention_weights(d["batch"], odd, lse, old, out=torch.zeros_like(old))
+    assert float(((got - want).abs() / want.abs().clamp(min=1e-3)).max()) < 2.0 ** -9     # each within its own bound
+    wide = torch.zeros(n, 16, 72, dtype=torch.bfloat16, device="cuda")[:, 8:, :64]
+    wide.copy_(q)
+    got = d["cache"].attention_weights(d["batch"], wide, lse, old, out=torch.zeros_like(old))
+    assert torch.equal(got, want)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros_like(old) for _ in range(6)]
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        d["cache"].attention_weights(d["batch"], q, lse, old, out=o, stream=streams[i % 2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    with pytest.raises(ValueError):
+        d["cache"].attention_weights(d["batch"], q, lse, old, out=outs[0], stream=streams[0].cuda_stream)
+    work, out = d["cache"].weights_workspace(8, n), torch.zeros_like(old)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        d["cache"].attention_weights(d["batch"], q, lse, old, out=out, workspace=work)
+    work.fill_(0xff)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    d["lengths"][0] = 517
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out[1:], want[1:]) and not torch.equal(out[0], want[0])
+
+
 def test_refusals_of_the_python_face():
     import torch
     pool = Pool([50], 2, 64, 16).fill()

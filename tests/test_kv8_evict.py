@@ -21,12 +21,15 @@ def test_what_stays():
     assert list(O.kept(x, 10, 99, 0, 0, 2)) == [3, 7] and len(O.kept(x, 10, -3, 1, 1, 9)) == 0
 
 
+B = A + (1 << 24)   # another one
+
+
 def weights_args(ks):
     return ks.KsKv8Weights(A, 4096, 128, 32, 0.1, 1.0, A, A, A, 256, A, 1 << 30)
 
 
 def evict_args(ks):
-    return ks.KsKv8Eviction(A, 256, A, 2, 3, A, 2, A, A, 128, A, 128)
+    return ks.KsKv8Eviction(A, 256, A, 2, 3, A, 2, B, B + (1 << 16), 128, B + (1 << 20), 128)
 
 
 WEIGHTS = [("q", None, 1), ("q", A + 1, 1), ("q_row", -1, 1), ("n_q_heads", 12, 1), ("n_q_heads", 0, 1),
@@ -51,6 +54,18 @@ def test_refusals_touch_no_device(lib, part, field, value, status):  # noqa: F81
     if part != "weights":
         assert lib.ks_kv8_evict(C.byref(cache), C.byref(batch), C.byref(e), None) == status
         assert lib.ks_last_error().decode().startswith("ks_kv8_evict")
+
+
+@pytest.mark.parametrize("field", ["lengths", "kept", "new_scores"])
+@pytest.mark.parametrize("place", [A, A + 4, A - 4])
+def test_results_that_overlap_what_is_read_are_refused(lib, field, place):  # noqa: F811
+    """The batch's lengths among them: heads read them while one writes the new ones."""
+    from paper_2602_20217_gb300 import knapspec as ks
+    cache, batch, _, _ = good(ks)
+    e = evict_args(ks)
+    setattr(e, field, place)
+    assert lib.ks_kv8_evict(C.byref(cache), C.byref(batch), C.byref(e), None) == ks.KS_ERR_INVALID_ARG
+    assert "overlap" in lib.ks_last_error().decode()
 
 
 def test_null_and_empty_calls(lib):  # noqa: F811
