@@ -22,9 +22,9 @@ namespace ks {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * (kWarps + 1), kCtas = 2;  // consumers; CTAs an SM
+constexpr int kWarps = 4, kThreads = 32 * (kWarps + 1), kCtas = 3;  // consumers; CTAs an SM
 constexpr int kWarpBlocks = 2;                      // blocks of 16 keys a warp
-constexpr int kTileLog = 7, kTile = 1 << kTileLog, kBlocks = kTile / kKv8Block, kStages = 4;
+constexpr int kTileLog = 7, kTile = 1 << kTileLog, kBlocks = kTile / kKv8Block, kStages = 3;
 constexpr int kUnitTiles = 2;                       // a unit's fixed cost, in tiles
 constexpr int kChunkBlocks = 4, kChunk = 8 * kChunkBlocks;      // queries in shared memory
 static_assert(kBlocks == kWarps * kWarpBlocks && kWarpBlocks == 2, "a tile is what the warps hold, a key a lane");
@@ -34,8 +34,6 @@ KS_DEV void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
-KS_DEV uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 template <int HD>
 struct Smem {
@@ -213,19 +211,6 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             const int key0 = tile * kTile + warp * kWarpBlocks * kKv8Block;
             if (alive) alive = mbar_wait(&sm.full[st], (it / kStages) & 1, kWaitLimitNs);
             const int have = alive ? present[st] >> (warp * kWarpBlocks) : 0;
-            uint32_t k[kWarpBlocks][2 * P][4];
-            float scale[kWarpBlocks];
-#pragma unroll
-            for (int kb = 0; kb < kWarpBlocks; ++kb) {
-                // matrices (tokens 0..7, dims 32 j ..), (tokens 8.., same), (tokens 0..7, dims 32 j + 16 ..), (tokens 8.., same)
-                const uint32_t base = smem_u32(sm.keys[st][warp * kWarpBlocks + kb]) + (lane >> 3 & 1) * (8 * HD) +
-                                      (lane >> 4) * 128 + (lane & 7) * 16;
-#pragma unroll
-                for (int j = 0; j < 2 * P; ++j) ldsm_x4(k[kb][j], base + j * 256);
-                scale[kb] = sm.scales[st][warp * kWarpBlocks + kb].x;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.empty[st]);
             float sum[kWarpBlocks][2] = {};
             // rows before the tile's first key see nothing of it
             for (int c = (int)(max(0, tile * kTile - rows.pos0) * (int64_t)G / kChunk); c < chunks; ++c) {
@@ -236,47 +221,49 @@ __global__ void __launch_bounds__(kThreads, kCtas)
                     held = c;
                 }
                 const bool edge = key0 + kWarpBlocks * kKv8Block - 1 > rows.pos0 + c * kChunk / G;
-                float part[kWarpBlocks][2] = {};     // of a chunk: sums of many rows keep their digits
                 const int blocks = min(kChunkBlocks, (rows.n - c * kChunk + 7) / 8);
-                for (int b = 0; b < blocks; ++b) {
-                    uint4 q[2][P];
+                // a block of keys at a time: its registers are what bounds the CTAs of an SM
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                for (int kb = 0; kb < kWarpBlocks; ++kb) {
+                    // matrices (tokens 0..7, dims 32 j ..), (tokens 8.., same), (tokens 0..7, dims 32 j + 16 ..), (tokens 8.., same)
+                    const uint32_t base = smem_u32(sm.keys[st][warp * kWarpBlocks + kb]) + (lane >> 3 & 1) * (8 * HD) +
+                                          (lane >> 4) * 128 + (lane & 7) * 16;
+                    uint32_t k[2 * P][4];
 #pragma unroll
-                        for (int j = 0; j < P; ++j) q[i][j] = sm.code[b][i][j][lane];
-                    const float4 f = *reinterpret_cast<const float4*>(&sm.factor[8 * b + 2 * q4]);
-                    int lim[2] = {INT32_MAX, INT32_MAX};
-                    if (edge) {
-                        lim[0] = sm.lim[8 * b + 2 * q4];
-                        lim[1] = sm.lim[8 * b + 2 * q4 + 1];
-                    }
-#pragma unroll
-                    for (int kb = 0; kb < kWarpBlocks; ++kb) {
-                        float s[4] = {};
+                    for (int j = 0; j < 2 * P; ++j) ldsm_x4(k[j], base + j * 256);
+                    const float scale = sm.scales[st][warp * kWarpBlocks + kb].x;
+                    const int key = key0 + 16 * kb + g;
+                    float part[2] = {};              // of a chunk: sums of many rows keep their digits
+                    for (int b = 0; b < blocks; ++b) {
+                        const float4 f = *reinterpret_cast<const float4*>(&sm.factor[8 * b + 2 * q4]);
+                        float s[2][4] = {};          // of the two codes: two chains of products
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int j = 0; j < 2 * P; ++j)
-                                mma_e4m3(s, k[kb][j], word(q[i][j / 2], j % 2 * 2), word(q[i][j / 2], j % 2 * 2 + 1));
-                        const float f0 = f.x * scale[kb], f1 = f.z * scale[kb];
-                        const int key = key0 + 16 * kb + g;
-                        float x[4] = {fmaf(s[0], f0, f.y), fmaf(s[1], f1, f.w), fmaf(s[2], f0, f.y), fmaf(s[3], f1, f.w)};
+                            for (int j = 0; j < P; ++j) {
+                                const uint4 q = sm.code[b][i][j][lane];
+                                mma_e4m3(s[i], k[2 * j], q.x, q.y);
+                                mma_e4m3(s[i], k[2 * j + 1], q.z, q.w);
+                            }
+                        const float f0 = f.x * scale, f1 = f.z * scale;
+                        float x[4] = {fmaf(s[0][0] + s[1][0], f0, f.y), fmaf(s[0][1] + s[1][1], f1, f.w),
+                                      fmaf(s[0][2] + s[1][2], f0, f.y), fmaf(s[0][3] + s[1][3], f1, f.w)};
                         if (edge) {
-                            if (key > lim[0]) x[0] = -INFINITY;
-                            if (key > lim[1]) x[1] = -INFINITY;
-                            if (key + 8 > lim[0]) x[2] = -INFINITY;
-                            if (key + 8 > lim[1]) x[3] = -INFINITY;
+                            const int lim0 = sm.lim[8 * b + 2 * q4], lim1 = sm.lim[8 * b + 2 * q4 + 1];
+                            if (key > lim0) x[0] = -INFINITY;
+                            if (key > lim1) x[1] = -INFINITY;
+                            if (key + 8 > lim0) x[2] = -INFINITY;
+                            if (key + 8 > lim1) x[3] = -INFINITY;
                         }
-                        part[kb][0] += exp2_approx(x[0]) + exp2_approx(x[1]);
-                        part[kb][1] += exp2_approx(x[2]) + exp2_approx(x[3]);
+                        part[0] += exp2_approx(x[0]) + exp2_approx(x[1]);
+                        part[1] += exp2_approx(x[2]) + exp2_approx(x[3]);
                     }
-                }
-#pragma unroll
-                for (int kb = 0; kb < kWarpBlocks; ++kb) {
-                    sum[kb][0] += part[kb][0];
-                    sum[kb][1] += part[kb][1];
+                    sum[kb][0] += part[0];
+                    sum[kb][1] += part[1];
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.empty[st]);
 #pragma unroll
             for (int kb = 0; kb < kWarpBlocks; ++kb)
 #pragma unroll
