@@ -206,6 +206,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    // queries that no chunk has: no NaN may come from there
+    for (int i = tid; i < kRing * (HD / 64) * (kQueries - p.tq * p.G) * 8; i += kThreads) {
+        const int each = (kQueries - p.tq * p.G) * 8, part = i / each;
+        reinterpret_cast<uint4*>(sm.q[0])[(part * kQueries + p.tq * p.G) * 8 + i - part * each] = make_uint4(0, 0, 0, 0);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     umma_fence_before();
     __syncthreads();
     umma_fence_after();
@@ -230,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int j = 32 * i + lane, tok = j / p.G;
-                x[i] = j < n ? t.lse[(size_t)(k.q.row0 + c * p.tq + tok) * t.hq + k.h * p.G + j - tok * p.G] : 0.f;
+                x[i] = j < n ? t.lse[(size_t)(k.q.row0 + c * p.tq + tok) * t.hq + k.h * p.G + j - tok * p.G] : -INFINITY;
             }
         };
         float x[4];
@@ -277,7 +283,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int c = at.c; c < at.end && ok; ++c, ++it) {
                     const int st = it % kRing;
                     ok = mbar_wait(&sm.q_full[st], (it / kRing) & 1, kWaitLimitNs);
-                    const uint32_t idesc = umma_idesc(kTile, (columns(at, c) + 15) / 16 * 16, false);
+                    const int n = columns(at, c);        // a whole chunk's columns behind them are zeros
+                    const uint32_t idesc = umma_idesc(kTile, n == p.tq * p.G ? kQueries : (n + 15) / 16 * 16, false);
                     for (int i = 0; i < kTiles && ok; ++i) {
                         if (c == at.c) ok = mbar_wait(&sm.k_full[i], seg & 1, kWaitLimitNs);
                         ok = ok && mbar_wait(&sm.s_free[i], (it & 1) ^ 1, kWaitLimitNs);
@@ -369,20 +376,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const bool edge = first + 31 > pos0 + tok0;          // a row of the chunk that does not see a key
                     float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     const uint32_t s_at = lanes + kQueries * tile + 64 * half;
-                    if (edge || n < 64 * half + 64) {
+                    if (edge || n < p.tq * p.G) {
                         // columns of rows that see this key
                         const int d = max(0, first + lane - pos0 - tok0);
-                        const int from = (d >= p.tq ? n : d * p.G) - 64 * half, to = min(n - 64 * half, 64);
+                        const int from = (d >= p.tq ? n : d * p.G) - 64 * half;
+                        const int to = first - pos0 - tok0 < p.tq ? min(n - 64 * half, 64) : 0;
 #pragma unroll 1
                         for (int j = 0; j < to; j += 32) {
+                            const int here_from = from - j, here_to = to - j;
                             uint32_t s[32];
                             tmem_ld32(s, s_at + j);
                             tmem_wait_ld();
                             tmem_pin(s);
 #pragma unroll
-                            for (int q = 0; q < 32; ++q) {
-                                const float x = fmaf(__uint_as_float(s[q]), c2, lse[j + q]);
-                                if (j + q >= from && j + q < to) part[0].x += exp2_approx(x);
+                            for (int q = 0; q < 32; q += 4) {
+                                const float4 l = *reinterpret_cast<const float4*>(&lse[j + q]);
+                                const float x[4] = {l.x, l.y, l.z, l.w};
+                                float w[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    w[e] = exp2_approx(fmaf(__uint_as_float(s[q + e]), c2, x[e]));
+                                    if (q + e < here_from || q + e >= here_to) w[e] = 0.f;
+                                }
+                                part[0] = __fadd2_rn(part[0], make_float2(w[0], w[1]));
+                                part[1] = __fadd2_rn(part[1], make_float2(w[2], w[3]));
                             }
                         }
                         umma_fence_before();

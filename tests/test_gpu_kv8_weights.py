@@ -197,6 +197,15 @@ def test_units_of_512_keys(n, rows):
     receive(Pool([n], 8, 128, 64, seed=n).fill(), [rows], 32, decay=0.9, place="same")
 
 
+@pytest.mark.parametrize("group", [5, 12, 48])
+def test_groups_that_do_not_fill_a_chunk(group):
+    """Whole chunks of fewer than 128 queries, and the rows of a sequence behind them, which are not finite."""
+    for rows in (3 * (128 // group), 3 * (128 // group) + 1):
+        q, lse = np.random.default_rng(group).standard_normal((rows + 20, 2 * group, 64)), np.full((rows + 20, 2 * group), 5.0)
+        q[rows:rows + 2] = math.nan
+        receive(Pool([700, 40], 2, 64, 16).fill(), [rows, 20], 2 * group, decay=0.5, lse=lse, q=q)
+
+
 def test_many_rows_out_of_range():
     receive(Pool([90, 64, 50], 2, 64, 16).fill(), [20, 20, 20], 8, lengths=[90, -5, 50], status=2)
     receive(Pool([96, 96], 2, 64, 16).fill(), [30, 8], 8, lengths=[96, 5000], status=2)
