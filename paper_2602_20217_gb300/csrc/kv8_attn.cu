@@ -420,18 +420,38 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[n][i][c] *= up;
         }
-        // the next segment's NaN marks: who read this buffer two segments ago has passed a barrier since
+        // the next segment's NaN marks begin empty: who read this buffer two segments ago has passed a barrier since
         const int clear = buf == 2 ? 0 : buf + 1;
         for (int i = tid; i < HD; i += 32 * kConsumers) sm.nan_from[clear][i] = INT32_MAX;
         if (tid == 0) sm.any_nan[clear] = 0;
-        consumers_sync();                                        // and this segment's are complete
+        const bool whole = at.tile == 0 && at.end == at.tiles;
+        bool joins = false;                                      // with what its group has in common
+        if constexpr (PART == kTail) joins = t.cut[at.s] > 0;
+        // the group's part of the rows that end here, all loads at once and before the joins: its own quarter of the
+        // dims, see below
+        float c_lse[PART == kTail ? NQ : 1], c_out[PART == kTail ? NQ : 1][2][PART == kTail ? DT / 2 : 1];
+        if constexpr (PART == kTail) {
+            if (whole && joins) {
+                const int d0 = 16 * ((warp & 2 ? DT / 2 : 0) + (warp & 1 ? DT / 4 : 0)) + g;
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    const int m_row = min(8 * n + g, rows.n - 1), tok = p.token(m_row);
+                    c_lse[n] = t.common_lse[(size_t)(rows.row0 + tok) * t.hq + at.h * G + m_row - tok * G];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = min(8 * n + 2 * q4 + e, rows.n - 1), tok_r = p.token(r);
+                        const float* c = t.common_out + ((size_t)(rows.row0 + tok_r) * t.hq + at.h * G + r - tok_r * G) * HD + d0;
+#pragma unroll
+                        for (int i = 0; i < DT / 2; ++i) c_out[n][e][i] = c[8 * i];
+                    }
+                }
+            }
+        }
+        consumers_sync();                                        // this segment's NaN marks are complete
         // join the warps; each ends with a quarter of the dims
         int dt0 = join<NQ, DT, DT>(o, m, l, sm.comb[0], sm.ml[0], warp, warp ^ 2, warp & 2);
         dt0 += join<NQ, DT, DT / 2>(o, m, l, sm.comb[0], sm.ml[0], warp, warp ^ 1, warp & 1);
-        const bool whole = at.tile == 0 && at.end == at.tiles;
         const bool any_nan = sm.any_nan[buf];
-        bool joins = false;                                      // with what its group has in common
-        if constexpr (PART == kTail) joins = t.cut[at.s] > 0;
         {
             float* slot = p.part + (size_t)(2 * blockIdx.x + (at.tile == 0)) * p.rg * (HD + 4);
 #pragma unroll
@@ -439,8 +459,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                 float inv = whole ? (l[n] == 0.f ? 0.f : 1.f / l[n]) : 1.f, other = 0.f, joined = 0.f;
                 if constexpr (PART == kTail) {
                     if (whole && joins) {
-                        const int m_row = min(8 * n + g, rows.n - 1), tok = p.token(m_row);
-                        const Joined j(m[n], l[n], t.common_lse[(size_t)(rows.row0 + tok) * t.hq + at.h * G + m_row - tok * G]);
+                        const Joined j(m[n], l[n], c_lse[n]);
                         inv = j.own;
                         other = j.other;
                         joined = j.lse;
@@ -471,12 +490,11 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     } else if (PART == kTail && whole && joins) {
                         const int tok = p.token(r);
                         const int64_t row = rows.row0 + tok, head = at.h * G + r - tok * G;
-                        const float* c = t.common_out + (row * t.hq + head) * HD + 16 * dt0 + g;
                         __nv_bfloat16* out = t.out + row * t.out_row + head * t.out_head + 16 * dt0 + g;
 #pragma unroll
                         for (int i = 0; i < DT / 4; ++i) {
-                            out[16 * i] = __float2bfloat16_rn(fmaf(o[n][i][e], f, c[16 * i] * fc));
-                            out[16 * i + 8] = __float2bfloat16_rn(fmaf(o[n][i][2 + e], f, c[16 * i + 8] * fc));
+                            out[16 * i] = __float2bfloat16_rn(fmaf(o[n][i][e], f, c_out[n][e][2 * i] * fc));
+                            out[16 * i + 8] = __float2bfloat16_rn(fmaf(o[n][i][2 + e], f, c_out[n][e][2 * i + 1] * fc));
                         }
                     } else if (whole) {
                         const int tok = p.token(r);
