@@ -76,6 +76,7 @@ struct Smem {
     unsigned char ring[kStages][TILE];
     float comb[kConsumers][HALF];
     uint32_t q[Q ? NQ * (HD / 32) * 4 * 32 : 4];                 // [NQ][HD / 32] A operands, 4 matrices each
+    float qf[8 * NQ];                                            // of their scores
     float2 ml[kConsumers][8 * NQ];
     int nan_from[3][HD];                                         // first key whose value is NaN, a segment each
     int any_nan[3];
@@ -229,18 +230,19 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     bool alive = true, began = false;
     for (int buf = 0;; buf = buf == 2 ? 0 : buf + 1) {
         const Rows rows(at, p.tq, G);
-        // this warp's queries, in two codes
-        uint32_t qa[S::Q ? 1 : NQ][S::Q ? 1 : KJ][4];
+        // the queries, in two codes: every warp's in its registers, or 8 rows by a warp for all
+        static_assert(S::Q ? NQ <= kConsumers : NQ == 1);
+        uint32_t qa[S::Q ? 1 : KJ][4];
         float qf[NQ];
         int lim[NQ];                                             // last key that the row sees
         const int lim_first = rows.pos0, lim_last = rows.pos0 + (rows.tokens - 1) * rows.step;
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
+        for (int n = 0; n < NQ; ++n) lim[n] = 8 * n + g < rows.n ? rows.pos0 + p.token(8 * n + g) * rows.step : INT32_MAX;
+        if (const int n = S::Q ? warp : 0; n < NQ) {
             const int m = 8 * n + g;
             const bool valid = m < rows.n;
             const int tok = valid ? p.token(m) : 0, head = at.h * G + (valid ? m - tok * G : 0);
             const __nv_bfloat16* src = t.q + (int64_t)(rows.row0 + tok) * t.q_row + (int64_t)head * t.q_head;
-            lim[n] = valid ? rows.pos0 + tok * rows.step : INT32_MAX;
             float x[KJ * 2][4], top = 0.f;
             // all loads first, without a branch between them
             uint2 raw[KJ * 2];
@@ -267,7 +269,10 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     else x[j][i] = __uint_as_float(0x7fc00000u);     // the row becomes NaN, as its scores are
                 }
             const float sc = scale_for(quad_max(top)), inv = inverse_pow2(sc);
-            qf[n] = sc * (t.scale * kLog2e);
+            qf[0] = sc * (t.scale * kLog2e);
+            if constexpr (S::Q) {
+                if (q4 == 0) sm.qf[m] = qf[0];
+            }
 #pragma unroll
             for (int j = 0; j < KJ; ++j)
 #pragma unroll
@@ -279,17 +284,20 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                     const uint32_t lo = to_e4m3x2(v[0] * inv - f0.x, v[1] * inv - f0.y) |
                                         (uint32_t)to_e4m3x2(v[2] * inv - f1.x, v[3] * inv - f1.y) << 16;
                     if constexpr (S::Q) {
-                        if (warp == 0) {             // matrix i of (n, j), row g, bytes 4 q4 ..
-                            sm.q[(n * KJ + j) * 128 + 64 * half + lane] = hi;
-                            sm.q[(n * KJ + j) * 128 + 64 * half + 32 + lane] = lo;
-                        }
+                        // matrix i of (n, j), row g, bytes 4 q4 ..
+                        sm.q[(n * KJ + j) * 128 + 64 * half + lane] = hi;
+                        sm.q[(n * KJ + j) * 128 + 64 * half + 32 + lane] = lo;
                     } else {
-                        qa[n][j][2 * half] = hi;
-                        qa[n][j][2 * half + 1] = lo;
+                        qa[j][2 * half] = hi;
+                        qa[j][2 * half + 1] = lo;
                     }
                 }
         }
-        if constexpr (S::Q) consumers_sync();
+        if constexpr (S::Q) {
+            consumers_sync();
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) qf[n] = sm.qf[8 * n + g];
+        }
         float m[NQ], l[NQ], vref = 0.f, o[NQ][DT][4];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -328,8 +336,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
                                 mma_e4m3(s[n][0], q, k0[2 * e], k0[2 * e + 1]);
                                 mma_e4m3(s[n][1], q, k1[2 * e], k1[2 * e + 1]);
                             } else {
-                                mma_e4m3(s[n][0], qa[n][2 * j + e], k0[2 * e], k0[2 * e + 1]);
-                                mma_e4m3(s[n][1], qa[n][2 * j + e], k1[2 * e], k1[2 * e + 1]);
+                                mma_e4m3(s[n][0], qa[2 * j + e], k0[2 * e], k0[2 * e + 1]);
+                                mma_e4m3(s[n][1], qa[2 * j + e], k1[2 * e], k1[2 * e + 1]);
                             }
                         }
                 }
