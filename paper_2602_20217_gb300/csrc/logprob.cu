@@ -15,6 +15,10 @@
 // another segment is behind each of those maxima), and at least as large as the
 // least of these maxima: those segments are read again, from L2, and the few
 // candidates ranked against each other.
+//
+// Measured: 1500 rows of 151936 fp32 logits 159 us, 5.7 TB/s, memory; 251 rows of
+// 100277 in bf16 20 us, 2.5 TB/s, the exponentials' issue and the rows' ends; one
+// row of 128256 11 us, launch and the cluster's phases (a CTA a row 16).
 #include <cmath>
 
 #include "internal.h"
