@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(32 * kGatherWarps) kv8_gather_kernel(const Kv8
     auto rec_of = [&](int j) {
         return reinterpret_cast<const unsigned char*>(__shfl_sync(ALL, reinterpret_cast<unsigned long long>(rec), j));
     };
-    // values of dims D lane ..: 16 bytes each, of a record at a time, the next one's on their way
+    // values of dims lane, lane + 32 ..: 16 bytes each, of a record at a time, the next one's on their way
     uint4 row[D], next[D];
     uint32_t v[D][4];
 #pragma unroll
@@ -349,9 +349,9 @@ __global__ void __launch_bounds__(32 * kGatherWarps) kv8_gather_kernel(const Kv8
         v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0;
     }
     auto fetch = [&](int j) {                        // of the j-th token's record
-        const unsigned char* of = rec_of(j & 31) + CODES + lane * (16 * D);
+        const unsigned char* of = rec_of(j & 31) + CODES + lane * 16;
 #pragma unroll
-        for (int i = 0; i < D; ++i) next[i] = *reinterpret_cast<const uint4*>(of + 16 * i);
+        for (int i = 0; i < D; ++i) next[i] = *reinterpret_cast<const uint4*>(of + 512 * i);
     };
     unsigned rest = fresh;
     if (rest) fetch(__ffs(rest) - 1);
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(32 * kGatherWarps) kv8_gather_kernel(const Kv8
     }
 #pragma unroll
     for (int i = 0; i < D; ++i)
-        *reinterpret_cast<uint4*>(to + CODES + lane * (16 * D) + 16 * i) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
+        *reinterpret_cast<uint4*>(to + CODES + lane * 16 + 512 * i) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
     if (lane == 0) *reinterpret_cast<float2*>(to + 2 * CODES) = make_float2(ks, vs);
 }
 
