@@ -6,7 +6,7 @@
 // whole numbers in the scores' order, 11, 11 and 10 bits at a time, then one pass
 // that numbers what stays: scores above it, and as many equal ones, the earlier
 // first, as there is room for.  A cluster of up to eight CTAs takes a sequence's
-// head, each a contiguous slice, in registers unless it is longer than 17 scores
+// head, each a contiguous slice, in registers unless it is longer than 24 scores
 // a thread; a warp has neighbouring ones, so that a ballot numbers them.  The CTAs
 // add their counts that are not zero to the first one's (reading all of each
 // other's counts took 25000 clocks a pass, five times the rest of it).
@@ -36,7 +36,7 @@ namespace ks {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048, kPer = 17, kRound = kThreads * kPer;
+constexpr int kThreads = 512, kWarps = kThreads / 32, kBins = 2048, kPer = 24, kRound = kThreads * kPer;
 constexpr int kCopies = 2;          // of a CTA's bins: scores crowd into few of them
 constexpr int kMaxCluster = 8;
 
@@ -131,12 +131,17 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
     }
     const int slice = (w.len + ctas - 1) / ctas, begin = rank * slice, end = min(w.len, begin + slice);
     const int rounds = max(0, end - begin + kRound - 1) / kRound;
-    // this thread's scores of a round
+    // this thread's scores of a round: as many in each round as it takes, in whole threes (looked at one by one 1 us more),
+    // so that short slices do not pay for the longest
+    const int per = rounds ? min(kPer, ((end - begin + rounds * kThreads - 1) / (rounds * kThreads) + 2) / 3 * 3) : 0;
     float v[kPer];
-    auto place = [&](int round, int e) { return begin + round * kRound + (warp * kPer + e) * 32 + lane; };
+    auto place = [&](int round, int e) { return begin + ((round * kWarps + warp) * per + e) * 32 + lane; };
     auto load = [&](int round) {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) v[e] = place(round, e) < end ? score[place(round, e)] : 0.f;
+        for (int e = 0; e < kPer; ++e) {
+            if (e % 3 == 0 && e >= per) break;
+            v[e] = place(round, e) < end ? score[place(round, e)] : 0.f;
+        }
     };
     if (rounds > 0) load(0);
     for (int i = tid; i < kCopies * kBins; i += kThreads) bins[0][i] = 0;
@@ -155,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
                 if (rounds > 1) load(round);
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
+                    if (e % 3 == 0 && e >= per) break;
                     const unsigned k = score_key(v[e]);
                     const int i = place(round, e);
                     if (i >= lo && i < min(hi, end) && (k & above) == prefix)
@@ -216,6 +222,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
             if (rounds > 1) load(round);
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
+                if (e % 3 == 0 && e >= per) break;
                 bool sure, equal;
                 mark(round, e, sure, equal);
                 n_sure += sure;
@@ -242,17 +249,17 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
     }
     for (int round = 0; round < rounds; ++round) {
         if (rounds > 1) load(round);
-        unsigned sure_of[kPer], equal_of[kPer];      // of the warp's 32 scores e
-        int n_sure = 0, n_equal = 0;
+        int n_sure = 0, n_equal = 0;                 // of the warp's
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
+            if (e % 3 == 0 && e >= per) break;
             bool sure, equal;
             mark(round, e, sure, equal);
-            sure_of[e] = __ballot_sync(0xffffffffu, sure);
-            equal_of[e] = __ballot_sync(0xffffffffu, equal);
-            n_sure += __popc(sure_of[e]);
-            n_equal += __popc(equal_of[e]);
+            n_sure += sure;
+            n_equal += equal;
         }
+        n_sure = __reduce_add_sync(0xffffffffu, n_sure);
+        n_equal = __reduce_add_sync(0xffffffffu, n_equal);
         __syncthreads();                             // the counts of the round before are read
         if (lane == 0) {
             in_warp[warp][0] = n_sure;
@@ -271,8 +278,12 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
         }
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
+            if (e % 3 == 0 && e >= per) break;
             const int rest = max(left - tie, 0);     // equal ones that there is still room for: the first of them
-            const bool stays = (sure_of[e] >> lane & 1) || ((equal_of[e] >> lane & 1) && __popc(equal_of[e] & below) < rest);
+            bool sure, equal;
+            mark(round, e, sure, equal);
+            const unsigned equals = __ballot_sync(0xffffffffu, equal);
+            const bool stays = sure || (equal && __popc(equals & below) < rest);
             const unsigned staying = __ballot_sync(0xffffffffu, stays);
             if (stays) {
                 const int to = o + __popc(staying & below);
@@ -280,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_select_kernel(const Kv8Args a
                 if (out) out[to] = v[e];
             }
             o += __popc(staying);
-            tie += __popc(equal_of[e]);
+            tie += __popc(equals);
         }
     }
     if (ctas > 1) cluster_sync();                    // nobody leaves before what it is sent has arrived
