@@ -19,14 +19,15 @@
 // 16: a lane takes four dims (two of heads of 64), reads their bytes of each record
 // that the block's tokens come from once, and has the new record's bytes of its
 // dims together without any exchange.  Four warps a block, which wait for each
-// other, and 16 reads of each row took 75 us where this takes 55 (24 sequences of
-// 300 to 12000 tokens, 8 KV heads of 128, cut to half: about 370 MB with the value
-// rows that a kept byte lies in, 6.7 TB/s); loading a block's keys to registers
-// first was slower (a 64k prompt cut to a tenth 57 us against 52, read back included).
+// other, and 16 reads of each row took 75 us where this takes 48 (24 sequences of
+// 300 to 12000 tokens, 8 KV heads of 128, cut to half).
 //
-// Measured: select 20 us for one sequence of 65537 tokens and 8 heads (one CTA a
-// head 89), 30 us for the 24 sequences, where two CTAs a head cost 6 more.  Its
-// fixed steps bound it, about 12000 clocks of counts, sums and cluster barriers.
+// Measured: gather 48 us there, 4 TB/s from DRAM beside L1's line look-ups (a lane
+// with neighbouring dims took 55, the next two records in flight the same); 24 us
+// for a 64k context cut to a tenth, where every kept token has a record of its own,
+// 2.6 KB of 64-byte accesses, 5.7 TB/s.  select 18 us in both: about 12000 clocks of
+// fixed steps, counts, sums and cluster barriers (one CTA a head took 89 for the
+// 64k context; a batch that fills the GPU gains nothing from clusters).
 #include <algorithm>
 
 #include "kv8.cuh"
