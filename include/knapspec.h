@@ -589,8 +589,9 @@ ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks_kv8_batch*
  * over the sequence's rows that see t and the query heads of h, lse [n_rows]
  * [n_q_heads] being what the attention of these rows returned.  The rows' own
  * tokens begin anew: their scores are not read; nor are any with a decay of 0,
- * and scores may be NULL then.  out may be scores.  Sequences without rows, and
- * places from lengths[s] on, are left as they are.
+ * and scores may be NULL then.  out may be scores, and overlaps nothing else that
+ * is read.  Sequences without rows, and places from lengths[s] on, are left as
+ * they are.
  * Scores and sums are fp32; queries as in ks_kv8_attention, or exact (in calls
  * of many rows).  A row with lse -inf gives no weight to keys that are numbers, a
  * token on a page outside the pool receives none (status bit 0), a NaN key, query
@@ -664,7 +665,7 @@ ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch* batch, con
  * row's logits makes its numbers NaN and its top_ids -1.
  * logits: dev, fp32 or bf16, row r at r * row_stride elements (at least vocab).  All other
  * arrays are dev, contiguous, and may be NULL where they have no elements
- * (entropy always).  vocab up to 2^22, n_tokens and n_top up to 64, n_top at most
+ * (entropy always); the results overlap nothing that is read.  vocab up to 2^22, n_tokens and n_top up to 64, n_top at most
  * vocab.  Sums are fp32; an exponential is off by at
  * most 2^-22 relative, and none where it is below 2^-126. */
 typedef struct {

@@ -701,6 +701,16 @@ extern "C" ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks
     return launched(launch_kv8_shared(a, g, t, static_cast<cudaStream_t>(stream)), who);
 }
 
+namespace {
+
+// Whether n bytes at p and m bytes at q have one in common.
+bool meet(const void* p, size_t n, const void* q, size_t m) {
+    const char *x = static_cast<const char*>(p), *y = static_cast<const char*>(q);
+    return p && q && x < y + m && y < x + n;
+}
+
+}  // namespace
+
 extern "C" size_t ks_kv8_attention_weights_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_rows) {
     if (ks_kv8_attention_workspace(cache, n_q_heads, 1, n_rows) == 0) return 0;
     return kv8_weights_workspace(n_q_heads / cache->n_kv_heads, n_rows, 1);
@@ -751,6 +761,17 @@ extern "C" ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const k
         set_error("%s: a workspace of %zu bytes, %zu needed", who, w->workspace_bytes, need);
         return KS_ERR_WORKSPACE;
     }
+    // scores may be the results, token by token, and nothing else that is read
+    const size_t results = 4 * (size_t)a.n_seqs * a.hk * w->score_ld;
+    const struct { const void* p; size_t n; } reads[] = {
+        {w->scores == w->out ? nullptr : w->scores, results}, {w->lse, 4 * (size_t)a.n_rows * w->n_q_heads},
+        {w->q, 2 * ((size_t)(a.n_rows - 1) * w->q_row + (size_t)(w->n_q_heads - 1) * w->q_head + a.hd)},
+        {a.table, 4 * (size_t)a.n_seqs * a.table_ld}, {a.offsets, 4 * ((size_t)a.n_seqs + 1)}, {a.lengths, 4 * (size_t)a.n_seqs}};
+    for (const auto& r : reads)
+        if (meet(w->out, results, r.p, r.n)) {
+            set_error("%s: results overlap what is read", who);
+            return KS_ERR_INVALID_ARG;
+        }
     Kv8WeightArgs t{};
     t.workspace = w->workspace;
     t.q = static_cast<const __nv_bfloat16*>(w->q);
@@ -799,10 +820,6 @@ extern "C" ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch*
         return KS_ERR_INVALID_ARG;
     }
     // what is written may not be what is read meanwhile
-    auto meet = [](const void* p, size_t n, const void* q, size_t m) {
-        const char *x = static_cast<const char*>(p), *y = static_cast<const char*>(q);
-        return p && q && x < y + m && y < x + n;
-    };
     const size_t seqs = (size_t)a.n_seqs, heads = seqs * a.hk;
     const struct { const void* p; size_t n; } writes[] = {{ev->lengths, 4 * seqs}, {ev->kept, 4 * heads * ev->kept_ld},
                                                           {ev->new_scores, 4 * heads * ev->new_score_ld}},

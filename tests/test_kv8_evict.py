@@ -25,7 +25,7 @@ B = A + (1 << 24)   # another one
 
 
 def weights_args(ks):
-    return ks.KsKv8Weights(A, 4096, 128, 32, 0.1, 1.0, A, A, A, 256, A, 1 << 30)
+    return ks.KsKv8Weights(A, 4096, 128, 32, 0.1, 1.0, A, B, B, 256, A, 1 << 30)
 
 
 def evict_args(ks):
@@ -48,6 +48,8 @@ def test_refusals_touch_no_device(lib, part, field, value, status):  # noqa: F81
     cache, batch, _, _ = good(ks)
     w, e = weights_args(ks), evict_args(ks)
     setattr({"cache": cache, "batch": batch, "weights": w, "evict": e}[part], field, value)
+    if field.startswith("workspace"):
+        batch.n_rows = 100                           # few rows need none
     if part != "evict":
         assert lib.ks_kv8_attention_weights(C.byref(cache), C.byref(batch), C.byref(w), None) == status
         assert lib.ks_last_error().decode().startswith("ks_kv8_attention_weights")
@@ -65,6 +67,16 @@ def test_results_that_overlap_what_is_read_are_refused(lib, field, place):  # no
     e = evict_args(ks)
     setattr(e, field, place)
     assert lib.ks_kv8_evict(C.byref(cache), C.byref(batch), C.byref(e), None) == ks.KS_ERR_INVALID_ARG
+    assert "overlap" in lib.ks_last_error().decode()
+
+
+@pytest.mark.parametrize("field,value", [("scores", B + 4), ("scores", B - 4), ("lse", B), ("q", B + 16), ("out", A)])
+def test_weights_that_overlap_what_is_read_are_refused(lib, field, value):  # noqa: F811
+    from paper_2602_20217_gb300 import knapspec as ks
+    cache, batch, _, _ = good(ks)
+    w = weights_args(ks)
+    setattr(w, field, value)
+    assert lib.ks_kv8_attention_weights(C.byref(cache), C.byref(batch), C.byref(w), None) == ks.KS_ERR_INVALID_ARG
     assert "overlap" in lib.ks_last_error().decode()
 
 
