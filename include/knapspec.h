@@ -663,11 +663,11 @@ ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch* batch, con
  * A logit of -inf has no probability; a row of nothing else gives log
  * probabilities of -inf, entropy 0 and the lowest ids.  A NaN or +inf among a
  * row's logits makes its numbers NaN and its top_ids -1.
- * logits: dev, fp32 or bf16, row r at r * row_stride elements (at least vocab).  All other
- * arrays are dev, contiguous, and may be NULL where they have no elements
- * (entropy always); the results overlap nothing that is read.  vocab up to 2^22, n_tokens and n_top up to 64, n_top at most
- * vocab.  Sums are fp32; an exponential is off by at
- * most 2^-22 relative, and none where it is below 2^-126. */
+ * logits: dev, fp32 or bf16, row r at r * row_stride elements (at least vocab).
+ * All other arrays are dev, contiguous, and may be NULL where they have no
+ * elements (entropy always); the results overlap nothing that is read.  vocab up
+ * to 2^22, n_tokens and n_top up to 64, n_top at most vocab.  Sums are fp32; an
+ * exponential is off by at most 2^-22 relative, and none where it is below 2^-126. */
 typedef struct {
     const void* logits;
     int32_t dtype;           /* KS_DTYPE_F32 or KS_DTYPE_BF16 */

@@ -12,7 +12,7 @@
 // alone would be units of 8.  Joining in the second launch's ends saves a third one
 // over all rows, and a pass over them.
 //
-// Measured, 64 samples of one row behind 16384 tokens, 32 heads over 8: 74 us of
+// Measured, 64 samples of one row behind 16384 tokens, 32 heads over 8: 72 us of
 // which the first launch is 40, the second 25, finding out what is shared 5; the
 // cache's bytes alone would be 11 us.  The first is bound as prompts are (see
 // kv8_tc.cu), the second by its units' ends: a unit has two or three tiles.
