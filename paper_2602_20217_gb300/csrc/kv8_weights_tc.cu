@@ -39,7 +39,7 @@ constexpr int kTiles = 4, kTile = 128, kUnit = kTiles * kTile;     // keys
 constexpr int kSoftmaxWarps = 4 * kTiles, kProductWarp = kSoftmaxWarps, kCopyWarp = kProductWarp + 1;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
 constexpr int kQueries = 128, kRing = 3, kSums = 5;
-constexpr int kUnitCost = 2;            // a unit's keys, in the time of chunks
+constexpr int kUnitCost = 2;            // a unit's keys, in the time of chunks: 1, 2 and 3 take 105.0, 104.1, 104.9 us
 
 struct WeightsPlan {
     int G, tq;              // query heads a KV head; tokens of a chunk
