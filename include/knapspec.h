@@ -689,8 +689,9 @@ ks_status ks_token_logprobs(const ks_logprobs* args, void* stream);
  * read.  Row i of a verify pass holds the logits of the token after its input
  * row i, so those of the tokens that ks_verify returned are rows 0 .. n_out - 1;
  * after a prefill the last row's is the pending token's.  Does not wait.
- * KS_ERR_STATE before a prefill, KS_ERR_INVALID_ARG for rows that the pass did
- * not have.  A layer selection may replace the logits (see ks_debug_read). */
+ * KS_ERR_INVALID_ARG for rows that the pass did not have, KS_ERR_STATE before a
+ * prefill, and after a layer selection that has replaced the logits (see
+ * ks_debug_read) until the next pass. */
 ks_status ks_model_logprobs(ks_model* m, int32_t first_row, const ks_logprobs* args);
 
 /* ------------------------------------------------------------ diagnostics */

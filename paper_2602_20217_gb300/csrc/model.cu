@@ -428,7 +428,7 @@ struct ks_model {
     int prompt_pending = 0;
     int prompt_rows = 0;
     int last_gamma = -1;
-    int last_pass_rows = 0;
+    int last_pass_rows = 0;   // whose logits are in `logits`; 0: a layer selection has replaced them
     std::vector<int> slot_off, slot_cnt;  // history ring rows per slot
     int hist_next = 0;
     int64_t launches = 0;
@@ -761,9 +761,11 @@ static ks_status forward(ks_model* m, const int32_t* tok, int R, int p0, const u
                 KS_TRY(add(l, CH_DOWN, next_gain(2 * l + 2), K_DOWN));
             }
         }
-        if (argmax) KS_TRY(add(0, CH_LM, nullptr, K_LMHEAD));
+        if (argmax) {
+            KS_TRY(add(0, CH_LM, nullptr, K_LMHEAD));
+            m->last_pass_rows = R;
+        }
         KS_TRY(flush());
-        m->last_pass_rows = R;
         return KS_OK;
     }
 
@@ -809,9 +811,9 @@ static ks_status forward(ks_model* m, const int32_t* tok, int R, int p0, const u
         lm.amax_val = m->amax_val;
         lm.amax_idx = m->amax_idx;
         lm.tokens = argmax;
+        m->last_pass_rows = R;
         KS_TRY(launch(m, K_LMHEAD, [&] { return launch_gemv(EPI_LMHEAD, lm, s); }, "lm-head"));
     }
-    m->last_pass_rows = R;
     return KS_OK;
 }
 
@@ -1647,8 +1649,9 @@ static int history_rows(ks_model* m, int32_t* idx) {
     return r;
 }
 
-// LM head + argmax of R rows whose input (x, xg, ss) is already in place.
+// LM head + argmax of R rows whose input (x, xg, ss) is already in place.  Their logits replace those of the last pass.
 static ks_status lm_head_rows(ks_model* m, int R, int32_t* tokens) {
+    m->last_pass_rows = 0;
     const ks_config& c = m->cfg;
     const int d = c.d_model, L = c.n_layers;
     cudaStream_t s = m->stream;
@@ -2381,6 +2384,10 @@ ks_status ks_model_logprobs(ks_model* m, int32_t first_row, const ks_logprobs* a
     }
     if (!m->have_seq) {
         set_error("ks_model_logprobs: no sequence (call ks_prefill first)");
+        return KS_ERR_STATE;
+    }
+    if (m->last_pass_rows == 0) {
+        set_error("ks_model_logprobs: a layer selection has replaced the last pass's logits");
         return KS_ERR_STATE;
     }
     if (first_row < 0 || args->rows < 0 || (int64_t)first_row + args->rows > m->last_pass_rows) {

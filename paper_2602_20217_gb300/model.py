@@ -136,7 +136,7 @@ class Model:
 
     def logprobs(self, tokens, n_top: int = 0, first_row: int = 0, temperature: float = 1.0):
         """Log probabilities of tokens [rows] or [rows, n] under rows first_row .. of the last pass, with the rows'
-        entropies and n_top best tokens: a logprobs.LogProbs of numpy arrays."""
+        entropies and n_top best tokens: a logprobs.LogProbs of numpy arrays, whose logprobs have the shape of tokens."""
         import torch
 
         from . import logprobs as lp
