@@ -609,7 +609,8 @@ typedef struct {
     float* out;
     int64_t score_ld;
     void* workspace;         /* dev, 256-byte aligned, ks_kv8_attention_weights_workspace() bytes for these query
-                                heads and rows (0 for few: NULL will do); calls that run at once need one each */
+                                heads and rows or more; NULL will do where it is 0, and where a sequence has on average
+                                fewer than 33 query rows of a KV head; calls that run at once need one each */
     size_t workspace_bytes;
 } ks_kv8_weights;
 size_t ks_kv8_attention_weights_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_rows);

@@ -713,7 +713,7 @@ bool meet(const void* p, size_t n, const void* q, size_t m) {
 
 extern "C" size_t ks_kv8_attention_weights_workspace(const ks_kv8_cache* cache, int32_t n_q_heads, int32_t n_rows) {
     if (ks_kv8_attention_workspace(cache, n_q_heads, 1, n_rows) == 0) return 0;
-    return kv8_weights_workspace(n_q_heads / cache->n_kv_heads, n_rows, 1);
+    return kv8_weights_workspace(n_q_heads / cache->n_kv_heads, n_rows, 1);     // of more sequences: as much, or none
 }
 
 extern "C" ks_status ks_kv8_attention_weights(const ks_kv8_cache* cache, const ks_kv8_batch* batch,

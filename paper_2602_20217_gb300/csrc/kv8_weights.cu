@@ -310,9 +310,7 @@ bool many_rows(int64_t group, int64_t n_rows, int64_t n_seqs) { return group * n
 }  // namespace
 
 size_t kv8_weights_workspace(int group, int64_t n_rows, int64_t n_seqs) {
-    // a call with fewer sequences may be one of many rows
-    (void)n_seqs;
-    return group * n_rows >= kManyRows ? kv8_weights_tc_workspace() : 0;
+    return many_rows(group, n_rows, n_seqs) ? kv8_weights_tc_workspace() : 0;
 }
 
 bool kv8_weights_fits(const Kv8Args& a, int hq) {

@@ -230,7 +230,7 @@ class Cache8:
         return out
 
     def weights_workspace(self, n_q_heads: int, n_rows: int):
-        """A workspace of attention_weights() for these sizes or smaller ones (empty for few rows); calls that run at
+        """A workspace of attention_weights() for these sizes or smaller ones (empty where none is needed); calls that run at
         once need one each."""
         return torch.empty(ks.ks_kv8_attention_weights_workspace(self.c, n_q_heads, n_rows), dtype=torch.uint8,
                            device=self.device)

@@ -57,3 +57,24 @@ def test_no_tokens_and_rows_before_the_first_one():
 @pytest.mark.parametrize("group", [3, 5, 64])
 def test_groups_and_rows_before_the_first_token(group):
     within_the_order(Pool([20, 530], 1, 64, 16).fill(), [90, 600], group)
+
+
+def test_a_batch_of_few_rows_each_needs_no_workspace():
+    """However many sequences there are; a batch of many rows each is refused one that is too small."""
+    import torch
+
+    from paper_2602_20217_gb300 import knapspec as ks
+    pool = Pool([40 + 3 * s for s in range(24)], 2, 64, 16).fill()
+    d = pool.device([1] * 24)
+    assert d["cache"].weights_workspace(8, 24).numel() > 0       # the same rows of one sequence do
+    q, lse = torch.randn(24, 8, 64, device="cuda").to(torch.bfloat16), torch.full((24, 8), 4.0, device="cuda")
+    old = torch.rand(24, 2, pool.ld * 16, device="cuda")
+    want = d["cache"].attention_weights(d["batch"], q, lse, old, out=torch.zeros_like(old))
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    got = d["cache"].attention_weights(d["batch"], q, lse, old, out=torch.zeros_like(old), workspace=none)
+    torch.cuda.synchronize()
+    assert int(d["status"]) == 0 and torch.equal(got, want)
+    pool = Pool([40], 2, 64, 16).fill()
+    d = pool.device([24])
+    with pytest.raises(ks.KsError):
+        d["cache"].attention_weights(d["batch"], q, lse, old[:1], out=torch.zeros_like(old[:1]), workspace=none)
