@@ -37,6 +37,9 @@
  *    a long job that hit a timeout ends quickly instead of waiting again.
  *  - One handle is used by one host thread at a time and issues all work on
  *    the stream given at creation.
+ *  - Argument structs may gain fields at their end, whose zero means what calls
+ *    did before (ks_kv8_rows.shift): clear a struct before filling it, and compile
+ *    a caller against the header of the library that it loads.
  *  - Greedy argmax ties resolve to the lowest token id.
  */
 #ifndef KNAPSPEC_H
@@ -570,8 +573,12 @@ ks_status ks_kv8_attention(const ks_kv8_cache* cache, const ks_kv8_batch* batch,
  * leave 0 .. n_seqs (no group shares anything then) and for tokens below 0 or
  * above the pages (taken as the nearest possible value).
  * Results, types and limits are ks_kv8_attention's; a value counts relative to
- * the loudest of its own part, the common or the sequence's own.  Groups of one
- * sequence, or a few common tokens, cost more than ks_kv8_attention.
+ * the loudest of its own part, the common or the sequence's own.
+ * A call is five launches, and costs more than ks_kv8_attention of the same batch
+ * where there is little to save: it is faster from about 130,000 common tokens on,
+ * counted for each sequence, where they have a row each (4 sequences behind 4096
+ * tokens 23 us and 13 there, 8 behind 16384 39 and 41, 64 behind 16384 59 and 271), and
+ * from about 50,000 where they have five.  Neither call chooses the other.
  * workspace: ks_kv8_shared_workspace() bytes for the call's sizes or larger ones. */
 typedef struct {
     const int32_t* group_offsets;
@@ -592,6 +599,11 @@ ks_status ks_kv8_shared_attention(const ks_kv8_cache* cache, const ks_kv8_batch*
  * and scores may be NULL then.  out may be scores, and overlaps nothing else that
  * is read.  Sequences without rows, and places from lengths[s] on, are left as
  * they are.
+ * A call is cut by its mean rows a sequence: one prompt's chunk among many single
+ * rows belongs in a call of its own (63 single rows and a chunk of 400, each over
+ * 4000 tokens, 32 heads over 8: 4.5 ms in one call, 0.09 in two).  Calls of many
+ * rows want queries that are 16-byte aligned with strides that are multiples of 8
+ * elements, at least head_dim (2001 rows over 8150 tokens 0.10 ms, else 2.1).
  * Scores and sums are fp32; queries as in ks_kv8_attention, or exact (in calls
  * of many rows).  A row with lse -inf gives no weight to keys that are numbers, a
  * token on a page outside the pool receives none (status bit 0), a NaN key, query
@@ -668,7 +680,10 @@ ks_status ks_kv8_evict(const ks_kv8_cache* cache, const ks_kv8_batch* batch, con
  * All other arrays are dev, contiguous, and may be NULL where they have no
  * elements (entropy always); the results overlap nothing that is read.  vocab up
  * to 2^22, n_tokens and n_top up to 64, n_top at most vocab.  Sums are fp32; an
- * exponential is off by at most 2^-22 relative, and none where it is below 2^-126. */
+ * exponential is off by at most 2^-22 + 2^-22 |z| relative, and counts as 0 below
+ * 2^-126.
+ * The largest logits are found soonest where n_top is at most the 2 KB pieces of a
+ * row, divided by 8 in calls of few rows; more of them can take ten times as long. */
 typedef struct {
     const void* logits;
     int32_t dtype;           /* KS_DTYPE_F32 or KS_DTYPE_BF16 */

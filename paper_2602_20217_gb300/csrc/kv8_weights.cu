@@ -13,11 +13,15 @@
 // of its own: no atomics, and the same bits from call to call.
 //
 // Measured: 24 sequences of 500 to 16000 tokens, a row of 32 heads over 8 each, 28
-// us for 106 MB, 3.8 TB/s; 4.8 TB/s between its first 6 us (runs found, first copies,
-// queries in codes) and its end.  Three CTAs an SM of three stages; two take 30.2
-// us, four 28.2, eight warps a CTA 33.9.
+// us for 106 MB, 3.8 TB/s: 6 us until runs are found, first keys there and queries
+// in codes, then 22 for the bytes, 4.8 TB/s.  Three CTAs an SM of three stages; two
+// take 30.2 us, four 28.2, eight warps a CTA 33.9.
 //
-// Calls of many rows go to kv8_weights_tc.cu.
+// Calls of many rows a sequence, on average, go to kv8_weights_tc.cu.  One long chunk
+// among single rows does not, and its queries are converted again for each tile:
+// 63 single rows and a chunk of 400 over 4000 tokens each take 4.5 ms, 0.063 and
+// 0.026 ms in two calls.  So do queries that no tensor map takes (2001 rows over 8150
+// tokens 2.1 ms, 0.10 there).
 #include <algorithm>
 #include <type_traits>
 

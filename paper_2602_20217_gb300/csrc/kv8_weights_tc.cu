@@ -21,7 +21,8 @@
 // (513 would be the rate: their operands are all of shared memory's bandwidth, and
 // the sums that the softmax reads are there too), its 16384 exponentials 512, both
 // together about 880; a unit's keys take 4 to 6 thousand clocks, which the 64 rows
-// pay after every fourth chunk.  Tried: keys as the operand in TMEM, 513 clocks, but
+// pay after every fourth chunk.  Five of the 18 warps share a scheduler, so a thread
+// has 96 registers, and the compiler spills 94 bytes of it.  Tried: keys as the operand in TMEM, 513 clocks, but
 // room for two S only, 122 and 47.6 us (N = 64 for four S: 217 and 77); the
 // groups' exponentials in turns 116 and 50; sums read once for two tiles 141 and 50;
 // the issuing loop unrolled 109 and 50 (its code is waited for).

@@ -7,17 +7,27 @@
 // so that a likely token's logarithm, -log1p(tail), keeps its digits.
 //
 // A cluster takes a row, each CTA every so many segments of it.  A warp reads a
-// segment, 32 times 64 bytes, at a time into registers, the next one while it works on it, and keeps the row's
-// maximum so far for all of its lanes: a segment that holds no larger logit,
-// nearly every one, adds to the sums without a look at single maxima.  The
+// segment, 32 times 64 bytes, at a time into registers, the next one while it works
+// on it, and keeps the row's maximum so far for all of its lanes: a segment that
+// holds no larger logit, nearly every one, adds to the sums without a look at single
+// maxima.  The
 // segments' maxima stay in shared memory.  The n_top largest logits are in the
 // n_top segments with the largest maxima (ties: the earlier one; every logit of
 // another segment is behind each of those maxima), and at least as large as the
 // least of these maxima: those segments are read again, from L2, and the few
 // candidates ranked against each other.
 //
+// That takes n_top segments in each CTA of the row.  With fewer there is no such
+// bound, and all logits of the CTA are candidates: ranked up to 1024, beyond that
+// read again for each bit that the n_top-th largest is searched by.  In us, at 5,
+// 20 and 64 alternatives: one row of 151936 in bf16 16, 232, 248, of 50257 in fp32
+// 17, 47, 57; 251 rows of 100277 in bf16 22, 26, 1075; 4000 rows of 20000 in fp32 82,
+// 95, 1066, of 5000 49, 360, 391.
+//
 // Measured: 1500 rows of 151936 fp32 logits 159 us, 5.7 TB/s, memory; 251 rows of
-// 100277 in bf16 20 us, 2.5 TB/s, the exponentials' issue and the rows' ends; one
+// 100277 in bf16 with 5 alternatives 20 us, 2.5 TB/s (of logits without peaks 22, and
+// 18 without alternatives): 0.44 instructions a scheduler and clock, barriers the
+// largest stall, as a row's end is serial and there is one partial wave of CTAs; one
 // row of 128256 11 us, launch and the cluster's phases (a CTA a row 16).
 #include <cmath>
 

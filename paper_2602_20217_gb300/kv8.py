@@ -192,7 +192,7 @@ class Cache8:
         """Causal attention of the batch's rows: q, out [n_rows, n_q_heads, head_dim] bf16, lse [n_rows, n_q_heads]
         fp32.  scale: head_dim ** -0.5 if not given.  Returns out.  The address of a stream that is not the current
         one needs out and workspace with it: torch cannot allocate for an address.  shared: groups of sequences with a
-        common beginning, which is read once a group."""
+        common beginning, which is read once a group; it pays from about 130,000 tokens on that are not read again."""
         s = self._stream(stream)
         if stream is not None and (out is None or workspace is None) and \
                 s != torch._C._cuda_getCurrentRawStream(self.device.index):
@@ -230,8 +230,8 @@ class Cache8:
         return out
 
     def weights_workspace(self, n_q_heads: int, n_rows: int):
-        """A workspace of attention_weights() for these sizes or smaller ones (empty where none is needed); calls that run at
-        once need one each."""
+        """A workspace of attention_weights() for these sizes or smaller ones (empty where none is needed); calls that run
+        at once need one each."""
         return torch.empty(ks.ks_kv8_attention_weights_workspace(self.c, n_q_heads, n_rows), dtype=torch.uint8,
                            device=self.device)
 
@@ -240,7 +240,8 @@ class Cache8:
         """Add the weight that each token receives from the batch's rows to scores [n_seqs, n_kv_heads, tokens of a
         page table row] fp32, times decay: q [n_rows, n_q_heads, head_dim] bf16 and lse [n_rows, n_q_heads] as
         attention() took and returned them.  Into out, or scores itself; scores may be None with a decay of 0 and an
-        out.  Returns out.  The address of a stream that is not the current one needs a workspace with it."""
+        out.  Returns out.  The address of a stream that is not the current one needs a workspace with it.  A long chunk
+        and many single rows belong in two calls."""
         s = self._stream(stream)
         if batch.device != self.device:
             raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")

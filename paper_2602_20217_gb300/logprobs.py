@@ -53,9 +53,9 @@ def marshal(logits, code: int, vocab: int, stride: int, tokens, n_top: int, temp
 def token_logprobs(logits, tokens, n_top: int = 0, temperature: float = 1.0, out: LogProbs | None = None,
                    stream=None) -> LogProbs:
     """Log probabilities of tokens [rows] or [rows, n] (int32) under logits [rows, vocab] (fp32 or bf16, rows any
-    distance apart), the rows' entropies and n_top largest logits.  out: the results of empty(rows, n, n_top).  Calls go to
-    torch's current stream unless one is given; with the address of a stream that is not the current one the results
-    have to be given."""
+    distance apart), the rows' entropies and n_top largest logits.  out: the results of empty(rows, n, n_top), n being 1
+    for tokens [rows].  Calls go to torch's current stream unless one is given; with the address of a stream that is not
+    the current one the results have to be given."""
     index = _cuda.current_device()
     device = logits.device
     if device.type != "cuda" or device.index != index:
